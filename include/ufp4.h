@@ -459,6 +459,68 @@ int ufp4_gemm_bwd_dx_grouped(const ufp4_qtensor *dy, const ufp4_qtensor *wt, con
 int ufp4_gemm_bwd_dw_grouped(const ufp4_qtensor *dyt, const ufp4_qtensor *xt, const int64_t *group_offsets_dev,
                              int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype, void *stream);
 
+/*
+ * The operators around an MoE layer's products: layer norm, and tokens sorted by expert and back. Tensors are row-major of
+ * `dtype` UFP4_OUT_F32 or UFP4_OUT_BF16 with any leading dimension >= cols (elements) and any base address that is aligned to
+ * an element; a tensor with no element may be NULL. Every sum, mean and variance is held in fp32 and an output is rounded
+ * once (RNE). Infinities and NaN go through as in the formulas. Results repeat bit for bit. Calls that need scratch memory
+ * take a workspace of the caller's (16-byte aligned), whose size a host-only function gives; its contents need not be set and
+ * say nothing afterwards. cols up to 2^30 (more: UFP4_ERR_UNSUPPORTED).
+ *
+ * ufp4_layer_norm -- per row: mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) rstd gamma + beta.
+ *   gamma_dev, beta_dev  [cols] of w_dtype (UFP4_OUT_*); NULL: 1 and 0.
+ *   eps                  finite, >= 0.
+ *   mean_dev, rstd_dev   fp32 [rows], for the backward call; either may be NULL. y may be x.
+ */
+int ufp4_layer_norm(int dtype, const void *x_dev, int64_t rows, int64_t cols, int64_t ldx, int w_dtype, const void *gamma_dev,
+                    const void *beta_dev, float eps, void *y_dev, int64_t ldy, float *mean_dev, float *rstd_dev,
+                    void *stream);
+
+/*
+ * ufp4_layer_norm_bwd -- with h = (x - mean) rstd and g = dy gamma: dx = rstd (g - mean_row(g) - h mean_row(g h)),
+ * dgamma = sum over rows of dy h, dbeta = sum over rows of dy.
+ *   dgamma_dev, dbeta_dev  fp32 [cols], overwritten (0 where there are no rows); either may be NULL, and with both NULL no
+ *                          workspace is needed. dx may be dy or x.
+ */
+int ufp4_layer_norm_bwd_workspace(int dtype, int64_t rows, int64_t cols, size_t *bytes);
+int ufp4_layer_norm_bwd(int dtype, const void *dy_dev, int64_t lddy, const void *x_dev, int64_t rows, int64_t cols,
+                        int64_t ldx, int w_dtype, const void *gamma_dev, const float *mean_dev, const float *rstd_dev,
+                        void *dx_dev, int64_t lddx, float *dgamma_dev, float *dbeta_dev, void *workspace_dev,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * ufp4_moe_sort -- the slots (t, j) of ids [tokens, k] in the order of (expert, t, j), as the grouped calls take them.
+ *   ids_dev      int32 or int64 (ids_bits 32 or 64) [tokens, k], contiguous: the expert of each slot; a slot whose id is not
+ *                in 0 .. experts - 1 is dropped.
+ *   offsets_dev  int64 [experts + 1]: expert e's rows are offsets[e] .. offsets[e + 1] - 1.
+ *   rows_dev     int32 [tokens, k]: each slot's row in that order, -1 for a dropped one.
+ *   source_dev   int32 [tokens * k]: the slot t * k + j of each row, -1 from offsets[experts] on; may be NULL.
+ * experts up to 1024, k up to 64, tokens * k below 2^31 (more: UFP4_ERR_UNSUPPORTED).
+ */
+int ufp4_moe_sort_workspace(int64_t tokens, int32_t k, int32_t experts, size_t *bytes);
+int ufp4_moe_sort(const void *ids_dev, int ids_bits, int64_t tokens, int32_t k, int32_t experts, int64_t *offsets_dev,
+                  int32_t *rows_dev, int32_t *source_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * ufp4_moe_dispatch -- y[rows[t, j]] = w[t, j] x[t] (weights_dev fp32 [tokens, k]; NULL: copies). y [tokens * k, cols]; its
+ *   rows from offsets[experts] on, which no slot takes, are zero.
+ * ufp4_moe_combine -- out[t] = sum_j w[t, j] y[rows[t, j]], added in the order of j; dropped slots add nothing (a token without
+ *   any gets zeros). It is the gradient of ufp4_moe_dispatch with the same rows and weights, and the reverse.
+ * ufp4_moe_combine_bwd -- both gradients of ufp4_moe_combine from one read: dy[rows[t, j]] = w[t, j] dout[t] (rows no slot takes:
+ *   zero) and dweights[t, j] = <dout[t], y[rows[t, j]]> (fp32; 0 for a dropped slot). dy may be y.
+ * rows and offsets as ufp4_moe_sort wrote them; a row outside 0 .. y_rows - 1 counts as dropped. k up to 64; tokens below 2^24
+ * and 2^26 / ceil(cols / 1024).
+ */
+int ufp4_moe_dispatch(int dtype, const void *x_dev, int64_t tokens, int64_t cols, int64_t ldx, const int32_t *rows_dev,
+                      int32_t k, const int64_t *offsets_dev, int32_t experts, const float *weights_dev, void *y_dev,
+                      int64_t y_rows, int64_t ldy, void *stream);
+int ufp4_moe_combine(int dtype, const void *y_dev, int64_t y_rows, int64_t cols, int64_t ldy, const int32_t *rows_dev,
+                     int64_t tokens, int32_t k, const float *weights_dev, void *out_dev, int64_t ldo, void *stream);
+int ufp4_moe_combine_bwd(int dtype, const void *dout_dev, int64_t tokens, int64_t cols, int64_t lddo, const void *y_dev,
+                         int64_t y_rows, int64_t ldy, const int32_t *rows_dev, int32_t k, const int64_t *offsets_dev,
+                         int32_t experts, const float *weights_dev, void *dy_dev, int64_t lddy, float *dweights_dev,
+                         void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -199,6 +199,81 @@ struct GemmJob {
 
 hipError_t launch_gemm(const GemmJob& job, hipStream_t stream);
 
+// Layer norm over rows of fp32 or bf16 numbers (any leading dimension and alignment); null gamma / beta: 1 / 0.
+struct NormJob {
+    int bf16, w_bf16;
+    const void* x;
+    int64_t rows, cols, ldx;
+    const void *gamma, *beta;
+    float eps;
+    void* y;
+    int64_t ldy;
+    float *mean, *rstd;  // either may be null
+};
+hipError_t launch_norm(const NormJob& job, hipStream_t stream);
+
+struct NormBwdJob {
+    int bf16, w_bf16;
+    const void *dy, *x;
+    int64_t rows, cols, lddy, ldx;
+    const void* gamma;
+    const float *mean, *rstd;
+    void* dx;
+    int64_t lddx;
+    float *dgamma, *dbeta;  // either may be null
+    float* part;            // [norm_bwd_parts][2][cols], null when neither is wanted
+};
+hipError_t launch_norm_bwd(const NormBwdJob& job, hipStream_t stream);
+int64_t norm_bwd_parts(int bf16, int64_t rows, int64_t cols);
+
+// Slots (token, choice) in the order of (expert, slot).
+constexpr int kMoeMaxExperts = 1024;
+constexpr int kMoeMaxK = 64;
+struct MoeSortJob {
+    const void* ids;
+    int ids64;
+    int64_t n;  // slots
+    int E;
+    int64_t* offsets;  // [E + 1]
+    int32_t* rows;     // [n]
+    int32_t* source;   // [n] or null
+    int32_t* counts;   // workspace [runs + 1][E] (runs > 1)
+    int64_t runs;      // moe_sort_runs(n)
+};
+hipError_t launch_moe_sort(const MoeSortJob& job, hipStream_t stream);
+int64_t moe_sort_runs(int64_t n);
+
+struct MoeRowsJob {  // dispatch: in x [tokens], out y [rows_y]; combine: in y, out x
+    int bf16;
+    const void* in;
+    int64_t ldi;
+    void* out;
+    int64_t ldo;
+    int64_t tokens, cols, rows_y;
+    int k, E;
+    const int32_t* rows;     // [tokens][k]
+    const int64_t* offsets;  // dispatch: [E + 1]
+    const float* w;          // [tokens][k] or null
+    int64_t segs;            // set by the launcher
+};
+hipError_t launch_moe_dispatch(MoeRowsJob job, hipStream_t stream);
+hipError_t launch_moe_combine(MoeRowsJob job, hipStream_t stream);
+
+struct MoeBwdJob {
+    int bf16;
+    const void *dout, *y;
+    int64_t lddo, ldy;
+    void* dy;
+    int64_t lddy;
+    int64_t tokens, cols, rows_y;
+    int k, E;
+    const int32_t* rows;
+    const int64_t* offsets;
+    const float* w;
+    float* dw;
+};
+hipError_t launch_moe_combine_bwd(const MoeBwdJob& job, hipStream_t stream);
+
 }  // namespace ufp4
 
 // The size rules asked from the host: exported for the tests, not part of the interface in include/ufp4.h.

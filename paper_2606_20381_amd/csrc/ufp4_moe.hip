@@ -1,0 +1,358 @@
+// Tokens sorted by expert and back.
+//
+// sort: ids [T, k] -> every slot (t, j)'s place in the order by (expert, t, j). A stable counting sort of n = T k slots by E
+//   keys, in runs of kRun slots per workgroup. Within a wave the slots of one expert find each other by ballots over the
+//   bits of the key, so a slot's rank is a count of lanes and no atomic decides an order.
+// dispatch: out[rows[t, j]] = w[t, j] x[t]; combine: out[t] = sum_j w[t, j] y[rows[t, j]]; each the other's adjoint.
+// combine_bwd: dy[rows[t, j]] = w[t, j] dout[t] and dw[t, j] = <dout[t], y[rows[t, j]]> from one read of both.
+//   All three are HBM bound: a wave (combine_bwd: a workgroup) takes one token, or a 4 KiB segment of one, reads its row
+//   once for all k experts and sums in fp32.
+
+#include "ufp4_internal.h"
+#include "ufp4_rows.h"
+
+namespace ufp4 {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------
+// sort
+// ------------------------------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kRounds = 4;                       // slots per thread
+constexpr int kRun = kSortThreads * kRounds;     // slots per workgroup
+constexpr int kWaveRun = 64 * kRounds;           // contiguous slots per wave
+
+// Expert of slot i, E where it has none (or lies past the last slot).
+__device__ __forceinline__ int sort_key(const MoeSortJob& j, int64_t i) {
+    if (i >= j.n) return j.E;
+    const int64_t id = j.ids64 ? static_cast<const int64_t*>(j.ids)[i] : static_cast<const int32_t*>(j.ids)[i];
+    return id >= 0 && id < j.E ? (int)id : j.E;
+}
+
+// Each workgroup's slots per expert: counts [workgroup][E].
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(MoeSortJob j) {
+    extern __shared__ int32_t s_count[];  // [E]
+    for (int e = threadIdx.x; e < j.E; e += kSortThreads) s_count[e] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * kRun;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int key = sort_key(j, first + r * kSortThreads + threadIdx.x);
+        if (key < j.E) atomicAdd(&s_count[key], 1);  // a count: the order of the additions does not show
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < j.E; e += kSortThreads) j.counts[(int64_t)blockIdx.x * j.E + e] = s_count[e];
+}
+
+// Counts of many workgroups: an exclusive sum over the workgroups per expert, in place, and the totals in row `runs`.
+// One wave per expert, 64 workgroups at a time.
+__global__ __launch_bounds__(256) void sort_scan_kernel(MoeSortJob j) {
+    const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (e >= j.E) return;
+    int32_t base = 0;
+    for (int64_t b0 = 0; b0 < j.runs; b0 += 64) {
+        const int64_t b = b0 + lane;
+        const int32_t c = b < j.runs ? j.counts[b * j.E + e] : 0;
+        int32_t inc = c;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t v = __shfl_up(inc, d, 64);
+            if (lane >= d) inc += v;
+        }
+        if (b < j.runs) j.counts[b * j.E + e] = base + inc - c;
+        base += __shfl(inc, 63, 64);
+    }
+    if (lane == 0) j.counts[j.runs * j.E + e] = base;
+}
+
+// Places. MANY: the counts have been summed over the workgroups (sort_scan_kernel); otherwise the workgroup adds them up
+// itself, or (one workgroup) they are its own.
+template <bool MANY>
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(MoeSortJob j) {
+    extern __shared__ char s_raw[];
+    const int E = j.E;
+    int32_t* const s_base = reinterpret_cast<int32_t*>(s_raw);              // [E] first place of this workgroup's slots
+    uint16_t* const s_wave = reinterpret_cast<uint16_t*>(s_base + E + 1);   // [wave][E] slots, then their exclusive sum
+    __shared__ int32_t s_scan[kSortWaves];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    for (int i = tid; i < kSortWaves * E; i += kSortThreads) s_wave[i] = 0;
+    __syncthreads();
+
+    const int64_t first = (int64_t)blockIdx.x * kRun + wave * kWaveRun;
+    int key[kRounds], rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) key[r] = sort_key(j, first + r * 64 + lane);
+    int bits = 0;
+    while ((1 << bits) <= E) ++bits;
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        uint64_t peers = ~0ull;  // the lanes with this lane's key
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((key[r] >> b) & 1);
+            peers &= (key[r] >> b) & 1 ? set : ~set;
+        }
+        rank[r] = 0;
+        if (key[r] < E) {
+            volatile uint16_t* const c = s_wave + wave * E + key[r];  // other lanes of the wave write it between the rounds
+            const int before = *c;
+            rank[r] = before + __popcll(peers & below);
+            if ((peers & below) == 0) *c = (uint16_t)(before + __popcll(peers));  // one lane per key, after all have read
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+
+    // Per expert: the waves' counts to their exclusive sum; the slots of this expert in earlier workgroups and in all.
+    // A thread takes expert tid (E <= kSortThreads).
+    int32_t before = 0, total = 0;
+    if (tid < E) {
+        int32_t own = 0;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int32_t c = s_wave[w * E + tid];
+            s_wave[w * E + tid] = (uint16_t)own;
+            own += c;
+        }
+        if constexpr (MANY) {
+            before = j.counts[(int64_t)blockIdx.x * E + tid];
+            total = j.counts[j.runs * E + tid];
+        } else if (j.runs > 1) {
+            for (int64_t b = 0; b < j.runs; ++b) {
+                const int32_t c = j.counts[b * E + tid];
+                if (b < blockIdx.x) before += c;
+                total += c;
+            }
+        } else {
+            total = own;
+        }
+    }
+    // exclusive sum of the totals over the experts
+    int32_t inc = total;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t v = __shfl_up(inc, d, 64);
+        if (lane >= d) inc += v;
+    }
+    if (lane == 63) s_scan[wave] = inc;
+    __syncthreads();
+    int32_t waves = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        if (w < wave) waves += s_scan[w];
+        all += s_scan[w];
+    }
+    const int32_t start = waves + inc - total;
+    if (tid < E) {
+        s_base[tid] = start + before;
+        if (blockIdx.x == 0) j.offsets[tid] = start;
+    }
+    if (blockIdx.x == 0 && tid == 0) j.offsets[E] = all;
+    __syncthreads();
+
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = first + r * 64 + lane;
+        if (i < j.n) {
+            int32_t place = -1;
+            if (key[r] < E) {
+                place = s_base[key[r]] + s_wave[wave * E + key[r]] + rank[r];
+                if (j.source) j.source[place] = (int32_t)i;
+            }
+            j.rows[i] = place;
+            if (j.source && i >= all) j.source[i] = -1;  // places that no slot takes
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// dispatch, combine
+// ------------------------------------------------------------------------------------------------
+constexpr int kSegPieces = 4;  // 16-byte pieces per lane of a segment: 4 KiB per wave
+
+// out rows [first, rows_out) zero, in segments: the rows that no slot takes. Called by every wave of a grid of `tokens` waves
+// per segment.
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* out, int64_t ldo, int64_t first, int64_t rows_out, int64_t token, int64_t tokens,
+                                          int64_t c0, int64_t cols) {
+    using P = Piece<T>;
+    const u32x4_any zero = {0, 0, 0, 0};
+    for (int64_t r = (first < 0 ? 0 : first) + token; r < rows_out; r += tokens)
+#pragma unroll
+        for (int p = 0; p < kSegPieces; ++p) {
+            const int64_t c = c0 + p * 64 * P::V;
+            P::store(out + r * ldo + c, cols - c, zero);
+        }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dispatch_kernel(MoeRowsJob j) {
+    using P = Piece<T>;
+    constexpr int V = P::V;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= j.tokens * j.segs) return;
+    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (kSegPieces * 64 * V) + (threadIdx.x & 63) * V;
+    const T* const x = static_cast<const T*>(j.in) + t * j.ldi;
+    T* const out = static_cast<T*>(j.out);
+    const int64_t used = j.offsets[j.E];
+    u32x4_any raw[kSegPieces];
+#pragma unroll
+    for (int p = 0; p < kSegPieces; ++p) {
+        const int64_t c = c0 + p * 64 * V;
+        raw[p] = P::load(x + c, j.cols - c);
+    }
+    for (int q = 0; q < j.k; ++q) {
+        const int32_t row = j.rows[t * j.k + q];
+        if (row < 0 || row >= j.rows_y) continue;
+        const float w = j.w ? j.w[t * j.k + q] : 1.0f;
+#pragma unroll
+        for (int p = 0; p < kSegPieces; ++p) {
+            const int64_t c = c0 + p * 64 * V;
+            u32x4_any r = raw[p];
+            if (j.w) {
+                float f[V];
+                P::unpack(r, f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] *= w;
+                r = P::pack(f);
+            }
+            P::store(out + row * j.ldo + c, j.cols - c, r);
+        }
+    }
+    zero_rows<T>(out, j.ldo, used, j.rows_y, t, j.tokens, c0, j.cols);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
+    using P = Piece<T>;
+    constexpr int V = P::V;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= j.tokens * j.segs) return;
+    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (kSegPieces * 64 * V) + (threadIdx.x & 63) * V;
+    const T* const y = static_cast<const T*>(j.in);
+    float acc[kSegPieces][V];
+#pragma unroll
+    for (int p = 0; p < kSegPieces; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[p][i] = 0.0f;
+    for (int q = 0; q < j.k; ++q) {
+        const int32_t row = j.rows[t * j.k + q];
+        if (row < 0 || row >= j.rows_y) continue;
+        const float w = j.w ? j.w[t * j.k + q] : 1.0f;
+#pragma unroll
+        for (int p = 0; p < kSegPieces; ++p) {
+            const int64_t c = c0 + p * 64 * V;
+            float f[V];
+            P::unpack(P::load(y + row * j.ldi + c, j.cols - c), f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[p][i] = __builtin_fmaf(w, f[i], acc[p][i]);
+        }
+    }
+    T* const out = static_cast<T*>(j.out) + t * j.ldo;
+#pragma unroll
+    for (int p = 0; p < kSegPieces; ++p) {
+        const int64_t c = c0 + p * 64 * V;
+        P::store(out + c, j.cols - c, P::pack(acc[p]));
+    }
+}
+
+// One workgroup per token: dout's segment in registers, each expert's row of y against it, the dot products added over the
+// lanes, then over the waves in order.
+template <typename T>
+__global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
+    using P = Piece<T>;
+    constexpr int V = P::V;
+    __shared__ float s_dot[4][kMoeMaxK];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int64_t t = blockIdx.x;
+    const T* const dout = static_cast<const T*>(j.dout) + t * j.lddo;
+    const T* const y = static_cast<const T*>(j.y);
+    T* const dy = static_cast<T*>(j.dy);
+    const int64_t used = j.offsets[j.E];
+    for (int q = tid; q < 4 * kMoeMaxK; q += 256) s_dot[q / kMoeMaxK][q % kMoeMaxK] = 0.0f;
+    __syncthreads();
+    for (int64_t seg = 0; seg < j.cols; seg += kSegPieces * 256 * V) {
+        const int64_t c0 = seg + (int64_t)tid * V;
+        u32x4_any raw[kSegPieces];
+#pragma unroll
+        for (int p = 0; p < kSegPieces; ++p) {
+            const int64_t c = c0 + p * 256 * V;
+            raw[p] = P::load(dout + c, j.cols - c);
+        }
+        for (int q = 0; q < j.k; ++q) {
+            const int32_t row = j.rows[t * j.k + q];
+            if (row < 0 || row >= j.rows_y) continue;
+            const float w = j.w ? j.w[t * j.k + q] : 1.0f;
+            float dot = 0.0f;
+#pragma unroll
+            for (int p = 0; p < kSegPieces; ++p) {
+                const int64_t c = c0 + p * 256 * V;
+                float d[V], f[V];
+                P::unpack(raw[p], d);
+                P::unpack(P::load(y + row * j.ldy + c, j.cols - c), f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    dot = __builtin_fmaf(d[i], f[i], dot);
+                    d[i] *= w;
+                }
+                P::store(dy + row * j.lddy + c, j.cols - c, P::pack(d));
+            }
+            dot = wave_sum(dot);
+            if (lane == 0) s_dot[wave][q] += dot;
+        }
+    }
+    __syncthreads();
+    for (int q = tid; q < j.k; q += 256)
+        j.dw[t * j.k + q] = (s_dot[0][q] + s_dot[1][q]) + (s_dot[2][q] + s_dot[3][q]);
+    const u32x4_any zero = {0, 0, 0, 0};
+    for (int64_t r = (used < 0 ? 0 : used) + t; r < j.rows_y; r += j.tokens)
+        for (int64_t c = (int64_t)tid * V; c < j.cols; c += 256 * V) P::store(dy + r * j.lddy + c, j.cols - c, zero);
+}
+
+template <typename T>
+int64_t segments(int64_t cols) {
+    constexpr int64_t seg = kSegPieces * 64 * Piece<T>::V;
+    return (cols + seg - 1) / seg;
+}
+
+}  // namespace
+
+int64_t moe_sort_runs(int64_t n) { return n > 0 ? (n + kRun - 1) / kRun : 1; }
+
+// Up to this many workgroups each adds up the others' counts itself; more have them summed by a launch of their own.
+constexpr int64_t kAddUp = 64;
+
+hipError_t launch_moe_sort(const MoeSortJob& j, hipStream_t s) {
+    if (j.runs > 1) {
+        sort_count_kernel<<<(unsigned)j.runs, kSortThreads, j.E * sizeof(int32_t), s>>>(j);
+        if (j.runs > kAddUp) sort_scan_kernel<<<(unsigned)((j.E + 3) / 4), 256, 0, s>>>(j);
+    }
+    const size_t lds = (j.E + 1) * sizeof(int32_t) + kSortWaves * j.E * sizeof(uint16_t);
+    if (j.runs > kAddUp) sort_place_kernel<true><<<(unsigned)j.runs, kSortThreads, lds, s>>>(j);
+    else sort_place_kernel<false><<<(unsigned)j.runs, kSortThreads, lds, s>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_dispatch(MoeRowsJob j, hipStream_t s) {
+    j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
+    const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
+    if (j.bf16) dispatch_kernel<uint16_t><<<g, 256, 0, s>>>(j);
+    else dispatch_kernel<float><<<g, 256, 0, s>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_combine(MoeRowsJob j, hipStream_t s) {
+    j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
+    const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
+    if (j.bf16) combine_kernel<uint16_t><<<g, 256, 0, s>>>(j);
+    else combine_kernel<float><<<g, 256, 0, s>>>(j);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_combine_bwd(const MoeBwdJob& j, hipStream_t s) {
+    if (j.bf16) combine_bwd_kernel<uint16_t><<<(unsigned)j.tokens, 256, 0, s>>>(j);
+    else combine_bwd_kernel<float><<<(unsigned)j.tokens, 256, 0, s>>>(j);
+    return hipGetLastError();
+}
+
+}  // namespace ufp4
