@@ -82,7 +82,7 @@ typedef enum {
     UFP4_ERR_HIP = 6          /* kernel launch failed                                                      */
 } ufp4_status;
 
-enum { UFP4_FMT_UNIFORM = 0, UFP4_FMT_E2M1 = 1, UFP4_FMT_UNIFORM_MX32 = 2 };
+enum { UFP4_FMT_UNIFORM = 0, UFP4_FMT_E2M1 = 1, UFP4_FMT_UNIFORM_MX32 = 2, UFP4_FMT_E2M1_MX32 = 4 }; /* 3 is none */
 enum { UFP4_ROUND_RTNE = 0, UFP4_ROUND_SR = 1 };
 enum { UFP4_OUT_F32 = 0, UFP4_OUT_BF16 = 1 };
 /* How a quantized operand's rows and reduction axis relate to the tensor it came from (ufp4_qtensor.layout):
@@ -408,6 +408,68 @@ int ufp4_mx_gemm_bwd_dx_grouped(const ufp4_qtensor *dy, const ufp4_qtensor *wt, 
                                 void *stream);
 int ufp4_mx_gemm_bwd_dw_grouped(const ufp4_qtensor *dyt, const ufp4_qtensor *xt, const int64_t *group_offsets_dev,
                                 int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype, void *stream);
+
+/*
+ * Microscaled 4-bit floating point (the OCP Microscaling format MXFP4): E2M1 levels with one E8M0 scale per 1x32 block, the
+ * operands that gfx950's scaled matrix instruction takes as they are. Arguments, errors and limits as the ufp4_mx_* calls of the
+ * same names, except as said here.
+ *
+ * ufp4_mxfp4_quantize -- per 1x32 block along the reduction axis: y = RHT16 of each half (rht != 0) or y = x; E =
+ *   max(floor(log2 amax |y|) - 2, -127); v = y 2^-E (|v| < 8); the E2M1 level nearest to v, ties to the even code, or by SR
+ *   (rule and Philox draws as above, the counters numbering 16-blocks), |v| > 6 cut to 6. red % 32 == 0; out->format becomes
+ *   UFP4_FMT_E2M1_MX32. A code keeps the sign of a value that it rounds to zero (the one form with a negative zero). A block that
+ *   holds an infinity or a NaN gets the scale byte 255 (NaN) and zero codes, which makes the rows of the products that use it NaN.
+ *   codes : block b of row 128p + i at codes + p * code_panel_ld + b * 2048 + i * 16 (16 bytes, element 2j the low nibble of
+ *           byte j); code_panel_ld >= 2048 * red/32.
+ *   scales: bytes E + 127 in groups of four blocks, block b of row 128p + i at scales + p * scale_panel_ld + (b / 4) * 512 +
+ *           (b % 2) * 256 + i * 2 + (b / 2) % 2; scale_panel_ld >= 512 * ceil(red / 128). Bytes of blocks past the last are 0.
+ *   Both strides multiples of 16, both pointers 16-byte aligned. Padding rows of the last panel: zero codes and scale bytes.
+ * ufp4_mxfp4_quantize_dual -- both operands of one tensor; equal, bit for bit, to two calls of ufp4_mxfp4_quantize.
+ * ufp4_mxfp4_quantize_grouped -- grouped rows (groups on panels, padded_total from block 128) or grouped reduction (groups
+ *   padded to 32 tokens, block 32).
+ * ufp4_mxfp4_dequantize -- level 2^E of every element as bf16 [rows, red], row-major, ldo >= red, ldo % 8 == 0, 16-byte aligned.
+ *   Exact; values past the bf16 range (from rotated inputs only) are infinite. The layout is the operand's own (a rotated operand
+ *   stays rotated, a grouped one padded).
+ * 2^24 or more workgroups (64 x 256 elements each rowwise, 128 x 128 transposed, 32 x 256 dequantized) return
+ * UFP4_ERR_UNSUPPORTED.
+ */
+int ufp4_mxfp4_quantize(const void *x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose, int rht,
+                        uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor *out,
+                        void *stream);
+int ufp4_mxfp4_quantize_dual(const void *x_dev, int64_t rows, int64_t cols, int64_t ld, int rht_rows,
+                             uint32_t sign_mask_rows, uint32_t stream_rows, int rht_cols, uint32_t sign_mask_cols,
+                             uint32_t stream_cols, int rounding, uint64_t seed, ufp4_qtensor *out_rows,
+                             ufp4_qtensor *out_cols, void *stream);
+int ufp4_mxfp4_quantize_grouped(const void *x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose,
+                                const int64_t *group_offsets_dev, int32_t num_groups, int64_t padded_total, int rht,
+                                uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor *out,
+                                void *stream);
+int ufp4_mxfp4_dequantize(const ufp4_qtensor *q, void *out_dev, int64_t ldo, void *stream);
+
+/*
+ * ufp4_mxfp4_gemm_* -- the three passes, dense and grouped, on two UFP4_FMT_E2M1_MX32 operands: as ufp4_mx_gemm_*. The grouped
+ *   bwd_dx needs N % 128 == 0 (its groups' blocks of W^T begin with a group of four scales), else UFP4_ERR_UNSUPPORTED, as do
+ *   outputs of 2^24 or more 256 x 256 tiles.
+ * ufp4_mxfp4_linear -- y [rows, N] = Q(x) W^T for the few tokens of a decode step, in one launch: x bf16 [rows, K] (ldx % 8 == 0,
+ *   16-byte aligned), quantized as ufp4_mxfp4_quantize does without RHT, to nearest; w a plain UFP4_FMT_E2M1_MX32 operand [N, K].
+ *   rows up to 16 and w without RHT (else UFP4_ERR_UNSUPPORTED: quantize x and use ufp4_mxfp4_gemm_fwd_y).
+ */
+int ufp4_mxfp4_gemm_fwd_y(const ufp4_qtensor *x, const ufp4_qtensor *w, void *y_dev, int64_t ldc, int out_dtype,
+                          void *stream);
+int ufp4_mxfp4_gemm_bwd_dx(const ufp4_qtensor *dy, const ufp4_qtensor *wt, void *dx_dev, int64_t ldc, int out_dtype,
+                           void *stream);
+int ufp4_mxfp4_gemm_bwd_dw(const ufp4_qtensor *dyt, const ufp4_qtensor *xt, void *dw_dev, int64_t ldc, int out_dtype,
+                           void *stream);
+int ufp4_mxfp4_gemm_fwd_y_grouped(const ufp4_qtensor *x, const ufp4_qtensor *w, const int64_t *group_offsets_dev,
+                                  int32_t num_groups, int64_t m_total, void *y_dev, int64_t ldc, int out_dtype,
+                                  void *stream);
+int ufp4_mxfp4_gemm_bwd_dx_grouped(const ufp4_qtensor *dy, const ufp4_qtensor *wt, const int64_t *group_offsets_dev,
+                                   int32_t num_groups, int64_t m_total, void *dx_dev, int64_t ldc, int out_dtype,
+                                   void *stream);
+int ufp4_mxfp4_gemm_bwd_dw_grouped(const ufp4_qtensor *dyt, const ufp4_qtensor *xt, const int64_t *group_offsets_dev,
+                                   int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype, void *stream);
+int ufp4_mxfp4_linear(const void *x_dev, int64_t rows, int64_t ldx, const ufp4_qtensor *w, void *y_dev, int64_t ldc,
+                      int out_dtype, void *stream);
 
 /*
  * Block-scaled 4-bit GEMMs (Sec. 2.2). All three passes are NT products of two quantized operands that

@@ -620,6 +620,39 @@ def quantize_rows_mx(a_f32: np.ndarray, rounding: int, rht: bool, sign_mask: int
     return idx.reshape(rows, red), (E + E8M0_BIAS).astype(np.uint8)
 
 
+def quantize_rows_mxfp4(a_f32: np.ndarray, rounding: int, rht: bool, sign_mask: int = 0, seed: int = 0, stream: int = 0,
+                        row_ids=None):
+    """Microscaled 4-bit quantization (OCP MXFP4) of an operand A [rows, red] (red % 32 == 0) along its contiguous axis.
+
+    As `quantize_rows_mx` (the same shared exponent: the top binade of E2M1, 4 and 6, is that of the levels 4..7) with the
+    E2M1 levels: v = y * 2^-E in (-8, 8) by RTNE (ties to the even code) or SR, |v| > 6 cut to 6. Returns (signed codes
+    int64 [rows, red], E8M0 bytes uint8 [rows, red/32])."""
+    a = np.asarray(a_f32, dtype=np.float32)
+    rows, red = a.shape
+    if red % MX_BLOCK:
+        raise ValueError("reduction length must be a multiple of 32")
+    n16, n32 = red // BLOCK, red // MX_BLOCK
+    y16 = a.reshape(rows, n16, BLOCK)
+    y = (rht_blocks(y16, sign_mask) if rht else y16.astype(np.float64)).reshape(rows, n32, MX_BLOCK)
+    E = mx_scale_exponent(np.abs(y).max(axis=-1))
+    v = np.clip(y * np.ldexp(1.0, -E)[..., None], -6.0, 6.0).astype(np.float32)
+    if rounding == RTNE:
+        idx = round_nearest_even(v, E2M1)
+    elif rounding == SR:
+        rid = np.arange(rows) if row_ids is None else np.asarray(row_ids)
+        u = sr_draws(np.arange(n16)[None, :], rid[:, None], seed, stream).reshape(rows, n32, MX_BLOCK)
+        idx = round_stochastic(v, u, E2M1)
+    else:
+        raise ValueError("unknown rounding mode")
+    return idx.reshape(rows, red), (E + E8M0_BIAS).astype(np.uint8)
+
+
+def dequantize_mxfp4(idx: np.ndarray, e8m0: np.ndarray) -> np.ndarray:
+    """fp64 values level(code) * 2^(e8m0 - 127) of quantize_rows_mxfp4."""
+    lv = level_values(idx, E2M1)
+    return lv * np.repeat(np.ldexp(1.0, np.asarray(e8m0, dtype=np.int64) - E8M0_BIAS), MX_BLOCK, axis=-1)
+
+
 def e2m3_value(bits) -> np.ndarray:
     """Value of a 6-bit FP6 E2M3 pattern (OCP MX formats): sign, 2 exponent bits (bias 1), 3 mantissa bits;
     exponent 0 is subnormal (m/8)."""

@@ -20,8 +20,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libufp4.so")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
-SOURCES = ["ufp4_quant.hip", "ufp4_gemm.hip", "ufp4_gemm_mx.hip", "ufp4_norm.hip", "ufp4_moe.hip", "ufp4_api.cpp",
-           "ufp4_api_layer.cpp"]
+SOURCES = ["ufp4_quant.hip", "ufp4_gemm.hip", "ufp4_gemm_mx.hip", "ufp4_mxfp4.hip", "ufp4_gemm_mxfp4.hip",
+           "ufp4_linear_mxfp4.hip", "ufp4_norm.hip", "ufp4_moe.hip", "ufp4_api.cpp", "ufp4_api_layer.cpp"]
 
 ARCH = "gfx950"
 FLAGS = [
@@ -31,11 +31,13 @@ FLAGS = [
     "-fPIC",
     "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # MFMA results in VGPRs: the GEMM epilogue reads them with plain VALU FMAs (no AGPR copies)
-    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-Wall",
     "-Wno-unused-function",
 ]
+# MFMA results in VGPRs: the GEMM epilogue reads them with plain VALU FMAs (no AGPR copies). Not the microscaled 4-bit GEMM,
+# whose largest tile holds 256 results a lane: with the operands that is more than the 256 VGPRs, so they are AGPRs.
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+AGPR_SOURCES = ("ufp4_gemm_mxfp4.hip",)
 
 
 def hipcc() -> str:
@@ -66,7 +68,8 @@ def build(verbose: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
         lang = ["-x", "hip"] if src.endswith(".cpp") else []
-        cmds.append([cc, *FLAGS, f"-I{INCLUDE}", *lang, "-c", os.path.join(CSRC, src), "-o", obj])
+        form = [] if src in AGPR_SOURCES else VGPR_FORM
+        cmds.append([cc, *FLAGS, *form, f"-I{INCLUDE}", *lang, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         list(ex.map(lambda c: _run(c, verbose), cmds))

@@ -45,17 +45,31 @@ void fill_grid(float max_fpx, QuantArgs& qa) {
 constexpr int64_t kMaxCodePanelLd = int64_t(1) << 29;   // bytes
 constexpr int64_t kMaxScalePanelLd = int64_t(1) << 27;  // floats
 
+// How a format stores a panel's reduction: values per block, and bytes of codes and scale elements of `nkb` blocks.
+bool one_byte_scales(int format) { return format == UFP4_FMT_UNIFORM_MX32 || format == UFP4_FMT_E2M1_MX32; }
+int64_t block_of(int format) { return one_byte_scales(format) ? 32 : 16; }
+int64_t panel_codes(int format, int64_t nkb) {
+    return nkb * (format == UFP4_FMT_UNIFORM_MX32 ? kMxPanelBlockBytes : format == UFP4_FMT_E2M1_MX32 ? kMicroBlockBytes
+                                                                                                     : kPanelBlockBytes);
+}
+int64_t panel_scales(int format, int64_t nkb) {
+    return format == UFP4_FMT_E2M1_MX32 ? ceil_div(nkb, 4) * kMicroGroupScales  // whole groups of four blocks
+                                        : nkb * (format == UFP4_FMT_UNIFORM_MX32 ? kMxPanelBlockScales : kPanelBlockScales);
+}
+bool known_format(int format) {
+    return format == UFP4_FMT_UNIFORM || format == UFP4_FMT_E2M1 || format == UFP4_FMT_UNIFORM_MX32 ||
+           format == UFP4_FMT_E2M1_MX32;
+}
+
 // Storage of `q` for a [rows, red] operand of `format`: pointers, panel strides, panel count.
 int check_storage(const ufp4_qtensor* q, int format, int64_t rows, int64_t red) {
     if (!q) return UFP4_ERR_INVALID_ARG;
     if (!q->codes || !q->scales || q->panels < 0 || rows < 0 || red < 0) return UFP4_ERR_INVALID_ARG;
-    const bool mx = format == UFP4_FMT_UNIFORM_MX32;
-    const int64_t blk = mx ? 32 : 16;
+    const bool mx = one_byte_scales(format);
+    const int64_t blk = block_of(format);
     if (red % blk != 0) return UFP4_ERR_SHAPE;
     const int64_t nkb = red / blk;
-    const int64_t cb = mx ? kMxPanelBlockBytes : kPanelBlockBytes;
-    const int64_t sb = mx ? kMxPanelBlockScales : kPanelBlockScales;
-    if (q->code_panel_ld < nkb * cb || q->scale_panel_ld < nkb * sb) return UFP4_ERR_SHAPE;
+    if (q->code_panel_ld < panel_codes(format, nkb) || q->scale_panel_ld < panel_scales(format, nkb)) return UFP4_ERR_SHAPE;
     if (q->panels < ceil_div(rows, kPanelRows)) return UFP4_ERR_SHAPE;
     if (q->code_panel_ld % 16 != 0 || q->scale_panel_ld % (mx ? 16 : 4) != 0) return UFP4_ERR_ALIGN;
     if (!aligned(q->codes, 16) || !aligned(q->scales, 16)) return UFP4_ERR_ALIGN;
@@ -152,16 +166,16 @@ int quantize_impl(int format, const void* x, int64_t rows, int64_t cols, int64_t
     return status_of(launch_quantize(j, static_cast<hipStream_t>(stream)));
 }
 
-// The two operands of a GEMM: known formats (the power-of-two-scale one for `mx`, the others otherwise), the
-// same format, RHT block and signs (Sec. 2.2: one H' for both), and storage that holds what they claim.
-int check_operands(const ufp4_qtensor* a, const ufp4_qtensor* b, bool mx) {
+// The two operands of a GEMM: known formats (with one-byte scales the one that the GEMM is for, `mx`; one of the others with
+// mx = kFp32Scales), the same format, RHT block and signs (Sec. 2.2: one H' for both), and storage that holds what they claim.
+constexpr int kFp32Scales = -1;
+int check_operands(const ufp4_qtensor* a, const ufp4_qtensor* b, int mx) {
     if (!a || !b) return UFP4_ERR_INVALID_ARG;
     for (const ufp4_qtensor* q : {a, b}) {
-        if (q->format != UFP4_FMT_UNIFORM && q->format != UFP4_FMT_E2M1 && q->format != UFP4_FMT_UNIFORM_MX32)
-            return UFP4_ERR_INVALID_ARG;
+        if (!known_format(q->format)) return UFP4_ERR_INVALID_ARG;
         if (q->rht_block != 0 && q->rht_block != 16 && q->rht_block != 32 && q->rht_block != 64 && q->rht_block != 128)
             return UFP4_ERR_INVALID_ARG;
-        if ((q->format == UFP4_FMT_UNIFORM_MX32) != mx) return UFP4_ERR_MISMATCH;
+        if ((one_byte_scales(q->format) ? q->format : kFp32Scales) != mx) return UFP4_ERR_MISMATCH;
     }
     if (a->format != b->format || a->rht_block != b->rht_block) return UFP4_ERR_MISMATCH;
     for (int k = 0; k < a->rht_block / 16; ++k)
@@ -209,7 +223,7 @@ GemmJob make_job(int mode, const ufp4_qtensor* a, const ufp4_qtensor* b, int64_t
 
 // A [M, red] . B [N, red]^T for the three dense passes.
 int gemm_dense(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype, void* stream) {
-    int st = check_operands(a, b, false);
+    int st = check_operands(a, b, kFp32Scales);
     if (st != UFP4_OK) return st;
     if (a->red != b->red) return UFP4_ERR_MISMATCH;
     st = check_output(c, ldc, b->rows, out_dtype, a->rows == 0 || b->rows == 0);
@@ -219,8 +233,19 @@ int gemm_dense(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ld
     return status_of(launch_gemm(j, static_cast<hipStream_t>(stream)));
 }
 
-int mx_gemm_impl(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype, void* stream) {
-    int st = check_operands(a, b, true);
+// Workgroups of a GEMM on operands with one-byte scales whose tile is `bm` x `bm`, with `rows` tile rows, that a launch allows:
+// the microscaled 4-bit kernels launch 256 threads for each of them, and a grid holds fewer than 2^32 threads.
+bool mx_grid_fits(int format, int64_t rows, int64_t cols) {
+    return rows * cols < (int64_t(1) << (format == UFP4_FMT_E2M1_MX32 ? 24 : 31));
+}
+
+int launch_mx(int format, const MxGemmJob& j, void* stream) {
+    hipStream_t const s = static_cast<hipStream_t>(stream);
+    return status_of(format == UFP4_FMT_E2M1_MX32 ? launch_gemm_mxfp4(j, s) : launch_gemm_mx(j, s));
+}
+
+int mx_gemm_impl(int format, const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype, void* stream) {
+    int st = check_operands(a, b, format);
     if (st != UFP4_OK) return st;
     if (a->red != b->red) return UFP4_ERR_MISMATCH;
     st = check_output(c, ldc, b->rows, out_dtype, a->rows == 0 || b->rows == 0);
@@ -228,6 +253,7 @@ int mx_gemm_impl(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t 
     // one workgroup per output tile on a one-dimensional grid (bounded by the count of 128 x 128 tiles; smaller ones are
     // taken only where their own grid fits)
     if (ceil_div(a->rows, 128) * ceil_div(b->rows, 128) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
+    if (!mx_grid_fits(format, ceil_div(a->rows, 256), ceil_div(b->rows, 256))) return UFP4_ERR_UNSUPPORTED;
     if (a->rows == 0 || b->rows == 0) return UFP4_OK;
     MxGemmJob j{};
     j.out_dtype = out_dtype;
@@ -247,7 +273,7 @@ int mx_gemm_impl(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t 
     j.c = c;
     j.ldc = ldc;
     j.mode = kGemmDense;
-    return status_of(launch_gemm_mx(j, static_cast<hipStream_t>(stream)));
+    return launch_mx(format, j, stream);
 }
 
 MxGemmJob mx_job(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype) {
@@ -266,6 +292,184 @@ MxGemmJob mx_job(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t 
     j.c = c;
     j.ldc = ldc;
     return j;
+}
+
+constexpr int64_t kMostMicroTiles = int64_t(1) << 24;  // workgroups of 256 threads in a grid of fewer than 2^32
+
+int launch_mx_quantize(int format, const MxQuantJob& j, void* stream) {
+    hipStream_t const s = static_cast<hipStream_t>(stream);
+    return status_of(format == UFP4_FMT_E2M1_MX32 ? launch_quantize_mxfp4(j, s) : launch_quantize_mx(j, s));
+}
+
+int mx_quantize_impl(int format, const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose, int rht,
+                     uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
+                     void* stream) {
+    if (transpose != 0 && transpose != 1) return UFP4_ERR_INVALID_ARG;
+    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
+    if (rht != 0 && rht != 1) return UFP4_ERR_INVALID_ARG;
+    if (sign_mask > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
+    const int si = check_input(x_dev, rows, cols, ld, 8);
+    if (si != UFP4_OK) return si;
+    const int64_t red = transpose ? rows : cols;
+    const int64_t qrows = transpose ? cols : rows;
+    const int st = check_storage(out, format, qrows, red);
+    if (st != UFP4_OK) return st;
+    if (qrows >= (int64_t(1) << 31) || red / 16 >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
+    if (format == UFP4_FMT_E2M1_MX32) {
+        if (micro_quant_tiles(transpose, qrows, red) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
+    } else {
+        if (!transpose && padded_rows(qrows) / 64 > 65535) return UFP4_ERR_UNSUPPORTED;
+        if (mx_tile_count(rows, cols, !transpose, transpose != 0) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
+    }
+    const uint16_t mask16 = (uint16_t)sign_mask;
+    record(out, format, qrows, red, rht ? 16 : 0, &mask16, 0.0f, rounding);
+    if (rows == 0 || cols == 0) return UFP4_OK;
+    MxQuantJob j{};
+    j.rounding = rounding;
+    j.rht = rht;
+    j.transpose = transpose;
+    j.x = x_dev;
+    j.xrows = rows;
+    j.ld = ld;
+    j.qrows = qrows;
+    j.red = red;
+    fill_sign_xor(sign_mask, j.qa.sign_xor);
+    j.qa.key0 = (uint32_t)seed;
+    j.qa.key1 = (uint32_t)(seed >> 32);
+    j.qa.stream = stream_id;
+    j.codes = out->codes;
+    j.code_pld = out->code_panel_ld;
+    j.scales = out->scales;
+    j.scale_pld = out->scale_panel_ld;
+    return launch_mx_quantize(format, j, stream);
+}
+
+int mx_quantize_grouped_impl(int format, const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose,
+                             const int64_t* group_offsets_dev, int32_t num_groups, int64_t padded_total, int rht,
+                             uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
+                             void* stream) {
+    if (transpose != 0 && transpose != 1) return UFP4_ERR_INVALID_ARG;
+    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
+    if (rht != 0 && rht != 1) return UFP4_ERR_INVALID_ARG;
+    if (sign_mask > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
+    if (padded_total < 0 || !group_offsets_dev) return UFP4_ERR_INVALID_ARG;
+    if (num_groups < 1) return UFP4_ERR_INVALID_ARG;
+    if (num_groups > max_groups_quantize()) return UFP4_ERR_UNSUPPORTED;
+    const int si = check_input(x_dev, rows, cols, ld, 8);
+    if (si != UFP4_OK) return si;
+    // transpose 0: [padded_total, cols], groups of rows on whole panels; transpose 1: [cols, padded_total]
+    const int64_t qrows = transpose ? cols : padded_total;
+    const int64_t red = transpose ? padded_total : cols;
+    if (transpose ? padded_total < rows : padded_total % kPanelRows != 0) return UFP4_ERR_SHAPE;
+    const int st = check_storage(out, format, qrows, red);
+    if (st != UFP4_OK) return st;
+    if (qrows >= (int64_t(1) << 31) || red / 16 >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
+    if (format == UFP4_FMT_E2M1_MX32) {
+        if (micro_quant_tiles(transpose, qrows, red) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
+    } else {
+        if (!transpose && padded_rows(qrows) / 64 > 65535) return UFP4_ERR_UNSUPPORTED;
+        // at most 65535 chunks of 1024 columns of X (its padded columns for the transposed form)
+        if (((transpose ? padded_rows(cols) : cols) + 1023) / 1024 > 65535) return UFP4_ERR_UNSUPPORTED;
+    }
+    const uint16_t mask16 = (uint16_t)sign_mask;
+    record(out, format, qrows, red, rht ? 16 : 0, &mask16, 0.0f, rounding,
+           transpose ? UFP4_LAYOUT_GROUPED_RED : UFP4_LAYOUT_GROUPED_ROWS);
+    if (qrows == 0 || red == 0) return UFP4_OK;
+    MxQuantJob j{};
+    j.rounding = rounding;
+    j.rht = rht;
+    j.transpose = transpose;
+    j.x = x_dev;
+    j.xrows = rows;
+    j.ld = ld;
+    j.qrows = qrows;
+    j.red = red;
+    j.group_off = group_offsets_dev;
+    j.num_groups = num_groups;
+    fill_sign_xor(sign_mask, j.qa.sign_xor);
+    j.qa.key0 = (uint32_t)seed;
+    j.qa.key1 = (uint32_t)(seed >> 32);
+    j.qa.stream = stream_id;
+    j.codes = out->codes;
+    j.code_pld = out->code_panel_ld;
+    j.scales = out->scales;
+    j.scale_pld = out->scale_panel_ld;
+    return launch_mx_quantize(format, j, stream);
+}
+
+int mx_fwd_y_grouped_impl(int format, const ufp4_qtensor* x, const ufp4_qtensor* w, const int64_t* group_offsets_dev,
+                               int32_t num_groups, int64_t m_total, void* y_dev, int64_t ldc, int out_dtype,
+                               void* stream) {
+    if (!group_offsets_dev || num_groups < 1 || m_total < 0) return UFP4_ERR_INVALID_ARG;
+    int st = check_operands(x, w, format);
+    if (st != UFP4_OK) return st;
+    if (x->layout != UFP4_LAYOUT_GROUPED_ROWS || w->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
+    if (x->red != w->red) return UFP4_ERR_MISMATCH;
+    if (w->rows % num_groups != 0) return UFP4_ERR_SHAPE;
+    const int64_t N = w->rows / num_groups;
+    if (N % kPanelRows != 0) return UFP4_ERR_UNSUPPORTED;  // each group's weight rows start on a panel
+    st = check_output(y_dev, ldc, N, out_dtype, m_total == 0 || N == 0);
+    if (st != UFP4_OK) return st;
+    if (m_total == 0 || N == 0 || x->rows == 0) return UFP4_OK;
+    MxGemmJob j = mx_job(x, w, y_dev, ldc, out_dtype);
+    j.mode = kGemmRaggedM;
+    j.M = m_total;
+    j.N = N;
+    j.nkb = x->red / 32;
+    j.offsets = group_offsets_dev;
+    j.G = num_groups;
+    j.b_group_rows = N;
+    j.b_group_kb = 0;
+    if (!mx_grid_fits(format, ceil_div(x->rows, 256) + num_groups, ceil_div(N, 256))) return UFP4_ERR_UNSUPPORTED;
+    return launch_mx(format, j, stream);
+}
+
+int mx_bwd_dx_grouped_impl(int format, const ufp4_qtensor* dy, const ufp4_qtensor* wt, const int64_t* group_offsets_dev,
+                                int32_t num_groups, int64_t m_total, void* dx_dev, int64_t ldc, int out_dtype,
+                                void* stream) {
+    if (!group_offsets_dev || num_groups < 1 || m_total < 0) return UFP4_ERR_INVALID_ARG;
+    int st = check_operands(dy, wt, format);
+    if (st != UFP4_OK) return st;
+    if (dy->layout != UFP4_LAYOUT_GROUPED_ROWS || wt->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
+    if (wt->red != dy->red * num_groups) return UFP4_ERR_MISMATCH;
+    // a group's blocks of W^T begin with a group of four (the unit of its scales)
+    if (format == UFP4_FMT_E2M1_MX32 && dy->red % 128 != 0) return UFP4_ERR_UNSUPPORTED;
+    st = check_output(dx_dev, ldc, wt->rows, out_dtype, m_total == 0 || wt->rows == 0);
+    if (st != UFP4_OK) return st;
+    if (m_total == 0 || wt->rows == 0 || dy->rows == 0) return UFP4_OK;
+    MxGemmJob j = mx_job(dy, wt, dx_dev, ldc, out_dtype);
+    j.mode = kGemmRaggedM;
+    j.M = m_total;
+    j.N = wt->rows;
+    j.nkb = dy->red / 32;
+    j.offsets = group_offsets_dev;
+    j.G = num_groups;
+    j.b_group_rows = 0;
+    j.b_group_kb = dy->red / 32;
+    if (!mx_grid_fits(format, ceil_div(dy->rows, 256) + num_groups, ceil_div(j.N, 256))) return UFP4_ERR_UNSUPPORTED;
+    return launch_mx(format, j, stream);
+}
+
+int mx_bwd_dw_grouped_impl(int format, const ufp4_qtensor* dyt, const ufp4_qtensor* xt, const int64_t* group_offsets_dev,
+                                int32_t num_groups, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
+    if (!group_offsets_dev || num_groups < 1) return UFP4_ERR_INVALID_ARG;
+    if (num_groups > 65535) return UFP4_ERR_UNSUPPORTED;
+    int st = check_operands(dyt, xt, format);
+    if (st != UFP4_OK) return st;
+    if (dyt->layout != UFP4_LAYOUT_GROUPED_RED || xt->layout != UFP4_LAYOUT_GROUPED_RED) return UFP4_ERR_MISMATCH;
+    if (dyt->red != xt->red) return UFP4_ERR_MISMATCH;
+    st = check_output(dw_dev, ldc, xt->rows, out_dtype, dyt->rows == 0 || xt->rows == 0);
+    if (st != UFP4_OK) return st;
+    if (dyt->rows == 0 || xt->rows == 0) return UFP4_OK;
+    if (!mx_grid_fits(format, ceil_div(dyt->rows, 256), ceil_div(xt->rows, 256))) return UFP4_ERR_UNSUPPORTED;
+    MxGemmJob j = mx_job(dyt, xt, dw_dev, ldc, out_dtype);
+    j.mode = kGemmRaggedK;
+    j.M = dyt->rows;
+    j.N = xt->rows;
+    j.nkb = dyt->red / 32;
+    j.offsets = group_offsets_dev;
+    j.G = num_groups;
+    return launch_mx(format, j, stream);
 }
 
 int grid_levels(int format, float max_fpx) {
@@ -295,17 +499,16 @@ const char* ufp4_version(void) { return "0.3.0"; }
 
 int ufp4_qtensor_bytes(int format, int64_t rows, int64_t red, int64_t* panels, int64_t* code_panel_ld,
                        int64_t* scale_panel_ld, size_t* codes_bytes, size_t* scales_bytes) {
-    if (format != UFP4_FMT_UNIFORM && format != UFP4_FMT_E2M1 && format != UFP4_FMT_UNIFORM_MX32)
-        return UFP4_ERR_INVALID_ARG;
+    if (!known_format(format)) return UFP4_ERR_INVALID_ARG;
     if (rows < 0 || red < 0) return UFP4_ERR_INVALID_ARG;
-    const bool mx = format == UFP4_FMT_UNIFORM_MX32;
-    const int64_t blk = mx ? 32 : 16;
+    const bool mx = one_byte_scales(format);
+    const int64_t blk = block_of(format);
     if (red % blk != 0) return UFP4_ERR_SHAPE;
     const int64_t nkb = red / blk;
     const int64_t p = rows > 0 ? ceil_div(rows, kPanelRows) : 1;
     // a zero-length reduction still gets 16 aligned bytes per panel
-    const int64_t cld = nkb > 0 ? nkb * (mx ? kMxPanelBlockBytes : kPanelBlockBytes) : 16;
-    const int64_t sld = nkb > 0 ? nkb * (mx ? kMxPanelBlockScales : kPanelBlockScales) : (mx ? 16 : 4);
+    const int64_t cld = nkb > 0 ? panel_codes(format, nkb) : 16;
+    const int64_t sld = nkb > 0 ? panel_scales(format, nkb) : (mx ? 16 : 4);
     if (panels) *panels = p;
     if (code_panel_ld) *code_panel_ld = cld;
     if (scale_panel_ld) *scale_panel_ld = sld;
@@ -577,40 +780,36 @@ int ufp4_quantize_dual(int format, const void* x_dev, int64_t rows, int64_t cols
 int ufp4_mx_quantize(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose, int rht,
                      uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
                      void* stream) {
-    if (transpose != 0 && transpose != 1) return UFP4_ERR_INVALID_ARG;
-    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
-    if (rht != 0 && rht != 1) return UFP4_ERR_INVALID_ARG;
-    if (sign_mask > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
-    const int si = check_input(x_dev, rows, cols, ld, 8);
-    if (si != UFP4_OK) return si;
-    const int64_t red = transpose ? rows : cols;
-    const int64_t qrows = transpose ? cols : rows;
-    const int st = check_storage(out, UFP4_FMT_UNIFORM_MX32, qrows, red);
-    if (st != UFP4_OK) return st;
-    if (qrows >= (int64_t(1) << 31) || red / 16 >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    if (!transpose && padded_rows(qrows) / 64 > 65535) return UFP4_ERR_UNSUPPORTED;
-    if (mx_tile_count(rows, cols, !transpose, transpose != 0) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    const uint16_t mask16 = (uint16_t)sign_mask;
-    record(out, UFP4_FMT_UNIFORM_MX32, qrows, red, rht ? 16 : 0, &mask16, 0.0f, rounding);
-    if (rows == 0 || cols == 0) return UFP4_OK;
-    MxQuantJob j{};
-    j.rounding = rounding;
-    j.rht = rht;
-    j.transpose = transpose;
-    j.x = x_dev;
-    j.xrows = rows;
-    j.ld = ld;
-    j.qrows = qrows;
-    j.red = red;
-    fill_sign_xor(sign_mask, j.qa.sign_xor);
-    j.qa.key0 = (uint32_t)seed;
-    j.qa.key1 = (uint32_t)(seed >> 32);
-    j.qa.stream = stream_id;
-    j.codes = out->codes;
-    j.code_pld = out->code_panel_ld;
-    j.scales = out->scales;
-    j.scale_pld = out->scale_panel_ld;
-    return status_of(launch_quantize_mx(j, static_cast<hipStream_t>(stream)));
+    return mx_quantize_impl(UFP4_FMT_UNIFORM_MX32, x_dev, rows, cols, ld, transpose, rht, sign_mask, rounding, seed, stream_id,
+                            out, stream);
+}
+
+int ufp4_mx_quantize_grouped(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose,
+                             const int64_t* group_offsets_dev, int32_t num_groups, int64_t padded_total, int rht,
+                             uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
+                             void* stream) {
+    return mx_quantize_grouped_impl(UFP4_FMT_UNIFORM_MX32, x_dev, rows, cols, ld, transpose, group_offsets_dev, num_groups,
+                                    padded_total, rht, sign_mask, rounding, seed, stream_id, out, stream);
+}
+
+int ufp4_mx_gemm_fwd_y_grouped(const ufp4_qtensor* x, const ufp4_qtensor* w, const int64_t* group_offsets_dev,
+                               int32_t num_groups, int64_t m_total, void* y_dev, int64_t ldc, int out_dtype,
+                               void* stream) {
+    return mx_fwd_y_grouped_impl(UFP4_FMT_UNIFORM_MX32, x, w, group_offsets_dev, num_groups, m_total, y_dev, ldc, out_dtype,
+                                 stream);
+}
+
+int ufp4_mx_gemm_bwd_dx_grouped(const ufp4_qtensor* dy, const ufp4_qtensor* wt, const int64_t* group_offsets_dev,
+                                int32_t num_groups, int64_t m_total, void* dx_dev, int64_t ldc, int out_dtype,
+                                void* stream) {
+    return mx_bwd_dx_grouped_impl(UFP4_FMT_UNIFORM_MX32, dy, wt, group_offsets_dev, num_groups, m_total, dx_dev, ldc,
+                                  out_dtype, stream);
+}
+
+int ufp4_mx_gemm_bwd_dw_grouped(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, const int64_t* group_offsets_dev,
+                                int32_t num_groups, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
+    return mx_bwd_dw_grouped_impl(UFP4_FMT_UNIFORM_MX32, dyt, xt, group_offsets_dev, num_groups, dw_dev, ldc, out_dtype,
+                                  stream);
 }
 
 int ufp4_mx_quantize_dual(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int rht_rows,
@@ -658,141 +857,126 @@ int ufp4_mx_quantize_dual(const void* x_dev, int64_t rows, int64_t cols, int64_t
     return status_of(launch_quantize_mx_dual(j, static_cast<hipStream_t>(stream)));
 }
 
-int ufp4_mx_quantize_grouped(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose,
-                             const int64_t* group_offsets_dev, int32_t num_groups, int64_t padded_total, int rht,
-                             uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
-                             void* stream) {
-    if (transpose != 0 && transpose != 1) return UFP4_ERR_INVALID_ARG;
-    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
-    if (rht != 0 && rht != 1) return UFP4_ERR_INVALID_ARG;
-    if (sign_mask > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
-    if (padded_total < 0 || !group_offsets_dev) return UFP4_ERR_INVALID_ARG;
-    if (num_groups < 1) return UFP4_ERR_INVALID_ARG;
-    if (num_groups > max_groups_quantize()) return UFP4_ERR_UNSUPPORTED;
-    const int si = check_input(x_dev, rows, cols, ld, 8);
-    if (si != UFP4_OK) return si;
-    // transpose 0: [padded_total, cols], groups of rows on whole panels; transpose 1: [cols, padded_total]
-    const int64_t qrows = transpose ? cols : padded_total;
-    const int64_t red = transpose ? padded_total : cols;
-    if (transpose ? padded_total < rows : padded_total % kPanelRows != 0) return UFP4_ERR_SHAPE;
-    const int st = check_storage(out, UFP4_FMT_UNIFORM_MX32, qrows, red);
-    if (st != UFP4_OK) return st;
-    if (qrows >= (int64_t(1) << 31) || red / 16 >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    if (!transpose && padded_rows(qrows) / 64 > 65535) return UFP4_ERR_UNSUPPORTED;
-    // at most 65535 chunks of 1024 columns of X (its padded columns for the transposed form)
-    if (((transpose ? padded_rows(cols) : cols) + 1023) / 1024 > 65535) return UFP4_ERR_UNSUPPORTED;
-    const uint16_t mask16 = (uint16_t)sign_mask;
-    record(out, UFP4_FMT_UNIFORM_MX32, qrows, red, rht ? 16 : 0, &mask16, 0.0f, rounding,
-           transpose ? UFP4_LAYOUT_GROUPED_RED : UFP4_LAYOUT_GROUPED_ROWS);
-    if (qrows == 0 || red == 0) return UFP4_OK;
-    MxQuantJob j{};
-    j.rounding = rounding;
-    j.rht = rht;
-    j.transpose = transpose;
-    j.x = x_dev;
-    j.xrows = rows;
-    j.ld = ld;
-    j.qrows = qrows;
-    j.red = red;
-    j.group_off = group_offsets_dev;
-    j.num_groups = num_groups;
-    fill_sign_xor(sign_mask, j.qa.sign_xor);
-    j.qa.key0 = (uint32_t)seed;
-    j.qa.key1 = (uint32_t)(seed >> 32);
-    j.qa.stream = stream_id;
-    j.codes = out->codes;
-    j.code_pld = out->code_panel_ld;
-    j.scales = out->scales;
-    j.scale_pld = out->scale_panel_ld;
-    return status_of(launch_quantize_mx(j, static_cast<hipStream_t>(stream)));
-}
-
-int ufp4_mx_gemm_fwd_y_grouped(const ufp4_qtensor* x, const ufp4_qtensor* w, const int64_t* group_offsets_dev,
-                               int32_t num_groups, int64_t m_total, void* y_dev, int64_t ldc, int out_dtype,
-                               void* stream) {
-    if (!group_offsets_dev || num_groups < 1 || m_total < 0) return UFP4_ERR_INVALID_ARG;
-    int st = check_operands(x, w, true);
-    if (st != UFP4_OK) return st;
-    if (x->layout != UFP4_LAYOUT_GROUPED_ROWS || w->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
-    if (x->red != w->red) return UFP4_ERR_MISMATCH;
-    if (w->rows % num_groups != 0) return UFP4_ERR_SHAPE;
-    const int64_t N = w->rows / num_groups;
-    if (N % kPanelRows != 0) return UFP4_ERR_UNSUPPORTED;  // each group's weight rows start on a panel
-    st = check_output(y_dev, ldc, N, out_dtype, m_total == 0 || N == 0);
-    if (st != UFP4_OK) return st;
-    if (m_total == 0 || N == 0 || x->rows == 0) return UFP4_OK;
-    MxGemmJob j = mx_job(x, w, y_dev, ldc, out_dtype);
-    j.mode = kGemmRaggedM;
-    j.M = m_total;
-    j.N = N;
-    j.nkb = x->red / 32;
-    j.offsets = group_offsets_dev;
-    j.G = num_groups;
-    j.b_group_rows = N;
-    j.b_group_kb = 0;
-    if ((ceil_div(x->rows, 256) + num_groups) * ceil_div(N, 256) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    return status_of(launch_gemm_mx(j, static_cast<hipStream_t>(stream)));
-}
-
-int ufp4_mx_gemm_bwd_dx_grouped(const ufp4_qtensor* dy, const ufp4_qtensor* wt, const int64_t* group_offsets_dev,
-                                int32_t num_groups, int64_t m_total, void* dx_dev, int64_t ldc, int out_dtype,
-                                void* stream) {
-    if (!group_offsets_dev || num_groups < 1 || m_total < 0) return UFP4_ERR_INVALID_ARG;
-    int st = check_operands(dy, wt, true);
-    if (st != UFP4_OK) return st;
-    if (dy->layout != UFP4_LAYOUT_GROUPED_ROWS || wt->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
-    if (wt->red != dy->red * num_groups) return UFP4_ERR_MISMATCH;
-    st = check_output(dx_dev, ldc, wt->rows, out_dtype, m_total == 0 || wt->rows == 0);
-    if (st != UFP4_OK) return st;
-    if (m_total == 0 || wt->rows == 0 || dy->rows == 0) return UFP4_OK;
-    MxGemmJob j = mx_job(dy, wt, dx_dev, ldc, out_dtype);
-    j.mode = kGemmRaggedM;
-    j.M = m_total;
-    j.N = wt->rows;
-    j.nkb = dy->red / 32;
-    j.offsets = group_offsets_dev;
-    j.G = num_groups;
-    j.b_group_rows = 0;
-    j.b_group_kb = dy->red / 32;
-    if ((ceil_div(dy->rows, 256) + num_groups) * ceil_div(j.N, 256) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    return status_of(launch_gemm_mx(j, static_cast<hipStream_t>(stream)));
-}
-
-int ufp4_mx_gemm_bwd_dw_grouped(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, const int64_t* group_offsets_dev,
-                                int32_t num_groups, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
-    if (!group_offsets_dev || num_groups < 1) return UFP4_ERR_INVALID_ARG;
-    if (num_groups > 65535) return UFP4_ERR_UNSUPPORTED;
-    int st = check_operands(dyt, xt, true);
-    if (st != UFP4_OK) return st;
-    if (dyt->layout != UFP4_LAYOUT_GROUPED_RED || xt->layout != UFP4_LAYOUT_GROUPED_RED) return UFP4_ERR_MISMATCH;
-    if (dyt->red != xt->red) return UFP4_ERR_MISMATCH;
-    st = check_output(dw_dev, ldc, xt->rows, out_dtype, dyt->rows == 0 || xt->rows == 0);
-    if (st != UFP4_OK) return st;
-    if (dyt->rows == 0 || xt->rows == 0) return UFP4_OK;
-    if (ceil_div(dyt->rows, 256) * ceil_div(xt->rows, 256) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    MxGemmJob j = mx_job(dyt, xt, dw_dev, ldc, out_dtype);
-    j.mode = kGemmRaggedK;
-    j.M = dyt->rows;
-    j.N = xt->rows;
-    j.nkb = dyt->red / 32;
-    j.offsets = group_offsets_dev;
-    j.G = num_groups;
-    return status_of(launch_gemm_mx(j, static_cast<hipStream_t>(stream)));
-}
-
 int ufp4_mx_gemm_fwd_y(const ufp4_qtensor* x, const ufp4_qtensor* w, void* y_dev, int64_t ldc, int out_dtype,
                        void* stream) {
-    return mx_gemm_impl(x, w, y_dev, ldc, out_dtype, stream);
+    return mx_gemm_impl(UFP4_FMT_UNIFORM_MX32, x, w, y_dev, ldc, out_dtype, stream);
 }
 
 int ufp4_mx_gemm_bwd_dx(const ufp4_qtensor* dy, const ufp4_qtensor* wt, void* dx_dev, int64_t ldc, int out_dtype,
                         void* stream) {
-    return mx_gemm_impl(dy, wt, dx_dev, ldc, out_dtype, stream);  // dX [M, K] = dY [M, N] . (W^T [K, N])^T
+    return mx_gemm_impl(UFP4_FMT_UNIFORM_MX32, dy, wt, dx_dev, ldc, out_dtype, stream);  // dX [M, K] = dY [M, N] . (W^T [K, N])^T
 }
 
 int ufp4_mx_gemm_bwd_dw(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, void* dw_dev, int64_t ldc, int out_dtype,
                         void* stream) {
-    return mx_gemm_impl(dyt, xt, dw_dev, ldc, out_dtype, stream);  // dW [N, K] = dY^T [N, M] . (X^T [K, M])^T
+    return mx_gemm_impl(UFP4_FMT_UNIFORM_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream);  // dW [N, K] = dY^T [N, M] . (X^T [K, M])^T
+}
+
+int ufp4_mxfp4_quantize(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose, int rht,
+                        uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
+                        void* stream) {
+    return mx_quantize_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, transpose, rht, sign_mask, rounding, seed, stream_id,
+                            out, stream);
+}
+
+int ufp4_mxfp4_quantize_grouped(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose,
+                                const int64_t* group_offsets_dev, int32_t num_groups, int64_t padded_total, int rht,
+                                uint32_t sign_mask, int rounding, uint64_t seed, uint32_t stream_id, ufp4_qtensor* out,
+                                void* stream) {
+    return mx_quantize_grouped_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, transpose, group_offsets_dev, num_groups,
+                                    padded_total, rht, sign_mask, rounding, seed, stream_id, out, stream);
+}
+
+int ufp4_mxfp4_gemm_fwd_y_grouped(const ufp4_qtensor* x, const ufp4_qtensor* w, const int64_t* group_offsets_dev,
+                                  int32_t num_groups, int64_t m_total, void* y_dev, int64_t ldc, int out_dtype,
+                                  void* stream) {
+    return mx_fwd_y_grouped_impl(UFP4_FMT_E2M1_MX32, x, w, group_offsets_dev, num_groups, m_total, y_dev, ldc, out_dtype,
+                                 stream);
+}
+
+int ufp4_mxfp4_gemm_bwd_dx_grouped(const ufp4_qtensor* dy, const ufp4_qtensor* wt, const int64_t* group_offsets_dev,
+                                   int32_t num_groups, int64_t m_total, void* dx_dev, int64_t ldc, int out_dtype,
+                                   void* stream) {
+    return mx_bwd_dx_grouped_impl(UFP4_FMT_E2M1_MX32, dy, wt, group_offsets_dev, num_groups, m_total, dx_dev, ldc,
+                                  out_dtype, stream);
+}
+
+int ufp4_mxfp4_gemm_bwd_dw_grouped(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, const int64_t* group_offsets_dev,
+                                   int32_t num_groups, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
+    return mx_bwd_dw_grouped_impl(UFP4_FMT_E2M1_MX32, dyt, xt, group_offsets_dev, num_groups, dw_dev, ldc, out_dtype,
+                                  stream);
+}
+
+int ufp4_mxfp4_quantize_dual(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int rht_rows, uint32_t sign_mask_rows,
+                             uint32_t stream_rows, int rht_cols, uint32_t sign_mask_cols, uint32_t stream_cols, int rounding,
+                             uint64_t seed, ufp4_qtensor* out_rows, ufp4_qtensor* out_cols, void* stream) {
+    if (out_rows == out_cols) return UFP4_ERR_INVALID_ARG;
+    // both outputs' checks before either launch
+    int st = check_input(x_dev, rows, cols, ld, 8);
+    if (st == UFP4_OK) st = check_storage(out_rows, UFP4_FMT_E2M1_MX32, rows, cols);
+    if (st == UFP4_OK) st = check_storage(out_cols, UFP4_FMT_E2M1_MX32, cols, rows);
+    if (st != UFP4_OK) return st;
+    if ((rht_cols != 0 && rht_cols != 1) || sign_mask_cols > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
+    if (cols >= (int64_t(1) << 31) || micro_quant_tiles(1, cols, rows) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
+    st = mx_quantize_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, 0, rht_rows, sign_mask_rows, rounding, seed, stream_rows,
+                          out_rows, stream);
+    if (st != UFP4_OK) return st;
+    return mx_quantize_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, 1, rht_cols, sign_mask_cols, rounding, seed, stream_cols,
+                            out_cols, stream);
+}
+
+int ufp4_mxfp4_dequantize(const ufp4_qtensor* q, void* out_dev, int64_t ldo, void* stream) {
+    if (!q) return UFP4_ERR_INVALID_ARG;
+    if (!known_format(q->format)) return UFP4_ERR_INVALID_ARG;
+    if (q->format != UFP4_FMT_E2M1_MX32) return UFP4_ERR_MISMATCH;
+    int st = check_storage(q, q->format, q->rows, q->red);
+    if (st != UFP4_OK) return st;
+    st = check_input(out_dev, q->rows, q->red, ldo, 8);
+    if (st != UFP4_OK) return st;
+    if (micro_decode_tiles(q->rows, q->red) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
+    return status_of(launch_dequantize_mxfp4(q->codes, q->code_panel_ld, q->scales, q->scale_panel_ld, q->rows, q->red, out_dev,
+                                             ldo, static_cast<hipStream_t>(stream)));
+}
+
+int ufp4_mxfp4_linear(const void* x_dev, int64_t rows, int64_t ldx, const ufp4_qtensor* w, void* y_dev, int64_t ldc,
+                      int out_dtype, void* stream) {
+    int st = check_operands(w, w, UFP4_FMT_E2M1_MX32);
+    if (st != UFP4_OK) return st;
+    if (w->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
+    st = check_input(x_dev, rows, w->red, ldx, 8);
+    if (st == UFP4_OK) st = check_output(y_dev, ldc, w->rows, out_dtype, rows == 0 || w->rows == 0);
+    if (st != UFP4_OK) return st;
+    if (rows > kLinearTokens || w->rht_block != 0) return UFP4_ERR_UNSUPPORTED;
+    if (rows == 0 || w->rows == 0) return UFP4_OK;
+    LinearJob j{};
+    j.out_dtype = out_dtype;
+    j.M = (int)rows;
+    j.x = static_cast<const uint16_t*>(x_dev);
+    j.ldx = ldx;
+    j.w = static_cast<const uint8_t*>(w->codes);
+    j.w_pld = w->code_panel_ld;
+    j.ws = static_cast<const uint8_t*>(w->scales);
+    j.ws_pld = w->scale_panel_ld;
+    j.N = w->rows;
+    j.nkb = w->red / 32;
+    j.y = y_dev;
+    j.ldc = ldc;
+    return status_of(launch_linear_mxfp4(j, static_cast<hipStream_t>(stream)));
+}
+
+int ufp4_mxfp4_gemm_fwd_y(const ufp4_qtensor* x, const ufp4_qtensor* w, void* y_dev, int64_t ldc, int out_dtype,
+                          void* stream) {
+    return mx_gemm_impl(UFP4_FMT_E2M1_MX32, x, w, y_dev, ldc, out_dtype, stream);
+}
+
+int ufp4_mxfp4_gemm_bwd_dx(const ufp4_qtensor* dy, const ufp4_qtensor* wt, void* dx_dev, int64_t ldc, int out_dtype,
+                           void* stream) {
+    return mx_gemm_impl(UFP4_FMT_E2M1_MX32, dy, wt, dx_dev, ldc, out_dtype, stream);
+}
+
+int ufp4_mxfp4_gemm_bwd_dw(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, void* dw_dev, int64_t ldc, int out_dtype,
+                           void* stream) {
+    return mx_gemm_impl(UFP4_FMT_E2M1_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream);
 }
 
 int ufp4_gemm_fwd_y(const ufp4_qtensor* x, const ufp4_qtensor* w, void* y_dev, int64_t ldc, int out_dtype,
@@ -813,7 +997,7 @@ int ufp4_gemm_bwd_dw(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, void* dw_d
 int ufp4_gemm_fwd_y_grouped(const ufp4_qtensor* x, const ufp4_qtensor* w, const int64_t* group_offsets_dev,
                             int32_t num_groups, void* y_dev, int64_t ldc, int out_dtype, void* stream) {
     if (!group_offsets_dev || num_groups < 1) return UFP4_ERR_INVALID_ARG;
-    int st = check_operands(x, w, false);
+    int st = check_operands(x, w, kFp32Scales);
     if (st != UFP4_OK) return st;
     if (x->layout != UFP4_LAYOUT_PLAIN || w->layout != UFP4_LAYOUT_PLAIN) return UFP4_ERR_MISMATCH;
     if (x->red != w->red) return UFP4_ERR_MISMATCH;
@@ -834,7 +1018,7 @@ int ufp4_gemm_bwd_dx_grouped(const ufp4_qtensor* dy, const ufp4_qtensor* wt, con
                              int32_t num_groups, void* dx_dev, int64_t ldc, int out_dtype, void* stream) {
     if (!group_offsets_dev || num_groups < 1) return UFP4_ERR_INVALID_ARG;
     // A = dY [M_total, N]; B = W^T [K, G*N], group g uses reduction columns [g*N, (g+1)*N)
-    int st = check_operands(dy, wt, false);
+    int st = check_operands(dy, wt, kFp32Scales);
     if (st != UFP4_OK) return st;
     // dY's reduction (N) is a multiple of 16, so W^T's equal groups need no padding: its grouped-transposed
     // and plain transposed forms coincide and both are accepted
@@ -856,7 +1040,7 @@ int ufp4_gemm_bwd_dw_grouped(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, co
     if (!group_offsets_dev || num_groups < 1) return UFP4_ERR_INVALID_ARG;
     if (num_groups > 65535) return UFP4_ERR_UNSUPPORTED;
     // A = dY^T [N, R], B = X^T [K, R]; group g reduces over [pad_g, pad_{g+1}) of that axis
-    int st = check_operands(dyt, xt, false);
+    int st = check_operands(dyt, xt, kFp32Scales);
     if (st != UFP4_OK) return st;
     // the kernel reduces each group over its tokens padded to 16, the layout ufp4_quantize_grouped_t writes
     if (dyt->layout != UFP4_LAYOUT_GROUPED_RED || xt->layout != UFP4_LAYOUT_GROUPED_RED) return UFP4_ERR_MISMATCH;

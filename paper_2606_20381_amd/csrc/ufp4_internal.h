@@ -199,6 +199,33 @@ struct GemmJob {
 
 hipError_t launch_gemm(const GemmJob& job, hipStream_t stream);
 
+// Microscaled 4-bit operands (E2M1 levels, one E8M0 scale per 32): in a panel the 32-block b of all 128 rows holds 128 x 16
+// code bytes at b * 2048; scales in groups of four blocks, 512 bytes each (layout in ufp4_mxfp4.hip).
+constexpr int64_t kMicroBlockBytes = kPanelRows * 16;
+constexpr int64_t kMicroGroupScales = kPanelRows * 4;
+hipError_t launch_quantize_mxfp4(const MxQuantJob& job, hipStream_t stream);
+hipError_t launch_dequantize_mxfp4(const void* codes, int64_t code_pld, const void* scales, int64_t scale_pld, int64_t rows,
+                                   int64_t red, void* out, int64_t ldo, hipStream_t stream);
+int64_t micro_quant_tiles(int transpose, int64_t qrows, int64_t red);  // workgroups
+int64_t micro_decode_tiles(int64_t rows, int64_t red);
+hipError_t launch_gemm_mxfp4(const MxGemmJob& job, hipStream_t stream);
+
+// y [M, N] = Q(x) W^T, M <= kLinearTokens tokens of bf16 x, W [N, nkb * 32] a plain microscaled 4-bit operand.
+constexpr int kLinearTokens = 16;
+struct LinearJob {
+    int out_dtype, M;
+    const uint16_t* x;
+    int64_t ldx;
+    const uint8_t* w;
+    int64_t w_pld;
+    const uint8_t* ws;
+    int64_t ws_pld;
+    int64_t N, nkb;
+    void* y;
+    int64_t ldc;
+};
+hipError_t launch_linear_mxfp4(const LinearJob& job, hipStream_t stream);
+
 // Layer norm over rows of fp32 or bf16 numbers (any leading dimension and alignment); null gamma / beta: 1 / 0.
 struct NormJob {
     int bf16, w_bf16;

@@ -1,0 +1,384 @@
+// Microscaled 4-bit floating point (the OCP Microscaling format MXFP4): E2M1 levels with one E8M0 scale per 32 values along
+// the reduction axis, the operands that gfx950's scaled matrix instruction takes as they are.
+//
+//   E = max(floor(log2 amax) - 2, -127), level = nearest of 0, .5, 1, 1.5, 2, 3, 4, 6 to x 2^-E (ties to the even code, cut
+//   at 6), or stochastically one of its two neighbours; a block that holds an infinity or a NaN gets the scale NaN.
+//
+// Layout (panels of 128 rows): block b of row 128 p + i has its 16 code bytes at p * code_panel_ld + b * 2048 + i * 16 -- what
+// one lane of the 32 x 32 x 64 matrix instruction holds, so the GEMM's LDS reads are 16 bytes of consecutive rows -- and its
+// scale at p * scale_panel_ld + (b / 4) * 512 + (b % 2) * 256 + i * 2 + (b / 2) % 2: the two scales that a lane needs over
+// four blocks (128 of the reduction) lie together. Scale bytes of the blocks that fill up the last four are 0.
+//
+// HBM bound: 2 bytes read and 17/32 written per value. amax is a packed 16-bit integer maximum of the bf16 patterns (their
+// order is that of the magnitudes) and the conversion one instruction per two values, so the plain form has little to compute;
+// rotated (fp64 sums, as the other quantizers) or stochastic (Philox) it is bound by vector issue.
+
+#include "ufp4_internal.h"
+#include "ufp4_device.h"
+#include "ufp4_mxfp4.h"
+
+namespace ufp4 {
+
+namespace {
+
+// The E2M1 code of v (|v| < 8, cut at 6) between its neighbours by a 16-bit draw: the upper one of the signed pair
+// g_a <= v < g_b iff u / 2^16 < (v - g_a) / (g_b - g_a). In units of the pair's spacing from the lower end `base` of its
+// binade, r = |v|: both comparisons are of exact numbers. A level never moves.
+__device__ __forceinline__ uint32_t fp4_sr(float v, uint32_t u16) {
+    const float a = __builtin_fminf(__builtin_fabsf(v), 6.0f), u = (float)u16 * 0x1p-16f;
+    const bool s1 = a < 2.0f, s2 = a < 4.0f;
+    const float r = (a - (s1 ? 0.0f : s2 ? 2.0f : 4.0f)) * (s1 ? 2.0f : s2 ? 1.0f : 0.5f);
+    const float j = floorf(r);
+    const bool up = v >= 0.0f ? j + u < r : !(r < j + 1.0f - u);
+    return (uint32_t)((s1 ? 0 : s2 ? 4 : 6) + (int)j + (up ? 1 : 0)) | (v < 0.0f ? 8u : 0u);
+}
+
+// Sixteen values of a block (half of it) on their way to codes.
+template <bool RHT>
+struct Half {
+    uint32_t w[8];  // bf16 pairs
+    float y[RHT ? 16 : 1];
+
+    // `unit` times the sums of the block-16 RHT, in fp64 as in the other quantizers, rounded once
+    __device__ __forceinline__ void rotate(const QuantArgs& qa, double unit) {
+        double d[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t p = w[j] ^ qa.sign_xor[j];
+            d[2 * j] = (double)bf16_lo(p);
+            d[2 * j + 1] = (double)bf16_hi(p);
+        }
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(i & s)) {
+                    const double a = d[i], b = d[i + s];
+                    d[i] = a + b;
+                    d[i + s] = a - b;
+                }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = (float)(d[i] * unit);
+    }
+
+    // exponent field of the largest magnitude
+    __device__ __forceinline__ uint32_t exponent() const {
+        uint32_t m = 0;
+        if constexpr (RHT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t b = __float_as_uint(y[i]) & 0x7FFFFFFFu;
+                m = b > m ? b : m;
+            }
+            return m >> 23;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max_u16x2(m, w[j] & 0x7FFF7FFFu);
+            const uint32_t lo = m & 0xFFFFu, hi = m >> 16;
+            return (lo > hi ? lo : hi) >> 7;
+        }
+    }
+
+    __device__ __forceinline__ bool finite_inputs() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max_u16x2(m, w[j] & 0x7FFF7FFFu);
+        return (m & 0xFFFFu) < 0x7F80u && (m >> 16) < 0x7F80u;
+    }
+
+    // 16 codes at the scale 2^(e8 - 127), element 2j in the low nibble of byte j
+    template <int ROUND>
+    __device__ __forceinline__ uint2 encode(uint32_t e8, const QuantArgs& qa, uint32_t blk16, uint32_t row) const {
+        uint32_t c[2] = {0, 0};
+        if constexpr (ROUND == kRoundSR) {
+            const Philox4 p0 = philox4x32_10(blk16, row, 0u, qa.stream, qa.key0, qa.key1);
+            const Philox4 p1 = philox4x32_10(blk16, row, 1u, qa.stream, qa.key0, qa.key1);
+            const uint32_t u[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+            const float mult = __uint_as_float((254u - e8) << 23);  // 2^-E: a normal number (e8 <= 252)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float v;
+                if constexpr (RHT) v = y[i];
+                else v = i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+                const uint32_t draw = i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xFFFFu;
+                c[i >> 3] |= fp4_sr(__fmul_rn(v, mult), draw) << (4 * (i & 7));
+            }
+        } else {
+            const float scale = __uint_as_float(e8 << 23);  // the instruction reads the exponent field only
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (RHT) {
+                    c[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[h], y[8 * h], y[8 * h + 1], scale, 0);
+                    c[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[h], y[8 * h + 2], y[8 * h + 3], scale, 1);
+                    c[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[h], y[8 * h + 4], y[8 * h + 5], scale, 2);
+                    c[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c[h], y[8 * h + 6], y[8 * h + 7], scale, 3);
+                } else {
+                    c[h] = fp4_pair<0>(c[h], w[4 * h], scale);
+                    c[h] = fp4_pair<1>(c[h], w[4 * h + 1], scale);
+                    c[h] = fp4_pair<2>(c[h], w[4 * h + 2], scale);
+                    c[h] = fp4_pair<3>(c[h], w[4 * h + 3], scale);
+                }
+            }
+        }
+        return make_uint2(c[0], c[1]);
+    }
+};
+
+constexpr double kUnit = 0.25;            // 1/4 = 1/sqrt(16)
+constexpr int kOverflowShift = 8;         // rotated values past FLT_MAX are taken 2^-8 as large
+constexpr double kUnitSmall = 0x1p-10;
+
+// ------------------------------------------------------------------------------------------------
+// Rowwise: a workgroup takes 64 rows x 256 columns (8 blocks). A thread takes 16 values of a row, its neighbour the block's
+// other half; loads are 512-byte runs, and codes and scales go through LDS, so that stores are runs of a block's rows (1 KiB
+// of codes) instead of 8 bytes each.
+// ------------------------------------------------------------------------------------------------
+constexpr int kRowsTile = 64, kColsTile = 256;
+constexpr int kCodeStride = kRowsTile * 16 + 64;  // a block's codes in LDS: 64 bytes apart in the banks
+
+struct MicroOut {
+    uint8_t* codes;
+    int64_t code_pld;
+    uint8_t* scales;
+    int64_t scale_pld;
+};
+
+template <int ROUND, bool RHT, bool GROUPED>
+__global__ __launch_bounds__(256) void micro_rows_kernel(const uint16_t* __restrict__ x, int64_t xrows, int64_t cols,
+                                                         int64_t ld, int64_t col_tiles, const int64_t* offsets, int G,
+                                                         QuantArgs qa, MicroOut o) {
+    __shared__ __align__(16) uint8_t s_codes[8 * kCodeStride];
+    __shared__ __align__(16) uint8_t s_scales[kRowsTile * 8];  // [group of 4][b % 2][row][2]
+    const int tid = threadIdx.x;
+    const int64_t rt = blockIdx.x / col_tiles, ct = blockIdx.x - rt * col_tiles;
+    const int64_t row0 = rt * kRowsTile, c0 = ct * kColsTile;
+    int64_t src = row0, left = xrows - row0;  // first row of x, rows that exist
+    if constexpr (GROUPED) {
+        if (!padded_position<128>(offsets, G, row0, src, left)) left = 0;
+        if (src < 0 || src >= xrows) left = 0;
+        if (left > xrows - src) left = xrows - src;
+    }
+    const int part = tid & 15, r0 = tid >> 4;  // 16 columns, row within 16
+    const int64_t col = c0 + part * 16;
+    Half<RHT> v[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int r = p * 16 + r0;
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;
+        if (r < left && col < cols) {
+            const uint4* const q = reinterpret_cast<const uint4*>(x + (src + r) * ld + col);
+            a = q[0];
+            b = q[1];
+        }
+        v[p].w[0] = a.x; v[p].w[1] = a.y; v[p].w[2] = a.z; v[p].w[3] = a.w;
+        v[p].w[4] = b.x; v[p].w[5] = b.y; v[p].w[6] = b.z; v[p].w[7] = b.w;
+    }
+    const int blk = part >> 1, half = part & 1;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int r = p * 16 + r0;
+        if constexpr (RHT) v[p].rotate(qa, kUnit);
+        uint32_t ef = v[p].exponent();
+        uint32_t other = __shfl_xor(ef, 1, 64);
+        ef = ef > other ? ef : other;
+        uint32_t e8 = scale_byte(ef), at = e8;  // stored scale, and the scale that the values in hand are taken at
+        if constexpr (RHT) {
+            if (__builtin_expect(ef == 255u, 0)) {  // a rotated value past FLT_MAX (or an input that is not finite)
+                const int fine = v[p].finite_inputs() ? 1 : 0;
+                v[p].rotate(qa, kUnitSmall);
+                uint32_t e = v[p].exponent();
+                other = __shfl_xor(e, 1, 64);
+                e = e > other ? e : other;
+                if (fine & __shfl_xor(fine, 1, 64)) {
+                    at = scale_byte(e);
+                    e8 = at + kOverflowShift;
+                }
+            }
+        }
+        const int64_t grow = GROUPED ? src + r : row0 + r;  // the SR counters number x's rows
+        uint2 c = v[p].template encode<ROUND>(at, qa, (uint32_t)(col >> 4), (uint32_t)grow);
+        if (e8 == kNaNScale) c = make_uint2(0, 0);
+        *reinterpret_cast<uint2*>(s_codes + blk * kCodeStride + r * 16 + half * 8) = c;
+        if (half == 0) s_scales[(blk >> 2) * 256 + (blk & 1) * 128 + r * 2 + ((blk >> 1) & 1)] = (uint8_t)e8;
+    }
+    __syncthreads();
+    const int64_t nkb = cols / 32, b0 = c0 / 32;
+    const int64_t panel = row0 / 128;
+    const int half_panel = (int)(row0 / 64) & 1;
+    uint8_t* const codes = o.codes + panel * o.code_pld + half_panel * 1024;
+    uint8_t* const scales = o.scales + panel * o.scale_pld + half_panel * 128;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int u = k * 256 + tid, b = u >> 6, r = u & 63;
+        if (b0 + b < nkb)
+            *reinterpret_cast<uint4*>(codes + (b0 + b) * 2048 + r * 16) =
+                *reinterpret_cast<const uint4*>(s_codes + b * kCodeStride + r * 16);
+    }
+    if (tid < 32) {
+        const int g = tid >> 4, h = (tid >> 3) & 1, k = tid & 7;
+        if (b0 + g * 4 < nkb)
+            *reinterpret_cast<uint4*>(scales + (b0 / 4 + g) * 512 + h * 256 + k * 16) =
+                *reinterpret_cast<const uint4*>(s_scales + g * 256 + h * 128 + k * 16);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Transposed: a workgroup takes 128 rows x 128 columns of x, each wave one block (32 rows); a lane holds two columns of it in
+// registers (32 loads of 256 contiguous bytes per wave) and stores 2 x 16 bytes of codes, the wave 2 KiB in one run.
+// ------------------------------------------------------------------------------------------------
+template <int ROUND, bool RHT, bool GROUPED>
+__global__ __launch_bounds__(256) void micro_cols_kernel(const uint16_t* __restrict__ x, int64_t xrows, int64_t cols,
+                                                         int64_t ld, int64_t nkb, int64_t col_tiles, const int64_t* offsets,
+                                                         int G, QuantArgs qa, MicroOut o) {
+    __shared__ __align__(16) uint8_t s_scales[512];  // [b % 2][row][2]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t g4 = blockIdx.x / col_tiles, panel = blockIdx.x - g4 * col_tiles;
+    const int64_t b = g4 * 4 + wave, col = panel * 128 + 2 * lane;
+    int64_t src = b * 32, left = b < nkb ? 32 : 0;
+    if constexpr (GROUPED) {
+        if (b >= nkb || !padded_position<32>(offsets, G, b * 32, src, left)) left = 0;
+    }
+    if (src < 0 || src >= xrows) left = 0;
+    if (left > xrows - src) left = xrows - src;
+    uint32_t m[32];
+    const uint16_t* const p = x + src * ld + col;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        m[i] = 0;
+        if (i < left) {
+            if (col + 1 < cols) m[i] = *reinterpret_cast<const uint32_t*>(p + i * ld);
+            else if (col < cols) m[i] = p[i * ld];
+        }
+    }
+    uint4 out[2];
+    uint32_t e8c[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {  // the lane's columns
+        Half<RHT> v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[h].w[j] = c == 0 ? __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x05040100u)
+                                   : __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x07060302u);
+        uint32_t ef[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (RHT) v[h].rotate(qa, kUnit);
+            ef[h] = v[h].exponent();
+        }
+        uint32_t top = ef[0] > ef[1] ? ef[0] : ef[1];
+        uint32_t e8 = scale_byte(top), at = e8;
+        if constexpr (RHT) {
+            if (__builtin_expect(top == 255u, 0)) {
+                const bool fine = v[0].finite_inputs() && v[1].finite_inputs();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v[h].rotate(qa, kUnitSmall);
+                    ef[h] = v[h].exponent();
+                }
+                if (fine) {
+                    at = scale_byte(ef[0] > ef[1] ? ef[0] : ef[1]);
+                    e8 = at + kOverflowShift;
+                }
+            }
+        }
+        const uint2 lo = v[0].template encode<ROUND>(at, qa, (uint32_t)(2 * b), (uint32_t)(col + c));
+        const uint2 hi = v[1].template encode<ROUND>(at, qa, (uint32_t)(2 * b + 1), (uint32_t)(col + c));
+        out[c] = e8 == kNaNScale ? make_uint4(0, 0, 0, 0) : make_uint4(lo.x, lo.y, hi.x, hi.y);
+        e8c[c] = e8;
+    }
+    if (b < nkb) {
+        uint4* const d = reinterpret_cast<uint4*>(o.codes + panel * o.code_pld + b * 2048 + lane * 32);
+        d[0] = out[0];
+        d[1] = out[1];
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) s_scales[(wave & 1) * 256 + (2 * lane + c) * 2 + (wave >> 1)] = (uint8_t)e8c[c];
+    __syncthreads();
+    if (threadIdx.x < 32)
+        *reinterpret_cast<uint4*>(o.scales + panel * o.scale_pld + g4 * 512 + threadIdx.x * 16) =
+            *reinterpret_cast<const uint4*>(s_scales + threadIdx.x * 16);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Codes and scales to bf16 (exact: a level has two significant bits; 6 * 2^127 is infinity): a lane takes 8 values, 32 lanes a
+// run of 512 bytes of a row.
+// ------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void micro_decode_kernel(MicroOut q, int64_t rows, int64_t red, int64_t col_tiles,
+                                                           uint16_t* __restrict__ out, int64_t ldo) {
+    const int64_t rt = blockIdx.x / col_tiles, ct = blockIdx.x - rt * col_tiles;
+    const int part = threadIdx.x & 31;
+    const int64_t col = ct * kColsTile + part * 8, b = col / 32;
+    if (col >= red) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t row = rt * 32 + k * 8 + (threadIdx.x >> 5);
+        if (row >= rows) return;
+        const int64_t p = row / 128;
+        const int i = (int)(row & 127);
+        const uint32_t c = *reinterpret_cast<const uint32_t*>(q.codes + p * q.code_pld + b * 2048 + i * 16 + (part & 3) * 4);
+        const uint32_t e8 = q.scales[p * q.scale_pld + (b / 4) * 512 + (b & 1) * 256 + i * 2 + ((b >> 1) & 1)];
+        const float scale = __uint_as_float(e8 << 23);
+        uint4 r;
+        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+        *reinterpret_cast<uint4*>(out + row * ldo + col) = r;
+    }
+}
+
+template <int ROUND, bool RHT, bool GROUPED>
+hipError_t launch_micro_t(const MxQuantJob& j, hipStream_t s) {
+    const MicroOut o{static_cast<uint8_t*>(j.codes), j.code_pld, static_cast<uint8_t*>(j.scales), j.scale_pld};
+    const uint16_t* const x = static_cast<const uint16_t*>(j.x);
+    const int64_t tiles = micro_quant_tiles(j.transpose, j.qrows, j.red);
+    if (tiles == 0) return hipSuccess;
+    if (j.transpose) {
+        const int64_t panels = padded_rows(j.qrows) / 128;
+        micro_cols_kernel<ROUND, RHT, GROUPED><<<(unsigned)tiles, 256, 0, s>>>(x, j.xrows, j.qrows, j.ld, j.red / 32, panels,
+                                                                              j.group_off, j.num_groups, j.qa, o);
+    } else {
+        micro_rows_kernel<ROUND, RHT, GROUPED><<<(unsigned)tiles, 256, 0, s>>>(x, j.xrows, j.red, j.ld,
+                                                                              (j.red + kColsTile - 1) / kColsTile, j.group_off,
+                                                                              j.num_groups, j.qa, o);
+    }
+    return hipGetLastError();
+}
+
+template <int ROUND, bool RHT>
+hipError_t launch_micro_g(const MxQuantJob& j, hipStream_t s) {
+    return j.group_off ? launch_micro_t<ROUND, RHT, true>(j, s) : launch_micro_t<ROUND, RHT, false>(j, s);
+}
+
+template <int ROUND>
+hipError_t launch_micro_r(const MxQuantJob& j, hipStream_t s) {
+    return j.rht ? launch_micro_g<ROUND, true>(j, s) : launch_micro_g<ROUND, false>(j, s);
+}
+
+}  // namespace
+
+int64_t micro_quant_tiles(int transpose, int64_t qrows, int64_t red) {
+    if (transpose) return padded_rows(qrows) / 128 * ((red / 32 + 3) / 4);
+    return padded_rows(qrows) / kRowsTile * ((red + kColsTile - 1) / kColsTile);
+}
+
+int64_t micro_decode_tiles(int64_t rows, int64_t red) { return (rows + 31) / 32 * ((red + kColsTile - 1) / kColsTile); }
+
+hipError_t launch_quantize_mxfp4(const MxQuantJob& j, hipStream_t s) {
+    return j.rounding == kRoundSR ? launch_micro_r<kRoundSR>(j, s) : launch_micro_r<kRoundRTNE>(j, s);
+}
+
+hipError_t launch_dequantize_mxfp4(const void* codes, int64_t code_pld, const void* scales, int64_t scale_pld, int64_t rows,
+                                   int64_t red, void* out, int64_t ldo, hipStream_t s) {
+    const MicroOut q{static_cast<uint8_t*>(const_cast<void*>(codes)), code_pld,
+                     static_cast<uint8_t*>(const_cast<void*>(scales)), scale_pld};
+    const int64_t tiles = micro_decode_tiles(rows, red);
+    if (tiles == 0) return hipSuccess;
+    micro_decode_kernel<<<(unsigned)tiles, 256, 0, s>>>(q, rows, red, (red + kColsTile - 1) / kColsTile,
+                                                        static_cast<uint16_t*>(out), ldo);
+    return hipGetLastError();
+}
+
+}  // namespace ufp4

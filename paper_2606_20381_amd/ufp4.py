@@ -17,6 +17,7 @@ import torch
 UNIFORM = 0
 E2M1 = 1
 UNIFORM_MX32 = 2  # uniform grid with power-of-two 1x32 scales
+E2M1_MX32 = 4  # E2M1 grid with power-of-two 1x32 scales (microscaled 4-bit floating point)
 RTNE = 0
 SR = 1
 OUT_F32 = 0
@@ -97,6 +98,18 @@ SIGNATURES = {
     "ufp4_gemm_fwd_y_grouped": (_GEMM_G_ARGS, _INT),
     "ufp4_gemm_bwd_dx_grouped": (_GEMM_G_ARGS, _INT),
     "ufp4_gemm_bwd_dw_grouped": (_GEMM_G_ARGS, _INT),
+    "ufp4_mxfp4_quantize": (_QUANT_ARGS, _INT),
+    "ufp4_mxfp4_quantize_dual": ([_P, _I64, _I64, _I64, _INT, _U32, _U32, _INT, _U32, _U32, _INT, _U64, _Q, _Q, _P], _INT),
+    "ufp4_mxfp4_quantize_grouped": ([_P, _I64, _I64, _I64, _INT, _P, _I32, _I64, _INT, _U32, _INT, _U64, _U32, _Q, _P],
+                                    _INT),
+    "ufp4_mxfp4_dequantize": ([_Q, _P, _I64, _P], _INT),
+    "ufp4_mxfp4_gemm_fwd_y": (_GEMM_ARGS, _INT),
+    "ufp4_mxfp4_gemm_bwd_dx": (_GEMM_ARGS, _INT),
+    "ufp4_mxfp4_gemm_bwd_dw": (_GEMM_ARGS, _INT),
+    "ufp4_mxfp4_gemm_fwd_y_grouped": ([_Q, _Q, _P, _I32, _I64, _P, _I64, _INT, _P], _INT),
+    "ufp4_mxfp4_gemm_bwd_dx_grouped": ([_Q, _Q, _P, _I32, _I64, _P, _I64, _INT, _P], _INT),
+    "ufp4_mxfp4_gemm_bwd_dw_grouped": (_GEMM_G_ARGS, _INT),
+    "ufp4_mxfp4_linear": ([_P, _I64, _I64, _Q, _P, _I64, _INT, _P], _INT),
     "ufp4_layer_norm": ([_INT, _P, _I64, _I64, _I64, _INT, _P, _P, _F, _P, _I64, _P, _P, _P], _INT),
     "ufp4_layer_norm_bwd_workspace": ([_INT, _I64, _I64, _P], _INT),
     "ufp4_layer_norm_bwd": ([_INT, _P, _I64, _P, _I64, _I64, _I64, _INT, _P, _P, _P, _P, _I64, _P, _P, _P, _SZ, _P], _INT),
@@ -165,7 +178,8 @@ class QTensor:
 
     Rows are grouped in panels of 128; within a panel, block b (16 reduction positions) of all 128 rows is
     contiguous: 128 x 8 bytes of codes at b * 1024 and 128 fp32 scales at b * 128 (power-of-two scales: 32-blocks
-    of 3 x 1024 code bytes and 128 E8M0 bytes). ``codes_rows()`` / ``scales_rows()`` give plain row-major copies.
+    of 3 x 1024 code bytes and 128 E8M0 bytes; microscaled 4-bit: 32-blocks of 128 x 16 code bytes, and E8M0 bytes in
+    groups of four blocks). ``codes_rows()`` / ``scales_rows()`` give plain row-major copies.
     """
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, desc: QDesc):
@@ -189,7 +203,11 @@ class QTensor:
         return ctypes.byref(self.desc)
 
     def codes_rows(self) -> torch.Tensor:
-        """Codes as uint8 [rows, red/2] (power-of-two scales: [rows, red * 3/4]), row-major (a copy)."""
+        """Codes as uint8 [rows, red/2] (power-of-two scales on the uniform grid: [rows, red * 3/4]), row-major (a copy)."""
+        if self.fmt == E2M1_MX32:
+            nkb = self.red // 32
+            v = self.codes[:, : nkb * 2048].reshape(self.panels, nkb, PANEL_ROWS, 16).permute(0, 2, 1, 3)
+            return v.reshape(self.panels * PANEL_ROWS, nkb * 16)[: self.rows]
         if self.fmt == UNIFORM_MX32:
             nkb = self.red // 32
             v = self.codes[:, : nkb * 3072].reshape(self.panels, nkb, 3, PANEL_ROWS, 8).permute(0, 3, 1, 2, 4)
@@ -200,6 +218,10 @@ class QTensor:
 
     def scales_rows(self) -> torch.Tensor:
         """Scales as [rows, red/16] fp32 (power-of-two scales: [rows, red/32] E8M0 bytes), row-major (a copy)."""
+        if self.fmt == E2M1_MX32:  # [group of four blocks][block % 2][row][block / 2 % 2]
+            nkb, ng = self.red // 32, -(-self.red // 128)
+            v = self.scales[:, : ng * 512].reshape(self.panels, ng, 2, PANEL_ROWS, 2).permute(0, 3, 1, 4, 2)
+            return v.reshape(self.panels * PANEL_ROWS, ng * 4)[: self.rows, :nkb]
         nkb = self.red // (32 if self.fmt == UNIFORM_MX32 else 16)
         v = self.scales[:, : nkb * PANEL_ROWS].reshape(self.panels, nkb, PANEL_ROWS).permute(0, 2, 1)
         return v.reshape(self.panels * PANEL_ROWS, nkb)[: self.rows]
@@ -211,7 +233,7 @@ def empty_qtensor(rows: int, red: int, fmt: int = UNIFORM, device="cuda") -> QTe
     _check(lib().ufp4_qtensor_bytes(fmt, rows, red, ctypes.byref(p), ctypes.byref(cld), ctypes.byref(sld), None, None),
            "ufp4_qtensor_bytes")
     codes = torch.empty((p.value, cld.value), dtype=torch.uint8, device=device)
-    sdt = torch.uint8 if fmt == UNIFORM_MX32 else torch.float32
+    sdt = torch.uint8 if fmt in (UNIFORM_MX32, E2M1_MX32) else torch.float32
     scales = torch.empty((p.value, sld.value), dtype=sdt, device=device)
     desc = QDesc(codes=codes.data_ptr(), scales=scales.data_ptr(), code_panel_ld=cld.value, scale_panel_ld=sld.value,
                  panels=p.value, rows=rows, red=red, format=fmt)
@@ -592,6 +614,118 @@ def mx_gemm_bwd_dw_grouped(dytq: QTensor, xtq: QTensor, offsets: torch.Tensor, o
     G = _offsets(offsets)
     return _gemm_grouped("ufp4_mx_gemm_bwd_dw_grouped", dytq, xtq, offsets,
                          _out((G, dytq.rows, xtq.rows), out_dtype, dytq.codes.device, out))
+
+
+# ---------------------------------------------------------------------------------------------------
+# microscaled 4-bit floating point: E2M1 levels with power-of-two 1x32 scales
+# ---------------------------------------------------------------------------------------------------
+
+def mxfp4_quantize(x: torch.Tensor, *, transpose: bool = False, rht: bool = False, sign_mask: int = 0,
+                   rounding: int = RTNE, seed: int = 0, stream_id: int = 0, out: QTensor | None = None) -> QTensor:
+    """Microscaled 4-bit quantization, after an optional block-16 RHT (ufp4_mxfp4_quantize)."""
+    return _quantize_call("ufp4_mxfp4_quantize", E2M1_MX32, x, transpose, rht, sign_mask, rounding, seed, stream_id, out)
+
+
+def mxfp4_quantize_dual(x: torch.Tensor, *, rht_rows: bool = False, rht_cols: bool = False, sign_mask_rows: int = 0,
+                        sign_mask_cols: int = 0, rounding: int = RTNE, seed: int = 0, stream_rows: int = 0,
+                        stream_cols: int = 0, out_rows: QTensor | None = None,
+                        out_cols: QTensor | None = None) -> tuple[QTensor, QTensor]:
+    """Both microscaled operands of x [rows, cols] (ufp4_mxfp4_quantize_dual): (Q_r [rows, cols] along cols, Q_c [cols, rows]
+    along rows)."""
+    _bf16_2d(x)
+    rows, cols = x.shape
+    qr = out_rows if out_rows is not None else empty_qtensor(rows, cols, E2M1_MX32, x.device)
+    qc = out_cols if out_cols is not None else empty_qtensor(cols, rows, E2M1_MX32, x.device)
+    st = lib().ufp4_mxfp4_quantize_dual(x.data_ptr(), rows, cols, x.stride(0), int(rht_rows), sign_mask_rows, stream_rows,
+                                        int(rht_cols), sign_mask_cols, stream_cols, rounding,
+                                        seed & 0xFFFFFFFFFFFFFFFF, qr.ref(), qc.ref(), _stream())
+    _check(st, "ufp4_mxfp4_quantize_dual")
+    return qr, qc
+
+
+def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total: int, *, transpose: bool,
+                           rht: bool = False, sign_mask: int = 0, rounding: int = RTNE, seed: int = 0, stream_id: int = 0,
+                           out: QTensor | None = None) -> QTensor:
+    """ufp4_mxfp4_quantize_grouped: the forms of mx_quantize_grouped (padded_total from group_offsets with block 128 for
+    transpose False, 32 for True)."""
+    _bf16_2d(x)
+    rows, cols = x.shape
+    G = _offsets(offsets)
+    qrows, red = (cols, padded_total) if transpose else (padded_total, cols)
+    q = out if out is not None else empty_qtensor(qrows, red, E2M1_MX32, x.device)
+    st = lib().ufp4_mxfp4_quantize_grouped(x.data_ptr(), rows, cols, x.stride(0), int(transpose), offsets.data_ptr(), G,
+                                           padded_total, int(rht), sign_mask, rounding, seed & 0xFFFFFFFFFFFFFFFF,
+                                           stream_id, q.ref(), _stream())
+    _check(st, "ufp4_mxfp4_quantize_grouped")
+    return q
+
+
+def mxfp4_dequantize(q: QTensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The operand's values as bf16 [rows, red] (ufp4_mxfp4_dequantize), exact."""
+    if out is None:
+        ld = -(-q.red // 8) * 8
+        out = torch.empty((q.rows, ld), dtype=torch.bfloat16, device=q.codes.device)[:, : q.red]
+    elif (out.dtype != torch.bfloat16 or tuple(out.shape) != (q.rows, q.red) or out.device != q.codes.device
+          or out.stride(1) != 1):
+        raise ValueError(f"out must be a row-major bf16 tensor of shape {(q.rows, q.red)} on {q.codes.device}")
+    _check(lib().ufp4_mxfp4_dequantize(q.ref(), out.data_ptr(), out.stride(0), _stream()), "ufp4_mxfp4_dequantize")
+    return out
+
+
+def mxfp4_gemm_fwd_y(xq: QTensor, wq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
+    """Y [M, N] = Q(X) Q(W)^T on microscaled operands (ufp4_mxfp4_gemm_fwd_y)."""
+    return _gemm("ufp4_mxfp4_gemm_fwd_y", xq, wq, _out((xq.rows, wq.rows), out_dtype, xq.codes.device, out))
+
+
+def mxfp4_gemm_bwd_dx(dyq: QTensor, wtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
+    """dX [M, K] = Q(dY) Q(W^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dx)."""
+    return _gemm("ufp4_mxfp4_gemm_bwd_dx", dyq, wtq, _out((dyq.rows, wtq.rows), out_dtype, dyq.codes.device, out))
+
+
+def mxfp4_gemm_bwd_dw(dytq: QTensor, xtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
+    """dW [N, K] = Q(dY^T) Q(X^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dw)."""
+    return _gemm("ufp4_mxfp4_gemm_bwd_dw", dytq, xtq, _out((dytq.rows, xtq.rows), out_dtype, dytq.codes.device, out))
+
+
+def mxfp4_gemm_fwd_y_grouped(xq: QTensor, wq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
+                             out=None) -> torch.Tensor:
+    """Y [m_total, N] per group from the grouped-rows X and W [G*N, K] (ufp4_mxfp4_gemm_fwd_y_grouped)."""
+    n = wq.rows // _offsets(offsets)
+    return _mx_gemm_ragged_m("ufp4_mxfp4_gemm_fwd_y_grouped", xq, wq, offsets, m_total,
+                             _out((m_total, n), out_dtype, xq.codes.device, out))
+
+
+def mxfp4_gemm_bwd_dx_grouped(dyq: QTensor, wtq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
+                              out=None) -> torch.Tensor:
+    """dX [m_total, K] per group from the grouped-rows dY and W^T [K, G*N] (ufp4_mxfp4_gemm_bwd_dx_grouped)."""
+    return _mx_gemm_ragged_m("ufp4_mxfp4_gemm_bwd_dx_grouped", dyq, wtq, offsets, m_total,
+                             _out((m_total, wtq.rows), out_dtype, dyq.codes.device, out))
+
+
+def mxfp4_gemm_bwd_dw_grouped(dytq: QTensor, xtq: QTensor, offsets: torch.Tensor, out_dtype=torch.float32,
+                              out=None) -> torch.Tensor:
+    """dW [G, N, K] from the grouped-reduction dY^T and X^T (ufp4_mxfp4_gemm_bwd_dw_grouped)."""
+    return _gemm_grouped("ufp4_mxfp4_gemm_bwd_dw_grouped", dytq, xtq, offsets,
+                         _out((_offsets(offsets), dytq.rows, xtq.rows), out_dtype, dytq.codes.device, out))
+
+
+LINEAR_TOKENS = 16  # tokens up to which ufp4_mxfp4_linear takes a product
+
+
+def mxfp4_linear(x: torch.Tensor, wq: QTensor, out_dtype=torch.bfloat16, out=None) -> torch.Tensor:
+    """Y [tokens, N] = Q(x) W^T with bf16 x and W kept microscaled: a decode step's few tokens in one launch
+    (ufp4_mxfp4_linear), more (or a rotated W) by quantizing x and one GEMM."""
+    _bf16_2d(x)
+    tokens, red = x.shape
+    if red != wq.red:
+        raise ValueError(f"x must have {wq.red} columns")
+    if tokens > LINEAR_TOKENS or wq.rht_block:
+        xq = mxfp4_quantize(x, rht=wq.rht_block != 0, sign_mask=wq.sign_mask)
+        return mxfp4_gemm_fwd_y(xq, wq, out_dtype, out)
+    y = _out((tokens, wq.rows), out_dtype, x.device, out)
+    st = lib().ufp4_mxfp4_linear(x.data_ptr(), tokens, x.stride(0), wq.ref(), y.data_ptr(), y.stride(0), _odt(y), _stream())
+    _check(st, "ufp4_mxfp4_linear")
+    return y
 
 
 # ---------------------------------------------------------------------------------------------------
