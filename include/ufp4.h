@@ -449,7 +449,7 @@ int ufp4_mxfp4_dequantize(const ufp4_qtensor *q, void *out_dev, int64_t ldo, voi
 /*
  * ufp4_mxfp4_gemm_* -- the three passes, dense and grouped, on two UFP4_FMT_E2M1_MX32 operands: as ufp4_mx_gemm_*. The grouped
  *   bwd_dx needs N % 128 == 0 (its groups' blocks of W^T begin with a group of four scales), else UFP4_ERR_UNSUPPORTED, as do
- *   outputs of 2^24 or more 256 x 256 tiles.
+ *   more than 1024 groups and 2^23 or more 256 x 256 tiles (bwd_dw: over all groups).
  * ufp4_mxfp4_linear -- y [rows, N] = Q(x) W^T for the few tokens of a decode step, in one launch: x bf16 [rows, K] (ldx % 8 == 0,
  *   16-byte aligned), quantized as ufp4_mxfp4_quantize does without RHT, to nearest; w a plain UFP4_FMT_E2M1_MX32 operand [N, K].
  *   rows up to 16 and w without RHT (else UFP4_ERR_UNSUPPORTED: quantize x and use ufp4_mxfp4_gemm_fwd_y).

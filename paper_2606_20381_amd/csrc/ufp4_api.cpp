@@ -233,10 +233,12 @@ int gemm_dense(const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ld
     return status_of(launch_gemm(j, static_cast<hipStream_t>(stream)));
 }
 
-// Workgroups of a GEMM on operands with one-byte scales whose tile is `bm` x `bm`, with `rows` tile rows, that a launch allows:
-// the microscaled 4-bit kernels launch 256 threads for each of them, and a grid holds fewer than 2^32 threads.
-bool mx_grid_fits(int format, int64_t rows, int64_t cols) {
-    return rows * cols < (int64_t(1) << (format == UFP4_FMT_E2M1_MX32 ? 24 : 31));
+// Whether a GEMM's grid of 256 x 256 tiles (`rows` x `cols` of them, for each of `groups` where the reduction is ragged) and its
+// number of groups are within the limits of the format's kernels: the microscaled 4-bit ones launch 512 threads for each tile on
+// one grid dimension, which holds fewer than 2^32, and keep a table of the groups.
+bool mx_grid_fits(int format, int64_t rows, int64_t cols, int64_t groups = 1, bool ragged_k = false) {
+    if (format != UFP4_FMT_E2M1_MX32) return rows * cols < (int64_t(1) << 31);
+    return groups <= kMxfp4Groups && rows * cols * (ragged_k ? groups : 1) < (int64_t(1) << 23);
 }
 
 int launch_mx(int format, const MxGemmJob& j, void* stream) {
@@ -420,7 +422,7 @@ int mx_fwd_y_grouped_impl(int format, const ufp4_qtensor* x, const ufp4_qtensor*
     j.G = num_groups;
     j.b_group_rows = N;
     j.b_group_kb = 0;
-    if (!mx_grid_fits(format, ceil_div(x->rows, 256) + num_groups, ceil_div(N, 256))) return UFP4_ERR_UNSUPPORTED;
+    if (!mx_grid_fits(format, ceil_div(x->rows, 256) + num_groups, ceil_div(N, 256), num_groups)) return UFP4_ERR_UNSUPPORTED;
     return launch_mx(format, j, stream);
 }
 
@@ -446,7 +448,7 @@ int mx_bwd_dx_grouped_impl(int format, const ufp4_qtensor* dy, const ufp4_qtenso
     j.G = num_groups;
     j.b_group_rows = 0;
     j.b_group_kb = dy->red / 32;
-    if (!mx_grid_fits(format, ceil_div(dy->rows, 256) + num_groups, ceil_div(j.N, 256))) return UFP4_ERR_UNSUPPORTED;
+    if (!mx_grid_fits(format, ceil_div(dy->rows, 256) + num_groups, ceil_div(j.N, 256), num_groups)) return UFP4_ERR_UNSUPPORTED;
     return launch_mx(format, j, stream);
 }
 
@@ -461,7 +463,7 @@ int mx_bwd_dw_grouped_impl(int format, const ufp4_qtensor* dyt, const ufp4_qtens
     st = check_output(dw_dev, ldc, xt->rows, out_dtype, dyt->rows == 0 || xt->rows == 0);
     if (st != UFP4_OK) return st;
     if (dyt->rows == 0 || xt->rows == 0) return UFP4_OK;
-    if (!mx_grid_fits(format, ceil_div(dyt->rows, 256), ceil_div(xt->rows, 256))) return UFP4_ERR_UNSUPPORTED;
+    if (!mx_grid_fits(format, ceil_div(dyt->rows, 256), ceil_div(xt->rows, 256), num_groups, true)) return UFP4_ERR_UNSUPPORTED;
     MxGemmJob j = mx_job(dyt, xt, dw_dev, ldc, out_dtype);
     j.mode = kGemmRaggedK;
     j.M = dyt->rows;

@@ -208,6 +208,7 @@ hipError_t launch_dequantize_mxfp4(const void* codes, int64_t code_pld, const vo
                                    int64_t red, void* out, int64_t ldo, hipStream_t stream);
 int64_t micro_quant_tiles(int transpose, int64_t qrows, int64_t red);  // workgroups
 int64_t micro_decode_tiles(int64_t rows, int64_t red);
+constexpr int kMxfp4Groups = 1024;  // groups of its grouped forms: as many as the quantizers take
 hipError_t launch_gemm_mxfp4(const MxGemmJob& job, hipStream_t stream);
 
 // y [M, N] = Q(x) W^T, M <= kLinearTokens tokens of bf16 x, W [N, nkb * 32] a plain microscaled 4-bit operand.
@@ -310,6 +311,8 @@ extern "C" {
 // threads of the grid's x dimension, which a launch limits to 2^32 - 1.
 int ufp4_plan_gemm(int mode, int format, int64_t M, int64_t N, int64_t red, int32_t G);
 int ufp4_plan_gemm_mx(int mode, int64_t M, int64_t N, int64_t red, int32_t G, int64_t a_rows, int64_t* threads_x);
+// The microscaled 4-bit GEMM's rule: 0 the 256 x 256 tile, 1 128 x 128, 2 64 x 64, 3 64 x 64 in four teams.
+int ufp4_plan_gemm_mxfp4(int mode, int64_t M, int64_t N, int64_t red, int32_t G, int64_t a_rows);
 // Threads in x of the (largest) launch of the transposed quantizer's tile kernel for an RHT block of 32, 64 or 128.
 int64_t ufp4_plan_cols_wide(int rht_block, int64_t cols);
 // Workgroups of a grouped quantizer over `tiles` tiles (mx: power-of-two scales), and the most tiles one of them takes.

@@ -5,6 +5,8 @@ magnitudes) for each instruction and 64 for what an instruction may lose inside,
 (K / 64 + 64 + splits) 2^-23 sum |a b|. bf16 outputs add 2^-8 of their value.
 """
 
+import ctypes
+
 import pytest
 import torch
 
@@ -51,7 +53,8 @@ def test_dense(M, N, K, dt):
     assert torch.equal(got, U.mxfp4_gemm_bwd_dw(a, b, dt))  # repeats
 
 
-@pytest.mark.parametrize("M,N,K", [(70, 90, 192), (2100, 2100, 320), (4200, 4100, 160)])
+@pytest.mark.parametrize("M,N,K", [(70, 90, 192), (2100, 2100, 320), (4200, 4100, 160), (8192, 8192, 1056), (9000, 8200, 1248),
+                                   (16384, 8192, 1024)])
 def test_exact_where_sums_are_small_integers(M, N, K):
     """Values in 0, +-1, +-2, +-3 at scale 1: every partial sum is a small integer, so the result is exact, and a wrong lane,
     block, scale or edge shows as a wrong integer."""
@@ -61,6 +64,48 @@ def test_exact_where_sums_are_small_integers(M, N, K):
     x[:, ::32], w[:, ::32] = 4, 4  # the block's top: scale 1
     got = U.mxfp4_gemm_fwd_y(U.mxfp4_quantize(x), U.mxfp4_quantize(w))
     assert torch.equal(got.double(), x.double() @ w.double().t())
+    bf = U.mxfp4_gemm_fwd_y(U.mxfp4_quantize(x), U.mxfp4_quantize(w), BF)
+    assert torch.equal(bf, got.to(BF))
+
+
+def _plan(M, N, K, mode=0, G=1, a_rows=None):
+    fn = ctypes.CDLL(U.library_path()).ufp4_plan_gemm_mxfp4
+    fn.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64]
+    return fn(mode, M, N, K, G, M if a_rows is None else a_rows)
+
+
+@pytest.mark.parametrize("kernel,M,N,K", [(0, 4096, 4096, 4096), (0, 4090, 4000, 2080), (1, 2048, 2048, 2048), (1, 2040, 1990, 2080),
+                                          (2, 256, 8192, 2048), (2, 250, 8130, 1952), (3, 64, 2048, 8192), (3, 70, 1000, 8224),
+                                          (3, 130, 66, 5000 * 32)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_every_kernel(kernel, M, N, K, dt):
+    """Each of the kernels at a size that its rule gives it, with whole and with partial tiles and stages."""
+    assert _plan(M, N, K) == kernel
+    a, b = _operand(M, K, M + K), _operand(N, K, N + 2 * K)
+    _within(U.mxfp4_gemm_fwd_y(a, b, dt), _values(a), _values(b), K, dt)
+
+
+@pytest.mark.parametrize("kernel,counts,N,K", [(0, [6000, 3, 0, 6000, 129], 1024, 1056), (1, [2000, 0, 1300, 7], 1024, 2048),
+                                               (2, [100, 5, 0, 77], 1280, 256), (3, [30, 0, 64, 1], 128, 4096)])
+def test_every_grouped_kernel(kernel, counts, N, K):
+    G, total = len(counts), sum(counts)
+    off, p128 = U.group_offsets(counts, block=128)
+    _, p32 = U.group_offsets(counts, block=32)
+    assert _plan(total, N, K, 1, G, p128) == kernel
+    g = torch.Generator(device="cuda").manual_seed(total)
+    x, dy = (torch.randn(total, n, generator=g, device="cuda").to(BF) for n in (K, N))
+    w = torch.randn(G * N, K, generator=g, device="cuda").to(BF)
+    wq = U.mxfp4_quantize(w)
+    y = U.mxfp4_gemm_fwd_y_grouped(U.mxfp4_quantize_grouped(x, off, p128, transpose=False), wq, off, total, BF)
+    xtq = U.mxfp4_quantize_grouped(x, off, p32, transpose=True)
+    dytq = U.mxfp4_quantize_grouped(dy, off, p32, transpose=True)
+    dw = U.mxfp4_gemm_bwd_dw_grouped(dytq, xtq, off)
+    vx, vw, vxt, vdyt = _values(U.mxfp4_quantize(x)), _values(wq), _values(xtq), _values(dytq)
+    pads = U.padded_offsets([0] + torch.tensor(counts).cumsum(0).tolist(), 32)
+    for e, s in enumerate(_groups(counts, total)):
+        _within(y[s], vx[s], vw[e * N : (e + 1) * N], K, BF)
+        r = slice(pads[e], pads[e + 1])
+        _within(dw[e], vdyt[:, r], vxt[:, r], pads[e + 1] - pads[e], F32)
 
 
 def test_scales_of_every_block_count():
