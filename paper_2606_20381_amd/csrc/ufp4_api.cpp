@@ -474,6 +474,57 @@ int mx_bwd_dw_grouped_impl(int format, const ufp4_qtensor* dyt, const ufp4_qtens
     return launch_mx(format, j, stream);
 }
 
+int mx_quantize_dual_impl(int format, const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int rht_rows,
+                          uint32_t sign_mask_rows, uint32_t stream_rows, int rht_cols, uint32_t sign_mask_cols,
+                          uint32_t stream_cols, int rounding, uint64_t seed, ufp4_qtensor* out_rows,
+                          ufp4_qtensor* out_cols, void* stream) {
+    // Q_r = X [rows, cols] along cols; Q_c = X^T [cols, rows] along rows
+    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
+    if ((rht_rows != 0 && rht_rows != 1) || (rht_cols != 0 && rht_cols != 1)) return UFP4_ERR_INVALID_ARG;
+    if (sign_mask_rows > 0xFFFFu || sign_mask_cols > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
+    if (out_rows == out_cols) return UFP4_ERR_INVALID_ARG;
+    const int si = check_input(x_dev, rows, cols, ld, 8);
+    if (si != UFP4_OK) return si;
+    int st = check_storage(out_rows, format, rows, cols);
+    if (st == UFP4_OK) st = check_storage(out_cols, format, cols, rows);
+    if (st != UFP4_OK) return st;
+    if (rows >= (int64_t(1) << 31) || cols >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
+    // 1-D grids
+    if (format == UFP4_FMT_E2M1_MX32) {
+        if (ceil_div(rows, 128) * ceil_div(cols, 128) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
+    } else if (mx_tile_count(rows, cols, true, true) >= (int64_t(1) << 31)) {
+        return UFP4_ERR_UNSUPPORTED;
+    }
+    const uint16_t mr = (uint16_t)sign_mask_rows, mc = (uint16_t)sign_mask_cols;
+    record(out_rows, format, rows, cols, rht_rows ? 16 : 0, &mr, 0.0f, rounding);
+    record(out_cols, format, cols, rows, rht_cols ? 16 : 0, &mc, 0.0f, rounding);
+    if (rows == 0 || cols == 0) return UFP4_OK;
+    MxDualJob j{};
+    j.rounding = rounding;
+    j.rht_r = rht_rows;
+    j.rht_c = rht_cols;
+    j.x = x_dev;
+    j.rows = rows;
+    j.cols = cols;
+    j.ld = ld;
+    fill_sign_xor(sign_mask_rows, j.qr.sign_xor);
+    fill_sign_xor(sign_mask_cols, j.qc.sign_xor);
+    j.qr.key0 = j.qc.key0 = (uint32_t)seed;
+    j.qr.key1 = j.qc.key1 = (uint32_t)(seed >> 32);
+    j.qr.stream = stream_rows;
+    j.qc.stream = stream_cols;
+    j.codes_r = out_rows->codes;
+    j.code_pld_r = out_rows->code_panel_ld;
+    j.scales_r = out_rows->scales;
+    j.scale_pld_r = out_rows->scale_panel_ld;
+    j.codes_c = out_cols->codes;
+    j.code_pld_c = out_cols->code_panel_ld;
+    j.scales_c = out_cols->scales;
+    j.scale_pld_c = out_cols->scale_panel_ld;
+    hipStream_t const s = static_cast<hipStream_t>(stream);
+    return status_of(format == UFP4_FMT_E2M1_MX32 ? launch_quantize_mxfp4_dual(j, s) : launch_quantize_mx_dual(j, s));
+}
+
 int grid_levels(int format, float max_fpx) {
     if (format == UFP4_FMT_E2M1 && max_fpx == 2.0f) return 5;
     if (format == UFP4_FMT_E2M1 && max_fpx == 4.0f) return 7;
@@ -818,45 +869,8 @@ int ufp4_mx_quantize_dual(const void* x_dev, int64_t rows, int64_t cols, int64_t
                           uint32_t sign_mask_rows, uint32_t stream_rows, int rht_cols, uint32_t sign_mask_cols,
                           uint32_t stream_cols, int rounding, uint64_t seed, ufp4_qtensor* out_rows,
                           ufp4_qtensor* out_cols, void* stream) {
-    // Q_r = X [rows, cols] along cols; Q_c = X^T [cols, rows] along rows
-    if (rounding != UFP4_ROUND_RTNE && rounding != UFP4_ROUND_SR) return UFP4_ERR_INVALID_ARG;
-    if ((rht_rows != 0 && rht_rows != 1) || (rht_cols != 0 && rht_cols != 1)) return UFP4_ERR_INVALID_ARG;
-    if (sign_mask_rows > 0xFFFFu || sign_mask_cols > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
-    if (out_rows == out_cols) return UFP4_ERR_INVALID_ARG;
-    const int si = check_input(x_dev, rows, cols, ld, 8);
-    if (si != UFP4_OK) return si;
-    int st = check_storage(out_rows, UFP4_FMT_UNIFORM_MX32, rows, cols);
-    if (st == UFP4_OK) st = check_storage(out_cols, UFP4_FMT_UNIFORM_MX32, cols, rows);
-    if (st != UFP4_OK) return st;
-    if (rows >= (int64_t(1) << 31) || cols >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;
-    if (mx_tile_count(rows, cols, true, true) >= (int64_t(1) << 31)) return UFP4_ERR_UNSUPPORTED;  // 1-D grid
-    const uint16_t mr = (uint16_t)sign_mask_rows, mc = (uint16_t)sign_mask_cols;
-    record(out_rows, UFP4_FMT_UNIFORM_MX32, rows, cols, rht_rows ? 16 : 0, &mr, 0.0f, rounding);
-    record(out_cols, UFP4_FMT_UNIFORM_MX32, cols, rows, rht_cols ? 16 : 0, &mc, 0.0f, rounding);
-    if (rows == 0 || cols == 0) return UFP4_OK;
-    MxDualJob j{};
-    j.rounding = rounding;
-    j.rht_r = rht_rows;
-    j.rht_c = rht_cols;
-    j.x = x_dev;
-    j.rows = rows;
-    j.cols = cols;
-    j.ld = ld;
-    fill_sign_xor(sign_mask_rows, j.qr.sign_xor);
-    fill_sign_xor(sign_mask_cols, j.qc.sign_xor);
-    j.qr.key0 = j.qc.key0 = (uint32_t)seed;
-    j.qr.key1 = j.qc.key1 = (uint32_t)(seed >> 32);
-    j.qr.stream = stream_rows;
-    j.qc.stream = stream_cols;
-    j.codes_r = out_rows->codes;
-    j.code_pld_r = out_rows->code_panel_ld;
-    j.scales_r = out_rows->scales;
-    j.scale_pld_r = out_rows->scale_panel_ld;
-    j.codes_c = out_cols->codes;
-    j.code_pld_c = out_cols->code_panel_ld;
-    j.scales_c = out_cols->scales;
-    j.scale_pld_c = out_cols->scale_panel_ld;
-    return status_of(launch_quantize_mx_dual(j, static_cast<hipStream_t>(stream)));
+    return mx_quantize_dual_impl(UFP4_FMT_UNIFORM_MX32, x_dev, rows, cols, ld, rht_rows, sign_mask_rows, stream_rows, rht_cols,
+                                 sign_mask_cols, stream_cols, rounding, seed, out_rows, out_cols, stream);
 }
 
 int ufp4_mx_gemm_fwd_y(const ufp4_qtensor* x, const ufp4_qtensor* w, void* y_dev, int64_t ldc, int out_dtype,
@@ -912,19 +926,8 @@ int ufp4_mxfp4_gemm_bwd_dw_grouped(const ufp4_qtensor* dyt, const ufp4_qtensor* 
 int ufp4_mxfp4_quantize_dual(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int rht_rows, uint32_t sign_mask_rows,
                              uint32_t stream_rows, int rht_cols, uint32_t sign_mask_cols, uint32_t stream_cols, int rounding,
                              uint64_t seed, ufp4_qtensor* out_rows, ufp4_qtensor* out_cols, void* stream) {
-    if (out_rows == out_cols) return UFP4_ERR_INVALID_ARG;
-    // both outputs' checks before either launch
-    int st = check_input(x_dev, rows, cols, ld, 8);
-    if (st == UFP4_OK) st = check_storage(out_rows, UFP4_FMT_E2M1_MX32, rows, cols);
-    if (st == UFP4_OK) st = check_storage(out_cols, UFP4_FMT_E2M1_MX32, cols, rows);
-    if (st != UFP4_OK) return st;
-    if ((rht_cols != 0 && rht_cols != 1) || sign_mask_cols > 0xFFFFu) return UFP4_ERR_INVALID_ARG;
-    if (cols >= (int64_t(1) << 31) || micro_quant_tiles(1, cols, rows) >= kMostMicroTiles) return UFP4_ERR_UNSUPPORTED;
-    st = mx_quantize_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, 0, rht_rows, sign_mask_rows, rounding, seed, stream_rows,
-                          out_rows, stream);
-    if (st != UFP4_OK) return st;
-    return mx_quantize_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, 1, rht_cols, sign_mask_cols, rounding, seed, stream_cols,
-                            out_cols, stream);
+    return mx_quantize_dual_impl(UFP4_FMT_E2M1_MX32, x_dev, rows, cols, ld, rht_rows, sign_mask_rows, stream_rows, rht_cols,
+                                 sign_mask_cols, stream_cols, rounding, seed, out_rows, out_cols, stream);
 }
 
 int ufp4_mxfp4_dequantize(const ufp4_qtensor* q, void* out_dev, int64_t ldo, void* stream) {

@@ -104,8 +104,8 @@ __host__ __device__ inline int64_t tile_rows(const MxGemmJob& j, int bm) {
     return j.mode == kGemmRaggedM ? (j.a_rows + bm - 1) / bm + j.G : (j.M + bm - 1) / bm;
 }
 
-// The groups' first panel of the padded rows (ragged reduction: first 32-block), first token, and, where a tile is two panels,
-// first tile row, in LDS, built by the first wave, 64 groups at a time. (A 64-row tile is half a panel: a group's tile rows are
+// Ragged rows: the groups' first panel of the padded rows, first token, and, where a tile is two panels, first tile row, in LDS,
+// built by the first wave, 64 groups at a time. (A 64-row tile is half a panel: a group's tile rows are
 // then twice its panels, the last of which may hold none of its rows.) Operands and outputs hold fewer than 2^31 rows; what
 // offsets claim past that is cut.
 template <int BM>
@@ -122,7 +122,7 @@ struct Groups {
             const int64_t start = g < G ? j.offsets[g] : 0;
             int64_t m = g < G ? j.offsets[g + 1] - start : 0;
             m = m < 0 ? 0 : m > (int64_t(1) << 30) ? int64_t(1) << 30 : m;
-            const int cnt = (int)((m + BM - 1) / BM), n = (int)(j.mode == kGemmRaggedK ? (m + 31) / 32 : (m + 127) / 128);
+            const int cnt = (int)((m + BM - 1) / BM), n = (int)((m + 127) / 128);
             int ti = cnt, ni = n;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
@@ -162,12 +162,27 @@ struct Groups {
     }
 };
 
-template <int OUT, class C, bool GROUPED>
+// Ragged reduction: the first 32-block of group g and the one past its last, by a sum over the lanes of each wave.
+__device__ __forceinline__ void group_blocks(const MxGemmJob& j, int g, int& first, int& end) {
+    const int lane = threadIdx.x & 63;
+    auto blocks = [&](int h) {
+        const int64_t m = j.offsets[h + 1] - j.offsets[h];
+        return m <= 0 ? 0 : m > (int64_t(1) << 30) ? 1 << 25 : (int)((m + 31) / 32);
+    };
+    int sum = 0;
+    for (int h = lane; h < g; h += 64) sum += blocks(h);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    first = uniform(sum);
+    end = first + uniform(blocks(g));
+}
+
+template <int OUT, class C, int MODE>
 __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGemmJob j) {
     using S = Slot<C>;
     constexpr int kRing = C::kRing;
     __shared__ __align__(16) uint8_t rings[C::kSplit * kRing * S::kSize];
-    __shared__ typename std::conditional<GROUPED, Groups<C::BM>, int>::type groups;
+    __shared__ typename std::conditional<MODE == kGemmRaggedM, Groups<C::BM>, int>::type groups;
     constexpr int BM = C::BM, BN = C::BN, WTM = C::WTM, WTN = C::WTN;
     constexpr int kRowsP = C::kRowsP;     // rows of a panel in LDS
     constexpr bool kHalf = kRowsP < 128;  // half a panel per operand
@@ -180,16 +195,14 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
     const int wm = (int)((unsigned)wave / C::WN), wn = (int)((unsigned)wave % C::WN);
     const uint32_t gx = (uint32_t)((j.N + BN - 1) / BN);
     uint32_t gy = (uint32_t)tile_rows(j, BM), total = gx * gy;
-    if constexpr (GROUPED) {
+    if constexpr (MODE == kGemmRaggedM) {
         if (tid < 64) groups.build(j);
         __syncthreads();
-        if (j.mode == kGemmRaggedM) {
-            const uint32_t have = (uint32_t)uniform(groups.first_tile(j.G));
-            gy = have < gy ? have : gy;
-            total = gx * gy;
-        } else {
-            total *= (uint32_t)j.G;
-        }
+        const uint32_t have = (uint32_t)uniform(groups.first_tile(j.G));
+        gy = have < gy ? have : gy;
+        total = gx * gy;
+    } else if constexpr (MODE == kGemmRaggedK) {
+        total *= (uint32_t)j.G;
     }
 
     // One output tile: the panels of its operands (A's, then B's) at the reduction's first block, this wave's scales, the stages,
@@ -205,7 +218,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
     const int unit = wave % (C::kPanels * kUnits), spanel = unit / kUnits;  // this wave's unit of the scales
     auto locate = [&](uint32_t L, Work& w) INLINE {
         int tm, tn, g = 0;
-        if (GROUPED && j.mode == kGemmRaggedK) {
+        if constexpr (MODE == kGemmRaggedK) {
             g = (int)(L / (gx * gy));
             L -= (uint32_t)g * (gx * gy);
         }
@@ -213,23 +226,22 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
         int64_t arow0 = (int64_t)tm * BM, brow0 = (int64_t)tn * BN, b_kb0 = 0, kbf = 0, kbe = j.nkb;
         int64_t row0 = arow0, rows = j.M - arow0;
         w.c_base = 0;
-        if constexpr (GROUPED) {
-            if (j.mode == kGemmRaggedM) {
-                g = groups.of(j.G, tm);
-                const int lt = tm - uniform(groups.first_tile(g));
-                arow0 = (int64_t)uniform(groups.unit[g]) * 128 + lt * BM;
-                const int start = uniform(groups.token[g]), end = uniform(groups.token[g + 1]);
-                row0 = (int64_t)start + lt * BM;
-                rows = end - row0 < j.M - row0 ? end - row0 : j.M - row0;  // token rows past the output are not stored
-                if (start < 0) rows = 0;
-                brow0 += g * j.b_group_rows;
-                b_kb0 = g * j.b_group_kb;
-            } else {
-                kbf = uniform(groups.unit[g]);
-                kbe = uniform(groups.unit[g + 1]);
-                if (kbe > j.nkb) kbe = j.nkb;  // clamped to the operands
-                w.c_base = (int64_t)g * j.M * j.ldc;
-            }
+        if constexpr (MODE == kGemmRaggedM) {
+            g = groups.of(j.G, tm);
+            const int lt = tm - uniform(groups.first_tile(g));
+            arow0 = (int64_t)uniform(groups.unit[g]) * 128 + lt * BM;
+            const int start = uniform(groups.token[g]), end = uniform(groups.token[g + 1]);
+            row0 = (int64_t)start + lt * BM;
+            rows = end - row0 < j.M - row0 ? end - row0 : j.M - row0;  // token rows past the output are not stored
+            if (start < 0) rows = 0;
+            brow0 += g * j.b_group_rows;
+            b_kb0 = g * j.b_group_kb;
+        } else if constexpr (MODE == kGemmRaggedK) {
+            int first, end;
+            group_blocks(j, g, first, end);
+            kbf = first;
+            kbe = end < j.nkb ? end : j.nkb;  // clamped to the operands
+            w.c_base = (int64_t)g * j.M * j.ldc;
         }
         // Stages are whole groups of four blocks (the scales' unit). A ragged reduction may begin and end inside one.
         w.kbf = (int)kbf;
@@ -590,8 +602,11 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
     // workgroups that are resident take the tiles in turn.
     if (j.mode == kGemmRaggedK) tiles *= j.G;
     else if (tiles > C::kResident) tiles = C::kResident;
-    if (j.mode == kGemmDense) gemm_mxfp4_kernel<OUT, C, false><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
-    else gemm_mxfp4_kernel<OUT, C, true><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
+    switch (j.mode) {
+        case kGemmRaggedM: gemm_mxfp4_kernel<OUT, C, kGemmRaggedM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+        case kGemmRaggedK: gemm_mxfp4_kernel<OUT, C, kGemmRaggedK><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+        default: gemm_mxfp4_kernel<OUT, C, kGemmDense><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+    }
     return hipGetLastError();
 }
 

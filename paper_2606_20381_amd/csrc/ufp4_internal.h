@@ -141,6 +141,7 @@ struct MxDualJob {
 };
 
 hipError_t launch_quantize_mx_dual(const MxDualJob& job, hipStream_t stream);
+hipError_t launch_quantize_mxfp4_dual(const MxDualJob& job, hipStream_t stream);  // microscaled 4-bit, 128 x 128 tiles
 // Workgroups of the power-of-two-scale tile kernel (32 x 256 tiles) for the outputs asked for.
 int64_t mx_tile_count(int64_t rows, int64_t cols, bool rows_out, bool cols_out);
 

@@ -22,15 +22,20 @@ namespace ufp4 {
 namespace {
 
 // The E2M1 code of v (|v| < 8, cut at 6) between its neighbours by a 16-bit draw: the upper one of the signed pair
-// g_a <= v < g_b iff u / 2^16 < (v - g_a) / (g_b - g_a). In units of the pair's spacing from the lower end `base` of its
-// binade, r = |v|: both comparisons are of exact numbers. A level never moves.
+// g_a <= v < g_b iff u / 2^16 < (v - g_a) / (g_b - g_a). On integers, exact, and a level never moves.
+// |v| >= 1: the levels are the fp32 numbers with one fraction bit, F the 22 bits below it. A positive v goes up iff U = 2^6 u <
+// F, that is if F + (2^22 - 1 - U) carries; a negative one goes away from zero unless U < 2^22 - F, that is if F + U carries.
+// |v| < 1: steps of 0.5; the upper level is ceil(2 v - u / 2^16) = -floor((u + floor(-2^17 v)) / 2^16).
 __device__ __forceinline__ uint32_t fp4_sr(float v, uint32_t u16) {
-    const float a = __builtin_fminf(__builtin_fabsf(v), 6.0f), u = (float)u16 * 0x1p-16f;
-    const bool s1 = a < 2.0f, s2 = a < 4.0f;
-    const float r = (a - (s1 ? 0.0f : s2 ? 2.0f : 4.0f)) * (s1 ? 2.0f : s2 ? 1.0f : 0.5f);
-    const float j = floorf(r);
-    const bool up = v >= 0.0f ? j + u < r : !(r < j + 1.0f - u);
-    return (uint32_t)((s1 ? 0 : s2 ? 4 : 6) + (int)j + (up ? 1 : 0)) | (v < 0.0f ? 8u : 0u);
+    const uint32_t bits = __float_as_uint(v);
+    const float a = __builtin_fminf(__builtin_fabsf(v), 6.0f);
+    const uint32_t flip = (uint32_t)((int32_t)~bits >> 31) & 0x3FFFFFu;  // positive: 2^22 - 1 - U
+    const uint32_t big = ((__float_as_uint(a) + ((u16 << 6) ^ flip)) >> 22) - 252u;
+    int32_t f;
+    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(f) : "v"(v * -131072.0f));
+    const int32_t lower = ((int32_t)u16 + f) >> 16;  // minus the level's steps
+    const uint32_t small = (uint32_t)(lower < 0 ? -lower : lower);
+    return (a >= 1.0f ? big : small) | ((bits >> 28) & 8u);
 }
 
 // Sixteen values of a block (half of it) on their way to codes.
@@ -128,6 +133,74 @@ constexpr double kUnit = 0.25;            // 1/4 = 1/sqrt(16)
 constexpr int kOverflowShift = 8;         // rotated values past FLT_MAX are taken 2^-8 as large
 constexpr double kUnitSmall = 0x1p-10;
 
+// One 32-block of two neighbouring columns, m[i] the pair of row i: codes and scale bytes of each.
+template <int ROUND, bool RHT>
+__device__ __forceinline__ void quantize_columns(const uint32_t (&m)[32], const QuantArgs& qa, int64_t b, int64_t col,
+                                                 uint4 (&out)[2], uint32_t (&e8c)[2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        Half<RHT> v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[h].w[j] = c == 0 ? __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x05040100u)
+                                   : __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x07060302u);
+        uint32_t ef[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (RHT) v[h].rotate(qa, kUnit);
+            ef[h] = v[h].exponent();
+        }
+        uint32_t top = ef[0] > ef[1] ? ef[0] : ef[1];
+        uint32_t e8 = scale_byte(top), at = e8;
+        if constexpr (RHT) {
+            if (__builtin_expect(top == 255u, 0)) {
+                const bool fine = v[0].finite_inputs() && v[1].finite_inputs();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v[h].rotate(qa, kUnitSmall);
+                    ef[h] = v[h].exponent();
+                }
+                if (fine) {
+                    at = scale_byte(ef[0] > ef[1] ? ef[0] : ef[1]);
+                    e8 = at + kOverflowShift;
+                }
+            }
+        }
+        const uint2 lo = v[0].template encode<ROUND>(at, qa, (uint32_t)(2 * b), (uint32_t)(col + c));
+        const uint2 hi = v[1].template encode<ROUND>(at, qa, (uint32_t)(2 * b + 1), (uint32_t)(col + c));
+        out[c] = e8 == kNaNScale ? make_uint4(0, 0, 0, 0) : make_uint4(lo.x, lo.y, hi.x, hi.y);
+        e8c[c] = e8;
+    }
+}
+
+// The scale of a row's block whose two halves lie in neighbouring lanes: the byte stored, and in `at` the scale that the values in
+// hand are taken at.
+template <bool RHT>
+__device__ __forceinline__ uint32_t pair_scale(Half<RHT>& v, const QuantArgs& qa, uint32_t& at) {
+    if constexpr (RHT) v.rotate(qa, kUnit);
+    uint32_t ef = v.exponent();
+    uint32_t other = __shfl_xor(ef, 1, 64);
+    ef = ef > other ? ef : other;
+    uint32_t e8 = scale_byte(ef);
+    at = e8;
+    if constexpr (RHT) {
+        if (__builtin_expect(ef == 255u, 0)) {  // a rotated value past FLT_MAX (or an input that is not finite)
+            const int fine = v.finite_inputs() ? 1 : 0;
+            v.rotate(qa, kUnitSmall);
+            uint32_t e = v.exponent();
+            other = __shfl_xor(e, 1, 64);
+            e = e > other ? e : other;
+            if (fine & __shfl_xor(fine, 1, 64)) {
+                at = scale_byte(e);
+                e8 = at + kOverflowShift;
+            }
+        }
+    }
+    return e8;
+}
+
 // ------------------------------------------------------------------------------------------------
 // Rowwise: a workgroup takes 64 rows x 256 columns (8 blocks). A thread takes 16 values of a row, its neighbour the block's
 // other half; loads are 512-byte runs, and codes and scales go through LDS, so that stores are runs of a block's rows (1 KiB
@@ -177,24 +250,8 @@ __global__ __launch_bounds__(256) void micro_rows_kernel(const uint16_t* __restr
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int r = p * 16 + r0;
-        if constexpr (RHT) v[p].rotate(qa, kUnit);
-        uint32_t ef = v[p].exponent();
-        uint32_t other = __shfl_xor(ef, 1, 64);
-        ef = ef > other ? ef : other;
-        uint32_t e8 = scale_byte(ef), at = e8;  // stored scale, and the scale that the values in hand are taken at
-        if constexpr (RHT) {
-            if (__builtin_expect(ef == 255u, 0)) {  // a rotated value past FLT_MAX (or an input that is not finite)
-                const int fine = v[p].finite_inputs() ? 1 : 0;
-                v[p].rotate(qa, kUnitSmall);
-                uint32_t e = v[p].exponent();
-                other = __shfl_xor(e, 1, 64);
-                e = e > other ? e : other;
-                if (fine & __shfl_xor(fine, 1, 64)) {
-                    at = scale_byte(e);
-                    e8 = at + kOverflowShift;
-                }
-            }
-        }
+        uint32_t at;
+        const uint32_t e8 = pair_scale(v[p], qa, at);
         const int64_t grow = GROUPED ? src + r : row0 + r;  // the SR counters number x's rows
         uint2 c = v[p].template encode<ROUND>(at, qa, (uint32_t)(col >> 4), (uint32_t)grow);
         if (e8 == kNaNScale) c = make_uint2(0, 0);
@@ -252,42 +309,7 @@ __global__ __launch_bounds__(256) void micro_cols_kernel(const uint16_t* __restr
     }
     uint4 out[2];
     uint32_t e8c[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {  // the lane's columns
-        Half<RHT> v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                v[h].w[j] = c == 0 ? __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x05040100u)
-                                   : __builtin_amdgcn_perm(m[16 * h + 2 * j + 1], m[16 * h + 2 * j], 0x07060302u);
-        uint32_t ef[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (RHT) v[h].rotate(qa, kUnit);
-            ef[h] = v[h].exponent();
-        }
-        uint32_t top = ef[0] > ef[1] ? ef[0] : ef[1];
-        uint32_t e8 = scale_byte(top), at = e8;
-        if constexpr (RHT) {
-            if (__builtin_expect(top == 255u, 0)) {
-                const bool fine = v[0].finite_inputs() && v[1].finite_inputs();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    v[h].rotate(qa, kUnitSmall);
-                    ef[h] = v[h].exponent();
-                }
-                if (fine) {
-                    at = scale_byte(ef[0] > ef[1] ? ef[0] : ef[1]);
-                    e8 = at + kOverflowShift;
-                }
-            }
-        }
-        const uint2 lo = v[0].template encode<ROUND>(at, qa, (uint32_t)(2 * b), (uint32_t)(col + c));
-        const uint2 hi = v[1].template encode<ROUND>(at, qa, (uint32_t)(2 * b + 1), (uint32_t)(col + c));
-        out[c] = e8 == kNaNScale ? make_uint4(0, 0, 0, 0) : make_uint4(lo.x, lo.y, hi.x, hi.y);
-        e8c[c] = e8;
-    }
+    quantize_columns<ROUND, RHT>(m, qa, b, col, out, e8c);
     if (b < nkb) {
         uint4* const d = reinterpret_cast<uint4*>(o.codes + panel * o.code_pld + b * 2048 + lane * 32);
         d[0] = out[0];
@@ -299,6 +321,86 @@ __global__ __launch_bounds__(256) void micro_cols_kernel(const uint16_t* __restr
     if (threadIdx.x < 32)
         *reinterpret_cast<uint4*>(o.scales + panel * o.scale_pld + g4 * 512 + threadIdx.x * 16) =
             *reinterpret_cast<const uint4*>(s_scales + threadIdx.x * 16);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Both operands from one read: a workgroup takes 128 x 128, which is four blocks of one panel of either output (8 KiB of codes
+// and 512 bytes of scales each, both contiguous). Rows as in the rowwise kernel, the tile kept in LDS on the way; then each wave
+// takes one block of 32 rows as in the transposed one.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTileStride = 2048 + 32;  // a block's row codes in LDS: 32 bytes apart in the banks
+
+template <int ROUND, bool RHT_R, bool RHT_C>
+__global__ __launch_bounds__(256) void micro_dual_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
+                                                         int64_t col_tiles, QuantArgs qr, QuantArgs qc, MicroOut o_r, MicroOut o_c) {
+    __shared__ __align__(16) uint16_t s_x[128 * 128];
+    __shared__ __align__(16) uint8_t s_codes[4 * kTileStride];
+    __shared__ __align__(16) uint8_t s_scales[2][512];  // of Q_r, of Q_c
+    const int tid = threadIdx.x;
+    const int64_t pr = blockIdx.x / col_tiles, pc = blockIdx.x - pr * col_tiles;
+    const int64_t nkb_r = cols / 32, nkb_c = rows / 32;  // blocks along the columns (Q_r), along the rows (Q_c)
+    const int part = tid & 7, r0 = tid >> 3;             // 16 columns, row within 32
+    const int64_t col = pc * 128 + part * 16;
+    Half<RHT_R> v[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int64_t row = pr * 128 + p * 32 + r0;
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;
+        if (row < rows && col < cols) {
+            const uint4* const q = reinterpret_cast<const uint4*>(x + row * ld + col);
+            a = q[0];
+            b = q[1];
+        }
+        v[p].w[0] = a.x; v[p].w[1] = a.y; v[p].w[2] = a.z; v[p].w[3] = a.w;
+        v[p].w[4] = b.x; v[p].w[5] = b.y; v[p].w[6] = b.z; v[p].w[7] = b.w;
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        uint4* const d = reinterpret_cast<uint4*>(s_x + (p * 32 + r0) * 128 + part * 16);
+        d[0] = make_uint4(v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]);
+        d[1] = make_uint4(v[p].w[4], v[p].w[5], v[p].w[6], v[p].w[7]);
+    }
+    const int blk = part >> 1, half = part & 1;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int r = p * 32 + r0;
+        uint32_t at;
+        const uint32_t e8 = pair_scale(v[p], qr, at);
+        uint2 c = v[p].template encode<ROUND>(at, qr, (uint32_t)(col >> 4), (uint32_t)(pr * 128 + r));
+        if (e8 == kNaNScale) c = make_uint2(0, 0);
+        *reinterpret_cast<uint2*>(s_codes + blk * kTileStride + r * 16 + half * 8) = c;
+        if (half == 0) s_scales[0][(blk & 1) * 256 + r * 2 + (blk >> 1)] = (uint8_t)e8;
+    }
+    __syncthreads();
+    uint8_t* const cr = o_r.codes + pr * o_r.code_pld + pc * 8192;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int u = k * 256 + tid, b = u >> 7, r = u & 127;
+        if (pc * 4 + b < nkb_r)
+            *reinterpret_cast<uint4*>(cr + b * 2048 + r * 16) = *reinterpret_cast<const uint4*>(s_codes + b * kTileStride + r * 16);
+    }
+    const int wave = tid >> 6, lane = tid & 63;
+    uint32_t m[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m[i] = *reinterpret_cast<const uint32_t*>(s_x + (wave * 32 + i) * 128 + lane * 2);
+    const int64_t bc = pr * 4 + wave;
+    uint4 out[2];
+    uint32_t e8c[2];
+    quantize_columns<ROUND, RHT_C>(m, qc, bc, pc * 128 + 2 * lane, out, e8c);
+    if (bc < nkb_c) {
+        uint4* const d = reinterpret_cast<uint4*>(o_c.codes + pc * o_c.code_pld + bc * 2048 + lane * 32);
+        d[0] = out[0];
+        d[1] = out[1];
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) s_scales[1][(wave & 1) * 256 + (2 * lane + c) * 2 + (wave >> 1)] = (uint8_t)e8c[c];
+    __syncthreads();
+    if (tid < 32)
+        *reinterpret_cast<uint4*>(o_r.scales + pr * o_r.scale_pld + pc * 512 + tid * 16) =
+            *reinterpret_cast<const uint4*>(s_scales[0] + tid * 16);
+    else if (tid < 64)
+        *reinterpret_cast<uint4*>(o_c.scales + pc * o_c.scale_pld + pr * 512 + (tid - 32) * 16) =
+            *reinterpret_cast<const uint4*>(s_scales[1] + (tid - 32) * 16);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -357,7 +459,28 @@ hipError_t launch_micro_r(const MxQuantJob& j, hipStream_t s) {
     return j.rht ? launch_micro_g<ROUND, true>(j, s) : launch_micro_g<ROUND, false>(j, s);
 }
 
+template <int ROUND>
+hipError_t launch_micro_dual_r(const MxDualJob& j, hipStream_t s) {
+    const int64_t row_tiles = padded_rows(j.rows) / 128, col_tiles = padded_rows(j.cols) / 128;
+    const unsigned g = (unsigned)(row_tiles * col_tiles);
+    const uint16_t* const x = static_cast<const uint16_t*>(j.x);
+    const MicroOut r{static_cast<uint8_t*>(j.codes_r), j.code_pld_r, static_cast<uint8_t*>(j.scales_r), j.scale_pld_r};
+    const MicroOut c{static_cast<uint8_t*>(j.codes_c), j.code_pld_c, static_cast<uint8_t*>(j.scales_c), j.scale_pld_c};
+    if (j.rht_r) {
+        if (j.rht_c) micro_dual_kernel<ROUND, true, true><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
+        else micro_dual_kernel<ROUND, true, false><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
+    } else {
+        if (j.rht_c) micro_dual_kernel<ROUND, false, true><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
+        else micro_dual_kernel<ROUND, false, false><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_quantize_mxfp4_dual(const MxDualJob& j, hipStream_t s) {
+    return j.rounding == kRoundSR ? launch_micro_dual_r<kRoundSR>(j, s) : launch_micro_dual_r<kRoundRTNE>(j, s);
+}
 
 int64_t micro_quant_tiles(int transpose, int64_t qrows, int64_t red) {
     if (transpose) return padded_rows(qrows) / 128 * ((red / 32 + 3) / 4);

@@ -172,15 +172,22 @@ def test_dequantize(rows, cols):
     assert torch.equal(U.mxfp4_dequantize(U.mxfp4_quantize(d)), d)  # values on the grid stay
 
 
+@pytest.mark.parametrize("rows,cols", [(32, 32), (128, 128), (160, 224), (96, 1056), (544, 64), (384, 640)])
 @pytest.mark.parametrize("rounding", [U.RTNE, U.SR])
-def test_dual_equals_two_calls(rounding):
-    x = _tensor(160, 224, 6)
-    a, b = U.mxfp4_quantize_dual(x, rht_cols=True, sign_mask_cols=MASK, rounding=rounding, seed=3, stream_rows=1,
-                                 stream_cols=2)
-    c = U.mxfp4_quantize(x, rounding=rounding, seed=3, stream_id=1)
-    d = U.mxfp4_quantize(x, transpose=True, rht=True, sign_mask=MASK, rounding=rounding, seed=3, stream_id=2)
+@pytest.mark.parametrize("rht_r,rht_c", [(False, False), (True, False), (False, True), (True, True)])
+def test_dual_equals_two_calls(rows, cols, rounding, rht_r, rht_c):
+    x = _tensor(rows, cols, rows + 6, pad=16)
+    x[3, 5] = float("inf")
+    out = [U.empty_qtensor(rows, cols, U.E2M1_MX32), U.empty_qtensor(cols, rows, U.E2M1_MX32)]
+    for q in out:
+        q.codes.fill_(0xEE)
+        q.scales.fill_(0xEE)
+    a, b = U.mxfp4_quantize_dual(x, rht_rows=rht_r, sign_mask_rows=0x1234, rht_cols=rht_c, sign_mask_cols=MASK, rounding=rounding,
+                                 seed=3, stream_rows=1, stream_cols=2, out_rows=out[0], out_cols=out[1])
+    c = U.mxfp4_quantize(x, rht=rht_r, sign_mask=0x1234, rounding=rounding, seed=3, stream_id=1)
+    d = U.mxfp4_quantize(x, transpose=True, rht=rht_c, sign_mask=MASK, rounding=rounding, seed=3, stream_id=2)
     for p, q in ((a, c), (b, d)):
-        assert torch.equal(p.codes_rows(), q.codes_rows()) and torch.equal(p.scales_rows(), q.scales_rows())
+        assert torch.equal(p.codes, q.codes) and torch.equal(p.scales, q.scales)  # with their padding
         assert (p.rht_block, p.sign_mask, p.rows, p.red) == (q.rht_block, q.sign_mask, q.rows, q.red)
 
 
