@@ -17,6 +17,8 @@
 #include "ufp4_device.h"
 #include "ufp4_mxfp4.h"
 
+#include <type_traits>
+
 namespace ufp4 {
 
 namespace {
@@ -280,76 +282,61 @@ __global__ __launch_bounds__(256) void micro_rows_kernel(const uint16_t* __restr
 }
 
 // ------------------------------------------------------------------------------------------------
-// Transposed: a workgroup takes 128 rows x 128 columns of x, each wave one block (32 rows); a lane holds two columns of it in
-// registers (32 loads of 256 contiguous bytes per wave) and stores 2 x 16 bytes of codes, the wave 2 KiB in one run.
-// ------------------------------------------------------------------------------------------------
-template <int ROUND, bool RHT, bool GROUPED>
-__global__ __launch_bounds__(256) void micro_cols_kernel(const uint16_t* __restrict__ x, int64_t xrows, int64_t cols,
-                                                         int64_t ld, int64_t nkb, int64_t col_tiles, const int64_t* offsets,
-                                                         int G, QuantArgs qa, MicroOut o) {
-    __shared__ __align__(16) uint8_t s_scales[512];  // [b % 2][row][2]
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int64_t g4 = blockIdx.x / col_tiles, panel = blockIdx.x - g4 * col_tiles;
-    const int64_t b = g4 * 4 + wave, col = panel * 128 + 2 * lane;
-    int64_t src = b * 32, left = b < nkb ? 32 : 0;
-    if constexpr (GROUPED) {
-        if (b >= nkb || !padded_position<32>(offsets, G, b * 32, src, left)) left = 0;
-    }
-    if (src < 0 || src >= xrows) left = 0;
-    if (left > xrows - src) left = xrows - src;
-    uint32_t m[32];
-    const uint16_t* const p = x + src * ld + col;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        m[i] = 0;
-        if (i < left) {
-            if (col + 1 < cols) m[i] = *reinterpret_cast<const uint32_t*>(p + i * ld);
-            else if (col < cols) m[i] = p[i * ld];
-        }
-    }
-    uint4 out[2];
-    uint32_t e8c[2];
-    quantize_columns<ROUND, RHT>(m, qa, b, col, out, e8c);
-    if (b < nkb) {
-        uint4* const d = reinterpret_cast<uint4*>(o.codes + panel * o.code_pld + b * 2048 + lane * 32);
-        d[0] = out[0];
-        d[1] = out[1];
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) s_scales[(wave & 1) * 256 + (2 * lane + c) * 2 + (wave >> 1)] = (uint8_t)e8c[c];
-    __syncthreads();
-    if (threadIdx.x < 32)
-        *reinterpret_cast<uint4*>(o.scales + panel * o.scale_pld + g4 * 512 + threadIdx.x * 16) =
-            *reinterpret_cast<const uint4*>(s_scales + threadIdx.x * 16);
-}
-
-// ------------------------------------------------------------------------------------------------
-// Both operands from one read: a workgroup takes 128 x 128, which is four blocks of one panel of either output (8 KiB of codes
-// and 512 bytes of scales each, both contiguous). Rows as in the rowwise kernel, the tile kept in LDS on the way; then each wave
-// takes one block of 32 rows as in the transposed one.
+// Transposed, and both operands from one read (DO_R): a workgroup takes 128 x 128 of x, which is four blocks of one panel of
+// either output (8 KiB of codes and 512 bytes of scales each, both contiguous). x comes in 256-byte runs of rows, 16 values a
+// thread, and goes to LDS (and, DO_R, through the rowwise quantization); then each wave takes one block of 32 rows of the LDS
+// tile, two columns a lane. (Without LDS, a wave loading two columns a lane from memory: 1 GiB 276 us instead of 257.)
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileStride = 2048 + 32;  // a block's row codes in LDS: 32 bytes apart in the banks
 
-template <int ROUND, bool RHT_R, bool RHT_C>
-__global__ __launch_bounds__(256) void micro_dual_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
-                                                         int64_t col_tiles, QuantArgs qr, QuantArgs qc, MicroOut o_r, MicroOut o_c) {
+// Eight columns of a row of which `left` exist.
+__device__ __forceinline__ uint4 load_columns(const uint16_t* p, int64_t left) {
+    if (left >= 8) return *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int ROUND, bool RHT_R, bool RHT_C, bool DO_R, bool GROUPED>
+__global__ __launch_bounds__(256) void micro_tile_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
+                                                         int64_t nkb_c, int64_t col_tiles, const int64_t* offsets, int G,
+                                                         QuantArgs qr, QuantArgs qc, MicroOut o_r, MicroOut o_c) {
     __shared__ __align__(16) uint16_t s_x[128 * 128];
-    __shared__ __align__(16) uint8_t s_codes[4 * kTileStride];
+    __shared__ __align__(16) uint8_t s_codes[DO_R ? 4 * kTileStride : 16];
     __shared__ __align__(16) uint8_t s_scales[2][512];  // of Q_r, of Q_c
-    const int tid = threadIdx.x;
+    __shared__ int64_t s_place[4][2];                   // grouped: each block's first row of x, rows that exist
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t pr = blockIdx.x / col_tiles, pc = blockIdx.x - pr * col_tiles;
-    const int64_t nkb_r = cols / 32, nkb_c = rows / 32;  // blocks along the columns (Q_r), along the rows (Q_c)
-    const int part = tid & 7, r0 = tid >> 3;             // 16 columns, row within 32
+    if constexpr (GROUPED) {
+        int64_t src = 0, left = 0;
+        const int64_t b = pr * 4 + wave;
+        if (b >= nkb_c || !padded_position<32>(offsets, G, b * 32, src, left)) left = 0;
+        if (src < 0 || src >= rows) left = 0;
+        if (lane == 0) {
+            s_place[wave][0] = src;
+            s_place[wave][1] = left < rows - src ? left : rows - src;
+        }
+        __syncthreads();
+    }
+    const int part = tid & 7, r0 = tid >> 3;  // 16 columns, row within 32
     const int64_t col = pc * 128 + part * 16;
+    const bool whole = (pc + 1) * 128 <= cols;  // no thread tests its columns
     Half<RHT_R> v[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const int64_t row = pr * 128 + p * 32 + r0;
+        const int64_t src = GROUPED ? s_place[p][0] : pr * 128 + p * 32, left = GROUPED ? s_place[p][1] : rows - src;
         uint4 a = make_uint4(0, 0, 0, 0), b = a;
-        if (row < rows && col < cols) {
-            const uint4* const q = reinterpret_cast<const uint4*>(x + row * ld + col);
-            a = q[0];
-            b = q[1];
+        const uint16_t* const q = x + (src + r0) * ld + col;
+        if (whole) {
+            if (r0 < left) {
+                a = reinterpret_cast<const uint4*>(q)[0];
+                b = reinterpret_cast<const uint4*>(q)[1];
+            }
+        } else if (r0 < left && col < cols) {
+            a = load_columns(q, cols - col);
+            if (col + 8 < cols) b = load_columns(q + 8, cols - col - 8);
         }
         v[p].w[0] = a.x; v[p].w[1] = a.y; v[p].w[2] = a.z; v[p].w[3] = a.w;
         v[p].w[4] = b.x; v[p].w[5] = b.y; v[p].w[6] = b.z; v[p].w[7] = b.w;
@@ -360,26 +347,30 @@ __global__ __launch_bounds__(256) void micro_dual_kernel(const uint16_t* __restr
         d[0] = make_uint4(v[p].w[0], v[p].w[1], v[p].w[2], v[p].w[3]);
         d[1] = make_uint4(v[p].w[4], v[p].w[5], v[p].w[6], v[p].w[7]);
     }
-    const int blk = part >> 1, half = part & 1;
+    if constexpr (DO_R) {
+        const int blk = part >> 1, half = part & 1;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const int r = p * 32 + r0;
-        uint32_t at;
-        const uint32_t e8 = pair_scale(v[p], qr, at);
-        uint2 c = v[p].template encode<ROUND>(at, qr, (uint32_t)(col >> 4), (uint32_t)(pr * 128 + r));
-        if (e8 == kNaNScale) c = make_uint2(0, 0);
-        *reinterpret_cast<uint2*>(s_codes + blk * kTileStride + r * 16 + half * 8) = c;
-        if (half == 0) s_scales[0][(blk & 1) * 256 + r * 2 + (blk >> 1)] = (uint8_t)e8;
+        for (int p = 0; p < 4; ++p) {
+            const int r = p * 32 + r0;
+            uint32_t at;
+            const uint32_t e8 = pair_scale(v[p], qr, at);
+            uint2 c = v[p].template encode<ROUND>(at, qr, (uint32_t)(col >> 4), (uint32_t)(pr * 128 + r));
+            if (e8 == kNaNScale) c = make_uint2(0, 0);
+            *reinterpret_cast<uint2*>(s_codes + blk * kTileStride + r * 16 + half * 8) = c;
+            if (half == 0) s_scales[0][(blk & 1) * 256 + r * 2 + (blk >> 1)] = (uint8_t)e8;
+        }
     }
     __syncthreads();
-    uint8_t* const cr = o_r.codes + pr * o_r.code_pld + pc * 8192;
+    if constexpr (DO_R) {
+        uint8_t* const cr = o_r.codes + pr * o_r.code_pld + pc * 8192;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int u = k * 256 + tid, b = u >> 7, r = u & 127;
-        if (pc * 4 + b < nkb_r)
-            *reinterpret_cast<uint4*>(cr + b * 2048 + r * 16) = *reinterpret_cast<const uint4*>(s_codes + b * kTileStride + r * 16);
+        for (int k = 0; k < 2; ++k) {
+            const int u = k * 256 + tid, b = u >> 7, r = u & 127;
+            if (pc * 4 + b < cols / 32)
+                *reinterpret_cast<uint4*>(cr + b * 2048 + r * 16) =
+                    *reinterpret_cast<const uint4*>(s_codes + b * kTileStride + r * 16);
+        }
     }
-    const int wave = tid >> 6, lane = tid & 63;
     uint32_t m[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) m[i] = *reinterpret_cast<const uint32_t*>(s_x + (wave * 32 + i) * 128 + lane * 2);
@@ -395,10 +386,10 @@ __global__ __launch_bounds__(256) void micro_dual_kernel(const uint16_t* __restr
 #pragma unroll
     for (int c = 0; c < 2; ++c) s_scales[1][(wave & 1) * 256 + (2 * lane + c) * 2 + (wave >> 1)] = (uint8_t)e8c[c];
     __syncthreads();
-    if (tid < 32)
+    if (DO_R && tid < 32)
         *reinterpret_cast<uint4*>(o_r.scales + pr * o_r.scale_pld + pc * 512 + tid * 16) =
             *reinterpret_cast<const uint4*>(s_scales[0] + tid * 16);
-    else if (tid < 64)
+    else if (tid >= 32 && tid < 64)
         *reinterpret_cast<uint4*>(o_c.scales + pc * o_c.scale_pld + pr * 512 + (tid - 32) * 16) =
             *reinterpret_cast<const uint4*>(s_scales[1] + (tid - 32) * 16);
 }
@@ -438,9 +429,8 @@ hipError_t launch_micro_t(const MxQuantJob& j, hipStream_t s) {
     const int64_t tiles = micro_quant_tiles(j.transpose, j.qrows, j.red);
     if (tiles == 0) return hipSuccess;
     if (j.transpose) {
-        const int64_t panels = padded_rows(j.qrows) / 128;
-        micro_cols_kernel<ROUND, RHT, GROUPED><<<(unsigned)tiles, 256, 0, s>>>(x, j.xrows, j.qrows, j.ld, j.red / 32, panels,
-                                                                              j.group_off, j.num_groups, j.qa, o);
+        micro_tile_kernel<ROUND, false, RHT, false, GROUPED><<<(unsigned)tiles, 256, 0, s>>>(
+            x, j.xrows, j.qrows, j.ld, j.red / 32, padded_rows(j.qrows) / 128, j.group_off, j.num_groups, j.qa, j.qa, o, o);
     } else {
         micro_rows_kernel<ROUND, RHT, GROUPED><<<(unsigned)tiles, 256, 0, s>>>(x, j.xrows, j.red, j.ld,
                                                                               (j.red + kColsTile - 1) / kColsTile, j.group_off,
@@ -466,13 +456,12 @@ hipError_t launch_micro_dual_r(const MxDualJob& j, hipStream_t s) {
     const uint16_t* const x = static_cast<const uint16_t*>(j.x);
     const MicroOut r{static_cast<uint8_t*>(j.codes_r), j.code_pld_r, static_cast<uint8_t*>(j.scales_r), j.scale_pld_r};
     const MicroOut c{static_cast<uint8_t*>(j.codes_c), j.code_pld_c, static_cast<uint8_t*>(j.scales_c), j.scale_pld_c};
-    if (j.rht_r) {
-        if (j.rht_c) micro_dual_kernel<ROUND, true, true><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
-        else micro_dual_kernel<ROUND, true, false><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
-    } else {
-        if (j.rht_c) micro_dual_kernel<ROUND, false, true><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
-        else micro_dual_kernel<ROUND, false, false><<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, col_tiles, j.qr, j.qc, r, c);
-    }
+    auto go = [&](auto rht_r, auto rht_c) {
+        micro_tile_kernel<ROUND, decltype(rht_r)::value, decltype(rht_c)::value, true, false>
+            <<<g, 256, 0, s>>>(x, j.rows, j.cols, j.ld, j.rows / 32, col_tiles, nullptr, 0, j.qr, j.qc, r, c);
+    };
+    if (j.rht_r) j.rht_c ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    else j.rht_c ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
     return hipGetLastError();
 }
 
