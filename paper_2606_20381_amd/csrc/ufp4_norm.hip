@@ -13,15 +13,52 @@
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
 
+#include <type_traits>
+
 namespace ufp4 {
 
 namespace {
 
-constexpr int kPieces = 4;  // 16-byte pieces per thread of a row in registers
 constexpr int kLongThreads = 1024;
 
 __device__ __forceinline__ float weight_at(const void* w, int w_bf16, int64_t c) {
     return w_bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(w)[c] << 16) : static_cast<const float*>(w)[c];
+}
+
+// A thread's pieces of a weight vector (bf16 or fp32, `otherwise` where there is none or past its end).
+template <int TPR, int NP, int V>
+__device__ __forceinline__ void load_weights(const void* w, int w_bf16, int64_t cols, int t, float otherwise, float (&f)[NP][V]) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[p][i] = otherwise;
+    if (!w) return;
+    auto some = [&](auto* q) {
+        using W = typename std::remove_const<typename std::remove_pointer<decltype(q)>::type>::type;
+        using P = Piece<W>;
+        constexpr int kV = V < P::V ? V : P::V;  // of a 16-byte load
+        u32x4_any raw[NP][V / kV];
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int k = 0; k < V / kV; ++k) {
+                const int64_t c = ((int64_t)p * TPR + t) * V + k * kV;
+                raw[p][k] = P::load(q + c, cols - c < kV ? cols - c : P::V <= cols - c ? P::V : kV);
+            }
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int k = 0; k < V / kV; ++k) {
+                const int64_t c = ((int64_t)p * TPR + t) * V + k * kV;
+                float g[P::V];
+                P::unpack(raw[p][k], g);
+#pragma unroll
+                for (int i = 0; i < kV; ++i)
+                    if (c + i < cols) f[p][k * kV + i] = g[i];
+            }
+    };
+    if (w_bf16) some(static_cast<const uint16_t*>(w));
+    else some(static_cast<const float*>(w));
 }
 
 // Sums of N values over the TPR threads of a row. TPR > 64: through `s` ([wave][N], one barrier; the caller alternates
@@ -47,42 +84,43 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* s) {
     }
 }
 
-template <typename T, int TPR>
+// NP 16-byte pieces per thread. The next row is on its way while this one is computed.
+template <typename T, int TPR, int NP>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormJob j) {
     using P = Piece<T>;
     constexpr int V = P::V, kRowsWG = TPR < 256 ? 256 / TPR : 1;
     __shared__ float s_sum[2][16];
     const int t = threadIdx.x % TPR;
-    float gm[kPieces][V], bt[kPieces][V];
+    const int64_t step = (int64_t)gridDim.x * kRowsWG;
+    int64_t row = (int64_t)blockIdx.x * kRowsWG + threadIdx.x / TPR;
+    auto load = [&](int64_t r, u32x4_any (&raw)[NP]) {
+        const T* const x = static_cast<const T*>(j.x) + r * j.ldx;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int64_t c = ((int64_t)p * TPR + t) * V + i;
-            gm[p][i] = j.gamma && c < j.cols ? weight_at(j.gamma, j.w_bf16, c) : 1.0f;
-            bt[p][i] = j.beta && c < j.cols ? weight_at(j.beta, j.w_bf16, c) : 0.0f;
-        }
-    const float inv_n = 1.0f / (float)j.cols;
-    for (int64_t row = (int64_t)blockIdx.x * kRowsWG + threadIdx.x / TPR; row < j.rows; row += (int64_t)gridDim.x * kRowsWG) {
-        const T* const x = static_cast<const T*>(j.x) + row * j.ldx;
-        u32x4_any raw[kPieces];
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < NP; ++p) {
             const int64_t c = ((int64_t)p * TPR + t) * V;
             raw[p] = P::load(x + c, j.cols - c);
         }
-        float f[kPieces][V], sum[1] = {0.0f};
+    };
+    u32x4_any raw[NP];
+    if (row < j.rows) load(row, raw);
+    float gm[NP][V], bt[NP][V];
+    load_weights<TPR, NP, V>(j.gamma, j.w_bf16, j.cols, t, 1.0f, gm);
+    load_weights<TPR, NP, V>(j.beta, j.w_bf16, j.cols, t, 0.0f, bt);
+    const float inv_n = 1.0f / (float)j.cols;
+    for (; row < j.rows; row += step) {
+        float f[NP][V], sum[1] = {0.0f};
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < NP; ++p) {
             P::unpack(raw[p], f[p]);
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[0] += f[p][i];
         }
+        if (row + step < j.rows) load(row + step, raw);
         row_sums<TPR, 1>(sum, s_sum[0]);
         const float mean = sum[0] * inv_n;
         float sq[1] = {0.0f};
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p)
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int64_t c = ((int64_t)p * TPR + t) * V + i;
@@ -97,7 +135,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormJob j) 
         }
         T* const y = static_cast<T*>(j.y) + row * j.ldy;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < NP; ++p) {
             const int64_t c = ((int64_t)p * TPR + t) * V;
             float o[V];
 #pragma unroll
@@ -151,74 +189,110 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob j) {
     }
 }
 
-// Backward. `part` is [gridDim.x][2][cols]: the workgroup's sums of dy h and of dy.
-template <typename T, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormBwdJob j) {
+// Backward. `part` is [gridDim.x][2][cols]: the workgroup's sums of dy h and of dy. A workgroup takes several rows at a time, as
+// many as a CU's registers hold, at one partial row per CU. kAhead: the next row is on its way while this one is computed.
+template <typename T, int TPR, int NP>
+struct BwdShape {
+    static constexpr int kRegs = NP * Piece<T>::V;  // columns per thread, about six registers each
+    static constexpr int kThreads = TPR == 1024 || kRegs <= 8 ? 1024 : 512, kRows = kThreads / TPR;
+    static constexpr bool kAhead = kThreads == 512 || kRegs <= 8;
+    static constexpr bool kFits = TPR < 1024 || kRegs <= 16;
+};
+template <typename T, int TPR, int NP>
+__global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_kernel(NormBwdJob j) {
     using P = Piece<T>;
-    constexpr int V = P::V, kRowsWG = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float s_sum[2][32];
+    using B = BwdShape<T, TPR, NP>;
+    constexpr int V = P::V, kRowsWG = B::kRows, kRowWaves = TPR / 64;
+    __shared__ float s_sum[2][B::kThreads / 64][2];
     __shared__ float s_part[kRowsWG > 1 ? kRowsWG - 1 : 1][kRowsWG > 1 ? TPR * V : 1];
     const int t = threadIdx.x % TPR, rw = threadIdx.x / TPR;
-    float gm[kPieces][V], ag[kPieces][V], ab[kPieces][V];
+    const int64_t step = (int64_t)gridDim.x * kRowsWG;
+    int64_t row = (int64_t)blockIdx.x * kRowsWG + rw;
+    u32x4_any rx[NP], rd[NP];
+    float mean = 0.0f, rstd = 0.0f;
+    auto load = [&](int64_t r) {
+        const T* const x = static_cast<const T*>(j.x) + r * j.ldx;
+        const T* const dy = static_cast<const T*>(j.dy) + r * j.lddy;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int64_t c = ((int64_t)p * TPR + t) * V + i;
-            gm[p][i] = j.gamma && c < j.cols ? weight_at(j.gamma, j.w_bf16, c) : 1.0f;
-            ag[p][i] = ab[p][i] = 0.0f;
-        }
-    const float inv_n = 1.0f / (float)j.cols;
-    int buf = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRowsWG + rw; row < j.rows; row += (int64_t)gridDim.x * kRowsWG) {
-        const T* const x = static_cast<const T*>(j.x) + row * j.ldx;
-        const T* const dy = static_cast<const T*>(j.dy) + row * j.lddy;
-        u32x4_any rx[kPieces], rd[kPieces];
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < NP; ++p) {
             const int64_t c = ((int64_t)p * TPR + t) * V;
             rx[p] = P::load(x + c, j.cols - c);
             rd[p] = P::load(dy + c, j.cols - c);  // zero past the row: its terms add nothing
         }
-        const float mean = j.mean[row], rstd = j.rstd[row];
+        mean = j.mean[r];
+        rstd = j.rstd[r];
+    };
+    if (B::kAhead && row < j.rows) load(row);
+    float gm[NP][V], ag[NP][V], ab[NP][V];
+    load_weights<TPR, NP, V>(j.gamma, j.w_bf16, j.cols, t, 1.0f, gm);
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int i = 0; i < V; ++i) ag[p][i] = ab[p][i] = 0.0f;
+    const float inv_n = 1.0f / (float)j.cols;
+    int buf = 0;
+    for (int64_t first = (int64_t)blockIdx.x * kRowsWG; first < j.rows; first += step, row += step) {  // the same for every thread
+        const bool live = row < j.rows;
         float sum[2] = {0.0f, 0.0f};
-        float h[kPieces][V], d[kPieces][V];
+        float h[NP][V], d[NP][V];
+        if (!B::kAhead && live) load(row);
+        const float r = rstd;
+        if (live) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            P::unpack(rx[p], h[p]);
-            P::unpack(rd[p], d[p]);
+            for (int p = 0; p < NP; ++p) {
+                P::unpack(rx[p], h[p]);
+                P::unpack(rd[p], d[p]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                // past the row: nothing, even where the statistics are not finite
-                const bool in = ((int64_t)p * TPR + t) * V + i < j.cols;
-                h[p][i] = in ? (h[p][i] - mean) * rstd : 0.0f;
-                ag[p][i] = __builtin_fmaf(d[p][i], h[p][i], ag[p][i]);
-                ab[p][i] += d[p][i];
-                d[p][i] *= gm[p][i];
-                sum[0] += d[p][i];
-                sum[1] = __builtin_fmaf(d[p][i], h[p][i], sum[1]);
+                for (int i = 0; i < V; ++i) {
+                    // past the row: nothing, even where the statistics are not finite
+                    const bool in = ((int64_t)p * TPR + t) * V + i < j.cols;
+                    h[p][i] = in ? (h[p][i] - mean) * r : 0.0f;
+                    ag[p][i] = __builtin_fmaf(d[p][i], h[p][i], ag[p][i]);
+                    ab[p][i] += d[p][i];
+                    d[p][i] *= gm[p][i];
+                    sum[0] += d[p][i];
+                    sum[1] = __builtin_fmaf(d[p][i], h[p][i], sum[1]);
+                }
             }
         }
-        row_sums<TPR, 2>(sum, s_sum[buf]);
-        buf ^= 1;
-        const float c1 = sum[0] * inv_n, c2 = sum[1] * inv_n;
-        T* const dx = static_cast<T*>(j.dx) + row * j.lddx;
+        if (B::kAhead && row + step < j.rows) load(row + step);
+        sum[0] = wave_sum(sum[0]);
+        sum[1] = wave_sum(sum[1]);
+        if constexpr (kRowWaves > 1) {  // one barrier a row: two arrays in turn, so that a wave ahead does not overwrite
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) {
+                s_sum[buf][wave][0] = sum[0];
+                s_sum[buf][wave][1] = sum[1];
+            }
+            __syncthreads();
+            sum[0] = sum[1] = 0.0f;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int64_t c = ((int64_t)p * TPR + t) * V;
-            float o[V];
+            for (int w = 0; w < kRowWaves; ++w) {
+                sum[0] += s_sum[buf][rw * kRowWaves + w][0];
+                sum[1] += s_sum[buf][rw * kRowWaves + w][1];
+            }
+            buf ^= 1;
+        }
+        if (live) {
+            const float c1 = sum[0] * inv_n, c2 = sum[1] * inv_n;
+            T* const dx = static_cast<T*>(j.dx) + row * j.lddx;
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = rstd * (d[p][i] - c1 - h[p][i] * c2);
-            P::store(dx + c, j.cols - c, P::pack(o));
+            for (int p = 0; p < NP; ++p) {
+                const int64_t c = ((int64_t)p * TPR + t) * V;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = r * (d[p][i] - c1 - h[p][i] * c2);
+                P::store(dx + c, j.cols - c, P::pack(o));
+            }
         }
     }
     if (!j.part) return;
-    // the workgroup's waves hold the same columns (TPR 64): added in the order of the waves, piece by piece
+    // the workgroup's rows have the same columns: added in their order, piece by piece
     float* const out = j.part + (int64_t)blockIdx.x * 2 * j.cols;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
+        for (int p = 0; p < NP; ++p) {
             if constexpr (kRowsWG > 1) {
                 __syncthreads();
                 if (rw > 0) {
@@ -319,8 +393,10 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;  // of 2 * cols
     float v = 0.0f;
-    if (c < 2 * cols)
+    if (c < 2 * cols) {
+#pragma unroll 8
         for (int i = wave; i < n; i += 16) v += part[(int64_t)i * 2 * cols + c];
+    }
     s[wave][lane] = v;
     __syncthreads();
     if (wave == 0 && c < 2 * cols) {
@@ -335,61 +411,75 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
     }
 }
 
+// Threads and pieces that a row of `pieces` 16-byte pieces takes: few pieces a thread, so that the weights (and, backward, their
+// gradient) leave registers for many waves; a wave by itself needs no barrier. A rule of kernel(threads, pieces per thread);
+// false for a row that is too long.
+template <typename F>
+bool for_row(int64_t pieces, F&& kernel) {
+    using std::integral_constant;
+    if (pieces <= 64) kernel(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (pieces <= 128) kernel(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (pieces <= 256) kernel(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (pieces <= 512) kernel(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (pieces <= 768) kernel(integral_constant<int, 256>{}, integral_constant<int, 3>{});
+    else if (pieces <= 1024) kernel(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    else if (pieces <= 2048) kernel(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    else if (pieces <= 4096) kernel(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    else return false;
+    return true;
+}
 template <typename T>
-int threads_per_row(int64_t cols) {
-    const int64_t one = (int64_t)Piece<T>::V * kPieces;  // columns per thread
-    return cols <= 64 * one ? 64 : cols <= 256 * one ? 256 : cols <= 1024 * one ? 1024 : 0;
+int64_t pieces_of(int64_t cols) {
+    return (cols + Piece<T>::V - 1) / Piece<T>::V;
 }
 
-unsigned norm_grid(int64_t rows, int tpr) {
-    const int64_t wgs = tpr == 64 ? (rows + 3) / 4 : rows;
-    const int64_t most = tpr == 1024 || tpr == 0 ? 512 : 2048;  // resident workgroups on 256 CUs
-    return (unsigned)(wgs < most ? wgs : most);
-}
+int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// Workgroups, and so partial rows of the weights' gradient, of the backward kernel.
-constexpr int64_t kMostParts = 512;
-unsigned norm_bwd_grid(int64_t rows, int tpr) {
-    const int64_t wgs = tpr == 64 ? (rows + 3) / 4 : rows;
-    return (unsigned)(wgs < kMostParts ? wgs : kMostParts);
+// Partial rows of the weights' gradient, one per workgroup of the backward kernel (one workgroup a CU); of long rows, the runs of
+// rows whose columns are summed.
+constexpr int64_t kMostParts = 256, kLongParts = 64;
+template <typename T>
+int64_t parts_of(int64_t rows, int64_t cols) {
+    int64_t n = min64(rows, kLongParts);
+    for_row(pieces_of<T>(cols), [&](auto tpr, auto np) {
+        using B = BwdShape<T, decltype(tpr)::value, decltype(np)::value>;
+        if (B::kFits) n = min64((rows + B::kRows - 1) / B::kRows, kMostParts);
+    });
+    return n;
 }
-constexpr int kLongParts = 64;
 
 template <typename T>
 hipError_t launch_norm_t(const NormJob& j, hipStream_t s) {
-    const int tpr = threads_per_row<T>(j.cols);
-    const unsigned g = norm_grid(j.rows, tpr);
-    switch (tpr) {
-        case 64: norm_kernel<T, 64><<<g, 256, 0, s>>>(j); break;
-        case 256: norm_kernel<T, 256><<<g, 256, 0, s>>>(j); break;
-        case 1024: norm_kernel<T, 1024><<<g, 1024, 0, s>>>(j); break;
-        default: norm_long_kernel<T><<<g, kLongThreads, 0, s>>>(j); break;
-    }
+    const bool fits = for_row(pieces_of<T>(j.cols), [&](auto tpr, auto np) {
+        constexpr int kTPR = decltype(tpr)::value, kThreads = kTPR < 256 ? 256 : kTPR, kRows = kThreads / kTPR;
+        const int64_t wgs = min64((j.rows + kRows - 1) / kRows, kThreads == 1024 ? 512 : 2048);  // resident on 256 CUs
+        norm_kernel<T, kTPR, decltype(np)::value><<<(unsigned)wgs, kThreads, 0, s>>>(j);
+    });
+    if (!fits) norm_long_kernel<T><<<(unsigned)min64(j.rows, 512), kLongThreads, 0, s>>>(j);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_norm_bwd_t(const NormBwdJob& j, hipStream_t s) {
-    const int tpr = threads_per_row<T>(j.cols);
-    unsigned g = norm_bwd_grid(j.rows, tpr);
-    if (g > 0) {
-        switch (tpr) {
-            case 64: norm_bwd_kernel<T, 64><<<g, 256, 0, s>>>(j); break;
-            case 256: norm_bwd_kernel<T, 256><<<g, 256, 0, s>>>(j); break;
-            case 1024: norm_bwd_kernel<T, 1024><<<g, 1024, 0, s>>>(j); break;
-            default: {
-                const unsigned rows_g = g;
-                if (j.part) {  // before dx, which may lie on x or dy
-                    g = (unsigned)(j.rows < kLongParts ? j.rows : kLongParts);
-                    norm_bwd_cols_kernel<T><<<dim3((unsigned)((j.cols + 255) / 256), g), 256, 0, s>>>(j);
-                }
-                norm_bwd_long_kernel<T><<<rows_g, kLongThreads, 0, s>>>(j);
+    const unsigned parts = (unsigned)parts_of<T>(j.rows, j.cols);
+    if (parts > 0) {
+        bool done = false;
+        for_row(pieces_of<T>(j.cols), [&](auto tpr, auto np) {
+            using B = BwdShape<T, decltype(tpr)::value, decltype(np)::value>;
+            if constexpr (B::kFits) {
+                norm_bwd_kernel<T, decltype(tpr)::value, decltype(np)::value><<<parts, B::kThreads, 0, s>>>(j);
+                done = true;
             }
+        });
+        if (!done) {
+            if (j.part)  // before dx, which may lie on x or dy
+                norm_bwd_cols_kernel<T><<<dim3((unsigned)((j.cols + 255) / 256), parts), 256, 0, s>>>(j);
+            norm_bwd_long_kernel<T><<<(unsigned)min64(j.rows, 512), kLongThreads, 0, s>>>(j);
         }
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!j.dgamma && !j.dbeta)) return e;
-    norm_reduce_kernel<<<(unsigned)((2 * j.cols + 63) / 64), 1024, 0, s>>>(j.part, (int)g, j.cols, j.dgamma, j.dbeta);
+    norm_reduce_kernel<<<(unsigned)((2 * j.cols + 63) / 64), 1024, 0, s>>>(j.part, (int)parts, j.cols, j.dgamma, j.dbeta);
     return hipGetLastError();
 }
 
@@ -404,9 +494,7 @@ hipError_t launch_norm_bwd(const NormBwdJob& j, hipStream_t s) {
 }
 
 int64_t norm_bwd_parts(int bf16, int64_t rows, int64_t cols) {
-    const int tpr = bf16 ? threads_per_row<uint16_t>(cols) : threads_per_row<float>(cols);
-    if (tpr == 0) return rows < kLongParts ? rows : kLongParts;
-    return norm_bwd_grid(rows, tpr);
+    return bf16 ? parts_of<uint16_t>(rows, cols) : parts_of<float>(rows, cols);
 }
 
 }  // namespace ufp4
