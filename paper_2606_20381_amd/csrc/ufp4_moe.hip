@@ -72,17 +72,28 @@ template <bool MANY>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(MoeSortJob j) {
     extern __shared__ char s_raw[];
     const int E = j.E;
-    int32_t* const s_base = reinterpret_cast<int32_t*>(s_raw);              // [E] first place of this workgroup's slots
-    uint16_t* const s_wave = reinterpret_cast<uint16_t*>(s_base + E + 1);   // [wave][E] slots, then their exclusive sum
+    int32_t* const s_base = reinterpret_cast<int32_t*>(s_raw);        // [E] first place of this workgroup's slots
+    int32_t* const s_total = s_base + E;                              // [E] slots in all workgroups
+    uint16_t* const s_wave = reinterpret_cast<uint16_t*>(s_total + E);  // [wave][E] slots, then their exclusive sum
     __shared__ int32_t s_scan[kSortWaves];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    for (int i = tid; i < kSortWaves * E; i += kSortThreads) s_wave[i] = 0;
-    __syncthreads();
-
     const int64_t first = (int64_t)blockIdx.x * kRun + wave * kWaveRun;
     int key[kRounds], rank[kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) key[r] = sort_key(j, first + r * 64 + lane);
+    for (int i = tid; i < kSortWaves * E; i += kSortThreads) s_wave[i] = 0;
+    if (!MANY && j.runs > 1)
+        for (int e = tid; e < E; e += kSortThreads) s_base[e] = s_total[e] = 0;
+    __syncthreads();
+    if (!MANY && j.runs > 1) {  // a workgroup's counts per wave (integers: the order of the additions does not show)
+        for (int64_t b = wave; b < j.runs; b += kSortWaves)
+            for (int e = lane; e < E; e += 64) {
+                const int32_t c = j.counts[b * E + e];
+                if (c == 0) continue;
+                atomicAdd(&s_total[e], c);
+                if (b < blockIdx.x) atomicAdd(&s_base[e], c);
+            }
+    }
     int bits = 0;
     while ((1 << bits) <= E) ++bits;
     const uint64_t below = (1ull << lane) - 1;
@@ -118,11 +129,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(MoeSortJob j) 
             before = j.counts[(int64_t)blockIdx.x * E + tid];
             total = j.counts[j.runs * E + tid];
         } else if (j.runs > 1) {
-            for (int64_t b = 0; b < j.runs; ++b) {
-                const int32_t c = j.counts[b * E + tid];
-                if (b < blockIdx.x) before += c;
-                total += c;
-            }
+            before = s_base[tid];
+            total = s_total[tid];
         } else {
             total = own;
         }
@@ -327,7 +335,7 @@ hipError_t launch_moe_sort(const MoeSortJob& j, hipStream_t s) {
         sort_count_kernel<<<(unsigned)j.runs, kSortThreads, j.E * sizeof(int32_t), s>>>(j);
         if (j.runs > kAddUp) sort_scan_kernel<<<(unsigned)((j.E + 3) / 4), 256, 0, s>>>(j);
     }
-    const size_t lds = (j.E + 1) * sizeof(int32_t) + kSortWaves * j.E * sizeof(uint16_t);
+    const size_t lds = 2 * j.E * sizeof(int32_t) + kSortWaves * j.E * sizeof(uint16_t);
     if (j.runs > kAddUp) sort_place_kernel<true><<<(unsigned)j.runs, kSortThreads, lds, s>>>(j);
     else sort_place_kernel<false><<<(unsigned)j.runs, kSortThreads, lds, s>>>(j);
     return hipGetLastError();
