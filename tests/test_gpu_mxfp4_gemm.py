@@ -202,7 +202,8 @@ def test_grouped_neighbours_with_extreme_scales():
 
 
 @pytest.mark.parametrize("tokens", [1, 2, 3, 5, 8, 15, 16, 17, 40])
-@pytest.mark.parametrize("N,K", [(1, 32), (16, 64), (100, 224), (256, 4096), (2048, 1056), (8300, 160), (520, 16384)])
+@pytest.mark.parametrize("N,K", [(1, 32), (16, 64), (100, 224), (256, 4096), (2048, 1056), (8300, 160), (520, 16384),
+                                 (33000, 288), (16500, 1024), (300, 33024)])
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_linear(tokens, N, K, dt):
     g = torch.Generator(device="cuda").manual_seed(tokens + N)
