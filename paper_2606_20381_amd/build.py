@@ -35,7 +35,7 @@ FLAGS = [
     "-Wno-unused-function",
 ]
 # MFMA results in VGPRs: the GEMM epilogue reads them with plain VALU FMAs (no AGPR copies). Not the microscaled 4-bit GEMM,
-# whose largest tile holds 256 results a lane: with the operands that is more than the 256 VGPRs, so they are AGPRs.
+# whose largest tile holds 128 results a lane and two sets of operands: with the results in AGPRs nothing is spilled.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 AGPR_SOURCES = ("ufp4_gemm_mxfp4.hip",)
 

@@ -3,9 +3,13 @@
 //
 // A lane of the instruction holds the 32 codes of one row and one 32-block: 16 bytes, one LDS read. K advances 128 (four
 // blocks) per stage; a panel's stage is 8 KiB of codes and 512 bytes of scales, both contiguous, copied unchanged into a
-// four-deep LDS ring by direct-to-LDS loads. Each wave keeps two sets of operands in registers: while the matrix core works
+// three-deep LDS ring by direct-to-LDS loads (a fourth slot measured the same). Each wave keeps two sets of operands in registers: while the matrix core works
 // on one half of a stage, the other half (or, past the barrier, the next stage's first half) is read from LDS, so that
 // neither the barrier nor the LDS latency stands between two matrix instructions.
+//
+// Bound by the matrix cores' power where the reduction is long: the instruction alone, on registers, reaches 5.5 PFLOP/s (the
+// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.78 ms = 4.9. Where it is short, by the stores, which take the memory
+// system from the loads: 16384 x 16384 x 2048 takes 0.29-0.31 ms = 3.6 PFLOP/s, without its stores 0.235 ms.
 
 #include "ufp4_internal.h"
 #include "ufp4_mxfp4.h"
@@ -177,7 +181,7 @@ __device__ __forceinline__ void group_blocks(const MxGemmJob& j, int g, int& fir
     end = first + uniform(blocks(g));
 }
 
-template <int OUT, class C, int MODE>
+template <int OUT, class C, int MODE, bool STREAM>
 __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGemmJob j) {
     using S = Slot<C>;
     constexpr int kRing = C::kRing;
@@ -393,17 +397,19 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
     constexpr bool kLine = OUT == kOutF32 || WTN % 2 == 0;  // a lone bf16 tile stays at 64 bytes
     auto store = [&](const Work& w, auto inside) INLINE {
         const int64_t N = j.N;
-        // one store: v, in rows r0 + lane's, columns c0 + lane's of the wave's part of the tile
+        // one store: v, at row lr and column col of the tile; at the output's right edge the pieces that are inside are still whole
         auto put = [&](const uint32_t (&v)[4], int lr, int col) INLINE {
             const int64_t off = w.c_base + (int64_t)(w.row0 + lr) * j.ldc + w.col0 + col;
-            if constexpr (decltype(inside)::value) {
+            const int64_t left = N - w.col0 - col;  // columns from this lane's first
+            if (decltype(inside)::value || (lr < w.rows && left >= kElems)) {
                 const u32x4_any x = {v[0], v[1], v[2], v[3]};
-                if constexpr (OUT == kOutF32) *reinterpret_cast<u32x4_any*>(static_cast<float*>(j.c) + off) = x;
-                else *reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(j.c) + off) = x;
+                u32x4_any* const to = reinterpret_cast<u32x4_any*>(static_cast<uint8_t*>(j.c) + off * (OUT == kOutF32 ? 4 : 2));
+                if constexpr (STREAM) __builtin_nontemporal_store(x, to);
+                else *to = x;
             } else if (lr < w.rows) {
 #pragma unroll
                 for (int e = 0; e < kElems; ++e) {
-                    if (w.col0 + col + e >= N) continue;
+                    if (e >= left) continue;
                     if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[off + e] = __uint_as_float(v[e]);
                     else static_cast<uint16_t*>(j.c)[off + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
                 }
@@ -594,7 +600,7 @@ using Tile64K = Tile<1, 1, 2, 2, 3, 1, 4>;   // 64 x 64 by four teams of 4 waves
 
 int64_t grid_tiles(const MxGemmJob& j, int bm, int bn) { return ((j.N + bn - 1) / bn) * tile_rows(j, bm); }
 
-template <int OUT, class C>
+template <int OUT, class C, bool STREAM>
 hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
     int64_t tiles = grid_tiles(j, C::BM, C::BN);
     if (tiles == 0) return hipSuccess;
@@ -603,11 +609,22 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
     if (j.mode == kGemmRaggedK) tiles *= j.G;
     else if (tiles > C::kResident) tiles = C::kResident;
     switch (j.mode) {
-        case kGemmRaggedM: gemm_mxfp4_kernel<OUT, C, kGemmRaggedM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
-        case kGemmRaggedK: gemm_mxfp4_kernel<OUT, C, kGemmRaggedK><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
-        default: gemm_mxfp4_kernel<OUT, C, kGemmDense><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+        case kGemmRaggedM: gemm_mxfp4_kernel<OUT, C, kGemmRaggedM, STREAM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+        case kGemmRaggedK: gemm_mxfp4_kernel<OUT, C, kGemmRaggedK, STREAM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
+        default: gemm_mxfp4_kernel<OUT, C, kGemmDense, STREAM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j); break;
     }
     return hipGetLastError();
+}
+
+// Outputs of 256 MiB and more (the memory-side cache holds that much) are stored nontemporally: they cannot stay in a cache, and
+// in the L2's recency order they push the operands out. Measured, us, nontemporal / plain: 16384 x 16384 x 2048 bf16 311 / 398,
+// fp32 393 / 602 (95 MB read instead of 212), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
+// gradient 259 / 322; at 256 MiB 8192 x 8192 fp32 of 1024 74 / 97, of 2048 107 / 99, of 8192 254 / 267; below, 8192 x 8192 x 2048
+// bf16 83 / 77. The 64-row tiles are not taken for outputs of that size.
+constexpr int64_t kStreamBytes = int64_t(256) << 20;
+
+bool streams(const MxGemmJob& j) {
+    return j.M * j.N * (j.mode == kGemmRaggedK ? j.G : 1) * (j.out_dtype == kOutF32 ? 4 : 2) >= kStreamBytes;
 }
 
 // Which tile takes a problem: the one with the smallest estimated time
@@ -615,8 +632,9 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
 // R the most tiles that one of 256 CUs takes, `alone` the time of a stage (128 of the reduction) on a CU with one tile, `busy`
 // what each tile's stage costs where they queue. Microseconds, measured on gfx950; the largest tile moves the fewest bytes per
 // product and wins where its tiles fill the chip. Measured, us, 256 / 128 / 64 / 64 in four teams:
-//     8192 x 8192 x 2048 80 / 93 / 145 / 262, 4096^3 37 / 42 / 72 / 103, 2048^3 17.2 / 10.2 / 12.3 / 18.9,
-//     256 x 8192 x 2048 16.4 / 9.1 / 8.2 / 10.9, 64 x 2048 x 8192 40 / 22 / 15.1 / 11.9, 256 x 256 x 32768 134 / 68 / 49 / 34.
+//     8192 x 8192 x 2048 78 / 89 / 155 / 266, 8192 x 4096 x 1024 31 / 30 / 46 / 99, 4096^3 36 / 42 / 68 / 100,
+//     2048^3 16.3 / 9.5 / 11.3 / 17.9, 256 x 8192 x 2048 15.8 / 9.0 / 7.5 / 10.4, 64 x 2048 x 8192 38 / 20 / 14.8 / 11.7,
+//     256 x 256 x 32768 133 / 67 / 49 / 33.
 // The four teams are bound by what one CU can load (64 bytes a clock); more would need sums across workgroups.
 enum { kTile256, kTile128, kTile64, kTile64K, kKernels };
 struct Cost {
@@ -624,8 +642,8 @@ struct Cost {
     double fixed, again, alone, busy;
 };
 constexpr Cost kCost[kKernels] = {
-    {Tile256::BM, Tile256::kThreads, 9.0, 3.5, 0.48, 0.85},
-    {Tile128::BM, Tile128::kThreads, 6.2, 0.6, 0.24, 0.28},
+    {Tile256::BM, Tile256::kThreads, 9.0, 4.5, 0.48, 0.85},
+    {Tile128::BM, Tile128::kThreads, 6.2, 0.75, 0.24, 0.28},
     {Tile64::BM, Tile64::kThreads, 5.4, 0.2, 0.15, 0.115},
     {Tile64K::BM, Tile64K::kThreads, 6.2, 3.0, 0.10, 0.10},
 };
@@ -654,10 +672,10 @@ int pick_tile(const MxGemmJob& j) {
 template <int OUT>
 hipError_t launch_out(const MxGemmJob& j, hipStream_t s) {
     switch (pick_tile(j)) {
-        case kTile256: return launch_tile<OUT, Tile256>(j, s);
-        case kTile128: return launch_tile<OUT, Tile128>(j, s);
-        case kTile64: return launch_tile<OUT, Tile64>(j, s);
-        default: return launch_tile<OUT, Tile64K>(j, s);
+        case kTile256: return streams(j) ? launch_tile<OUT, Tile256, true>(j, s) : launch_tile<OUT, Tile256, false>(j, s);
+        case kTile128: return streams(j) ? launch_tile<OUT, Tile128, true>(j, s) : launch_tile<OUT, Tile128, false>(j, s);
+        case kTile64: return launch_tile<OUT, Tile64, false>(j, s);
+        default: return launch_tile<OUT, Tile64K, false>(j, s);
     }
 }
 

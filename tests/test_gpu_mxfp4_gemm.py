@@ -282,3 +282,47 @@ def test_refusals():
     dyq = U.mxfp4_quantize_grouped(dy, off, 256, transpose=False)
     with pytest.raises(U.UFP4Error):
         U.mxfp4_gemm_bwd_dx_grouped(dyq, U.mxfp4_quantize(torch.randn(192, 64, device="cuda").to(BF), transpose=True), off, 4)
+
+
+def _small(rows, cols, seed, by_rows):
+    """Small integers whose blocks along the rows (by_rows) or the columns have the scale 1."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randint(-3, 4, (rows, cols), generator=g, device="cuda").to(BF)
+    if by_rows:
+        x[:, ::32] = 4
+    else:
+        x[::32] = 4
+    return x
+
+
+@pytest.mark.parametrize("kernel,counts,N,K", [(1, [9000, 0, 1, 5000, 2390], 8192, 128), (0, [12000, 3, 4600], 8192, 1056)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_large_grouped_outputs(kernel, counts, N, K, dt):
+    """Outputs of 256 MiB and more are stored by kernels of their own: exact products again."""
+    G, total = len(counts), sum(counts)
+    assert total * N * 2 >= 1 << 28
+    off, p128 = U.group_offsets(counts, block=128)
+    assert _plan(total, N, K, 1, G, p128) == kernel
+    x, w = _small(total, K, 1, True), _small(G * N, K, 2, True)
+    y = U.mxfp4_gemm_fwd_y_grouped(U.mxfp4_quantize_grouped(x, off, p128, transpose=False), U.mxfp4_quantize(w), off, total, dt)
+    for e, s in enumerate(_groups(counts, total)):
+        assert torch.equal(y[s], (x[s].double() @ w[e * N : (e + 1) * N].double().t()).to(dt))
+
+
+@pytest.mark.parametrize("kernel,counts,N,K", [(1, [96, 0, 1, 128, 70], 4096, 3400), (0, [3500, 3, 3000], 4200, 5400)])
+def test_large_weight_gradients(kernel, counts, N, K):
+    G, total = len(counts), sum(counts)
+    assert G * N * K * 4 >= 1 << 28
+    off, p32 = U.group_offsets(counts, block=32)
+    assert _plan(N, K, p32, 2, G, N) == kernel
+    starts = [0] + torch.tensor(counts).cumsum(0).tolist()
+    x, dy = _small(total, K, 1, False), _small(total, N, 2, False)
+    for a in starts[:-1]:  # each group's blocks begin with its first token
+        if a < total:
+            x[a : a + 1], dy[a : a + 1] = 4, 4
+    for e, s in enumerate(_groups(counts, total)):
+        x[s][::32], dy[s][::32] = 4, 4
+    q = [U.mxfp4_quantize_grouped(t, off, p32, transpose=True) for t in (dy, x)]
+    dw = U.mxfp4_gemm_bwd_dw_grouped(*q, off)
+    for e, s in enumerate(_groups(counts, total)):
+        assert torch.equal(dw[e].double(), dy[s].double().t().contiguous() @ x[s].double())
