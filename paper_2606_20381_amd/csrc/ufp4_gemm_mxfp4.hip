@@ -120,40 +120,41 @@ struct Groups {
 
     __device__ __forceinline__ void build(const MxGemmJob& j) {
         const int G = j.G, lane = threadIdx.x & 63;
-        int tiles = 0, units = 0;
+        int64_t tiles = 0, units = 0;  // what offsets claim can sum to more than 32 bits; 64 groups of it cannot
+        auto cut = [](int64_t v) { return v > INT32_MAX ? INT32_MAX : (int)v; };
         for (int g0 = 0; g0 < G; g0 += 64) {
             const int g = g0 + lane;
             const int64_t start = g < G ? j.offsets[g] : 0;
             int64_t m = g < G ? j.offsets[g + 1] - start : 0;
-            m = m < 0 ? 0 : m > (int64_t(1) << 30) ? int64_t(1) << 30 : m;
-            const int cnt = (int)((m + BM - 1) / BM), n = (int)((m + 127) / 128);
-            int ti = cnt, ni = n;
+            m = m < 0 ? 0 : m > INT32_MAX ? INT32_MAX : m;
+            const uint32_t cnt = (uint32_t)((m + BM - 1) / BM), n = (uint32_t)((m + 127) / 128);
+            uint32_t ti = cnt, ni = n;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
-                const int vt = __shfl_up(ti, d, 64), vn = __shfl_up(ni, d, 64);
+                const uint32_t vt = __shfl_up(ti, d, 64), vn = __shfl_up(ni, d, 64);
                 if (lane >= d) {
                     ti += vt;
                     ni += vn;
                 }
             }
             if (g < G) {
-                unit[g] = units + ni - n;
-                token[g] = start < 0 ? -1 : start > INT32_MAX ? INT32_MAX : (int)start;
-                if constexpr (BM > 128) tile[g] = tiles + ti - cnt;
+                unit[g] = cut(units + (ni - n));
+                token[g] = start < 0 ? -1 : cut(start);
+                if constexpr (BM > 128) tile[g] = cut(tiles + (ti - cnt));
             }
-            tiles += __shfl(ti, 63, 64);
-            units += __shfl(ni, 63, 64);
+            tiles += (uint32_t)__shfl(ti, 63, 64);
+            units += (uint32_t)__shfl(ni, 63, 64);
         }
         if (lane == 0) {
             const int64_t end = j.offsets[G];
-            unit[G] = units;
-            token[G] = end < 0 ? -1 : end > INT32_MAX ? INT32_MAX : (int)end;
-            if constexpr (BM > 128) tile[G] = tiles;
+            unit[G] = cut(units);
+            token[G] = end < 0 ? -1 : cut(end);
+            if constexpr (BM > 128) tile[G] = cut(tiles);
         }
     }
     __device__ __forceinline__ int first_tile(int g) const {
         if constexpr (BM > 128) return tile[g];
-        else return unit[g] * kTilesPerPanel;
+        else return unit[g] > INT32_MAX / kTilesPerPanel ? INT32_MAX : unit[g] * kTilesPerPanel;
     }
     // The group that holds tile row t: the last one whose first tile row is at most t (empty groups share their successor's).
     __device__ __forceinline__ int of(int G, int t) const {
@@ -171,14 +172,15 @@ __device__ __forceinline__ void group_blocks(const MxGemmJob& j, int g, int& fir
     const int lane = threadIdx.x & 63;
     auto blocks = [&](int h) {
         const int64_t m = j.offsets[h + 1] - j.offsets[h];
-        return m <= 0 ? 0 : m > (int64_t(1) << 30) ? 1 << 25 : (int)((m + 31) / 32);
+        return m <= 0 ? 0 : m > INT32_MAX ? int64_t(1) << 26 : (m + 31) / 32;
     };
-    int sum = 0;
+    int64_t sum = 0;
     for (int h = lane; h < g; h += 64) sum += blocks(h);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-    first = uniform(sum);
-    end = first + uniform(blocks(g));
+    const int64_t stop = sum + blocks(g);  // clamped to the operands: fewer than 2^31 blocks
+    first = uniform((int)(sum < j.nkb ? sum : j.nkb));
+    end = uniform((int)(stop < j.nkb ? stop : j.nkb));
 }
 
 template <int OUT, class C, int MODE, bool STREAM>
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
             int first, end;
             group_blocks(j, g, first, end);
             kbf = first;
-            kbe = end < j.nkb ? end : j.nkb;  // clamped to the operands
+            kbe = end;
             w.c_base = (int64_t)g * j.M * j.ldc;
         }
         // Stages are whole groups of four blocks (the scales' unit). A ragged reduction may begin and end inside one.

@@ -326,3 +326,22 @@ def test_large_weight_gradients(kernel, counts, N, K):
     dw = U.mxfp4_gemm_bwd_dw_grouped(*q, off)
     for e, s in enumerate(_groups(counts, total)):
         assert torch.equal(dw[e].double(), dy[s].double().t().contiguous() @ x[s].double())
+
+
+@pytest.mark.parametrize("claim", [2**20, 2**31 - 1, 2**33, 2**40])
+def test_offsets_that_claim_too_much(claim):
+    """Groups past the tokens that there are, in numbers whose sums pass 32 bits: the first group's results stand, and nothing
+    past the output is written."""
+    N, K, G = 256, 160, 130
+    x, dy = torch.randn(100, K, device="cuda").to(BF), torch.randn(100, N, device="cuda").to(BF)
+    wq = U.mxfp4_quantize(torch.randn(G * N, K, device="cuda").to(BF))
+    off = torch.tensor([0] + [100 + g * claim for g in range(G)], device="cuda")
+    xq = U.mxfp4_quantize_grouped(x, off, 256, transpose=False)
+    out = torch.full((130, N), -7.0, dtype=F32, device="cuda")
+    U.mxfp4_gemm_fwd_y_grouped(xq, wq, off, 100, F32, out=out[:100])
+    _within(out[:100], _values(U.mxfp4_quantize(x)), _values(wq)[:N], K, F32)
+    assert (out[100:] == -7).all()
+    xtq, dytq = (U.mxfp4_quantize_grouped(t, off, 160, transpose=True) for t in (x, dy))
+    dw = U.mxfp4_gemm_bwd_dw_grouped(dytq, xtq, off)
+    _within(dw[0], _values(dytq)[:, :128], _values(xtq)[:, :128], 128, F32)
+    assert not dw[2:].any()
