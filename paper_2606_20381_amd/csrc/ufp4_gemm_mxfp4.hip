@@ -618,13 +618,11 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Outputs of 256 MiB and more (the memory-side cache holds that much) are stored nontemporally: they cannot stay in a cache, and
+// Outputs of kStreamBytes and more are stored nontemporally: they cannot stay in a cache, and
 // in the L2's recency order they push the operands out. Measured, us, nontemporal / plain: 16384 x 16384 x 2048 bf16 311 / 398,
 // fp32 393 / 602 (95 MB read instead of 212), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
 // gradient 259 / 322; at 256 MiB 8192 x 8192 fp32 of 1024 74 / 97, of 2048 107 / 99, of 8192 254 / 267; below, 8192 x 8192 x 2048
 // bf16 83 / 77. The 64-row tiles are not taken for outputs of that size.
-constexpr int64_t kStreamBytes = int64_t(256) << 20;
-
 bool streams(const MxGemmJob& j) {
     return j.M * j.N * (j.mode == kGemmRaggedK ? j.G : 1) * (j.out_dtype == kOutF32 ? 4 : 2) >= kStreamBytes;
 }

@@ -212,6 +212,10 @@ int64_t micro_decode_tiles(int64_t rows, int64_t red);
 constexpr int kMxfp4Groups = 1024;  // groups of its grouped forms: as many as the quantizers take
 hipError_t launch_gemm_mxfp4(const MxGemmJob& job, hipStream_t stream);
 
+// What a kernel streams past the 256 MiB of the memory-side cache cannot stay there: from this size on outputs are stored (or
+// inputs read) nontemporally, so that they do not push what is used again out of the L2s.
+constexpr int64_t kStreamBytes = int64_t(256) << 20;
+
 // y [M, N] = Q(x) W^T, M <= kLinearTokens tokens of bf16 x, W [N, nkb * 32] a plain microscaled 4-bit operand.
 constexpr int kLinearTokens = 16;
 struct LinearJob {

@@ -193,7 +193,7 @@ __device__ __forceinline__ void zero_rows(T* out, int64_t ldo, int64_t first, in
         }
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void dispatch_kernel(MoeRowsJob j) {
     using P = Piece<T>;
     constexpr int V = P::V;
@@ -224,13 +224,13 @@ __global__ __launch_bounds__(256) void dispatch_kernel(MoeRowsJob j) {
                 for (int i = 0; i < V; ++i) f[i] *= w;
                 r = P::pack(f);
             }
-            P::store(out + row * j.ldo + c, j.cols - c, r);
+            P::template store<STREAM>(out + row * j.ldo + c, j.cols - c, r);
         }
     }
     zero_rows<T>(out, j.ldo, used, j.rows_y, t, j.tokens, c0, j.cols);
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
     using P = Piece<T>;
     constexpr int V = P::V;
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
         for (int p = 0; p < kSegPieces; ++p) {
             const int64_t c = c0 + p * 64 * V;
             float f[V];
-            P::unpack(P::load(y + row * j.ldi + c, j.cols - c), f);
+            P::unpack(P::template load<STREAM>(y + row * j.ldi + c, j.cols - c), f);
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[p][i] = __builtin_fmaf(w, f[i], acc[p][i]);
         }
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
 
 // One workgroup per token: dout's segment in registers, each expert's row of y against it, the dot products added over the
 // lanes, then over the waves in order.
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
     using P = Piece<T>;
     constexpr int V = P::V;
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
                     dot = __builtin_fmaf(d[i], f[i], dot);
                     d[i] *= w;
                 }
-                P::store(dy + row * j.lddy + c, j.cols - c, P::pack(d));
+                P::template store<STREAM>(dy + row * j.lddy + c, j.cols - c, P::pack(d));
             }
             dot = wave_sum(dot);
             if (lane == 0) s_dot[wave][q] += dot;
@@ -341,25 +341,35 @@ hipError_t launch_moe_sort(const MoeSortJob& j, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Rows by expert of kStreamBytes and more are stored (dispatch) and read (combine) nontemporally: no cache holds them until they
+// are used again, and kept in order of recency they push out what is. bf16, 16384 tokens x 6 x 2048 (403 MB), us, nontemporal /
+// plain: dispatch 80 / 92, combine 80 / 95, one after the other 160 / 204; 8192 tokens (201 MB) 42 / 35, 42 / 36, 84 / 72.
+// combine_bwd reads one such tensor and writes another, so its stores take half the size: 16384 tokens 217 / 222, 8192 94 / 117,
+// 4096 51 / 52.
 hipError_t launch_moe_dispatch(MoeRowsJob j, hipStream_t s) {
     j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
     const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
-    if (j.bf16) dispatch_kernel<uint16_t><<<g, 256, 0, s>>>(j);
-    else dispatch_kernel<float><<<g, 256, 0, s>>>(j);
+    const bool stream = j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
+    if (j.bf16) stream ? dispatch_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : dispatch_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
+    else stream ? dispatch_kernel<float, true><<<g, 256, 0, s>>>(j) : dispatch_kernel<float, false><<<g, 256, 0, s>>>(j);
     return hipGetLastError();
 }
 
 hipError_t launch_moe_combine(MoeRowsJob j, hipStream_t s) {
     j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
     const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
-    if (j.bf16) combine_kernel<uint16_t><<<g, 256, 0, s>>>(j);
-    else combine_kernel<float><<<g, 256, 0, s>>>(j);
+    const bool stream = j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
+    if (j.bf16) stream ? combine_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : combine_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
+    else stream ? combine_kernel<float, true><<<g, 256, 0, s>>>(j) : combine_kernel<float, false><<<g, 256, 0, s>>>(j);
     return hipGetLastError();
 }
 
 hipError_t launch_moe_combine_bwd(const MoeBwdJob& j, hipStream_t s) {
-    if (j.bf16) combine_bwd_kernel<uint16_t><<<(unsigned)j.tokens, 256, 0, s>>>(j);
-    else combine_bwd_kernel<float><<<(unsigned)j.tokens, 256, 0, s>>>(j);
+    const unsigned g = (unsigned)j.tokens;
+    const bool stream = 2 * j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
+    if (j.bf16)
+        stream ? combine_bwd_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
+    else stream ? combine_bwd_kernel<float, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<float, false><<<g, 256, 0, s>>>(j);
     return hipGetLastError();
 }
 

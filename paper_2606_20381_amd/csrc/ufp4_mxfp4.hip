@@ -16,6 +16,7 @@
 #include "ufp4_internal.h"
 #include "ufp4_device.h"
 #include "ufp4_mxfp4.h"
+#include "ufp4_rows.h"
 
 #include <type_traits>
 
@@ -396,8 +397,10 @@ __global__ __launch_bounds__(256) void micro_tile_kernel(const uint16_t* __restr
 
 // ------------------------------------------------------------------------------------------------
 // Codes and scales to bf16 (exact: a level has two significant bits; 6 * 2^127 is infinity): a lane takes 8 values, 32 lanes a
-// run of 512 bytes of a row.
+// run of 512 bytes of a row. Outputs of kStreamBytes and more are stored nontemporally (us, so / plainly: 1 GiB 243 / 258, 512 MiB
+// 99 / 131, 369 MB 67 / 92, 134 MB 26 / 26).
 // ------------------------------------------------------------------------------------------------
+template <bool STREAM>
 __global__ __launch_bounds__(256) void micro_decode_kernel(MicroOut q, int64_t rows, int64_t red, int64_t col_tiles,
                                                            uint16_t* __restrict__ out, int64_t ldo) {
     const int64_t rt = blockIdx.x / col_tiles, ct = blockIdx.x - rt * col_tiles;
@@ -413,12 +416,12 @@ __global__ __launch_bounds__(256) void micro_decode_kernel(MicroOut q, int64_t r
         const uint32_t c = *reinterpret_cast<const uint32_t*>(q.codes + p * q.code_pld + b * 2048 + i * 16 + (part & 3) * 4);
         const uint32_t e8 = q.scales[p * q.scale_pld + (b / 4) * 512 + (b & 1) * 256 + i * 2 + ((b >> 1) & 1)];
         const float scale = __uint_as_float(e8 << 23);
-        uint4 r;
-        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
-        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
-        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
-        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
-        *reinterpret_cast<uint4*>(out + row * ldo + col) = r;
+        u32x4_any r;
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+        r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+        r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+        Piece<uint16_t>::store<STREAM>(out + row * ldo + col, 8, r);
     }
 }
 
@@ -488,8 +491,8 @@ hipError_t launch_dequantize_mxfp4(const void* codes, int64_t code_pld, const vo
                      static_cast<uint8_t*>(const_cast<void*>(scales)), scale_pld};
     const int64_t tiles = micro_decode_tiles(rows, red);
     if (tiles == 0) return hipSuccess;
-    micro_decode_kernel<<<(unsigned)tiles, 256, 0, s>>>(q, rows, red, (red + kColsTile - 1) / kColsTile,
-                                                        static_cast<uint16_t*>(out), ldo);
+    const auto kernel = rows * red * 2 >= kStreamBytes ? micro_decode_kernel<true> : micro_decode_kernel<false>;
+    kernel<<<(unsigned)tiles, 256, 0, s>>>(q, rows, red, (red + kColsTile - 1) / kColsTile, static_cast<uint16_t*>(out), ldo);
     return hipGetLastError();
 }
 

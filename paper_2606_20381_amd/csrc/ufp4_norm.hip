@@ -85,7 +85,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* s) {
 }
 
 // NP 16-byte pieces per thread. The next row is on its way while this one is computed.
-template <typename T, int TPR, int NP>
+template <typename T, int TPR, int NP, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormJob j) {
     using P = Piece<T>;
     constexpr int V = P::V, kRowsWG = TPR < 256 ? 256 / TPR : 1;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormJob j) 
             float o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = __builtin_fmaf(f[p][i] * rstd, gm[p][i], bt[p][i]);
-            P::store(y + c, j.cols - c, P::pack(o));
+            P::template store<STREAM>(y + c, j.cols - c, P::pack(o));
         }
     }
 }
@@ -198,7 +198,7 @@ struct BwdShape {
     static constexpr bool kAhead = kThreads == 512 || kRegs <= 8;
     static constexpr bool kFits = TPR < 1024 || kRegs <= 16;
 };
-template <typename T, int TPR, int NP>
+template <typename T, int TPR, int NP, bool STREAM>
 __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_kernel(NormBwdJob j) {
     using P = Piece<T>;
     using B = BwdShape<T, TPR, NP>;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
                 float o[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) o[i] = r * (d[p][i] - c1 - h[p][i] * c2);
-                P::store(dx + c, j.cols - c, P::pack(o));
+                P::template store<STREAM>(dx + c, j.cols - c, P::pack(o));
             }
         }
     }
@@ -448,12 +448,22 @@ int64_t parts_of(int64_t rows, int64_t cols) {
     return n;
 }
 
+// Whether `n` tensors of this shape, read and written, are kStreamBytes and more: the output is then stored nontemporally. us, so /
+// plainly, bf16: forward 16384 x 5120 55 / 65, 65536 x 2048 90 / 107, 32768 x 5120 127 / 131; backward 32768 x 2048 68 / 80,
+// 16384 x 5120 101 / 103.
+template <typename T>
+bool streams(int n, int64_t rows, int64_t cols) {
+    return rows * cols * (int64_t)sizeof(T) * n >= kStreamBytes;
+}
+
 template <typename T>
 hipError_t launch_norm_t(const NormJob& j, hipStream_t s) {
     const bool fits = for_row(pieces_of<T>(j.cols), [&](auto tpr, auto np) {
         constexpr int kTPR = decltype(tpr)::value, kThreads = kTPR < 256 ? 256 : kTPR, kRows = kThreads / kTPR;
         const int64_t wgs = min64((j.rows + kRows - 1) / kRows, kThreads == 1024 ? 512 : 2048);  // resident on 256 CUs
-        norm_kernel<T, kTPR, decltype(np)::value><<<(unsigned)wgs, kThreads, 0, s>>>(j);
+        const auto kernel = streams<T>(2, j.rows, j.cols) ? norm_kernel<T, kTPR, decltype(np)::value, true>
+                                                          : norm_kernel<T, kTPR, decltype(np)::value, false>;
+        kernel<<<(unsigned)wgs, kThreads, 0, s>>>(j);
     });
     if (!fits) norm_long_kernel<T><<<(unsigned)min64(j.rows, 512), kLongThreads, 0, s>>>(j);
     return hipGetLastError();
@@ -467,7 +477,10 @@ hipError_t launch_norm_bwd_t(const NormBwdJob& j, hipStream_t s) {
         for_row(pieces_of<T>(j.cols), [&](auto tpr, auto np) {
             using B = BwdShape<T, decltype(tpr)::value, decltype(np)::value>;
             if constexpr (B::kFits) {
-                norm_bwd_kernel<T, decltype(tpr)::value, decltype(np)::value><<<parts, B::kThreads, 0, s>>>(j);
+                const auto kernel = streams<T>(3, j.rows, j.cols)
+                                        ? norm_bwd_kernel<T, decltype(tpr)::value, decltype(np)::value, true>
+                                        : norm_bwd_kernel<T, decltype(tpr)::value, decltype(np)::value, false>;
+                kernel<<<parts, B::kThreads, 0, s>>>(j);
                 done = true;
             }
         });

@@ -19,8 +19,14 @@ struct Piece;
 template <>
 struct Piece<float> {
     static constexpr int V = 4;
+    // S: nontemporally
+    template <bool S = false>
     static __device__ __forceinline__ u32x4_any load(const float* p, int64_t left) {
-        if (left >= V) return *reinterpret_cast<const u32x4_any*>(p);
+        if (left >= V) {
+            const u32x4_any* const q = reinterpret_cast<const u32x4_any*>(p);
+            if constexpr (S) return __builtin_nontemporal_load(q);
+            else return *q;
+        }
         u32x4_any r = {0, 0, 0, 0};
         if (left > 0) r[0] = __float_as_uint(p[0]);
         if (left > 1) r[1] = __float_as_uint(p[1]);
@@ -34,9 +40,11 @@ struct Piece<float> {
     static __device__ __forceinline__ u32x4_any pack(const float (&f)[V]) {
         return u32x4_any{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
     }
+    template <bool S = false>
     static __device__ __forceinline__ void store(float* p, int64_t left, const u32x4_any& r) {
         if (left >= V) {
-            *reinterpret_cast<u32x4_any*>(p) = r;
+            if constexpr (S) __builtin_nontemporal_store(r, reinterpret_cast<u32x4_any*>(p));
+            else *reinterpret_cast<u32x4_any*>(p) = r;
             return;
         }
         if (left > 0) p[0] = __uint_as_float(r[0]);
@@ -48,8 +56,13 @@ struct Piece<float> {
 template <>
 struct Piece<uint16_t> {  // bf16 bits
     static constexpr int V = 8;
+    template <bool S = false>
     static __device__ __forceinline__ u32x4_any load(const uint16_t* p, int64_t left) {
-        if (left >= V) return *reinterpret_cast<const u32x4_any*>(p);
+        if (left >= V) {
+            const u32x4_any* const q = reinterpret_cast<const u32x4_any*>(p);
+            if constexpr (S) return __builtin_nontemporal_load(q);
+            else return *q;
+        }
         u32x4_any r = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < V - 1; ++i)
@@ -72,9 +85,11 @@ struct Piece<uint16_t> {  // bf16 bits
                    (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f[2 * i + 1]) << 16;
         return r;
     }
+    template <bool S = false>
     static __device__ __forceinline__ void store(uint16_t* p, int64_t left, const u32x4_any& r) {
         if (left >= V) {
-            *reinterpret_cast<u32x4_any*>(p) = r;
+            if constexpr (S) __builtin_nontemporal_store(r, reinterpret_cast<u32x4_any*>(p));
+            else *reinterpret_cast<u32x4_any*>(p) = r;
             return;
         }
 #pragma unroll

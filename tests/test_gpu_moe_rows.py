@@ -246,3 +246,32 @@ def test_refusals():
         U.moe_combine(x.half(), rows)
     with pytest.raises(U.UFP4Error):
         U.moe_combine_bwd(x, x, rows, off)  # y must hold tokens * k rows
+
+
+@pytest.mark.parametrize("tokens,k,cols,dt", [(9000, 7, 2200, torch.bfloat16), (8000, 3, 3001, torch.float32)])
+def test_large_tensors(tokens, k, cols, dt):
+    """Tensors that no cache holds are read and stored by kernels of their own."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x = torch.randn(tokens, cols, generator=g, device="cuda").to(dt)
+    assert tokens * k * cols * x.element_size() >= 1 << 28
+    ids = torch.topk(torch.rand(tokens, 16, generator=g, device="cuda"), k, dim=1).indices
+    ids[torch.rand(tokens, k, generator=g, device="cuda") < 0.03] = -1
+    w = torch.rand(tokens, k, generator=g, device="cuda")
+    off, rows, source = U.moe_sort(ids, 16)
+    used = int(off[-1])
+    y = U.moe_dispatch(x, rows, off)
+    assert torch.equal(y[:used], x[source[:used].long() // k]) and not y[used:].any()
+    out, small = U.moe_combine(y, rows, w), 1000
+    dy, dw = U.moe_combine_bwd(x, y, rows, off, w)
+    for a in range(0, tokens, small):  # fewer tokens at a time: the other kernels, on the rows that these tokens have
+        s = slice(a, min(tokens, a + small))
+        at = rows[s].reshape(-1)
+        part = torch.where(at[:, None] >= 0, y[at.clamp(min=0).long()], torch.zeros((), dtype=dt, device="cuda"))
+        place = torch.arange(at.numel(), device="cuda", dtype=torch.int32)
+        local = torch.where(at >= 0, place, torch.full_like(place, -1)).view(-1, k)
+        assert torch.equal(U.moe_combine(part, local, w[s]), out[s])
+        n = torch.tensor([0, at.numel()], device="cuda")
+        pdy, pdw = U.moe_combine_bwd(x[s], part, local, n, w[s])
+        have = at >= 0
+        assert torch.equal(pdw, dw[s]) and torch.equal(pdy[have], dy[at[have].long()])
+    assert not dy[used:].any()

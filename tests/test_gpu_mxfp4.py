@@ -259,3 +259,11 @@ def test_empty_and_refusals():
     q = U.mxfp4_quantize(x)
     with pytest.raises(ValueError):
         U.mxfp4_dequantize(q, out=torch.empty(40, 32, dtype=BF, device="cuda"))
+
+
+def test_large_tensor_and_back():
+    """Outputs that no cache holds are stored by a kernel of their own: the same values as from a part of the rows."""
+    x = torch.randn(16384 + 96, 8224, device="cuda").to(torch.bfloat16)
+    got = U.mxfp4_dequantize(U.mxfp4_quantize(x))
+    for a in range(0, x.shape[0], 4096):
+        assert torch.equal(got[a : a + 4096], U.mxfp4_dequantize(U.mxfp4_quantize(x[a : a + 4096])))

@@ -245,3 +245,19 @@ def test_refusals():
         U.layer_norm_bwd(x.float(), x, None, st, st)
     with pytest.raises(ValueError):
         U.layer_norm_bwd(x, x, None, st[:3], st)
+
+
+@pytest.mark.parametrize("rows,cols,dt", [(30011, 2304, torch.bfloat16), (20000, 1411, torch.float32), (4100, 16392, torch.bfloat16)])
+def test_large_tensors(rows, cols, dt):
+    """Tensors that no cache holds are stored by kernels of their own: the same numbers as from pieces of them."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(dt)
+    dy = torch.randn(rows, cols, generator=g, device="cuda").to(dt)
+    gamma, beta = torch.randn(cols, generator=g, device="cuda"), torch.randn(cols, generator=g, device="cuda")
+    assert 2 * x.numel() * x.element_size() >= 1 << 28 or 3 * x.numel() * x.element_size() >= 1 << 28
+    y, mean, rstd = U.layer_norm(x, gamma, beta)
+    dx = U.layer_norm_bwd(dy, x, gamma, mean, rstd)[0]
+    for a in range(0, rows, 1000):
+        s = slice(a, min(rows, a + 1000))
+        assert all(torch.equal(p, q[s]) for p, q in zip(U.layer_norm(x[s], gamma, beta), (y, mean, rstd)))
+        assert torch.equal(U.layer_norm_bwd(dy[s], x[s], gamma, mean[s], rstd[s], weights=False)[0], dx[s])
