@@ -79,7 +79,7 @@ int ufp4_layer_norm_bwd(int dtype, const void* dy_dev, int64_t lddy, const void*
         if (workspace_bytes < need) return UFP4_ERR_SHAPE;
         if (!aligned(workspace_dev, 16)) return UFP4_ERR_ALIGN;
     }
-    if (cols == 0) return UFP4_OK;
+    if (cols == 0 || (rows == 0 && !weights)) return UFP4_OK;
     const NormBwdJob j{dtype == UFP4_OUT_BF16, w_dtype == UFP4_OUT_BF16, dy_dev, x_dev, rows, cols, lddy, ldx, gamma_dev,
                        mean_dev, rstd_dev, dx_dev, lddx, dgamma_dev, dbeta_dev,
                        some && weights ? static_cast<float*>(workspace_dev) : nullptr};
