@@ -102,3 +102,44 @@ def test_refusals():
     layer = moe.MoELayer(2, 128, 128, 1)
     with pytest.raises(ValueError):
         layer.load_weights(torch.zeros(128, 128, dtype=BF, device="cuda"), torch.zeros(256, 128, dtype=BF, device="cuda"))
+
+
+def test_graph_replays():
+    """Forward and backward captured once, replayed on other inputs, with eager work in between; on a stream of their own."""
+    tokens, experts, k, H, F = 257, 8, 2, 256, 384
+    g = torch.Generator(device="cuda").manual_seed(4)
+
+    def draw():
+        return {"x": torch.randn(tokens, H, generator=g, device="cuda").to(BF),
+                "dout": torch.randn(tokens, H, generator=g, device="cuda").to(BF),
+                "ids": torch.topk(torch.rand(tokens, experts, generator=g, device="cuda"), k, dim=1).indices,
+                "gate": torch.rand(tokens, k, generator=g, device="cuda")}
+
+    gamma, beta = torch.ones(H, device="cuda"), torch.zeros(H, device="cuda")
+    layer = moe.MoELayer(experts, H, F, k)
+    layer.load_weights(torch.randn(experts * F, H, generator=g, device="cuda").to(BF),
+                       torch.randn(experts * H, F, generator=g, device="cuda").to(BF))
+
+    def step(s):
+        out = layer.forward(s["x"], s["ids"], s["gate"], gamma, beta)
+        return dict(layer.backward(s["dout"], seed=7), out=out)
+
+    still = draw()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(still)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(still)
+    for _ in range(4):
+        fresh = draw()
+        want = step(fresh)
+        for n in still:
+            still[n].copy_(fresh[n])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in want:
+            assert torch.equal(want[n], got[n]), n

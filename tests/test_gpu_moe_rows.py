@@ -275,3 +275,20 @@ def test_large_tensors(tokens, k, cols, dt):
         have = at >= 0
         assert torch.equal(pdw, dw[s]) and torch.equal(pdy[have], dy[at[have].long()])
     assert not dy[used:].any()
+
+
+def test_rows_past_32_bit_offsets():
+    """Leading dimensions that put rows past 2^31 elements."""
+    ld, cols = (1 << 29) + 4099, 700
+    ids = torch.tensor([[0, 2], [1, 0], [2, -1]], device="cuda")
+    off, rows, _ = U.moe_sort(ids, 3)
+    x = torch.randn(3, cols, device="cuda").to(torch.bfloat16)
+    w = torch.rand(3, 2, device="cuda")
+    hold = torch.empty(5 * ld + cols, dtype=torch.bfloat16, device="cuda")
+    y = hold.as_strided((6, cols), (ld, 1))
+    U.moe_dispatch(x, rows, off, w, out=y)
+    near = U.moe_dispatch(x, rows, off, w)
+    assert torch.equal(y, near) and torch.equal(U.moe_combine(y, rows, w), U.moe_combine(near, rows, w))
+    want = U.moe_combine_bwd(x, near, rows, off, w)
+    dy, dw = U.moe_combine_bwd(x, y, rows, off, w, out=y)
+    assert torch.equal(dy, want[0]) and torch.equal(dw, want[1])

@@ -261,3 +261,20 @@ def test_large_tensors(rows, cols, dt):
         s = slice(a, min(rows, a + 1000))
         assert all(torch.equal(p, q[s]) for p, q in zip(U.layer_norm(x[s], gamma, beta), (y, mean, rstd)))
         assert torch.equal(U.layer_norm_bwd(dy[s], x[s], gamma, mean[s], rstd[s], weights=False)[0], dx[s])
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [300, 40000])
+def test_rows_past_32_bit_offsets(dt, cols):
+    """Leading dimensions that put the third row past 2^31 elements."""
+    ld = (1 << 30) + 4099
+    hold = [torch.empty(2 * ld + cols, dtype=dt, device="cuda") for _ in range(2)]
+    x, y = (h.as_strided((3, cols), (ld, 1)) for h in hold)
+    x.copy_(torch.randn(3, cols, device="cuda"))
+    g, b = torch.randn(cols, device="cuda"), torch.randn(cols, device="cuda")
+    want, mean, rstd = U.layer_norm(x.contiguous(), g, b)
+    got, m, r = U.layer_norm(x, g, b, out=y)
+    assert torch.equal(got, want) and torch.equal(m, mean) and torch.equal(r, rstd)
+    dy = torch.randn(3, cols, device="cuda").to(dt)
+    assert all(torch.equal(p, q) for p, q in zip(U.layer_norm_bwd(dy, x, g, mean, rstd, out=y),
+                                                 U.layer_norm_bwd(dy, x.contiguous(), g, mean, rstd)))
