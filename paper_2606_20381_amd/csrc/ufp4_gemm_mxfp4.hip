@@ -8,8 +8,8 @@
 // neither the barrier nor the LDS latency stands between two matrix instructions.
 //
 // Bound by the matrix cores' power where the reduction is long: the instruction alone, on registers, reaches 5.5 PFLOP/s (the
-// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.78 ms = 4.9. Where it is short, by the stores, which take the memory
-// system from the loads: 16384 x 16384 x 2048 takes 0.29-0.31 ms = 3.6 PFLOP/s, without its stores 0.235 ms.
+// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.76 ms = 5.0. Where it is short, by the stores, which take the memory
+// system from the loads: 16384 x 16384 x 2048 takes 0.29 ms = 3.8 PFLOP/s, without its stores 0.235 ms.
 
 #include "ufp4_internal.h"
 #include "ufp4_mxfp4.h"
@@ -350,14 +350,15 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
         asm volatile("" ::: "memory");
     };
 
-    // Stage i: the first half's products while the second half's operands are read; then, past the barrier that lets the next
+    // A stage: the first half's products while the second half's operands are read; then, past the barrier that lets the next
     // stage be read and this one be overwritten, the second half's products while the next stage's first half is read and the
     // stage kRing ahead is loaded. The order is pinned: one product, then what its 32 cycles cover. There is no branch inside:
-    // the compiler would move products across it. OUTSTANDING: as of arrive() for the next stage, -1 in the last stage.
+    // the compiler would move products across it. The next stage is stage ni of tile nw, the one loaded (if `loads`) stage li of
+    // tile lw. OUTSTANDING: as of arrive() for the next stage, -1 if there is none.
     constexpr int kOpsPer = (kOps + kTiles - 1) / kTiles, kLoadsPer = (C::kWaveLoads + kTiles - 1) / kTiles;
     Operands f0, f1;
     Scales s;
-    auto stage = [&](const Work& w, int i, uint32_t cur, uint32_t next, auto outstanding, auto loads) INLINE {
+    auto stage = [&](uint32_t cur, uint32_t next, const Work& nw, int ni, auto outstanding, const Work& lw, int li, auto loads) INLINE {
         constexpr bool kMore = decltype(outstanding)::value >= 0, kLoads = decltype(loads)::value;
         Scales sn;
 #pragma unroll
@@ -380,12 +381,12 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
             }
             if constexpr (kLoads) {
 #pragma unroll
-                for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(w, q, i + kRing, cur);
+                for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (kMore) {
-            mask_scales(w, i + 1, sn);
+            mask_scales(nw, ni, sn);
             s = sn;
         }
     };
@@ -485,73 +486,115 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
         }
     };
 
-    // The workgroup's tiles. The next tile's first stages are loaded before this one's results are stored; the stores are then
-    // younger than those loads, and memory operations complete in order, so the first kRing waits of a long enough tile count
-    // them in instead of waiting for them.
-    constexpr int L1 = C::kWaveLoads;
-    uint32_t L = blockIdx.x;
-    if (L >= total) return;
-    Work w;
-    locate(L, w);
-    fill(w);
-    bool behind = false;  // kStores stores were issued after the loads
-    while (true) {
+    auto clear = [&] INLINE {
 #pragma unroll
         for (int a = 0; a < WTM; ++a)
 #pragma unroll
             for (int b = 0; b < WTN; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-        if (w.nst > 0) {
-            uint32_t cur = 0, next = S::kSize;
-            auto advance = [&] INLINE {
-                cur = next;
-                next = next == (kRing - 1) * S::kSize ? 0 : next + S::kSize;
-            };
-            auto begin = [&] INLINE {
+    };
+    auto is_inside = [&](const Work& w) INLINE { return w.rows == BM && (int64_t)w.col0 + BN <= j.N; };
+    constexpr int L1 = C::kWaveLoads;
+    uint32_t L = blockIdx.x;
+    if (L >= total) return;
+    Work w;
+    locate(L, w);
+    fill(w);
+    uint32_t cur = 0, next = S::kSize;
+    auto advance = [&] INLINE {
+        cur = next;
+        next = next == (kRing - 1) * S::kSize ? 0 : next + S::kSize;
+    };
+    auto begin = [&] INLINE {
 #pragma unroll
-                for (int t = 0; t < kOps; ++t) {
-                    read_one(t, 0, 0, f0);
-                    read_scale(t, 0, s);
+        for (int t = 0; t < kOps; ++t) {
+            read_one(t, cur, 0, f0);
+            read_scale(t, cur, s);
+        }
+        mask_scales(w, 0, s);
+    };
+    using std::integral_constant;
+    // The last kRing stages of a tile, whose loads are on their way; nothing follows them.
+    auto finish = [&](int i) INLINE {
+        static_assert(kRing == 3, "");
+        if (i + 2 < w.nst) {
+            stage(cur, next, w, i + 1, integral_constant<int, L1>{}, w, 0, std::false_type{});
+            advance();
+            ++i;
+        }
+        if (i + 1 < w.nst) {
+            stage(cur, next, w, i + 1, integral_constant<int, 0>{}, w, 0, std::false_type{});
+            advance();
+            ++i;
+        }
+        stage(cur, next, w, 0, integral_constant<int, -1>{}, w, 0, std::false_type{});
+    };
+
+    // The workgroup's tiles, all of as many stages. The stages of one tile follow those of the one before without a gap: its last
+    // kRing stages load the next tile's first ones (after the last tile its own first ones again, which nobody reads: a branch here
+    // makes the compiler spill the sums), and the last reads the first's operands. A tile's stores are then younger than those
+    // loads, and memory operations complete in order, so the next tile's first waits count them in instead of waiting for them.
+    // (Filling the ring anew for each tile: 8192 x 8192 x 2048 92 us instead of 79, 98304 x 2048 x 1408 182 instead of 168.)
+    if constexpr (kSplit == 1 && MODE != kGemmRaggedK) {
+        if (w.nst >= kRing) {
+            arrive(integral_constant<int, (kRing - 1) * L1>{});
+            begin();
+            bool behind = false;  // kStores stores were issued after the loads
+            while (true) {
+                clear();
+                L += gridDim.x;
+                const bool more = L < total;
+                Work n = w;
+                if (more) locate(L, n);
+                int i = 0;
+                if (behind && w.nst >= 2 * kRing) {
+                    for (; i < kRing - 1; ++i) {
+                        stage(cur, next, w, i + 1, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, std::true_type{});
+                        advance();
+                    }
                 }
-                mask_scales(w, 0, s);
-            };
-            int i = 0;
-            if (behind && w.nst >= 2 * kRing) {
-                arrive(std::integral_constant<int, (kRing - 1) * L1 + kStores>{});
-                begin();
-                for (; i < kRing - 1; ++i) {
-                    stage(w, i, cur, next, std::integral_constant<int, (kRing - 2) * L1 + kStores>{}, std::true_type{});
+                for (; i + kRing < w.nst; ++i) {
+                    stage(cur, next, w, i + 1, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
                     advance();
                 }
-            } else {
-                arrive(std::integral_constant<int, 0>{});
-                begin();
+                constexpr integral_constant<int, (kRing - 2) * L1> kept{};
+                stage(cur, next, w, i + 1, kept, n, 0, std::true_type{});
+                advance();
+                stage(cur, next, w, i + 2, kept, n, 1, std::true_type{});
+                advance();
+                stage(cur, next, n, 0, kept, n, 2, std::true_type{});
+                advance();
+                asm volatile("" ::: "memory");
+                behind = is_inside(w);
+                if (behind) store(w, std::true_type{});
+                else store(w, std::false_type{});
+                if (!more) {
+                    wait_loads<0>();  // the LDS must not be another workgroup's before they have landed
+                    return;
+                }
+                w = n;
             }
+        }
+    }
+
+    // Tiles of different length, or of few stages, or of several teams: one after the other.
+    while (true) {
+        clear();
+        if (w.nst > 0) {
+            cur = 0, next = S::kSize;
+            arrive(integral_constant<int, 0>{});
+            begin();
+            int i = 0;
             for (; i + kRing < w.nst; ++i) {
-                stage(w, i, cur, next, std::integral_constant<int, (kRing - 2) * L1>{}, std::true_type{});
+                stage(cur, next, w, i + 1, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
                 advance();
             }
-            // the last kRing, whose loads are on their way
-            static_assert(kRing == 3 || kRing == 4, "");
-            if (kRing == 4 && i + 3 < w.nst) {
-                stage(w, i++, cur, next, std::integral_constant<int, 2 * L1>{}, std::false_type{});
-                advance();
-            }
-            if (i + 2 < w.nst) {
-                stage(w, i++, cur, next, std::integral_constant<int, L1>{}, std::false_type{});
-                advance();
-            }
-            if (i + 1 < w.nst) {
-                stage(w, i++, cur, next, std::integral_constant<int, 0>{}, std::false_type{});
-                advance();
-            }
-            stage(w, i, cur, next, std::integral_constant<int, -1>{}, std::false_type{});
+            finish(i);
         }
         L += gridDim.x;
         const bool more = L < total;
         const Work done = w;
-        behind = kSplit == 1 && done.rows == BM && (int64_t)done.col0 + BN <= j.N;  // inside the output: kStores stores a wave
         if constexpr (kSplit > 1) {
             // the other teams' sums, added by the first in the order of the teams
             static_assert(kSplit == 1 || (kSplit - 1) * C::kWaves * 64 * kTiles * 16 * 4 <= kSplit * kRing * S::kSize, "");
@@ -588,7 +631,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
         }
         asm volatile("" ::: "memory");
         if (kSplit == 1 || team == 0) {
-            if (done.rows == BM && (int64_t)done.col0 + BN <= j.N) store(done, std::true_type{});
+            if (is_inside(done)) store(done, std::true_type{});
             else store(done, std::false_type{});
         }
         if (!more) return;
@@ -620,7 +663,7 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
 
 // Outputs of kStreamBytes and more are stored nontemporally: they cannot stay in a cache, and
 // in the L2's recency order they push the operands out. Measured, us, nontemporal / plain: 16384 x 16384 x 2048 bf16 311 / 398,
-// fp32 393 / 602 (95 MB read instead of 212), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
+// fp32 393 / 602 (190 MB read instead of 425), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
 // gradient 259 / 322; at 256 MiB 8192 x 8192 fp32 of 1024 74 / 97, of 2048 107 / 99, of 8192 254 / 267; below, 8192 x 8192 x 2048
 // bf16 83 / 77. The 64-row tiles are not taken for outputs of that size.
 bool streams(const MxGemmJob& j) {
