@@ -228,17 +228,22 @@ class QTensor:
         return v.reshape(self.panels * PANEL_ROWS, nkb)[: self.rows]
 
 
-def empty_qtensor(rows: int, red: int, fmt: int = UNIFORM, device="cuda") -> QTensor:
-    """Buffers for a [rows, red] operand of `fmt`, sized by the library (ufp4_qtensor_bytes)."""
+@functools.lru_cache(maxsize=1024)
+def _operand_size(fmt: int, rows: int, red: int) -> tuple[int, int, int]:
+    """(panels, code_panel_ld, scale_panel_ld) of a [rows, red] operand of `fmt` (ufp4_qtensor_bytes)."""
     p, cld, sld = _I64(), _I64(), _I64()
     _check(lib().ufp4_qtensor_bytes(fmt, rows, red, ctypes.byref(p), ctypes.byref(cld), ctypes.byref(sld), None, None),
            "ufp4_qtensor_bytes")
-    codes = torch.empty((p.value, cld.value), dtype=torch.uint8, device=device)
+    return p.value, cld.value, sld.value
+
+
+def empty_qtensor(rows: int, red: int, fmt: int = UNIFORM, device="cuda") -> QTensor:
+    """Buffers for a [rows, red] operand of `fmt`, sized by the library (ufp4_qtensor_bytes)."""
+    panels, cld, sld = _operand_size(fmt, rows, red)
+    codes = torch.empty((panels, cld), dtype=torch.uint8, device=device)
     sdt = torch.uint8 if fmt in (UNIFORM_MX32, E2M1_MX32) else torch.float32
-    scales = torch.empty((p.value, sld.value), dtype=sdt, device=device)
-    desc = QDesc(codes=codes.data_ptr(), scales=scales.data_ptr(), code_panel_ld=cld.value, scale_panel_ld=sld.value,
-                 panels=p.value, rows=rows, red=red, format=fmt)
-    return QTensor(codes, scales, desc)
+    scales = torch.empty((panels, sld), dtype=sdt, device=device)
+    return QTensor(codes, scales, QDesc(codes.data_ptr(), scales.data_ptr(), cld, sld, panels, rows, red, fmt))
 
 
 def empty_qtensor_mx(rows: int, red: int, device="cuda") -> QTensor:
@@ -721,7 +726,7 @@ def mxfp4_linear(x: torch.Tensor, wq: QTensor, out_dtype=torch.bfloat16, out=Non
     if red != wq.red:
         raise ValueError(f"x must have {wq.red} columns")
     if tokens > LINEAR_TOKENS or wq.rht_block:
-        xq = mxfp4_quantize(x, rht=wq.rht_block != 0, sign_mask=wq.sign_mask)
+        xq = mxfp4_quantize(x, rht=True, sign_mask=wq.sign_mask) if wq.rht_block else mxfp4_quantize(x)
         return mxfp4_gemm_fwd_y(xq, wq, out_dtype, out)
     y = _out((tokens, wq.rows), out_dtype, x.device, out)
     st = lib().ufp4_mxfp4_linear(x.data_ptr(), tokens, x.stride(0), wq.ref(), y.data_ptr(), y.stride(0), _odt(y), _stream())
@@ -765,7 +770,7 @@ def _rows_like(t: torch.Tensor, what: str, like: torch.Tensor, rows: int, cols: 
 def _rows_out(out: torch.Tensor | None, like: torch.Tensor, rows: int, cols: int) -> tuple[torch.Tensor, int]:
     """The output tensor, a new one for None, and its leading dimension."""
     if out is None:
-        return torch.empty((rows, cols), dtype=like.dtype, device=like.device), cols
+        return like.new_empty((rows, cols)), cols
     return out, _rows_like(out, "out", like, rows, cols)
 
 
