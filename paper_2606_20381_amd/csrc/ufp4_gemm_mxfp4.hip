@@ -8,7 +8,7 @@
 // neither the barrier nor the LDS latency stands between two matrix instructions.
 //
 // Bound by the matrix cores' power where the reduction is long: the instruction alone, on registers, reaches 5.5 PFLOP/s (the
-// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.76 ms = 5.0. Where it is short, by the stores, which take the memory
+// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.75-1.84 ms = 4.8-5.0 (matrix cores busy 75% of the time at 1.45 GHz). Where it is short, by the stores, which take the memory
 // system from the loads: 16384 x 16384 x 2048 takes 0.29 ms = 3.8 PFLOP/s, without its stores 0.235 ms.
 
 #include "ufp4_internal.h"

@@ -4,6 +4,8 @@
 // workgroup takes R rows of W at a time (all of K) and its waves split K. It quantizes x into LDS in the layout of W, once if
 // all of it fits, with the first loads of W already in flight. W goes from memory straight to the registers that the matrix
 // instruction reads (runs of R * 16 bytes), and the waves' sums are added through LDS in a fixed order.
+// Up to 8 MiB of W it takes about 4-6 us whatever its size (launch, one read's latency, the waves' sums); 32768 x 4096 14 us = 5.2
+// TB/s, 16384 x 16384 25 us = 5.8 TB/s for one token.
 // R = 16 (16 x 16 x 128 instruction) gives a narrow W twice the workgroups; R = 32 (32 x 32 x 64) halves what each reads of x.
 
 #include "ufp4_internal.h"

@@ -7,6 +7,10 @@
 // combine_bwd: dy[rows[t, j]] = w[t, j] dout[t] and dw[t, j] = <dout[t], y[rows[t, j]]> from one read of both.
 //   All three are HBM bound: a wave (combine_bwd: a workgroup) takes one token, or a 4 KiB segment of one, reads its row
 //   once for all k experts and sums in fp32.
+//
+// Measured, 16384 tokens to 6 of 64 experts, 2048 bf16 columns: sort 4.8 + 7.6 us (two launches of 24 workgroups, bound by their
+// own latency), dispatch 80 us and combine 79 us (470 MB each: 5.9 TB/s; a copy of 1 GiB runs at 5.1), combine_bwd 217 us (873 MB:
+// 4.0 TB/s; 5003 x 2 x 5120 fp32 92 us, 512 MB: 5.6 TB/s).
 
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"

@@ -11,7 +11,9 @@
 //
 // HBM bound: 2 bytes read and 17/32 written per value. amax is a packed 16-bit integer maximum of the bf16 patterns (their
 // order is that of the magnitudes) and the conversion one instruction per two values, so the plain form has little to compute;
-// rotated (fp64 sums, as the other quantizers) or stochastic (Philox) it is bound by vector issue.
+// rotated (fp64 sums, as the other quantizers) or stochastic (Philox) it is bound by vector issue. Measured, 32768 x 16384 (1 GiB),
+// us: rowwise 230 (5.9 TB/s), transposed 256 (5.3), both 306 (5.4), rowwise / transposed rotated 244 / 316, stochastic 380 / 411,
+// back to bf16 243 (5.6).
 
 #include "ufp4_internal.h"
 #include "ufp4_device.h"

@@ -9,6 +9,10 @@
 // and, backward, the partial dgamma and dbeta stay in its registers, and the weights' gradient costs one fp32 row per
 // workgroup instead of a second pass over x and dy. The partial rows are then added in a fixed order, so results repeat.
 // Rows too long for the registers are read again per pass (`*_long_kernel`).
+//
+// Measured: forward 16384 x 5120 bf16 55 us = 6.1 TB/s with tensors in place, 65 us = 5.2 TB/s with new ones each time (a copy of
+// 1 GiB runs at 5.1); backward 8192 x 2048 bf16 25 us in two launches (21 and 3; its 101 MB are 20 us at the copy's rate),
+// 32768 x 5120 187 us = 5.4 TB/s; 4 x 2048 3.6 us, launch and two dependent sums.
 
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
