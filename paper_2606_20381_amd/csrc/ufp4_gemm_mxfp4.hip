@@ -15,6 +15,8 @@
 #include "ufp4_mxfp4.h"
 #include "ufp4_rows.h"
 
+#include <math.h>
+
 #include <type_traits>
 
 namespace ufp4 {
@@ -686,7 +688,7 @@ struct Cost {
 };
 constexpr Cost kCost[kKernels] = {
     {Tile256::BM, Tile256::kThreads, 9.0, 4.5, 0.48, 0.85},
-    {Tile128::BM, Tile128::kThreads, 6.2, 0.75, 0.24, 0.28},
+    {Tile128::BM, Tile128::kThreads, 6.2, 0.75, 0.24, 0.30},
     {Tile64::BM, Tile64::kThreads, 5.4, 0.2, 0.15, 0.115},
     {Tile64K::BM, Tile64K::kThreads, 6.2, 3.0, 0.10, 0.10},
 };
@@ -702,7 +704,10 @@ int pick_tile(const MxGemmJob& j) {
         const int64_t tiles = grid_tiles(j, c.tile, c.tile) * groups;
         // a grid holds fewer than 2^32 threads: what fits with the largest tile must not fail on a smaller one's grid
         if (k != kTile256 && tiles * c.threads > int64_t(UINT32_MAX)) continue;
-        const double R = (double)((tiles + 255) / 256);
+        // Ragged rows: the operand is padded to panels, and every other group leaves half of a 256-row tile empty.
+        const double rows = j.mode == kGemmRaggedM ? (double)j.a_rows / c.tile + (c.tile > 128 ? j.G / 4.0 : 0.0) : 0.0;
+        const double some = j.mode == kGemmRaggedM ? rows * (double)((j.N + c.tile - 1) / c.tile) : (double)tiles;
+        const double R = ceil(some / 256.0);
         const double us = c.fixed + (R - 1.0) * c.again + stages * (R * c.busy > c.alone ? R * c.busy : c.alone);
         if (k == 0 || us < best_us) {
             best = k;
