@@ -1,4 +1,4 @@
-"""Build libufp4.so (gfx950) in-tree with hipcc.
+"""Build libufp4.so (gfx950) and the binding's host module in-tree with hipcc.
 
 Usage: python -m paper_2606_20381_amd.build [--verbose]
 
@@ -8,16 +8,19 @@ off (the quantizer's arithmetic must round exactly as written) and denormals pre
 
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libufp4.so")
+HOST = os.path.join(PKG, "_host.so")  # a Python module: the host side of short calls, on torch's C++ interface and libufp4.so
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
 SOURCES = ["ufp4_quant.hip", "ufp4_gemm.hip", "ufp4_gemm_mx.hip", "ufp4_mxfp4.hip", "ufp4_gemm_mxfp4.hip",
@@ -59,8 +62,18 @@ def _run(cmd, verbose):
     return r
 
 
+def _host_object(cc: str) -> tuple[list, str, str]:
+    """(command that compiles the host module, its object file, torch's library folder)."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    inc = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    obj = os.path.join(BUILD, "ufp4_host.o")
+    return ([cc, "-x", "c++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{INCLUDE}",
+             f"-I{sysconfig.get_paths()['include']}", *(x for i in inc for x in ("-isystem", i)), "-c",
+             os.path.join(CSRC, "ufp4_host.cpp"), "-o", obj], obj, os.path.join(torch, "lib"))
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source and link the shared library; always rebuilds. Returns the library path."""
+    """Compile every source and link the shared library and the host module; always rebuilds. Returns the library path."""
     os.makedirs(BUILD, exist_ok=True)
     cc = hipcc()
     objs = []
@@ -71,11 +84,17 @@ def build(verbose: bool = False) -> str:
         form = [] if src in AGPR_SOURCES else VGPR_FORM
         cmds.append([cc, *FLAGS, *form, f"-I{INCLUDE}", *lang, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
+    host_cmd, host_obj, torch_lib = _host_object(cc)
+    cmds.append(host_cmd)
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         list(ex.map(lambda c: _run(c, verbose), cmds))
     tmp = LIB + ".tmp"
     _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB)
+    tmp = HOST + ".tmp"  # torch's libraries are loaded by the time the module is
+    _run([cc, "-shared", "-fPIC", "-o", tmp, host_obj, f"-L{PKG}", "-l:libufp4.so", "-Wl,-rpath,$ORIGIN", f"-L{torch_lib}",
+          "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+    os.replace(tmp, HOST)
     return LIB
 
 

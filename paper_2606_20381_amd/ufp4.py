@@ -626,10 +626,41 @@ def mx_gemm_bwd_dw_grouped(dytq: QTensor, xtq: QTensor, offsets: torch.Tensor, o
 # microscaled 4-bit floating point: E2M1 levels with power-of-two 1x32 scales
 # ---------------------------------------------------------------------------------------------------
 
+# The short calls of a decode step are bound by the host: the checks, output tensors and library call of these and of the row
+# operators below are native code (csrc/ufp4_host.cpp).
+_host_module = None
+_addressof = ctypes.addressof
+
+
+def _host():
+    """The host module (loaded once)."""
+    global _host_module
+    if _host_module is None:
+        lib()
+        try:
+            from . import _host as module
+        except ImportError as e:
+            raise RuntimeError("the host module is not built; run `python -m paper_2606_20381_amd.build`") from e
+        module.set_error(UFP4Error)
+        _host_module = module
+    return _host_module
+
+
+def _code_of(dtype: torch.dtype) -> int:
+    """UFP4_OUT_* of an output type, -1 for another."""
+    return OUT_BF16 if dtype is torch.bfloat16 else OUT_F32 if dtype is torch.float32 else -1
+
+
 def mxfp4_quantize(x: torch.Tensor, *, transpose: bool = False, rht: bool = False, sign_mask: int = 0,
                    rounding: int = RTNE, seed: int = 0, stream_id: int = 0, out: QTensor | None = None) -> QTensor:
     """Microscaled 4-bit quantization, after an optional block-16 RHT (ufp4_mxfp4_quantize)."""
-    return _quantize_call("ufp4_mxfp4_quantize", E2M1_MX32, x, transpose, rht, sign_mask, rounding, seed, stream_id, out)
+    h = _host_module or _host()
+    if out is not None:
+        h.mxfp4_quantize(x, transpose, rht, sign_mask, rounding, seed, stream_id, _addressof(out.desc), False, _stream())
+        return out
+    desc = QDesc()
+    codes, scales = h.mxfp4_quantize(x, transpose, rht, sign_mask, rounding, seed, stream_id, _addressof(desc), True, _stream())
+    return QTensor(codes, scales, desc)
 
 
 def mxfp4_quantize_dual(x: torch.Tensor, *, rht_rows: bool = False, rht_cols: bool = False, sign_mask_rows: int = 0,
@@ -668,29 +699,22 @@ def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total:
 
 def mxfp4_dequantize(q: QTensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """The operand's values as bf16 [rows, red] (ufp4_mxfp4_dequantize), exact."""
-    if out is None:
-        ld = -(-q.red // 8) * 8
-        out = torch.empty((q.rows, ld), dtype=torch.bfloat16, device=q.codes.device)[:, : q.red]
-    elif (out.dtype != torch.bfloat16 or tuple(out.shape) != (q.rows, q.red) or out.device != q.codes.device
-          or out.stride(1) != 1):
-        raise ValueError(f"out must be a row-major bf16 tensor of shape {(q.rows, q.red)} on {q.codes.device}")
-    _check(lib().ufp4_mxfp4_dequantize(q.ref(), out.data_ptr(), out.stride(0), _stream()), "ufp4_mxfp4_dequantize")
-    return out
+    return (_host_module or _host()).mxfp4_dequantize(q.codes, _addressof(q.desc), out, _stream())
 
 
 def mxfp4_gemm_fwd_y(xq: QTensor, wq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """Y [M, N] = Q(X) Q(W)^T on microscaled operands (ufp4_mxfp4_gemm_fwd_y)."""
-    return _gemm("ufp4_mxfp4_gemm_fwd_y", xq, wq, _out((xq.rows, wq.rows), out_dtype, xq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_fwd_y(xq.codes, _addressof(xq.desc), _addressof(wq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dx(dyq: QTensor, wtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """dX [M, K] = Q(dY) Q(W^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dx)."""
-    return _gemm("ufp4_mxfp4_gemm_bwd_dx", dyq, wtq, _out((dyq.rows, wtq.rows), out_dtype, dyq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_bwd_dx(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dw(dytq: QTensor, xtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """dW [N, K] = Q(dY^T) Q(X^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dw)."""
-    return _gemm("ufp4_mxfp4_gemm_bwd_dw", dytq, xtq, _out((dytq.rows, xtq.rows), out_dtype, dytq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_bwd_dw(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_fwd_y_grouped(xq: QTensor, wq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
@@ -721,120 +745,23 @@ LINEAR_TOKENS = 16  # tokens up to which ufp4_mxfp4_linear takes a product
 def mxfp4_linear(x: torch.Tensor, wq: QTensor, out_dtype=torch.bfloat16, out=None) -> torch.Tensor:
     """Y [tokens, N] = Q(x) W^T with bf16 x and W kept microscaled: a decode step's few tokens in one launch
     (ufp4_mxfp4_linear), more (or a rotated W) by quantizing x and one GEMM."""
-    _bf16_2d(x)
-    tokens, red = x.shape
-    if red != wq.red:
-        raise ValueError(f"x must have {wq.red} columns")
-    if tokens > LINEAR_TOKENS or wq.rht_block:
-        xq = mxfp4_quantize(x, rht=True, sign_mask=wq.sign_mask) if wq.rht_block else mxfp4_quantize(x)
-        return mxfp4_gemm_fwd_y(xq, wq, out_dtype, out)
-    y = _out((tokens, wq.rows), out_dtype, x.device, out)
-    st = lib().ufp4_mxfp4_linear(x.data_ptr(), tokens, x.stride(0), wq.ref(), y.data_ptr(), y.stride(0), _odt(y), _stream())
-    _check(st, "ufp4_mxfp4_linear")
-    return y
+    return (_host_module or _host()).mxfp4_linear(x, _addressof(wq.desc), _code_of(out_dtype), out, LINEAR_TOKENS, _stream())
 
 
 # ---------------------------------------------------------------------------------------------------
 # layer norm
 # ---------------------------------------------------------------------------------------------------
 
-# These checks run before every launch, and a decode step's norm is bound by the host: one pass over a tensor's properties, and
-# contiguous tensors (which need no look at their strides) first. layer_norm of 4 x 2048: 12.7 -> 9.9 us a call.
-
-def _rows_of(t: torch.Tensor, what: str) -> tuple[int, int, int, int]:
-    """(rows, cols, leading dimension, UFP4_OUT_*) of a 2-D row-major float32 or bfloat16 tensor on the GPU."""
-    dt = t.dtype
-    code = OUT_BF16 if dt is torch.bfloat16 else OUT_F32 if dt is torch.float32 else -1
-    if code < 0 or not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 CUDA tensor")
-    rows, cols = t.shape
-    if t.is_contiguous():
-        return rows, cols, cols, code
-    if t.numel() and cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{what} must be row-major")
-    if rows > 1 and t.stride(0) < cols:
-        raise ValueError(f"{what}'s rows must not overlap")
-    return rows, cols, t.stride(0) if rows > 1 else cols, code
-
-
-def _rows_like(t: torch.Tensor, what: str, like: torch.Tensor, rows: int, cols: int) -> int:
-    """The leading dimension of a [rows, cols] tensor of `like`'s type and device."""
-    got = _rows_of(t, what)
-    if t.dtype is not like.dtype or t.device != like.device:
-        raise ValueError(f"{what} must be of type {like.dtype} on {like.device}")
-    if got[0] != rows or got[1] != cols:
-        raise ValueError(f"{what} must be of shape {(rows, cols)}")
-    return got[2]
-
-
-def _rows_out(out: torch.Tensor | None, like: torch.Tensor, rows: int, cols: int) -> tuple[torch.Tensor, int]:
-    """The output tensor, a new one for None, and its leading dimension."""
-    if out is None:
-        return like.new_empty((rows, cols)), cols
-    return out, _rows_like(out, "out", like, rows, cols)
-
-
-def _vector(t: torch.Tensor | None, what: str, n: int, device, bf16: bool = False) -> int | None:
-    """The address of a contiguous float32 (or, with bf16, bfloat16) tensor of n elements, None for None."""
-    if t is None:
-        return None
-    if (not (t.dtype is torch.float32 or (bf16 and t.dtype is torch.bfloat16)) or t.numel() != n or t.device != device
-            or not t.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous float32 {'or bfloat16 ' if bf16 else ''}tensor of {n} elements on {device}")
-    return t.data_ptr()
-
-
-def _weights(gamma, beta, cols, device):
-    if gamma is not None and beta is not None and gamma.dtype is not beta.dtype:
-        raise ValueError("gamma and beta must be of one type")
-    w = gamma if gamma is not None else beta
-    code = OUT_BF16 if w is not None and w.dtype is torch.bfloat16 else OUT_F32
-    return code, _vector(gamma, "gamma", cols, device, True), _vector(beta, "beta", cols, device, True)
-
-
-@functools.lru_cache(maxsize=256)
-def _workspace_bytes(name: str, *sizes) -> int:
-    """The workspace that the library's size function `name` asks for."""
-    need = _SZ(0)
-    _check(getattr(lib(), name)(*sizes, ctypes.byref(need)), name)
-    return need.value
-
-
 def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, *, eps: float = 1e-5,
                out: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(y, mean, rstd) of the layer norm of x's rows (ufp4_layer_norm); mean and rstd are fp32, for layer_norm_bwd."""
-    rows, cols, ld, code = _rows_of(x, "x")
-    device = x.device
-    wdt, g, b = _weights(gamma, beta, cols, device)
-    y, ldy = _rows_out(out, x, rows, cols)
-    mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty_like(mean)
-    st = lib().ufp4_layer_norm(code, x.data_ptr(), rows, cols, ld, wdt, g, b, eps, y.data_ptr(), ldy, mean.data_ptr(),
-                               rstd.data_ptr(), _stream())
-    _check(st, "ufp4_layer_norm")
-    return y, mean, rstd
+    return (_host_module or _host()).layer_norm(x, gamma, beta, eps, out, _stream())
 
 
 def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor, *,
                    weights: bool = True, out: torch.Tensor | None = None):
     """(dx, dgamma, dbeta) of layer_norm (ufp4_layer_norm_bwd); dgamma and dbeta are fp32, None with weights False."""
-    rows, cols, ldx, code = _rows_of(x, "x")
-    lddy = _rows_like(dy, "dy", x, rows, cols)
-    device = x.device
-    wdt, g, _ = _weights(gamma, None, cols, device)
-    dx, lddx = _rows_out(out, x, rows, cols)
-    need, dgamma, dbeta, ws = 0, None, None, None
-    if weights:
-        dgamma = torch.empty(cols, dtype=torch.float32, device=device)
-        dbeta = torch.empty_like(dgamma)
-        need = _workspace_bytes("ufp4_layer_norm_bwd_workspace", code, rows, cols)
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    st = lib().ufp4_layer_norm_bwd(code, dy.data_ptr(), lddy, x.data_ptr(), rows, cols, ldx, wdt, g,
-                                   _vector(mean, "mean", rows, device), _vector(rstd, "rstd", rows, device), dx.data_ptr(),
-                                   lddx, dgamma.data_ptr() if weights else None, dbeta.data_ptr() if weights else None,
-                                   ws.data_ptr() if weights else None, need, _stream())
-    _check(st, "ufp4_layer_norm_bwd")
-    return dx, dgamma, dbeta
+    return (_host_module or _host()).layer_norm_bwd(dy, x, gamma, mean, rstd, weights, out, _stream())
 
 
 # ---------------------------------------------------------------------------------------------------
@@ -844,66 +771,23 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None
 def moe_sort(ids: torch.Tensor, experts: int) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(offsets int64 [experts + 1], rows int32 [tokens, k], source int32 [tokens * k]) of ids [tokens, k]
     (ufp4_moe_sort): the order that the grouped quantizers and GEMMs take. Ids outside 0 .. experts - 1 are dropped."""
-    dt = ids.dtype
-    if not (dt is torch.int32 or dt is torch.int64) or not ids.is_cuda or ids.dim() != 2 or not ids.is_contiguous():
-        raise ValueError("ids must be a contiguous int32 or int64 CUDA tensor [tokens, k]")
-    (tokens, k), device = ids.shape, ids.device
-    need = _workspace_bytes("ufp4_moe_sort_workspace", tokens, k, experts)
-    offsets = torch.empty(experts + 1, dtype=torch.int64, device=device)
-    rows = torch.empty((tokens, k), dtype=torch.int32, device=device)
-    source = torch.empty(tokens * k, dtype=torch.int32, device=device)
-    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    st = lib().ufp4_moe_sort(ids.data_ptr(), 32 if dt is torch.int32 else 64, tokens, k, experts, offsets.data_ptr(),
-                             rows.data_ptr(), source.data_ptr(), ws.data_ptr() if need else None, need, _stream())
-    _check(st, "ufp4_moe_sort")
-    return offsets, rows, source
-
-
-def _moe_rows(rows: torch.Tensor, weights: torch.Tensor | None, device) -> tuple[int, int, int | None]:
-    if rows.dtype is not torch.int32 or rows.dim() != 2 or rows.device != device or not rows.is_contiguous():
-        raise ValueError(f"rows must be a contiguous int32 tensor [tokens, k] on {device}")
-    tokens, k = rows.shape
-    if weights is not None and weights.shape != rows.shape:
-        raise ValueError(f"weights must be of shape {(tokens, k)}")
-    return tokens, k, _vector(weights, "weights", tokens * k, device)
+    return (_host_module or _host()).moe_sort(ids, experts, _stream())
 
 
 def moe_dispatch(x: torch.Tensor, rows: torch.Tensor, offsets: torch.Tensor, weights: torch.Tensor | None = None, *,
                  out: torch.Tensor | None = None) -> torch.Tensor:
     """y [tokens * k, cols] with y[rows[t, j]] = weights[t, j] x[t] (ufp4_moe_dispatch), zero where no slot goes."""
-    have, cols, ld, code = _rows_of(x, "x")
-    tokens, k, w = _moe_rows(rows, weights, x.device)
-    if have != tokens:
-        raise ValueError(f"x must hold {tokens} tokens")
-    y, ldy = _rows_out(out, x, tokens * k, cols)
-    st = lib().ufp4_moe_dispatch(code, x.data_ptr(), tokens, cols, ld, rows.data_ptr(), k, offsets.data_ptr(),
-                                 _offsets(offsets), w, y.data_ptr(), tokens * k, ldy, _stream())
-    _check(st, "ufp4_moe_dispatch")
-    return y
+    return (_host_module or _host()).moe_dispatch(x, rows, offsets, weights, out, _stream())
 
 
 def moe_combine(y: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor | None = None, *,
                 out: torch.Tensor | None = None) -> torch.Tensor:
     """out [tokens, cols] with out[t] = sum_j weights[t, j] y[rows[t, j]] (ufp4_moe_combine). With moe_dispatch's weights
     (or none) it is moe_dispatch's gradient in x."""
-    y_rows, cols, ldy, code = _rows_of(y, "y")
-    tokens, k, w = _moe_rows(rows, weights, y.device)
-    o, ldo = _rows_out(out, y, tokens, cols)
-    st = lib().ufp4_moe_combine(code, y.data_ptr(), y_rows, cols, ldy, rows.data_ptr(), tokens, k, w, o.data_ptr(), ldo,
-                                _stream())
-    _check(st, "ufp4_moe_combine")
-    return o
+    return (_host_module or _host()).moe_combine(y, rows, weights, out, _stream())
 
 
 def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, rows: torch.Tensor, offsets: torch.Tensor,
                     weights: torch.Tensor | None = None, *, out: torch.Tensor | None = None):
     """(dy, dweights) of moe_combine (ufp4_moe_combine_bwd); dweights is fp32 [tokens, k]."""
-    y_rows, cols, ldy, code = _rows_of(y, "y")
-    tokens, k, w = _moe_rows(rows, weights, y.device)
-    lddo = _rows_like(dout, "dout", y, tokens, cols)
-    dy, lddy = _rows_out(out, y, y_rows, cols)
-    dw = torch.empty((tokens, k), dtype=torch.float32, device=y.device)
-    st = lib().ufp4_moe_combine_bwd(code, dout.data_ptr(), tokens, cols, lddo, y.data_ptr(), y_rows, ldy, rows.data_ptr(), k,
-                                    offsets.data_ptr(), _offsets(offsets), w, dy.data_ptr(), lddy, dw.data_ptr(), _stream())
-    _check(st, "ufp4_moe_combine_bwd")
-    return dy, dw
+    return (_host_module or _host()).moe_combine_bwd(dout, y, rows, offsets, weights, out, _stream())

@@ -9,6 +9,7 @@ from fractions import Fraction
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2606_20381_amd import ufp4 as U
 
@@ -308,3 +309,39 @@ def test_microscaled_oracle_stochastic_rounding_stays_between_neighbours():
     assert ((np.abs(q) == lo) | (np.abs(q) == hi)).all()
     # unbiased: the mean error of 4096 roundings, each of variance up to 1 (a step of 2 halves at most)
     assert abs(float((q - v).mean())) < 5 * 0.5 / 64
+
+
+# ------------------------------------------------------------------------------------------------
+# the binding's host module
+# ------------------------------------------------------------------------------------------------
+
+def test_host_module_refuses_before_the_library(lib):
+    """Tensors that the calls cannot take: ValueError, and TypeError for what is no tensor; nothing is launched."""
+    h, null = U._host(), 0  # the stream
+    x, rows, off = torch.zeros(2, 32, dtype=torch.bfloat16), torch.zeros(2, 1, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    v, a = torch.zeros(2), ctypes.addressof
+    d, other = desc(2, 32), desc(2, 64)
+    calls = [
+        lambda t: h.layer_norm(t, None, None, 1e-5, None, null), lambda t: h.layer_norm_bwd(x, t, None, v, v, True, None, null),
+        lambda t: h.moe_sort(t, 4, null), lambda t: h.moe_dispatch(t, rows, off, None, None, null),
+        lambda t: h.moe_combine(t, rows, None, None, null), lambda t: h.moe_combine_bwd(x, t, rows, off, None, None, null),
+        lambda t: h.mxfp4_quantize(t, False, False, 0, 0, 0, 0, a(d), False, null), lambda t: h.mxfp4_linear(t, a(d), BF16, None, 16, null),
+    ]
+    for call in calls:
+        with pytest.raises(ValueError, match="CUDA"):
+            call(x)
+        with pytest.raises(TypeError, match="tensor"):
+            call(3)
+    codes = torch.zeros(1, 2048, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="out_dtype"):
+        h.mxfp4_gemm_fwd_y(codes, a(d), a(d), -1, None, null)
+    for bad in (torch.zeros(2, 3), torch.zeros(2, 2, dtype=torch.float64), torch.zeros(2, 2).t()[:, :1]):
+        with pytest.raises(ValueError, match="out"):
+            h.mxfp4_gemm_fwd_y(codes, a(d), a(d), BF16, bad, null)
+    with pytest.raises(ValueError, match="bf16"):
+        h.mxfp4_dequantize(codes, a(d), torch.zeros(2, 32), null)
+    with pytest.raises(U.UFP4Error) as e:  # a status of the library: its number and the call's name
+        h.mxfp4_gemm_fwd_y(codes, a(d), a(other), F32, torch.zeros(2, 2), null)
+    assert e.value.status == MISMATCH and "ufp4_mxfp4_gemm_fwd_y" in str(e.value)
+    with pytest.raises(TypeError, match="arguments"):
+        h.layer_norm(x)
