@@ -268,8 +268,8 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
     }
 }
 
-// One workgroup per token: dout's segment in registers, each expert's row of y against it, the dot products added over the
-// lanes, then over the waves in order.
+// One workgroup per token (where tokens are few, per slot: gridDim.y = k): dout's segment in registers, each expert's row of y against
+// it, the dot products added over the lanes, then over the waves in order.
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
     using P = Piece<T>;
@@ -277,6 +277,7 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
     __shared__ float s_dot[4][kMoeMaxK];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t t = blockIdx.x;
+    const int q0 = gridDim.y > 1 ? (int)blockIdx.y : 0, q1 = gridDim.y > 1 ? q0 + 1 : j.k;  // this workgroup's slots
     const T* const dout = static_cast<const T*>(j.dout) + t * j.lddo;
     const T* const y = static_cast<const T*>(j.y);
     T* const dy = static_cast<T*>(j.dy);
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
             const int64_t c = c0 + p * 256 * V;
             raw[p] = P::load(dout + c, j.cols - c);
         }
-        for (int q = 0; q < j.k; ++q) {
+        for (int q = q0; q < q1; ++q) {
             const int32_t row = j.rows[t * j.k + q];
             if (row < 0 || row >= j.rows_y) continue;
             const float w = j.w ? j.w[t * j.k + q] : 1.0f;
@@ -314,10 +315,10 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(MoeBwdJob j) {
         }
     }
     __syncthreads();
-    for (int q = tid; q < j.k; q += 256)
+    for (int q = q0 + tid; q < q1; q += 256)
         j.dw[t * j.k + q] = (s_dot[0][q] + s_dot[1][q]) + (s_dot[2][q] + s_dot[3][q]);
     const u32x4_any zero = {0, 0, 0, 0};
-    for (int64_t r = (used < 0 ? 0 : used) + t; r < j.rows_y; r += j.tokens)
+    for (int64_t r = (used < 0 ? 0 : used) + t * gridDim.y + blockIdx.y; r < j.rows_y; r += j.tokens * gridDim.y)
         for (int64_t c = (int64_t)tid * V; c < j.cols; c += 256 * V) P::store(dy + r * j.lddy + c, j.cols - c, zero);
 }
 
@@ -368,8 +369,13 @@ hipError_t launch_moe_combine(MoeRowsJob j, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Up to this many slots (workgroups that 256 CUs hold at once) the gradient takes a workgroup per slot: a token's k rows one after
+// the other are k times a read's latency. us, so / a workgroup per token, bf16: 7 tokens x 6 x 2048 4.5 / 12.0, 64 x 8 x 7168 5.2 /
+// 13.3, 256 x 6 x 2048 7.7 / 12.5; 1024 x 6 x 2048 21.7 / 18.8 (dout is read k times).
+constexpr int64_t kFewSlots = 2048;
+
 hipError_t launch_moe_combine_bwd(const MoeBwdJob& j, hipStream_t s) {
-    const unsigned g = (unsigned)j.tokens;
+    const dim3 g((unsigned)j.tokens, j.tokens * j.k <= kFewSlots ? (unsigned)j.k : 1u);
     const bool stream = 2 * j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
     if (j.bf16)
         stream ? combine_bwd_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);

@@ -193,7 +193,13 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(NormJob j) {
     }
 }
 
-// Backward. `part` is [gridDim.x][2][cols]: the workgroup's sums of dy h and of dy. A workgroup takes several rows at a time, as
+// Where workgroup `at` of `n` puts its sums of dy h (q = 0) and of dy (q = 1): in its row of `part` [n][2][cols], or, alone, where
+// they are asked for (null: nowhere).
+__device__ __forceinline__ float* sums_at(const NormBwdJob& j, unsigned n, unsigned at, int q) {
+    return n > 1 ? j.part + ((int64_t)at * 2 + q) * j.cols : q ? j.dbeta : j.dgamma;
+}
+
+// Backward. A workgroup takes several rows at a time, as
 // many as a CU's registers hold, at one partial row per CU. kAhead: the next row is on its way while this one is computed.
 template <typename T, int TPR, int NP>
 struct BwdShape {
@@ -292,9 +298,9 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
     }
     if (!j.part) return;
     // the workgroup's rows have the same columns: added in their order, piece by piece
-    float* const out = j.part + (int64_t)blockIdx.x * 2 * j.cols;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
+        float* const out = sums_at(j, gridDim.x, blockIdx.x, q);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             if constexpr (kRowsWG > 1) {
@@ -314,7 +320,7 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
                         for (int w = 0; w < kRowsWG - 1; ++w) v += s_part[w][i * TPR + t];
                     }
                     const int64_t c = ((int64_t)p * TPR + t) * V + i;
-                    if (c < j.cols) out[q * j.cols + c] = v;
+                    if (c < j.cols && out) out[c] = v;
                 }
             }
         }
@@ -384,9 +390,9 @@ __global__ __launch_bounds__(256) void norm_bwd_cols_kernel(NormBwdJob j) {
         ag = __builtin_fmaf(d, (x - j.mean[row]) * j.rstd[row], ag);
         ab += d;
     }
-    float* const out = j.part + (int64_t)blockIdx.y * 2 * j.cols;
-    out[c] = ag;
-    out[j.cols + c] = ab;
+    float *const g = sums_at(j, gridDim.y, blockIdx.y, 0), *const b = sums_at(j, gridDim.y, blockIdx.y, 1);
+    if (g) g[c] = ag;
+    if (b) b[c] = ab;
 }
 
 // dgamma and dbeta from `n` partial rows of 2 * cols sums: 64 columns per workgroup, 16 waves over the partial rows, then
@@ -495,7 +501,7 @@ hipError_t launch_norm_bwd_t(const NormBwdJob& j, hipStream_t s) {
         }
     }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || (!j.dgamma && !j.dbeta)) return e;
+    if (e != hipSuccess || (!j.dgamma && !j.dbeta) || parts == 1) return e;  // a lone workgroup's sums are in place
     norm_reduce_kernel<<<(unsigned)((2 * j.cols + 63) / 64), 1024, 0, s>>>(j.part, (int)parts, j.cols, j.dgamma, j.dbeta);
     return hipGetLastError();
 }
