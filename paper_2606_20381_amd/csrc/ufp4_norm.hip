@@ -4,15 +4,16 @@
 //   g = dy gamma, dx = r (g - mean(g) - h mean(g h)), dgamma = sum over rows of dy h, dbeta = sum over rows of dy
 //
 // HBM bound: forward reads x and writes y once, backward reads x and dy and writes dx once. A row lives in the registers
-// of TPR threads (one wave, 256 or 1024 threads), so that mean and variance are two sums over registers (no cancellation
+// of TPR threads (an eighth of a wave up to 1024 threads), so that mean and variance are two sums over registers (no cancellation
 // of E[x^2] - mu^2) without a second read. A thread keeps its columns over all rows that its workgroup takes: gamma, beta
 // and, backward, the partial dgamma and dbeta stay in its registers, and the weights' gradient costs one fp32 row per
 // workgroup instead of a second pass over x and dy. The partial rows are then added in a fixed order, so results repeat.
 // Rows too long for the registers are read again per pass (`*_long_kernel`).
 //
 // Measured: forward 16384 x 5120 bf16 55 us = 6.1 TB/s with tensors in place, 65 us = 5.2 TB/s with new ones each time (a copy of
-// 1 GiB runs at 5.1); backward 8192 x 2048 bf16 25 us in two launches (21 and 3; its 101 MB are 20 us at the copy's rate),
-// 32768 x 5120 187 us = 5.4 TB/s; 4 x 2048 3.6 us, launch and two dependent sums.
+// 1 GiB runs at 5.1); backward 8192 x 2048 bf16 22.5 us in two launches (its 101 MB are 20 us at the copy's rate), 32768 x 5120
+// 187 us = 5.4 TB/s; short rows, 262144 x 128 bf16, 24 and 34 us (a wave per row: 61 and 91); 4 x 2048 3.6 us, launch and two
+// dependent sums.
 
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
@@ -65,12 +66,24 @@ __device__ __forceinline__ void load_weights(const void* w, int w_bf16, int64_t 
     else some(static_cast<const float*>(w));
 }
 
+// Sum over the 64 lanes of a wave, or over each TPR of them.
+template <int TPR>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (TPR >= 64) {
+        return wave_sum(v);
+    } else {
+#pragma unroll
+        for (int d = TPR / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+        return v;
+    }
+}
+
 // Sums of N values over the TPR threads of a row. TPR > 64: through `s` ([wave][N], one barrier; the caller alternates
 // between two such arrays, so that a wave that is ahead does not overwrite what another still reads).
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* s) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+    for (int n = 0; n < N; ++n) v[n] = lanes_sum<TPR>(v[n]);
     if constexpr (TPR > 64) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
@@ -199,8 +212,8 @@ __device__ __forceinline__ float* sums_at(const NormBwdJob& j, unsigned n, unsig
     return n > 1 ? j.part + ((int64_t)at * 2 + q) * j.cols : q ? j.dbeta : j.dgamma;
 }
 
-// Backward. A workgroup takes several rows at a time, as
-// many as a CU's registers hold, at one partial row per CU. kAhead: the next row is on its way while this one is computed.
+// Backward. A workgroup takes several rows at a time, as many as a CU's registers hold, at one partial row per CU. kAhead: the next
+// row is on its way while this one is computed.
 template <typename T, int TPR, int NP>
 struct BwdShape {
     static constexpr int kRegs = NP * Piece<T>::V;  // columns per thread, about six registers each
@@ -213,8 +226,9 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
     using P = Piece<T>;
     using B = BwdShape<T, TPR, NP>;
     constexpr int V = P::V, kRowsWG = B::kRows, kRowWaves = TPR / 64;
+    constexpr int kSums = TPR < 64 ? B::kThreads / 64 : kRowsWG;  // sums of a column that are left at the end: per wave, or per row
     __shared__ float s_sum[2][B::kThreads / 64][2];
-    __shared__ float s_part[kRowsWG > 1 ? kRowsWG - 1 : 1][kRowsWG > 1 ? TPR * V : 1];
+    __shared__ float s_part[kSums > 1 ? kSums - 1 : 1][kSums > 1 ? TPR * V : 1];
     const int t = threadIdx.x % TPR, rw = threadIdx.x / TPR;
     const int64_t step = (int64_t)gridDim.x * kRowsWG;
     int64_t row = (int64_t)blockIdx.x * kRowsWG + rw;
@@ -266,8 +280,8 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
             }
         }
         if (B::kAhead && row + step < j.rows) load(row + step);
-        sum[0] = wave_sum(sum[0]);
-        sum[1] = wave_sum(sum[1]);
+        sum[0] = lanes_sum<TPR>(sum[0]);
+        sum[1] = lanes_sum<TPR>(sum[1]);
         if constexpr (kRowWaves > 1) {  // one barrier a row: two arrays in turn, so that a wave ahead does not overwrite
             const int wave = threadIdx.x >> 6;
             if ((threadIdx.x & 63) == 0) {
@@ -297,30 +311,38 @@ __global__ __launch_bounds__((BwdShape<T, TPR, NP>::kThreads)) void norm_bwd_ker
         }
     }
     if (!j.part) return;
-    // the workgroup's rows have the same columns: added in their order, piece by piece
+    // the workgroup's rows have the same columns: those of a wave are added by shuffles, then the sums in their order, piece by piece
+    const int at = TPR < 64 ? (int)(threadIdx.x >> 6) : rw;
+    const bool holds = TPR >= 64 || (threadIdx.x & 63) < TPR;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         float* const out = sums_at(j, gridDim.x, blockIdx.x, q);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            if constexpr (kRowsWG > 1) {
-                __syncthreads();
-                if (rw > 0) {
+            float v[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) s_part[rw - 1][i * TPR + t] = q ? ab[p][i] : ag[p][i];
+            for (int i = 0; i < V; ++i) {
+                v[i] = q ? ab[p][i] : ag[p][i];
+#pragma unroll
+                for (int d = TPR; d < 64; d <<= 1) v[i] += __shfl_xor(v[i], d, 64);
+            }
+            if constexpr (kSums > 1) {
+                __syncthreads();
+                if (at > 0 && holds) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s_part[at - 1][i * TPR + t] = v[i];
                 }
                 __syncthreads();
             }
-            if (rw == 0) {
+            if (at == 0 && holds) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float v = q ? ab[p][i] : ag[p][i];
-                    if constexpr (kRowsWG > 1) {
+                    if constexpr (kSums > 1) {
 #pragma unroll
-                        for (int w = 0; w < kRowsWG - 1; ++w) v += s_part[w][i * TPR + t];
+                        for (int w = 0; w < kSums - 1; ++w) v[i] += s_part[w][i * TPR + t];
                     }
                     const int64_t c = ((int64_t)p * TPR + t) * V + i;
-                    if (c < j.cols && out) out[c] = v;
+                    if (c < j.cols && out) out[c] = v[i];
                 }
             }
         }
@@ -422,12 +444,15 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restri
 }
 
 // Threads and pieces that a row of `pieces` 16-byte pieces takes: few pieces a thread, so that the weights (and, backward, their
-// gradient) leave registers for many waves; a wave by itself needs no barrier. A rule of kernel(threads, pieces per thread);
+// gradient) leave registers for many waves; a wave by itself needs no barrier; short rows share a wave. A rule of kernel(threads, pieces per thread);
 // false for a row that is too long.
 template <typename F>
 bool for_row(int64_t pieces, F&& kernel) {
     using std::integral_constant;
-    if (pieces <= 64) kernel(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    if (pieces <= 8) kernel(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (pieces <= 16) kernel(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (pieces <= 32) kernel(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (pieces <= 64) kernel(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     else if (pieces <= 128) kernel(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else if (pieces <= 256) kernel(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (pieces <= 512) kernel(integral_constant<int, 256>{}, integral_constant<int, 2>{});
