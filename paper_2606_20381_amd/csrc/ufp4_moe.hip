@@ -15,6 +15,8 @@
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
 
+#include <type_traits>
+
 namespace ufp4 {
 
 namespace {
@@ -184,41 +186,60 @@ constexpr int kSegPieces = 4;  // 16-byte pieces per lane of a segment: 4 KiB pe
 
 // out rows [first, rows_out) zero, in segments: the rows that no slot takes. Called by every wave of a grid of `tokens` waves
 // per segment.
-template <typename T>
+template <typename T, int PIECES>
 __device__ __forceinline__ void zero_rows(T* out, int64_t ldo, int64_t first, int64_t rows_out, int64_t token, int64_t tokens,
                                           int64_t c0, int64_t cols) {
     using P = Piece<T>;
     const u32x4_any zero = {0, 0, 0, 0};
     for (int64_t r = (first < 0 ? 0 : first) + token; r < rows_out; r += tokens)
 #pragma unroll
-        for (int p = 0; p < kSegPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int64_t c = c0 + p * 64 * P::V;
             P::store(out + r * ldo + c, cols - c, zero);
         }
 }
 
-template <typename T, bool STREAM>
+// A token's rows and weights, one a lane (k <= 64), all read at once: row(q) is -1 for a slot that has none. Every lane of the wave
+// takes part.
+struct Slots {
+    int32_t mine;
+    float w;
+    __device__ __forceinline__ Slots(const int32_t* rows, const float* weights, int64_t t, int k, int64_t rows_y) {
+        const int lane = threadIdx.x & 63;
+        const int32_t r = lane < k ? rows[t * k + lane] : -1;
+        mine = r < rows_y ? r : -1;
+        w = weights && lane < k ? weights[t * k + lane] : 1.0f;
+    }
+    __device__ __forceinline__ int32_t row(int q) const { return __builtin_amdgcn_readlane(mine, q); }
+    __device__ __forceinline__ float weight(int q) const {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), q));
+    }
+};
+
+// A wave takes PIECES pieces a lane of a token.
+template <typename T, bool STREAM, int PIECES>
 __global__ __launch_bounds__(256) void dispatch_kernel(MoeRowsJob j) {
     using P = Piece<T>;
     constexpr int V = P::V;
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= j.tokens * j.segs) return;
-    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (kSegPieces * 64 * V) + (threadIdx.x & 63) * V;
+    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (PIECES * 64 * V) + (threadIdx.x & 63) * V;
     const T* const x = static_cast<const T*>(j.in) + t * j.ldi;
     T* const out = static_cast<T*>(j.out);
     const int64_t used = j.offsets[j.E];
-    u32x4_any raw[kSegPieces];
+    const Slots slots(j.rows, j.w, t, j.k, j.rows_y);
+    u32x4_any raw[PIECES];
 #pragma unroll
-    for (int p = 0; p < kSegPieces; ++p) {
+    for (int p = 0; p < PIECES; ++p) {
         const int64_t c = c0 + p * 64 * V;
         raw[p] = P::load(x + c, j.cols - c);
     }
     for (int q = 0; q < j.k; ++q) {
-        const int32_t row = j.rows[t * j.k + q];
-        if (row < 0 || row >= j.rows_y) continue;
-        const float w = j.w ? j.w[t * j.k + q] : 1.0f;
+        const int32_t row = slots.row(q);
+        if (row < 0) continue;
+        const float w = slots.weight(q);
 #pragma unroll
-        for (int p = 0; p < kSegPieces; ++p) {
+        for (int p = 0; p < PIECES; ++p) {
             const int64_t c = c0 + p * 64 * V;
             u32x4_any r = raw[p];
             if (j.w) {
@@ -231,41 +252,121 @@ __global__ __launch_bounds__(256) void dispatch_kernel(MoeRowsJob j) {
             P::template store<STREAM>(out + row * j.ldo + c, j.cols - c, r);
         }
     }
-    zero_rows<T>(out, j.ldo, used, j.rows_y, t, j.tokens, c0, j.cols);
+    zero_rows<T, PIECES>(out, j.ldo, used, j.rows_y, t, j.tokens, c0, j.cols);
 }
 
-template <typename T, bool STREAM>
+// A wave takes PIECES pieces a lane of a token and reads kSegPieces / PIECES of its rows at a time: short rows leave the registers
+// for it, and need it (a row after the other is k times a read's latency).
+template <typename T, bool STREAM, int PIECES>
 __global__ __launch_bounds__(256) void combine_kernel(MoeRowsJob j) {
     using P = Piece<T>;
-    constexpr int V = P::V;
+    constexpr int V = P::V, kAtOnce = kSegPieces / PIECES;
     const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= j.tokens * j.segs) return;
-    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (kSegPieces * 64 * V) + (threadIdx.x & 63) * V;
+    const int64_t t = item / j.segs, c0 = (item - t * j.segs) * (PIECES * 64 * V) + (threadIdx.x & 63) * V;
     const T* const y = static_cast<const T*>(j.in);
-    float acc[kSegPieces][V];
+    const Slots slots(j.rows, j.w, t, j.k, j.rows_y);
+    float acc[PIECES][V];
 #pragma unroll
-    for (int p = 0; p < kSegPieces; ++p)
+    for (int p = 0; p < PIECES; ++p)
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[p][i] = 0.0f;
-    for (int q = 0; q < j.k; ++q) {
-        const int32_t row = j.rows[t * j.k + q];
-        if (row < 0 || row >= j.rows_y) continue;
-        const float w = j.w ? j.w[t * j.k + q] : 1.0f;
+    for (int q0 = 0; q0 < j.k; q0 += kAtOnce) {
+        u32x4_any raw[kAtOnce][PIECES];
 #pragma unroll
-        for (int p = 0; p < kSegPieces; ++p) {
-            const int64_t c = c0 + p * 64 * V;
-            float f[V];
-            P::unpack(P::template load<STREAM>(y + row * j.ldi + c, j.cols - c), f);
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int32_t row = q0 + s < j.k ? slots.row(q0 + s) : -1;
+            if (row < 0) continue;
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[p][i] = __builtin_fmaf(w, f[i], acc[p][i]);
+            for (int p = 0; p < PIECES; ++p) {
+                const int64_t c = c0 + p * 64 * V;
+                raw[s][p] = P::template load<STREAM>(y + row * j.ldi + c, j.cols - c);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            if (q0 + s >= j.k || slots.row(q0 + s) < 0) continue;
+            const float w = slots.weight(q0 + s);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                float f[V];
+                P::unpack(raw[s][p], f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[p][i] = __builtin_fmaf(w, f[i], acc[p][i]);
+            }
         }
     }
     T* const out = static_cast<T*>(j.out) + t * j.ldo;
 #pragma unroll
-    for (int p = 0; p < kSegPieces; ++p) {
+    for (int p = 0; p < PIECES; ++p) {
         const int64_t c = c0 + p * 64 * V;
         P::store(out + c, j.cols - c, P::pack(acc[p]));
     }
+}
+
+// The combine's gradient for rows that a wave holds in PIECES pieces a lane: a wave per token, rows read as above.
+template <typename T, bool STREAM, int PIECES>
+__global__ __launch_bounds__(256) void combine_bwd_wave_kernel(MoeBwdJob j) {
+    using P = Piece<T>;
+    constexpr int V = P::V, kAtOnce = kSegPieces / PIECES;
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= j.tokens) return;
+    const T* const dout = static_cast<const T*>(j.dout) + t * j.lddo;
+    const T* const y = static_cast<const T*>(j.y);
+    T* const dy = static_cast<T*>(j.dy);
+    const int64_t used = j.offsets[j.E];
+    const Slots slots(j.rows, j.w, t, j.k, j.rows_y);
+    u32x4_any raw[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        const int64_t c = (p * 64 + lane) * V;
+        raw[p] = P::load(dout + c, j.cols - c);
+    }
+    float dots = 0.0f;  // lane q: slot q's
+    for (int q0 = 0; q0 < j.k; q0 += kAtOnce) {
+        u32x4_any ry[kAtOnce][PIECES];
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int32_t row = q0 + s < j.k ? slots.row(q0 + s) : -1;
+            if (row < 0) continue;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int64_t c = (p * 64 + lane) * V;
+                ry[s][p] = P::load(y + row * j.ldy + c, j.cols - c);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int32_t row = q0 + s < j.k ? slots.row(q0 + s) : -1;
+            if (row < 0) continue;
+            const float w = slots.weight(q0 + s);
+            float dot = 0.0f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int64_t c = (p * 64 + lane) * V;
+                float d[V], f[V];
+                P::unpack(raw[p], d);
+                P::unpack(ry[s][p], f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    dot = __builtin_fmaf(d[i], f[i], dot);
+                    d[i] *= w;
+                }
+                P::template store<STREAM>(dy + row * j.lddy + c, j.cols - c, P::pack(d));
+            }
+            dot = wave_sum(dot);
+            if (lane == q0 + s) dots = dot;
+        }
+    }
+    if (lane < j.k) j.dw[t * j.k + lane] = dots;
+    const u32x4_any zero = {0, 0, 0, 0};
+    for (int64_t r = (used < 0 ? 0 : used) + t; r < j.rows_y; r += j.tokens)
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int64_t c = (p * 64 + lane) * V;
+            P::store(dy + r * j.lddy + c, j.cols - c, zero);
+        }
 }
 
 // One workgroup per token (where tokens are few, per slot: gridDim.y = k): dout's segment in registers, each expert's row of y against
@@ -351,22 +452,46 @@ hipError_t launch_moe_sort(const MoeSortJob& j, hipStream_t s) {
 // plain: dispatch 80 / 92, combine 80 / 95, one after the other 160 / 204; 8192 tokens (201 MB) 42 / 35, 42 / 36, 84 / 72.
 // combine_bwd reads one such tensor and writes another, so its stores take half the size: 16384 tokens 217 / 222, 8192 94 / 117,
 // 4096 51 / 52.
-hipError_t launch_moe_dispatch(MoeRowsJob j, hipStream_t s) {
-    j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
+// Pieces a lane of rows of `cols`: 1, 2 or 4.
+template <typename T, typename F>
+void for_pieces(int64_t cols, F&& kernel) {
+    using std::integral_constant;
+    const int64_t pieces = (cols + 64 * Piece<T>::V - 1) / (64 * Piece<T>::V);
+    if (pieces <= 1) kernel(integral_constant<int, 1>{});
+    else if (pieces <= 2) kernel(integral_constant<int, 2>{});
+    else kernel(integral_constant<int, kSegPieces>{});
+}
+
+template <typename T>
+hipError_t launch_dispatch_t(MoeRowsJob j, hipStream_t s) {
+    j.segs = segments<T>(j.cols);
     const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
-    const bool stream = j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
-    if (j.bf16) stream ? dispatch_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : dispatch_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
-    else stream ? dispatch_kernel<float, true><<<g, 256, 0, s>>>(j) : dispatch_kernel<float, false><<<g, 256, 0, s>>>(j);
+    const bool stream = j.rows_y * j.cols * (int64_t)sizeof(T) >= kStreamBytes;
+    for_pieces<T>(j.cols, [&](auto pieces) {
+        constexpr int kP = decltype(pieces)::value;
+        stream ? dispatch_kernel<T, true, kP><<<g, 256, 0, s>>>(j) : dispatch_kernel<T, false, kP><<<g, 256, 0, s>>>(j);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_dispatch(MoeRowsJob j, hipStream_t s) {
+    return j.bf16 ? launch_dispatch_t<uint16_t>(j, s) : launch_dispatch_t<float>(j, s);
+}
+
+template <typename T>
+hipError_t launch_combine_t(MoeRowsJob j, hipStream_t s) {
+    j.segs = segments<T>(j.cols);
+    const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
+    const bool stream = j.rows_y * j.cols * (int64_t)sizeof(T) >= kStreamBytes;
+    for_pieces<T>(j.cols, [&](auto pieces) {
+        constexpr int kP = decltype(pieces)::value;
+        stream ? combine_kernel<T, true, kP><<<g, 256, 0, s>>>(j) : combine_kernel<T, false, kP><<<g, 256, 0, s>>>(j);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_moe_combine(MoeRowsJob j, hipStream_t s) {
-    j.segs = j.bf16 ? segments<uint16_t>(j.cols) : segments<float>(j.cols);
-    const unsigned g = (unsigned)((j.tokens * j.segs + 3) / 4);
-    const bool stream = j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
-    if (j.bf16) stream ? combine_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : combine_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
-    else stream ? combine_kernel<float, true><<<g, 256, 0, s>>>(j) : combine_kernel<float, false><<<g, 256, 0, s>>>(j);
-    return hipGetLastError();
+    return j.bf16 ? launch_combine_t<uint16_t>(j, s) : launch_combine_t<float>(j, s);
 }
 
 // Up to this many slots (workgroups that 256 CUs hold at once) the gradient takes a workgroup per slot: a token's k rows one after
@@ -374,13 +499,24 @@ hipError_t launch_moe_combine(MoeRowsJob j, hipStream_t s) {
 // 13.3, 256 x 6 x 2048 7.7 / 12.5; 1024 x 6 x 2048 21.7 / 18.8 (dout is read k times).
 constexpr int64_t kFewSlots = 2048;
 
-hipError_t launch_moe_combine_bwd(const MoeBwdJob& j, hipStream_t s) {
-    const dim3 g((unsigned)j.tokens, j.tokens * j.k <= kFewSlots ? (unsigned)j.k : 1u);
-    const bool stream = 2 * j.rows_y * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
-    if (j.bf16)
-        stream ? combine_bwd_kernel<uint16_t, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<uint16_t, false><<<g, 256, 0, s>>>(j);
-    else stream ? combine_bwd_kernel<float, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<float, false><<<g, 256, 0, s>>>(j);
+template <typename T>
+hipError_t launch_combine_bwd_t(const MoeBwdJob& j, hipStream_t s) {
+    const bool stream = 2 * j.rows_y * j.cols * (int64_t)sizeof(T) >= kStreamBytes, few = j.tokens * j.k <= kFewSlots;
+    if (!few && segments<T>(j.cols) <= 1) {
+        const unsigned g = (unsigned)((j.tokens + 3) / 4);
+        for_pieces<T>(j.cols, [&](auto pieces) {
+            constexpr int kP = decltype(pieces)::value;
+            stream ? combine_bwd_wave_kernel<T, true, kP><<<g, 256, 0, s>>>(j) : combine_bwd_wave_kernel<T, false, kP><<<g, 256, 0, s>>>(j);
+        });
+    } else {
+        const dim3 g((unsigned)j.tokens, few ? (unsigned)j.k : 1u);
+        stream ? combine_bwd_kernel<T, true><<<g, 256, 0, s>>>(j) : combine_bwd_kernel<T, false><<<g, 256, 0, s>>>(j);
+    }
     return hipGetLastError();
+}
+
+hipError_t launch_moe_combine_bwd(const MoeBwdJob& j, hipStream_t s) {
+    return j.bf16 ? launch_combine_bwd_t<uint16_t>(j, s) : launch_combine_bwd_t<float>(j, s);
 }
 
 }  // namespace ufp4

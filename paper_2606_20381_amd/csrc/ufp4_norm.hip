@@ -11,7 +11,7 @@
 // Rows too long for the registers are read again per pass (`*_long_kernel`).
 //
 // Measured: forward 16384 x 5120 bf16 55 us = 6.1 TB/s with tensors in place, 65 us = 5.2 TB/s with new ones each time (a copy of
-// 1 GiB runs at 5.1); backward 8192 x 2048 bf16 22.5 us in two launches (its 101 MB are 20 us at the copy's rate), 32768 x 5120
+// 1 GiB runs at 5.1); backward 8192 x 2048 bf16 22.5 us in two launches (25 with new tensors; its 101 MB are 20 us at the copy's rate), 32768 x 5120
 // 187 us = 5.4 TB/s; short rows, 262144 x 128 bf16, 24 and 34 us (a wave per row: 61 and 91); 4 x 2048 3.6 us, launch and two
 // dependent sums.
 

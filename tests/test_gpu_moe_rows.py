@@ -292,3 +292,29 @@ def test_rows_past_32_bit_offsets():
     want = U.moe_combine_bwd(x, near, rows, off, w)
     dy, dw = U.moe_combine_bwd(x, y, rows, off, w, out=y)
     assert torch.equal(dy, want[0]) and torch.equal(dw, want[1])
+
+
+@pytest.mark.parametrize("cols", [40, 500, 512, 700, 1024, 1030, 2041, 2056])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("k", [1, 3, 5, 8])
+def test_many_tokens_of_every_width(cols, dt, k):
+    """Tokens past those that take a workgroup per slot: rows of one, two and four pieces a lane, and of several segments."""
+    tokens = 2500
+    rows, offsets, x, y, w = _case(tokens, k, 16, cols, dt, cols)
+    assert tokens * k > 2048
+    used, flat = int(offsets[-1]), rows.reshape(-1).long()
+    have = flat >= 0
+    want = torch.zeros(tokens * k, cols, dtype=torch.float64, device="cuda")
+    want[flat[have]] = (x.double()[:, None, :] * w.double()[:, :, None]).reshape(-1, cols)[have]
+    got = U.moe_dispatch(x, rows, offsets, w)
+    assert ((got.double() - want).abs() <= _unit(dt) * want.abs()).all() and not got[used:].any()
+    each = _gather64(y, rows, w)
+    ref, size = each.sum(1), each.abs().sum(1)
+    assert ((U.moe_combine(y, rows, w).double() - ref).abs() <= (k + 1) * 2.0**-24 * size + _unit(dt) * ref.abs()).all()
+    dy, dw = U.moe_combine_bwd(x, y, rows, offsets, w)
+    assert torch.equal(dy, got)
+    terms = _gather64(y, rows, None) * x.double()[:, None, :]
+    assert ((dw.double() - terms.sum(2)).abs() <= (48 + cols / 256) * 2.0**-24 * terms.abs().sum(2)).all()
+    over = y.clone()
+    again = U.moe_combine_bwd(x, over, rows, offsets, w, out=over)
+    assert torch.equal(again[0], dy) and torch.equal(again[1], dw)
