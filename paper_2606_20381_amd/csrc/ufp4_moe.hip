@@ -5,12 +5,14 @@
 //   bits of the key, so a slot's rank is a count of lanes and no atomic decides an order.
 // dispatch: out[rows[t, j]] = w[t, j] x[t]; combine: out[t] = sum_j w[t, j] y[rows[t, j]]; each the other's adjoint.
 // combine_bwd: dy[rows[t, j]] = w[t, j] dout[t] and dw[t, j] = <dout[t], y[rows[t, j]]> from one read of both.
-//   All three are HBM bound: a wave (combine_bwd: a workgroup) takes one token, or a 4 KiB segment of one, reads its row
-//   once for all k experts and sums in fp32.
+//   All three are HBM bound: a wave takes one token, or a 4 KiB segment of one, reads its row once for all k experts and sums in
+//   fp32. Short rows (one or two 16-byte pieces a lane) leave registers for several of a token's rows at a time, without which a
+//   token takes k times a read's latency: 32768 tokens x 8 x 128 bf16 dispatch 53 -> 22 us, combine 61 -> 26. The gradient of
+//   longer rows (more than a segment) takes a workgroup per token, of few tokens one per slot.
 //
-// Measured, 16384 tokens to 6 of 64 experts, 2048 bf16 columns: sort 4.8 + 7.6 us (two launches of 24 workgroups, bound by their
-// own latency), dispatch 80 us and combine 79 us (470 MB each: 5.9 TB/s; a copy of 1 GiB runs at 5.1), combine_bwd 217 us (873 MB:
-// 4.0 TB/s; 5003 x 2 x 5120 fp32 92 us, 512 MB: 5.6 TB/s).
+// Measured, 16384 tokens to 6 of 64 experts, 2048 bf16 columns: sort 4.7 + 7.7 us (two launches of 24 workgroups, bound by their
+// own latency), dispatch 79 us and combine 80 us (470 MB each: 5.9 TB/s; a copy of 1 GiB runs at 5.1), combine_bwd 173 us (873 MB:
+// 5.0 TB/s; 5003 x 2 x 5120 fp32 92 us, 512 MB: 5.6 TB/s).
 
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
@@ -447,11 +449,6 @@ hipError_t launch_moe_sort(const MoeSortJob& j, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Rows by expert of kStreamBytes and more are stored (dispatch) and read (combine) nontemporally: no cache holds them until they
-// are used again, and kept in order of recency they push out what is. bf16, 16384 tokens x 6 x 2048 (403 MB), us, nontemporal /
-// plain: dispatch 80 / 92, combine 80 / 95, one after the other 160 / 204; 8192 tokens (201 MB) 42 / 35, 42 / 36, 84 / 72.
-// combine_bwd reads one such tensor and writes another, so its stores take half the size: 16384 tokens 217 / 222, 8192 94 / 117,
-// 4096 51 / 52.
 // Pieces a lane of rows of `cols`: 1, 2 or 4.
 template <typename T, typename F>
 void for_pieces(int64_t cols, F&& kernel) {
@@ -462,6 +459,11 @@ void for_pieces(int64_t cols, F&& kernel) {
     else kernel(integral_constant<int, kSegPieces>{});
 }
 
+// Rows by expert of kStreamBytes and more are stored (dispatch) and read (combine) nontemporally: no cache holds them until they
+// are used again, and kept in order of recency they push out what is. bf16, 16384 tokens x 6 x 2048 (403 MB), us, nontemporal /
+// plain: dispatch 80 / 92, combine 80 / 95, one after the other 160 / 204; 8192 tokens (201 MB) 42 / 35, 42 / 36, 84 / 72.
+// combine_bwd reads one such tensor and writes another, so its stores take half the size (a workgroup per token: 16384 tokens 217 /
+// 222, 8192 94 / 117, 4096 51 / 52).
 template <typename T>
 hipError_t launch_dispatch_t(MoeRowsJob j, hipStream_t s) {
     j.segs = segments<T>(j.cols);
