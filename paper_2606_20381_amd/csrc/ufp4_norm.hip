@@ -417,29 +417,34 @@ __global__ __launch_bounds__(256) void norm_bwd_cols_kernel(NormBwdJob j) {
     if (b) b[c] = ab;
 }
 
-// dgamma and dbeta from `n` partial rows of 2 * cols sums: 64 columns per workgroup, 16 waves over the partial rows, then
-// the waves' sums in order.
+// dgamma and dbeta from `n` partial rows of 2 * cols sums: a workgroup takes 64 columns at a time, 16 waves over the partial rows,
+// then the waves' sums in order. Rows of up to kReduceGroups * 32 columns have a workgroup for each 64 sums; a grid holds fewer
+// than 2^32 threads, so those of longer ones take several in turn.
+constexpr int64_t kReduceGroups = int64_t(1) << 16;
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restrict__ part, int n, int64_t cols, float* dgamma,
                                                            float* dbeta) {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;  // of 2 * cols
-    float v = 0.0f;
-    if (c < 2 * cols) {
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < 2 * cols; c0 += (int64_t)gridDim.x * 64) {  // the same for every thread
+        const int64_t c = c0 + lane;  // of 2 * cols
+        float v = 0.0f;
+        if (c < 2 * cols) {
 #pragma unroll 8
-        for (int i = wave; i < n; i += 16) v += part[(int64_t)i * 2 * cols + c];
-    }
-    s[wave][lane] = v;
-    __syncthreads();
-    if (wave == 0 && c < 2 * cols) {
-        float t = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) t += s[w][lane];
-        if (c < cols) {
-            if (dgamma) dgamma[c] = t;
-        } else if (dbeta) {
-            dbeta[c - cols] = t;
+            for (int i = wave; i < n; i += 16) v += part[(int64_t)i * 2 * cols + c];
         }
+        s[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0 && c < 2 * cols) {
+            float t = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 16; ++w) t += s[w][lane];
+            if (c < cols) {
+                if (dgamma) dgamma[c] = t;
+            } else if (dbeta) {
+                dbeta[c - cols] = t;
+            }
+        }
+        __syncthreads();  // the sums have been read
     }
 }
 
@@ -527,7 +532,8 @@ hipError_t launch_norm_bwd_t(const NormBwdJob& j, hipStream_t s) {
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!j.dgamma && !j.dbeta) || parts == 1) return e;  // a lone workgroup's sums are in place
-    norm_reduce_kernel<<<(unsigned)((2 * j.cols + 63) / 64), 1024, 0, s>>>(j.part, (int)parts, j.cols, j.dgamma, j.dbeta);
+    norm_reduce_kernel<<<(unsigned)min64((2 * j.cols + 63) / 64, kReduceGroups), 1024, 0, s>>>(j.part, (int)parts, j.cols, j.dgamma,
+                                                                                            j.dbeta);
     return hipGetLastError();
 }
 

@@ -278,3 +278,19 @@ def test_rows_past_32_bit_offsets(dt, cols):
     dy = torch.randn(3, cols, device="cuda").to(dt)
     assert all(torch.equal(p, q) for p, q in zip(U.layer_norm_bwd(dy, x, g, mean, rstd, out=y),
                                                  U.layer_norm_bwd(dy, x.contiguous(), g, mean, rstd)))
+
+
+def test_weight_gradient_of_very_long_rows():
+    """Rows whose 2 * cols sums are more than a grid of one workgroup for each 64 of them holds. The statistics are given as 0 and 1, so
+    a column's dgamma is one product and one fused product and sum (two roundings of at most 2^-24 of the magnitudes each), its dbeta
+    one sum of two numbers."""
+    cols = (1 << 27) + 40
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.empty(2, cols, device="cuda", dtype=BF).normal_(generator=g) for _ in range(2))
+    mean, rstd = torch.zeros(2, device="cuda"), torch.ones(2, device="cuda")
+    _, dgamma, dbeta = U.layer_norm_bwd(dy, x, None, mean, rstd)
+    for a in range(0, cols, 1 << 24):
+        s = slice(a, min(cols, a + (1 << 24)))
+        d, v = dy[:, s].double(), x[:, s].double()
+        assert ((dgamma[s] - (d * v).sum(0)).abs() <= 4 * 2.0**-24 * (d * v).abs().sum(0)).all()
+        assert torch.equal(dbeta[s], d.sum(0).float())
