@@ -1,8 +1,9 @@
-// The host's side of the calls whose kernels take a few microseconds: a decode step's norm, routing and products. Argument checks,
-// output tensors and the C ABI call in one step of native code; the binding's Python functions (which document them) pass their
-// arguments on. In Python each output tensor costs 1.2 - 1.8 us, the checks 1 - 2 and the foreign call 1. us a call, so / here:
+// The host's side of the calls whose kernels take a few microseconds: a decode step's norm, routing and products, and the
+// quantizers and products of a training step, which issues eight of them for the same experts. Argument checks, output tensors and the
+// C ABI call in one step of native code; the binding's Python functions (which document them) pass their arguments on. In Python each output tensor costs 1.2 - 1.8 us, the checks 1 - 2 and the foreign call 1. us a call, so / here:
 // norm 9.9 / 5.6, its gradient 15.1 / 9.0, sort 8.8 / 5.4, dispatch 7.1 / 3.9, combine 6.9 / 3.9, quantizing 9.2 / 5.2, a dense
-// product 6.5 / 4.1, a product of 3 tokens 7.0 / 4.1, of 64 16.1 / 8.1 (a launch alone is about 2).
+// product 6.5 / 4.1, a product of 3 tokens 7.0 / 4.1, of 64 16.1 / 8.1, both operands of a tensor 13.7 / 7.7, grouped quantizing 10.1 /
+// 6.0, a grouped product 7.7 / 4.7 (a launch alone is about 2).
 // Errors: ValueError for a tensor that a call cannot take, TypeError for what is no tensor, the binding's error class for a status of
 // the library.
 
@@ -155,14 +156,14 @@ bool slots_of(PyObject* o, PyObject* w, const at::Device& device, Slots& s) {
     return vector(w, "weights", at::kFloat, s.tokens * s.k, device, false, s.w);
 }
 
-// offsets int64 [experts + 1]
-bool offsets_of(PyObject* o, const at::Device& device, void*& p, int64_t& experts) {
+// offsets int64 [groups + 1]
+bool offsets_of(PyObject* o, const at::Device& device, void*& p, int64_t& groups) {
     const at::Tensor* const t = tensor(o, "offsets");
     if (!t) return false;
     if (t->scalar_type() != at::kLong || t->dim() != 1 || t->device() != device || !t->is_contiguous())
-        return refuse("offsets", "a contiguous int64 tensor [experts + 1] on the input's device");
+        return refuse("offsets", "a contiguous int64 tensor [groups + 1] on the input's device");
     p = t->data_ptr();
-    experts = t->numel() - 1;
+    groups = t->numel() - 1;
     return true;
 }
 
@@ -365,19 +366,28 @@ bool new_operand(const at::Tensor& like, int64_t rows, int64_t red, ufp4_qtensor
     return true;
 }
 
-// The output [rows, cols] of a product, float32 or bfloat16: `o`, or a new tensor of type `code` for None.
-bool product_out(PyObject* o, const at::Tensor& like, int64_t rows, int64_t cols, int code, at::Tensor& out) {
+// The output of a product, row-major float32 or bfloat16 [rows, cols] or, of groups > 0 matrices rows apart, [groups, rows, cols]: `o`,
+// or a new tensor of type `code` for None.
+bool product_out(PyObject* o, const at::Tensor& like, int64_t groups, int64_t rows, int64_t cols, int code, at::Tensor& out) {
+    const int64_t size[3] = {groups, rows, cols};
+    const at::IntArrayRef shape(size + (groups ? 0 : 1), groups ? 3 : 2);
     if (o == Py_None) {
         if (code < 0) return refuse("out_dtype", "float32 or bfloat16");
-        out = at::empty({rows, cols}, like.options().dtype(code == UFP4_OUT_BF16 ? at::kBFloat16 : at::kFloat));
+        out = at::empty(shape, like.options().dtype(code == UFP4_OUT_BF16 ? at::kBFloat16 : at::kFloat));
         return true;
     }
     const at::Tensor* const t = tensor(o, "out");
     if (!t) return false;
-    if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || t->stride(1) != 1 || t->device() != like.device()) {
-        PyErr_Format(PyExc_ValueError, "out must be a row-major tensor of shape (%lld, %lld) on the input's device", (long long)rows, (long long)cols);
+    if (t->sizes() != shape || t->stride(-1) != 1 || t->device() != like.device()) {
+        if (groups)
+            PyErr_Format(PyExc_ValueError, "out must be a row-major tensor of shape (%lld, %lld, %lld) on the input's device", (long long)groups,
+                         (long long)rows, (long long)cols);
+        else
+            PyErr_Format(PyExc_ValueError, "out must be a row-major tensor of shape (%lld, %lld) on the input's device", (long long)rows,
+                         (long long)cols);
         return false;
     }
+    if (groups > 1 && t->stride(0) != rows * t->stride(1)) return refuse("out", "of groups that lie their rows apart");
     if (code_of(*t) < 0) return refuse("out", "float32 or bfloat16");
     out = *t;
     return true;
@@ -399,6 +409,56 @@ CALL(mxfp4_quantize, 10)
     if (fresh && !new_operand(*x, transpose ? cols : rows, transpose ? rows : cols, *d, codes, scales)) return nullptr;
     if (!check(ufp4_mxfp4_quantize(x->data_ptr(), rows, cols, x->stride(0), transpose, rht, mask, rounding, seed, id, d, stream),
                "ufp4_mxfp4_quantize"))
+        return nullptr;
+    if (!fresh) Py_RETURN_NONE;
+    return pair(codes, THPVariable_Wrap(scales));
+END_CALL
+
+// (x, rht_rows, rht_cols, sign_mask_rows, sign_mask_cols, rounding, seed, stream_rows, stream_cols, descriptor of the rows, fresh,
+// descriptor of the columns, fresh, stream) -> (codes, scales, codes, scales), None for those of a descriptor that is not fresh
+CALL(mxfp4_quantize_dual, 14)
+    const at::Tensor* const x = bf16_of(a[0]);
+    if (!x) return nullptr;
+    const int rht_r = PyObject_IsTrue(a[1]), rht_c = PyObject_IsTrue(a[2]), fresh_r = PyObject_IsTrue(a[10]), fresh_c = PyObject_IsTrue(a[12]);
+    const uint32_t mask_r = (uint32_t)PyLong_AsUnsignedLongMask(a[3]), mask_c = (uint32_t)PyLong_AsUnsignedLongMask(a[4]);
+    const int rounding = (int)PyLong_AsLong(a[5]);
+    const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[6]);
+    const uint32_t id_r = (uint32_t)PyLong_AsUnsignedLongMask(a[7]), id_c = (uint32_t)PyLong_AsUnsignedLongMask(a[8]);
+    ufp4_qtensor *const r = operand_of(a[9]), *const c = operand_of(a[11]);
+    void* const stream = pointer(a[13]);
+    if (PyErr_Occurred()) return nullptr;
+    const int64_t rows = x->size(0), cols = x->size(1);
+    at::Tensor codes_r, scales_r, codes_c, scales_c;
+    if ((fresh_r && !new_operand(*x, rows, cols, *r, codes_r, scales_r)) || (fresh_c && !new_operand(*x, cols, rows, *c, codes_c, scales_c)) ||
+        !check(ufp4_mxfp4_quantize_dual(x->data_ptr(), rows, cols, x->stride(0), rht_r, mask_r, id_r, rht_c, mask_c, id_c, rounding, seed, r, c,
+                                        stream), "ufp4_mxfp4_quantize_dual"))
+        return nullptr;
+    PyObject* const t[4] = {THPVariable_Wrap(codes_r), THPVariable_Wrap(scales_r), THPVariable_Wrap(codes_c), THPVariable_Wrap(scales_c)};
+    PyObject* const all = t[0] && t[1] && t[2] && t[3] ? PyTuple_Pack(4, t[0], t[1], t[2], t[3]) : nullptr;
+    for (PyObject* o : t) Py_XDECREF(o);
+    return all;
+END_CALL
+
+// (x, offsets, padded_total, transpose, rht, sign_mask, rounding, seed, stream_id, descriptor, fresh, stream) -> (codes, scales) of a
+// fresh descriptor, or None
+CALL(mxfp4_quantize_grouped, 12)
+    const at::Tensor* const x = bf16_of(a[0]);
+    void* offsets;
+    int64_t groups;
+    if (!x || !offsets_of(a[1], x->device(), offsets, groups)) return nullptr;
+    const int64_t padded = PyLong_AsLongLong(a[2]);
+    const int transpose = PyObject_IsTrue(a[3]), rht = PyObject_IsTrue(a[4]), fresh = PyObject_IsTrue(a[10]);
+    const uint32_t mask = (uint32_t)PyLong_AsUnsignedLongMask(a[5]), id = (uint32_t)PyLong_AsUnsignedLongMask(a[8]);
+    const int rounding = (int)PyLong_AsLong(a[6]);
+    const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[7]);
+    ufp4_qtensor* const d = operand_of(a[9]);
+    void* const stream = pointer(a[11]);
+    if (PyErr_Occurred()) return nullptr;
+    const int64_t rows = x->size(0), cols = x->size(1);
+    at::Tensor codes, scales;
+    if (fresh && !new_operand(*x, transpose ? cols : padded, transpose ? padded : cols, *d, codes, scales)) return nullptr;
+    if (!check(ufp4_mxfp4_quantize_grouped(x->data_ptr(), rows, cols, x->stride(0), transpose, static_cast<int64_t*>(offsets), (int32_t)groups,
+                                           padded, rht, mask, rounding, seed, id, d, stream), "ufp4_mxfp4_quantize_grouped"))
         return nullptr;
     if (!fresh) Py_RETURN_NONE;
     return pair(codes, THPVariable_Wrap(scales));
@@ -439,7 +499,7 @@ PyObject* product(const char* name, PyObject* const* a, Py_ssize_t n_args) {
     void* const stream = pointer(a[5]);
     if (!codes || PyErr_Occurred()) return nullptr;
     at::Tensor out;
-    if (!product_out(a[4], *codes, x->rows, w->rows, code, out)) return nullptr;
+    if (!product_out(a[4], *codes, 0, x->rows, w->rows, code, out)) return nullptr;
     if (!check(GEMM(x, w, out.data_ptr(), out.stride(0), code_of(out), stream), name)) return nullptr;
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
@@ -449,6 +509,55 @@ PyObject* product(const char* name, PyObject* const* a, Py_ssize_t n_args) {
 PRODUCT(mxfp4_gemm_fwd_y)
 PRODUCT(mxfp4_gemm_bwd_dx)
 PRODUCT(mxfp4_gemm_bwd_dw)
+
+// (codes of A, descriptor of A, of B, offsets, rows of the output, out type, out, stream) -> out. BY_GROUP: B holds the groups' rows one
+// after the other (W), otherwise their columns (W transposed).
+template <int (*GEMM)(const ufp4_qtensor*, const ufp4_qtensor*, const int64_t*, int32_t, int64_t, void*, int64_t, int, void*), bool BY_GROUP>
+PyObject* product_rows(const char* name, PyObject* const* a, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (!arguments(n_args, 8)) return nullptr;
+    const at::Tensor* const codes = tensor(a[0], "codes");
+    void* offsets;
+    int64_t groups;
+    if (!codes || !offsets_of(a[3], codes->device(), offsets, groups)) return nullptr;
+    const ufp4_qtensor *const x = operand_of(a[1]), *const w = operand_of(a[2]);
+    const int64_t rows = PyLong_AsLongLong(a[4]);
+    const int code = (int)PyLong_AsLong(a[5]);
+    void* const stream = pointer(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor out;
+    if (groups < 1) return refuse("offsets", "of one group at least"), nullptr;
+    if (!product_out(a[6], *codes, 0, rows, BY_GROUP ? w->rows / groups : w->rows, code, out)) return nullptr;
+    if (!check(GEMM(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, rows, out.data_ptr(), out.stride(0), code_of(out), stream), name))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* mxfp4_gemm_fwd_y_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return product_rows<ufp4_mxfp4_gemm_fwd_y_grouped, true>("ufp4_mxfp4_gemm_fwd_y_grouped", a, n);
+}
+PyObject* mxfp4_gemm_bwd_dx_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return product_rows<ufp4_mxfp4_gemm_bwd_dx_grouped, false>("ufp4_mxfp4_gemm_bwd_dx_grouped", a, n);
+}
+
+// (codes of A, descriptor of A, of B, offsets, out type, out, stream) -> out [groups, rows of A, rows of B]
+CALL(mxfp4_gemm_bwd_dw_grouped, 7)
+    const at::Tensor* const codes = tensor(a[0], "codes");
+    void* offsets;
+    int64_t groups;
+    if (!codes || !offsets_of(a[3], codes->device(), offsets, groups)) return nullptr;
+    const ufp4_qtensor *const x = operand_of(a[1]), *const w = operand_of(a[2]);
+    const int code = (int)PyLong_AsLong(a[4]);
+    void* const stream = pointer(a[6]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor out;
+    if (groups < 1) return refuse("offsets", "of one group at least"), nullptr;
+    if (!product_out(a[5], *codes, groups, x->rows, w->rows, code, out)) return nullptr;
+    if (!check(ufp4_mxfp4_gemm_bwd_dw_grouped(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, out.data_ptr(), out.stride(1), code_of(out),
+                                              stream), "ufp4_mxfp4_gemm_bwd_dw_grouped"))
+        return nullptr;
+    return THPVariable_Wrap(out);
+END_CALL
 
 // (x, descriptor of W, out type, out, most tokens of the one-launch product, stream) -> y
 CALL(mxfp4_linear, 6)
@@ -465,7 +574,7 @@ CALL(mxfp4_linear, 6)
         return nullptr;
     }
     at::Tensor out;
-    if (!product_out(a[3], *x, tokens, w->rows, code, out)) return nullptr;
+    if (!product_out(a[3], *x, 0, tokens, w->rows, code, out)) return nullptr;
     if (tokens <= most && w->rht_block == 0) {
         if (!check(ufp4_mxfp4_linear(x->data_ptr(), tokens, x->stride(0), w, out.data_ptr(), out.stride(0), code_of(out), stream),
                    "ufp4_mxfp4_linear"))
@@ -494,6 +603,8 @@ PyMethodDef kMethods[] = {METHOD(layer_norm),   METHOD(layer_norm_bwd), METHOD(m
                           METHOD(moe_dispatch), METHOD(moe_combine),    METHOD(moe_combine_bwd),
                           METHOD(mxfp4_quantize), METHOD(mxfp4_dequantize), METHOD(mxfp4_gemm_fwd_y),
                           METHOD(mxfp4_gemm_bwd_dx), METHOD(mxfp4_gemm_bwd_dw), METHOD(mxfp4_linear),
+                          METHOD(mxfp4_quantize_dual), METHOD(mxfp4_quantize_grouped), METHOD(mxfp4_gemm_fwd_y_grouped),
+                          METHOD(mxfp4_gemm_bwd_dx_grouped), METHOD(mxfp4_gemm_bwd_dw_grouped),
                           {"set_error", set_error, METH_O, nullptr},    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", "Host side of the short calls of ufp4.py", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

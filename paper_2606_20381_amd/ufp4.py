@@ -669,15 +669,12 @@ def mxfp4_quantize_dual(x: torch.Tensor, *, rht_rows: bool = False, rht_cols: bo
                         out_cols: QTensor | None = None) -> tuple[QTensor, QTensor]:
     """Both microscaled operands of x [rows, cols] (ufp4_mxfp4_quantize_dual): (Q_r [rows, cols] along cols, Q_c [cols, rows]
     along rows)."""
-    _bf16_2d(x)
-    rows, cols = x.shape
-    qr = out_rows if out_rows is not None else empty_qtensor(rows, cols, E2M1_MX32, x.device)
-    qc = out_cols if out_cols is not None else empty_qtensor(cols, rows, E2M1_MX32, x.device)
-    st = lib().ufp4_mxfp4_quantize_dual(x.data_ptr(), rows, cols, x.stride(0), int(rht_rows), sign_mask_rows, stream_rows,
-                                        int(rht_cols), sign_mask_cols, stream_cols, rounding,
-                                        seed & 0xFFFFFFFFFFFFFFFF, qr.ref(), qc.ref(), _stream())
-    _check(st, "ufp4_mxfp4_quantize_dual")
-    return qr, qc
+    dr = out_rows.desc if out_rows is not None else QDesc()
+    dc = out_cols.desc if out_cols is not None else QDesc()
+    cr, sr, cc, sc = (_host_module or _host()).mxfp4_quantize_dual(
+        x, rht_rows, rht_cols, sign_mask_rows, sign_mask_cols, rounding, seed, stream_rows, stream_cols, _addressof(dr), out_rows is None,
+        _addressof(dc), out_cols is None, _stream())
+    return (out_rows if out_rows is not None else QTensor(cr, sr, dr)), (out_cols if out_cols is not None else QTensor(cc, sc, dc))
 
 
 def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total: int, *, transpose: bool,
@@ -685,16 +682,15 @@ def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total:
                            out: QTensor | None = None) -> QTensor:
     """ufp4_mxfp4_quantize_grouped: the forms of mx_quantize_grouped (padded_total from group_offsets with block 128 for
     transpose False, 32 for True)."""
-    _bf16_2d(x)
-    rows, cols = x.shape
-    G = _offsets(offsets)
-    qrows, red = (cols, padded_total) if transpose else (padded_total, cols)
-    q = out if out is not None else empty_qtensor(qrows, red, E2M1_MX32, x.device)
-    st = lib().ufp4_mxfp4_quantize_grouped(x.data_ptr(), rows, cols, x.stride(0), int(transpose), offsets.data_ptr(), G,
-                                           padded_total, int(rht), sign_mask, rounding, seed & 0xFFFFFFFFFFFFFFFF,
-                                           stream_id, q.ref(), _stream())
-    _check(st, "ufp4_mxfp4_quantize_grouped")
-    return q
+    h = _host_module or _host()
+    if out is not None:
+        h.mxfp4_quantize_grouped(x, offsets, padded_total, transpose, rht, sign_mask, rounding, seed, stream_id, _addressof(out.desc), False,
+                                 _stream())
+        return out
+    desc = QDesc()
+    codes, scales = h.mxfp4_quantize_grouped(x, offsets, padded_total, transpose, rht, sign_mask, rounding, seed, stream_id,
+                                             _addressof(desc), True, _stream())
+    return QTensor(codes, scales, desc)
 
 
 def mxfp4_dequantize(q: QTensor, out: torch.Tensor | None = None) -> torch.Tensor:
@@ -720,23 +716,22 @@ def mxfp4_gemm_bwd_dw(dytq: QTensor, xtq: QTensor, out_dtype=torch.float32, out=
 def mxfp4_gemm_fwd_y_grouped(xq: QTensor, wq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
                              out=None) -> torch.Tensor:
     """Y [m_total, N] per group from the grouped-rows X and W [G*N, K] (ufp4_mxfp4_gemm_fwd_y_grouped)."""
-    n = wq.rows // _offsets(offsets)
-    return _mx_gemm_ragged_m("ufp4_mxfp4_gemm_fwd_y_grouped", xq, wq, offsets, m_total,
-                             _out((m_total, n), out_dtype, xq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_fwd_y_grouped(xq.codes, _addressof(xq.desc), _addressof(wq.desc), offsets, m_total,
+                                                              _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dx_grouped(dyq: QTensor, wtq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
                               out=None) -> torch.Tensor:
     """dX [m_total, K] per group from the grouped-rows dY and W^T [K, G*N] (ufp4_mxfp4_gemm_bwd_dx_grouped)."""
-    return _mx_gemm_ragged_m("ufp4_mxfp4_gemm_bwd_dx_grouped", dyq, wtq, offsets, m_total,
-                             _out((m_total, wtq.rows), out_dtype, dyq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_bwd_dx_grouped(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), offsets, m_total,
+                                                               _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dw_grouped(dytq: QTensor, xtq: QTensor, offsets: torch.Tensor, out_dtype=torch.float32,
                               out=None) -> torch.Tensor:
     """dW [G, N, K] from the grouped-reduction dY^T and X^T (ufp4_mxfp4_gemm_bwd_dw_grouped)."""
-    return _gemm_grouped("ufp4_mxfp4_gemm_bwd_dw_grouped", dytq, xtq, offsets,
-                         _out((_offsets(offsets), dytq.rows, xtq.rows), out_dtype, dytq.codes.device, out))
+    return (_host_module or _host()).mxfp4_gemm_bwd_dw_grouped(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), offsets,
+                                                               _code_of(out_dtype), out, _stream())
 
 
 LINEAR_TOKENS = 16  # tokens up to which ufp4_mxfp4_linear takes a product

@@ -345,3 +345,45 @@ def test_host_module_refuses_before_the_library(lib):
     assert e.value.status == MISMATCH and "ufp4_mxfp4_gemm_fwd_y" in str(e.value)
     with pytest.raises(TypeError, match="arguments"):
         h.layer_norm(x)
+
+
+def test_host_module_refuses_grouped_calls_before_the_library(lib):
+    """The same of the grouped calls and of the two-operand quantizer, and a status of the library with the call's name."""
+    h, null, a = U._host(), 0, ctypes.addressof
+    x, off, codes = torch.zeros(2, 32, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64), torch.zeros(1, 2048, dtype=torch.uint8)
+    d, e = desc(2, 32), desc(4, 32)
+    for bad, error in ((x, ValueError), (3, TypeError)):
+        with pytest.raises(error):
+            h.mxfp4_quantize_dual(bad, False, False, 0, 0, 0, 0, 0, 0, a(d), False, a(e), False, null)
+        with pytest.raises(error):
+            h.mxfp4_quantize_grouped(bad, off, 32, True, False, 0, 0, 0, 0, a(d), False, null)
+
+    def y(offsets, out=None, code=BF16, rows=7):
+        return h.mxfp4_gemm_fwd_y_grouped(codes, a(d), a(e), offsets, rows, code, out, null)
+
+    def dx(offsets, out=None, code=BF16):
+        return h.mxfp4_gemm_bwd_dx_grouped(codes, a(d), a(e), offsets, 7, code, out, null)
+
+    def dw(offsets, out=None, code=BF16):
+        return h.mxfp4_gemm_bwd_dw_grouped(codes, a(d), a(e), offsets, code, out, null)
+
+    for call, shape in ((y, (7, 2)), (dx, (7, 4)), (dw, (2, 2, 4))):
+        for offsets in (off.int(), off[None], off[:1], torch.zeros(6, dtype=torch.int64)[::2]):
+            with pytest.raises(ValueError, match="offsets"):
+                call(offsets)
+        with pytest.raises(TypeError, match="offsets"):
+            call(None)
+        with pytest.raises(ValueError, match="out_dtype"):
+            call(off, code=-1)
+        wrong = torch.zeros(*shape[:-1], shape[-1] + 1)
+        for out in (wrong, wrong[..., 0], torch.zeros(shape, dtype=torch.float64), torch.zeros(*shape[:-1], 2 * shape[-1])[..., ::2]):
+            with pytest.raises(ValueError, match="out"):
+                call(off, out)
+        with pytest.raises(TypeError, match="arguments"):
+            getattr(h, "mxfp4_gemm_bwd_dw_grouped")(codes, a(d))
+    with pytest.raises(ValueError, match="apart"):
+        dw(off, torch.zeros(2, 3, 4)[:, :2])
+    with pytest.raises(U.UFP4Error, match="ufp4_mxfp4_gemm_bwd_dw_grouped"):  # plain operands
+        dw(off)
+    with pytest.raises(RuntimeError):
+        y(off, rows=-1)
