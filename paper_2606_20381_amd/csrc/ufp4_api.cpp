@@ -246,7 +246,8 @@ int launch_mx(int format, const MxGemmJob& j, void* stream) {
     return status_of(format == UFP4_FMT_E2M1_MX32 ? launch_gemm_mxfp4(j, s) : launch_gemm_mx(j, s));
 }
 
-int mx_gemm_impl(int format, const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype, void* stream) {
+int mx_gemm_impl(int format, const ufp4_qtensor* a, const ufp4_qtensor* b, void* c, int64_t ldc, int out_dtype, void* stream,
+                 bool weight_grad = false) {
     int st = check_operands(a, b, format);
     if (st != UFP4_OK) return st;
     if (a->red != b->red) return UFP4_ERR_MISMATCH;
@@ -275,6 +276,7 @@ int mx_gemm_impl(int format, const ufp4_qtensor* a, const ufp4_qtensor* b, void*
     j.c = c;
     j.ldc = ldc;
     j.mode = kGemmDense;
+    j.weight_grad = weight_grad;
     return launch_mx(format, j, stream);
 }
 
@@ -466,6 +468,7 @@ int mx_bwd_dw_grouped_impl(int format, const ufp4_qtensor* dyt, const ufp4_qtens
     if (!mx_grid_fits(format, ceil_div(dyt->rows, 256), ceil_div(xt->rows, 256), num_groups, true)) return UFP4_ERR_UNSUPPORTED;
     MxGemmJob j = mx_job(dyt, xt, dw_dev, ldc, out_dtype);
     j.mode = kGemmRaggedK;
+    j.weight_grad = true;
     j.M = dyt->rows;
     j.N = xt->rows;
     j.nkb = dyt->red / 32;
@@ -885,7 +888,7 @@ int ufp4_mx_gemm_bwd_dx(const ufp4_qtensor* dy, const ufp4_qtensor* wt, void* dx
 
 int ufp4_mx_gemm_bwd_dw(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, void* dw_dev, int64_t ldc, int out_dtype,
                         void* stream) {
-    return mx_gemm_impl(UFP4_FMT_UNIFORM_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream);  // dW [N, K] = dY^T [N, M] . (X^T [K, M])^T
+    return mx_gemm_impl(UFP4_FMT_UNIFORM_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream, true);  // dW [N, K] = dY^T [N, M] . (X^T [K, M])^T
 }
 
 int ufp4_mxfp4_quantize(const void* x_dev, int64_t rows, int64_t cols, int64_t ld, int transpose, int rht,
@@ -981,7 +984,7 @@ int ufp4_mxfp4_gemm_bwd_dx(const ufp4_qtensor* dy, const ufp4_qtensor* wt, void*
 
 int ufp4_mxfp4_gemm_bwd_dw(const ufp4_qtensor* dyt, const ufp4_qtensor* xt, void* dw_dev, int64_t ldc, int out_dtype,
                            void* stream) {
-    return mx_gemm_impl(UFP4_FMT_E2M1_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream);
+    return mx_gemm_impl(UFP4_FMT_E2M1_MX32, dyt, xt, dw_dev, ldc, out_dtype, stream, true);
 }
 
 int ufp4_gemm_fwd_y(const ufp4_qtensor* x, const ufp4_qtensor* w, void* y_dev, int64_t ldc, int out_dtype,

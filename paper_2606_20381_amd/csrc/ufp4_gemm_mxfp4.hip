@@ -668,8 +668,13 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
 // fp32 393 / 602 (190 MB read instead of 425), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
 // gradient 259 / 322; at 256 MiB 8192 x 8192 fp32 of 1024 74 / 97, of 2048 107 / 99, of 8192 254 / 267; below, 8192 x 8192 x 2048
 // bf16 83 / 77. The 64-row tiles are not taken for outputs of that size.
+// A weights' gradient is read when the whole step's have been computed, hundreds of MB later, so it is stored so from 64 MiB on. Whole
+// steps (quantizers and the three products), us, nontemporal / plain: 16 experts 4823 x 1920 x 1600 (188 MiB of gradients) 132 / 150, 8
+// experts 1602 x 3456 x 1600 (169) 106 / 119, 16508 x 4736 x 1344 (194) 403 / 418, 16 experts 2069 x 7552 x 256 (118) 102 / 106, dense
+// 5120 x 6016 x 2976 (68) 202 / 208-214; below 32 MiB the same within 1%. (Where 64-row tiles take such a gradient they store plainly.)
+constexpr int64_t kStreamGradBytes = int64_t(64) << 20;
 bool streams(const MxGemmJob& j) {
-    return j.M * j.N * (j.mode == kGemmRaggedK ? j.G : 1) * (j.out_dtype == kOutF32 ? 4 : 2) >= kStreamBytes;
+    return j.M * j.N * (j.mode == kGemmRaggedK ? j.G : 1) * (j.out_dtype == kOutF32 ? 4 : 2) >= (j.weight_grad ? kStreamGradBytes : kStreamBytes);
 }
 
 // Which tile takes a problem: the one with the smallest estimated time

@@ -169,6 +169,7 @@ struct MxGemmJob {
     int32_t G;
     int64_t b_group_rows;
     int64_t b_group_kb;
+    bool weight_grad;  // C is a weights' gradient, which a step reads when all of it has been computed
 };
 
 hipError_t launch_gemm_mx(const MxGemmJob& job, hipStream_t stream);
