@@ -345,3 +345,17 @@ def test_offsets_that_claim_too_much(claim):
     dw = U.mxfp4_gemm_bwd_dw_grouped(dytq, xtq, off)
     _within(dw[0], _values(dytq)[:, :128], _values(xtq)[:, :128], 128, F32)
     assert not dw[2:].any()
+
+
+@pytest.mark.parametrize("n,k,dt", [(4133, 4099, F32), (6001, 6007, BF), (4096, 4104, F32)])
+def test_weight_gradients_stored_past_the_caches(n, k, dt):
+    """A dense weights' gradient of 64 MiB and more is stored by a kernel of its own: the same numbers, bit for bit, as the forward
+    product of these operands, and nothing beside the rows of a wider output."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    a, b = (U.mxfp4_quantize(torch.randn(r, 416, generator=g, device="cuda").to(BF)) for r in (n, k))
+    want = U.mxfp4_gemm_fwd_y(a, b, dt)
+    assert 64 << 20 <= want.numel() * want.element_size() < 256 << 20
+    assert torch.equal(U.mxfp4_gemm_bwd_dw(a, b, dt), want)
+    wide = torch.full((n, k + 8), 7.0, device="cuda", dtype=dt)
+    U.mxfp4_gemm_bwd_dw(a, b, dt, out=wide[:, :k])
+    assert torch.equal(wide[:, :k], want) and (wide[:, k:] == 7.0).all()
