@@ -532,7 +532,8 @@ int ufp4_gemm_bwd_dw_grouped(const ufp4_qtensor *dyt, const ufp4_qtensor *xt, co
  * ufp4_layer_norm -- per row: mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) rstd gamma + beta.
  *   gamma_dev, beta_dev  [cols] of w_dtype (UFP4_OUT_*); NULL: 1 and 0.
  *   eps                  finite, >= 0.
- *   mean_dev, rstd_dev   fp32 [rows], for the backward call; either may be NULL. y may be x.
+ *   mean_dev, rstd_dev   fp32 [rows], for the backward call; either may be NULL. Rows without columns: nothing is launched and both
+ *                        stay as they were (0 / 0; the Python binding returns NaN). y may be x.
  */
 int ufp4_layer_norm(int dtype, const void *x_dev, int64_t rows, int64_t cols, int64_t ldx, int w_dtype, const void *gamma_dev,
                     const void *beta_dev, float eps, void *y_dev, int64_t ldy, float *mean_dev, float *rstd_dev,

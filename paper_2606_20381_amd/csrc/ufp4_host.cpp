@@ -14,6 +14,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <math.h>
+
 #include "../../include/ufp4.h"
 
 namespace {
@@ -207,6 +209,10 @@ CALL(layer_norm, 6)
     at::Tensor out;
     if (!rows_out(a[4], x, x.rows, x.cols, out, y)) return nullptr;
     const at::Tensor mean = floats(x.rows, *x.t), rstd = floats(x.rows, *x.t);
+    if (x.cols == 0) {  // 0 / 0; the library has nothing to read and writes nothing
+        mean.fill_(NAN);
+        rstd.fill_(NAN);
+    }
     if (!check(ufp4_layer_norm(x.code, x.data(), x.rows, x.cols, x.ld, wdt, g, b, (float)eps, y.data(), y.ld, mean.data_ptr<float>(),
                                rstd.data_ptr<float>(), stream), "ufp4_layer_norm"))
         return nullptr;

@@ -749,7 +749,8 @@ def mxfp4_linear(x: torch.Tensor, wq: QTensor, out_dtype=torch.bfloat16, out=Non
 
 def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, *, eps: float = 1e-5,
                out: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-    """(y, mean, rstd) of the layer norm of x's rows (ufp4_layer_norm); mean and rstd are fp32, for layer_norm_bwd."""
+    """(y, mean, rstd) of the layer norm of x's rows (ufp4_layer_norm); mean and rstd are fp32, for layer_norm_bwd
+    (NaN where x has no columns)."""
     return (_host_module or _host()).layer_norm(x, gamma, beta, eps, out, _stream())
 
 

@@ -294,3 +294,16 @@ def test_weight_gradient_of_very_long_rows():
         d, v = dy[:, s].double(), x[:, s].double()
         assert ((dgamma[s] - (d * v).sum(0)).abs() <= 4 * 2.0**-24 * (d * v).abs().sum(0)).all()
         assert torch.equal(dbeta[s], d.sum(0).float())
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 5, 300])
+def test_rows_without_columns(dt, rows):
+    """The mean and the variance of no numbers are 0 / 0; a row's statistics are never what the memory held before."""
+    for _ in range(4):  # memory that the outputs are likely to get
+        torch.full((rows,), 7.0, device="cuda")
+        y, mean, rstd = U.layer_norm(torch.empty(rows, 0, dtype=dt, device="cuda"))
+        assert y.shape == (rows, 0) and mean.shape == rstd.shape == (rows,)
+        assert torch.isnan(mean).all() and torch.isnan(rstd).all()
+    dx, dgamma, dbeta = U.layer_norm_bwd(y, y, None, mean, rstd)
+    assert dx.shape == (rows, 0) and dgamma.shape == dbeta.shape == (0,)
