@@ -579,6 +579,8 @@ CALL(mxfp4_linear, 6)
         PyErr_Format(PyExc_ValueError, "x must have %lld columns", (long long)w->red);
         return nullptr;
     }
+    // a grouped W's rows or reduction are padded: as the few-token product, the two calls below must not multiply the padding
+    if (w->layout != UFP4_LAYOUT_PLAIN) return check(UFP4_ERR_MISMATCH, "ufp4_mxfp4_linear"), nullptr;
     at::Tensor out;
     if (!product_out(a[3], *x, 0, tokens, w->rows, code, out)) return nullptr;
     if (tokens <= most && w->rht_block == 0) {

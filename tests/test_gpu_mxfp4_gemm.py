@@ -359,3 +359,18 @@ def test_weight_gradients_stored_past_the_caches(n, k, dt):
     wide = torch.full((n, k + 8), 7.0, device="cuda", dtype=dt)
     U.mxfp4_gemm_bwd_dw(a, b, dt, out=wide[:, :k])
     assert torch.equal(wide[:, :k], want) and (wide[:, k:] == 7.0).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 4, 16, 17, 40])
+def test_linear_refuses_a_grouped_weight(tokens):
+    """W as a grouped call lays it out, rows or reduction padded: refused whatever the number of tokens."""
+    x = torch.randn(tokens, 64, device="cuda").to(BF)
+    off, p128 = U.group_offsets([100, 60], block=128)
+    rows = U.mxfp4_quantize_grouped(torch.randn(160, 64, device="cuda").to(BF), off, p128, transpose=False)
+    off, p32 = U.group_offsets([20, 12], block=32)
+    red = U.mxfp4_quantize_grouped(torch.randn(32, 24, device="cuda").to(BF), off, p32, transpose=True)
+    assert rows.red == red.red == 64
+    for w in (rows, red):
+        with pytest.raises(U.UFP4Error) as e:
+            U.mxfp4_linear(x, w)
+        assert e.value.status == 4
