@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256) void micro_rows_kernel(const uint16_t* __restr
         const uint32_t e8 = pair_scale(v[p], qa, at);
         const int64_t grow = GROUPED ? src + r : row0 + r;  // the SR counters number x's rows
         uint2 c = v[p].template encode<ROUND>(at, qa, (uint32_t)(col >> 4), (uint32_t)grow);
-        if (e8 == kNaNScale) c = make_uint2(0, 0);
+        if (e8 == kNaNScale || r >= left) c = make_uint2(0, 0);  // padding: some signs rotate its zeros to -0
         *reinterpret_cast<uint2*>(s_codes + blk * kCodeStride + r * 16 + half * 8) = c;
         if (half == 0) s_scales[(blk >> 2) * 256 + (blk & 1) * 128 + r * 2 + ((blk >> 1) & 1)] = (uint8_t)e8;
     }
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(256) void micro_tile_kernel(const uint16_t* __restr
             uint32_t at;
             const uint32_t e8 = pair_scale(v[p], qr, at);
             uint2 c = v[p].template encode<ROUND>(at, qr, (uint32_t)(col >> 4), (uint32_t)(pr * 128 + r));
-            if (e8 == kNaNScale) c = make_uint2(0, 0);
+            if (e8 == kNaNScale || pr * 128 + r >= rows) c = make_uint2(0, 0);
             *reinterpret_cast<uint2*>(s_codes + blk * kTileStride + r * 16 + half * 8) = c;
             if (half == 0) s_scales[0][(blk & 1) * 256 + r * 2 + (blk >> 1)] = (uint8_t)e8;
         }
@@ -381,6 +381,11 @@ __global__ __launch_bounds__(256) void micro_tile_kernel(const uint16_t* __restr
     uint4 out[2];
     uint32_t e8c[2];
     quantize_columns<ROUND, RHT_C>(m, qc, bc, pc * 128 + 2 * lane, out, e8c);
+    if constexpr (RHT_C) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            if (pc * 128 + 2 * lane + c >= cols) out[c] = make_uint4(0, 0, 0, 0);
+    }
     if (bc < nkb_c) {
         uint4* const d = reinterpret_cast<uint4*>(o_c.codes + pc * o_c.code_pld + bc * 2048 + lane * 32);
         d[0] = out[0];

@@ -267,3 +267,36 @@ def test_large_tensor_and_back():
     got = U.mxfp4_dequantize(U.mxfp4_quantize(x))
     for a in range(0, x.shape[0], 4096):
         assert torch.equal(got[a : a + 4096], U.mxfp4_dequantize(U.mxfp4_quantize(x[a : a + 4096])))
+
+
+@pytest.mark.parametrize("rounding", [U.RTNE, U.SR])
+@pytest.mark.parametrize("form", ["rows", "transposed", "both", "groups"])
+def test_padding_of_a_rotated_operand_is_zero(form, rounding):
+    """The signs that turn the zeros of a rotated padding row into negative ones: its codes are zero all the same."""
+    kw = dict(rounding=rounding, seed=3)
+    x, mask = _tensor(160, 96, 4), 0xFFFF
+    rows, cols = (U.empty_qtensor(r, c, U.E2M1_MX32) for r, c in ((256 if form == "groups" else 160, 96), (96, 160)))
+    for q in (rows, cols):
+        q.codes.fill_(0xEE)
+        q.scales.fill_(0xEE)
+    pads = {}  # of an operand: its blocks, and where its rows are none of x's
+    if form in ("rows", "both"):
+        pads[rows] = 3, [(1, slice(32, 128))]
+    if form in ("transposed", "both"):
+        pads[cols] = 5, [(0, slice(96, 128))]
+    if form == "rows":
+        U.mxfp4_quantize(x, rht=True, sign_mask=mask, out=rows, **kw)
+    elif form == "transposed":
+        U.mxfp4_quantize(x, transpose=True, rht=True, sign_mask=mask, out=cols, **kw)
+    elif form == "both":
+        U.mxfp4_quantize_dual(x, rht_rows=True, sign_mask_rows=mask, rht_cols=True, sign_mask_cols=mask, out_rows=rows, out_cols=cols, **kw)
+    else:
+        pads[rows] = 3, [(0, slice(100, 128)), (1, slice(60, 128))]
+        off, padded = U.group_offsets([100, 60], block=128)
+        assert padded == 256
+        U.mxfp4_quantize_grouped(x, off, padded, transpose=False, rht=True, sign_mask=mask, out=rows, **kw)
+    for q, (nkb, places) in pads.items():
+        codes, scales = q.codes.view(q.panels, nkb, 128, 16), q.scales.view(q.panels, -1, 2, 128, 2)
+        for p, r in places:
+            assert not codes[p, :, r].any() and not scales[p, :, :, r].any()
+        assert codes[0, :, :60].any(-1).all()  # and x's own are there
