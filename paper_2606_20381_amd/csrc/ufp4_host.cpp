@@ -37,6 +37,27 @@ bool check(int status, const char* call) {
     return false;
 }
 
+// A status of the library and the call that gave it.
+struct Done {
+    int status;
+    const char* call;
+};
+
+// f(), which allocates and calls the library, without the interpreter's lock: a launch waits where the queue is full, an allocation where
+// memory has to be freed first, and what the GPU waits for may be another Python thread's.
+template <class F>
+bool unlocked(F&& f) {
+    Done done;
+    {
+        struct Lock {
+            PyThreadState* const state = PyEval_SaveThread();
+            ~Lock() { PyEval_RestoreThread(state); }  // also when f throws
+        } lock;
+        done = f();
+    }
+    return check(done.status, done.call);
+}
+
 bool arguments(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return true;
     PyErr_Format(PyExc_TypeError, "%zd arguments instead of %zd", have, want);
@@ -93,19 +114,22 @@ bool rows_like(PyObject* o, const char* what, const Rows& like, int64_t rows, in
     return true;
 }
 
-// The output: `o`, or a new tensor for None, which `fresh` then holds.
-bool rows_out(PyObject* o, const Rows& like, int64_t rows, int64_t cols, at::Tensor& fresh, Rows& r) {
+// The output: `o`, which `out` then holds, or for None a tensor that rows_new allocates.
+bool rows_out(PyObject* o, const Rows& like, int64_t rows, int64_t cols, at::Tensor& out, Rows& r) {
     if (o != Py_None) {
         if (!rows_like(o, "out", like, rows, cols, r)) return false;
-        fresh = *r.t;
+        out = *r.t;
         return true;
     }
-    fresh = at::empty({rows, cols}, like.t->options());
-    r.t = &fresh;
     r.rows = rows;
     r.cols = r.ld = cols;
     r.code = like.code;
     return true;
+}
+
+void rows_new(const Rows& like, at::Tensor& out, Rows& r) {
+    if (!out.defined()) out = at::empty({r.rows, r.cols}, like.t->options());
+    r.t = &out;
 }
 
 at::Tensor floats(int64_t n, const at::Tensor& like) { return at::empty({n}, like.options().dtype(at::kFloat)); }
@@ -208,13 +232,18 @@ CALL(layer_norm, 6)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (!rows_out(a[4], x, x.rows, x.cols, out, y)) return nullptr;
-    const at::Tensor mean = floats(x.rows, *x.t), rstd = floats(x.rows, *x.t);
-    if (x.cols == 0) {  // 0 / 0; the library has nothing to read and writes nothing
-        mean.fill_(NAN);
-        rstd.fill_(NAN);
-    }
-    if (!check(ufp4_layer_norm(x.code, x.data(), x.rows, x.cols, x.ld, wdt, g, b, (float)eps, y.data(), y.ld, mean.data_ptr<float>(),
-                               rstd.data_ptr<float>(), stream), "ufp4_layer_norm"))
+    at::Tensor mean, rstd;
+    if (!unlocked([&]() -> Done {
+            rows_new(x, out, y);
+            mean = floats(x.rows, *x.t);
+            rstd = floats(x.rows, *x.t);
+            if (x.cols == 0) {  // 0 / 0; the library has nothing to read and writes nothing
+                mean.fill_(NAN);
+                rstd.fill_(NAN);
+            }
+            return {ufp4_layer_norm(x.code, x.data(), x.rows, x.cols, x.ld, wdt, g, b, (float)eps, y.data(), y.ld, mean.data_ptr<float>(),
+                                    rstd.data_ptr<float>(), stream), "ufp4_layer_norm"};
+        }))
         return nullptr;
     return triple(out, mean, rstd);
 END_CALL
@@ -234,17 +263,21 @@ CALL(layer_norm_bwd, 8)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out, dgamma, dbeta, ws;
     if (!rows_out(a[6], x, x.rows, x.cols, out, dx)) return nullptr;
-    size_t need = 0;
-    if (some) {
-        if (!check(ufp4_layer_norm_bwd_workspace(x.code, x.rows, x.cols, &need), "ufp4_layer_norm_bwd_workspace")) return nullptr;
-        dgamma = floats(x.cols, *x.t);
-        dbeta = floats(x.cols, *x.t);
-        ws = floats((int64_t)(need / 4), *x.t);
-    }
-    if (!check(ufp4_layer_norm_bwd(x.code, dy.data(), dy.ld, x.data(), x.rows, x.cols, x.ld, wdt, g, static_cast<float*>(mean),
-                                   static_cast<float*>(rstd), dx.data(), dx.ld, some ? dgamma.data_ptr<float>() : nullptr,
-                                   some ? dbeta.data_ptr<float>() : nullptr, some ? ws.data_ptr() : nullptr, need, stream),
-               "ufp4_layer_norm_bwd"))
+    if (!unlocked([&]() -> Done {
+            size_t need = 0;
+            rows_new(x, out, dx);
+            if (some) {
+                const int st = ufp4_layer_norm_bwd_workspace(x.code, x.rows, x.cols, &need);
+                if (st != UFP4_OK) return {st, "ufp4_layer_norm_bwd_workspace"};
+                dgamma = floats(x.cols, *x.t);
+                dbeta = floats(x.cols, *x.t);
+                ws = floats((int64_t)(need / 4), *x.t);
+            }
+            return {ufp4_layer_norm_bwd(x.code, dy.data(), dy.ld, x.data(), x.rows, x.cols, x.ld, wdt, g, static_cast<float*>(mean),
+                                        static_cast<float*>(rstd), dx.data(), dx.ld, some ? dgamma.data_ptr<float>() : nullptr,
+                                        some ? dbeta.data_ptr<float>() : nullptr, some ? ws.data_ptr() : nullptr, need, stream),
+                    "ufp4_layer_norm_bwd"};
+        }))
         return nullptr;
     return triple(out, dgamma, dbeta);
 END_CALL
@@ -264,15 +297,20 @@ CALL(moe_sort, 3)
     const int64_t tokens = ids->size(0), k = ids->size(1);
     const int32_t k32 = k > INT32_MAX ? INT32_MAX : (int32_t)k;
     const int32_t e32 = experts > INT32_MAX ? INT32_MAX : experts < 0 ? -1 : (int32_t)experts;
-    size_t need = 0;
-    if (!check(ufp4_moe_sort_workspace(tokens, k32, e32, &need), "ufp4_moe_sort_workspace")) return nullptr;
-    const auto ints = ids->options().dtype(at::kInt);
-    const at::Tensor offsets = at::empty({experts + 1}, ids->options().dtype(at::kLong));
-    const at::Tensor rows = at::empty({tokens, k}, ints), source = at::empty({tokens * k}, ints);
-    at::Tensor ws;
-    if (need) ws = at::empty({(int64_t)(need / 4)}, ints);
-    if (!check(ufp4_moe_sort(ids->data_ptr(), st == at::kInt ? 32 : 64, tokens, k32, e32, offsets.data_ptr<int64_t>(), rows.data_ptr<int32_t>(),
-                             source.data_ptr<int32_t>(), need ? ws.data_ptr() : nullptr, need, stream), "ufp4_moe_sort"))
+    at::Tensor offsets, rows, source, ws;
+    if (!unlocked([&]() -> Done {
+            size_t need = 0;
+            const int bytes = ufp4_moe_sort_workspace(tokens, k32, e32, &need);
+            if (bytes != UFP4_OK) return {bytes, "ufp4_moe_sort_workspace"};
+            const auto ints = ids->options().dtype(at::kInt);
+            offsets = at::empty({experts + 1}, ids->options().dtype(at::kLong));
+            rows = at::empty({tokens, k}, ints);
+            source = at::empty({tokens * k}, ints);
+            if (need) ws = at::empty({(int64_t)(need / 4)}, ints);
+            return {ufp4_moe_sort(ids->data_ptr(), st == at::kInt ? 32 : 64, tokens, k32, e32, offsets.data_ptr<int64_t>(),
+                                  rows.data_ptr<int32_t>(), source.data_ptr<int32_t>(), need ? ws.data_ptr() : nullptr, need, stream),
+                    "ufp4_moe_sort"};
+        }))
         return nullptr;
     return triple(offsets, rows, source);
 END_CALL
@@ -294,9 +332,12 @@ CALL(moe_dispatch, 6)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (!rows_out(a[4], x, s.tokens * s.k, x.cols, out, y)) return nullptr;
-    if (!check(ufp4_moe_dispatch(x.code, x.data(), x.rows, x.cols, x.ld, static_cast<int32_t*>(s.rows), (int32_t)s.k,
-                                 static_cast<int64_t*>(offsets), (int32_t)experts, static_cast<float*>(s.w), y.data(), y.rows, y.ld, stream),
-               "ufp4_moe_dispatch"))
+    if (!unlocked([&]() -> Done {
+            rows_new(x, out, y);
+            return {ufp4_moe_dispatch(x.code, x.data(), x.rows, x.cols, x.ld, static_cast<int32_t*>(s.rows), (int32_t)s.k,
+                                      static_cast<int64_t*>(offsets), (int32_t)experts, static_cast<float*>(s.w), y.data(), y.rows, y.ld,
+                                      stream), "ufp4_moe_dispatch"};
+        }))
         return nullptr;
     return THPVariable_Wrap(out);
 END_CALL
@@ -311,8 +352,11 @@ CALL(moe_combine, 5)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (!rows_out(a[3], y, s.tokens, y.cols, out, o)) return nullptr;
-    if (!check(ufp4_moe_combine(y.code, y.data(), y.rows, y.cols, y.ld, static_cast<int32_t*>(s.rows), s.tokens, (int32_t)s.k,
-                                static_cast<float*>(s.w), o.data(), o.ld, stream), "ufp4_moe_combine"))
+    if (!unlocked([&]() -> Done {
+            rows_new(y, out, o);
+            return {ufp4_moe_combine(y.code, y.data(), y.rows, y.cols, y.ld, static_cast<int32_t*>(s.rows), s.tokens, (int32_t)s.k,
+                                     static_cast<float*>(s.w), o.data(), o.ld, stream), "ufp4_moe_combine"};
+        }))
         return nullptr;
     return THPVariable_Wrap(out);
 END_CALL
@@ -331,10 +375,14 @@ CALL(moe_combine_bwd, 7)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (!rows_out(a[5], y, y.rows, y.cols, out, dy)) return nullptr;
-    const at::Tensor dw = at::empty({s.tokens, s.k}, y.t->options().dtype(at::kFloat));
-    if (!check(ufp4_moe_combine_bwd(y.code, dout.data(), s.tokens, y.cols, dout.ld, y.data(), y.rows, y.ld, static_cast<int32_t*>(s.rows),
-                                    (int32_t)s.k, static_cast<int64_t*>(offsets), (int32_t)experts, static_cast<float*>(s.w), dy.data(), dy.ld,
-                                    dw.data_ptr<float>(), stream), "ufp4_moe_combine_bwd"))
+    at::Tensor dw;
+    if (!unlocked([&]() -> Done {
+            rows_new(y, out, dy);
+            dw = at::empty({s.tokens, s.k}, y.t->options().dtype(at::kFloat));
+            return {ufp4_moe_combine_bwd(y.code, dout.data(), s.tokens, y.cols, dout.ld, y.data(), y.rows, y.ld, static_cast<int32_t*>(s.rows),
+                                         (int32_t)s.k, static_cast<int64_t*>(offsets), (int32_t)experts, static_cast<float*>(s.w), dy.data(),
+                                         dy.ld, dw.data_ptr<float>(), stream), "ufp4_moe_combine_bwd"};
+        }))
         return nullptr;
     return pair(out, THPVariable_Wrap(dw));
 END_CALL
@@ -354,9 +402,10 @@ ufp4_qtensor* operand_of(PyObject* o) {  // the address of a descriptor
 }
 
 // Buffers for a microscaled operand [rows, red], which `d` describes from then on.
-bool new_operand(const at::Tensor& like, int64_t rows, int64_t red, ufp4_qtensor& d, at::Tensor& codes, at::Tensor& scales) {
+Done new_operand(const at::Tensor& like, int64_t rows, int64_t red, ufp4_qtensor& d, at::Tensor& codes, at::Tensor& scales) {
     int64_t panels = 0, cld = 0, sld = 0;
-    if (!check(ufp4_qtensor_bytes(UFP4_FMT_E2M1_MX32, rows, red, &panels, &cld, &sld, nullptr, nullptr), "ufp4_qtensor_bytes")) return false;
+    const Done done{ufp4_qtensor_bytes(UFP4_FMT_E2M1_MX32, rows, red, &panels, &cld, &sld, nullptr, nullptr), "ufp4_qtensor_bytes"};
+    if (done.status != UFP4_OK) return done;
     const auto bytes = like.options().dtype(at::kByte);
     codes = at::empty({panels, cld}, bytes);
     scales = at::empty({panels, sld}, bytes);
@@ -369,22 +418,23 @@ bool new_operand(const at::Tensor& like, int64_t rows, int64_t red, ufp4_qtensor
     d.rows = rows;
     d.red = red;
     d.format = UFP4_FMT_E2M1_MX32;
-    return true;
+    return done;
 }
 
-// The output of a product, row-major float32 or bfloat16 [rows, cols] or, of groups > 0 matrices rows apart, [groups, rows, cols]: `o`,
-// or a new tensor of type `code` for None.
-bool product_out(PyObject* o, const at::Tensor& like, int64_t groups, int64_t rows, int64_t cols, int code, at::Tensor& out) {
-    const int64_t size[3] = {groups, rows, cols};
-    const at::IntArrayRef shape(size + (groups ? 0 : 1), groups ? 3 : 2);
-    if (o == Py_None) {
-        if (code < 0) return refuse("out_dtype", "float32 or bfloat16");
-        out = at::empty(shape, like.options().dtype(code == UFP4_OUT_BF16 ? at::kBFloat16 : at::kFloat));
-        return true;
-    }
+// The shape of a product's output: [rows, cols] or, of groups > 0 matrices, [groups, rows, cols].
+struct Shape {
+    int64_t size[3];  // groups, 0 for the former
+    at::IntArrayRef sizes() const { return {size + (size[0] ? 0 : 1), size_t(size[0] ? 3 : 2)}; }
+};
+
+// The output of a product, row-major float32 or bfloat16, matrices rows apart: `o`, which `out` then holds, or for None a tensor of type
+// `code` that product_new allocates.
+bool product_out(PyObject* o, const at::Tensor& like, const Shape& s, int code, at::Tensor& out) {
+    const int64_t groups = s.size[0], rows = s.size[1], cols = s.size[2];
+    if (o == Py_None) return code >= 0 || refuse("out_dtype", "float32 or bfloat16");
     const at::Tensor* const t = tensor(o, "out");
     if (!t) return false;
-    if (t->sizes() != shape || t->stride(-1) != 1 || t->device() != like.device()) {
+    if (t->sizes() != s.sizes() || t->stride(-1) != 1 || t->device() != like.device()) {
         if (groups)
             PyErr_Format(PyExc_ValueError, "out must be a row-major tensor of shape (%lld, %lld, %lld) on the input's device", (long long)groups,
                          (long long)rows, (long long)cols);
@@ -397,6 +447,10 @@ bool product_out(PyObject* o, const at::Tensor& like, int64_t groups, int64_t ro
     if (code_of(*t) < 0) return refuse("out", "float32 or bfloat16");
     out = *t;
     return true;
+}
+
+void product_new(const at::Tensor& like, const Shape& s, int code, at::Tensor& out) {
+    if (!out.defined()) out = at::empty(s.sizes(), like.options().dtype(code == UFP4_OUT_BF16 ? at::kBFloat16 : at::kFloat));
 }
 
 // (x, transpose, rht, sign_mask, rounding, seed, stream_id, descriptor, fresh, stream) -> (codes, scales) of a fresh descriptor, or None
@@ -412,9 +466,14 @@ CALL(mxfp4_quantize, 10)
     if (PyErr_Occurred()) return nullptr;
     const int64_t rows = x->size(0), cols = x->size(1);
     at::Tensor codes, scales;
-    if (fresh && !new_operand(*x, transpose ? cols : rows, transpose ? rows : cols, *d, codes, scales)) return nullptr;
-    if (!check(ufp4_mxfp4_quantize(x->data_ptr(), rows, cols, x->stride(0), transpose, rht, mask, rounding, seed, id, d, stream),
-               "ufp4_mxfp4_quantize"))
+    if (!unlocked([&]() -> Done {
+            if (fresh) {
+                const Done made = new_operand(*x, transpose ? cols : rows, transpose ? rows : cols, *d, codes, scales);
+                if (made.status != UFP4_OK) return made;
+            }
+            return {ufp4_mxfp4_quantize(x->data_ptr(), rows, cols, x->stride(0), transpose, rht, mask, rounding, seed, id, d, stream),
+                    "ufp4_mxfp4_quantize"};
+        }))
         return nullptr;
     if (!fresh) Py_RETURN_NONE;
     return pair(codes, THPVariable_Wrap(scales));
@@ -435,9 +494,14 @@ CALL(mxfp4_quantize_dual, 14)
     if (PyErr_Occurred()) return nullptr;
     const int64_t rows = x->size(0), cols = x->size(1);
     at::Tensor codes_r, scales_r, codes_c, scales_c;
-    if ((fresh_r && !new_operand(*x, rows, cols, *r, codes_r, scales_r)) || (fresh_c && !new_operand(*x, cols, rows, *c, codes_c, scales_c)) ||
-        !check(ufp4_mxfp4_quantize_dual(x->data_ptr(), rows, cols, x->stride(0), rht_r, mask_r, id_r, rht_c, mask_c, id_c, rounding, seed, r, c,
-                                        stream), "ufp4_mxfp4_quantize_dual"))
+    if (!unlocked([&]() -> Done {
+            Done made{UFP4_OK, nullptr};
+            if (fresh_r) made = new_operand(*x, rows, cols, *r, codes_r, scales_r);
+            if (made.status == UFP4_OK && fresh_c) made = new_operand(*x, cols, rows, *c, codes_c, scales_c);
+            if (made.status != UFP4_OK) return made;
+            return {ufp4_mxfp4_quantize_dual(x->data_ptr(), rows, cols, x->stride(0), rht_r, mask_r, id_r, rht_c, mask_c, id_c, rounding, seed,
+                                             r, c, stream), "ufp4_mxfp4_quantize_dual"};
+        }))
         return nullptr;
     PyObject* const t[4] = {THPVariable_Wrap(codes_r), THPVariable_Wrap(scales_r), THPVariable_Wrap(codes_c), THPVariable_Wrap(scales_c)};
     PyObject* const all = t[0] && t[1] && t[2] && t[3] ? PyTuple_Pack(4, t[0], t[1], t[2], t[3]) : nullptr;
@@ -462,9 +526,15 @@ CALL(mxfp4_quantize_grouped, 12)
     if (PyErr_Occurred()) return nullptr;
     const int64_t rows = x->size(0), cols = x->size(1);
     at::Tensor codes, scales;
-    if (fresh && !new_operand(*x, transpose ? cols : padded, transpose ? padded : cols, *d, codes, scales)) return nullptr;
-    if (!check(ufp4_mxfp4_quantize_grouped(x->data_ptr(), rows, cols, x->stride(0), transpose, static_cast<int64_t*>(offsets), (int32_t)groups,
-                                           padded, rht, mask, rounding, seed, id, d, stream), "ufp4_mxfp4_quantize_grouped"))
+    if (!unlocked([&]() -> Done {
+            if (fresh) {
+                const Done made = new_operand(*x, transpose ? cols : padded, transpose ? padded : cols, *d, codes, scales);
+                if (made.status != UFP4_OK) return made;
+            }
+            return {ufp4_mxfp4_quantize_grouped(x->data_ptr(), rows, cols, x->stride(0), transpose, static_cast<int64_t*>(offsets),
+                                                (int32_t)groups, padded, rht, mask, rounding, seed, id, d, stream),
+                    "ufp4_mxfp4_quantize_grouped"};
+        }))
         return nullptr;
     if (!fresh) Py_RETURN_NONE;
     return pair(codes, THPVariable_Wrap(scales));
@@ -477,9 +547,7 @@ CALL(mxfp4_dequantize, 4)
     void* const stream = pointer(a[3]);
     if (!codes || PyErr_Occurred()) return nullptr;
     at::Tensor out;
-    if (a[2] == Py_None) {
-        out = at::empty({d->rows, d->red}, codes->options().dtype(at::kBFloat16));
-    } else {
+    if (a[2] != Py_None) {
         const at::Tensor* const t = tensor(a[2], "out");
         if (!t) return nullptr;
         if (t->scalar_type() != at::kBFloat16 || t->dim() != 2 || t->size(0) != d->rows || t->size(1) != d->red ||
@@ -490,7 +558,11 @@ CALL(mxfp4_dequantize, 4)
         }
         out = *t;
     }
-    if (!check(ufp4_mxfp4_dequantize(d, out.data_ptr(), out.stride(0), stream), "ufp4_mxfp4_dequantize")) return nullptr;
+    if (!unlocked([&]() -> Done {
+            if (!out.defined()) out = at::empty({d->rows, d->red}, codes->options().dtype(at::kBFloat16));
+            return {ufp4_mxfp4_dequantize(d, out.data_ptr(), out.stride(0), stream), "ufp4_mxfp4_dequantize"};
+        }))
+        return nullptr;
     return THPVariable_Wrap(out);
 END_CALL
 
@@ -505,8 +577,13 @@ PyObject* product(const char* name, PyObject* const* a, Py_ssize_t n_args) {
     void* const stream = pointer(a[5]);
     if (!codes || PyErr_Occurred()) return nullptr;
     at::Tensor out;
-    if (!product_out(a[4], *codes, 0, x->rows, w->rows, code, out)) return nullptr;
-    if (!check(GEMM(x, w, out.data_ptr(), out.stride(0), code_of(out), stream), name)) return nullptr;
+    const Shape shape{{0, x->rows, w->rows}};
+    if (!product_out(a[4], *codes, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*codes, shape, code, out);
+            return {GEMM(x, w, out.data_ptr(), out.stride(0), code_of(out), stream), name};
+        }))
+        return nullptr;
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -533,8 +610,12 @@ PyObject* product_rows(const char* name, PyObject* const* a, Py_ssize_t n_args) 
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (groups < 1) return refuse("offsets", "of one group at least"), nullptr;
-    if (!product_out(a[6], *codes, 0, rows, BY_GROUP ? w->rows / groups : w->rows, code, out)) return nullptr;
-    if (!check(GEMM(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, rows, out.data_ptr(), out.stride(0), code_of(out), stream), name))
+    const Shape shape{{0, rows, BY_GROUP ? w->rows / groups : w->rows}};
+    if (!product_out(a[6], *codes, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*codes, shape, code, out);
+            return {GEMM(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, rows, out.data_ptr(), out.stride(0), code_of(out), stream), name};
+        }))
         return nullptr;
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
@@ -558,9 +639,13 @@ CALL(mxfp4_gemm_bwd_dw_grouped, 7)
     if (PyErr_Occurred()) return nullptr;
     at::Tensor out;
     if (groups < 1) return refuse("offsets", "of one group at least"), nullptr;
-    if (!product_out(a[5], *codes, groups, x->rows, w->rows, code, out)) return nullptr;
-    if (!check(ufp4_mxfp4_gemm_bwd_dw_grouped(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, out.data_ptr(), out.stride(1), code_of(out),
-                                              stream), "ufp4_mxfp4_gemm_bwd_dw_grouped"))
+    const Shape shape{{groups, x->rows, w->rows}};
+    if (!product_out(a[5], *codes, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*codes, shape, code, out);
+            return {ufp4_mxfp4_gemm_bwd_dw_grouped(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, out.data_ptr(), out.stride(1),
+                                                   code_of(out), stream), "ufp4_mxfp4_gemm_bwd_dw_grouped"};
+        }))
         return nullptr;
     return THPVariable_Wrap(out);
 END_CALL
@@ -581,20 +666,23 @@ CALL(mxfp4_linear, 6)
     }
     // a grouped W's rows or reduction are padded: as the few-token product, the two calls below must not multiply the padding
     if (w->layout != UFP4_LAYOUT_PLAIN) return check(UFP4_ERR_MISMATCH, "ufp4_mxfp4_linear"), nullptr;
+    const Shape shape{{0, tokens, w->rows}};
     at::Tensor out;
-    if (!product_out(a[3], *x, 0, tokens, w->rows, code, out)) return nullptr;
-    if (tokens <= most && w->rht_block == 0) {
-        if (!check(ufp4_mxfp4_linear(x->data_ptr(), tokens, x->stride(0), w, out.data_ptr(), out.stride(0), code_of(out), stream),
-                   "ufp4_mxfp4_linear"))
-            return nullptr;
-        return THPVariable_Wrap(out);
-    }
-    ufp4_qtensor d;  // x as W was rotated
-    at::Tensor codes, scales;
-    if (!new_operand(*x, tokens, red, d, codes, scales) ||
-        !check(ufp4_mxfp4_quantize(x->data_ptr(), tokens, red, x->stride(0), 0, w->rht_block != 0, w->rht_block ? w->sign_words[0] : 0,
-                                   UFP4_ROUND_RTNE, 0, 0, &d, stream), "ufp4_mxfp4_quantize") ||
-        !check(ufp4_mxfp4_gemm_fwd_y(&d, w, out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_mxfp4_gemm_fwd_y"))
+    if (!product_out(a[3], *x, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*x, shape, code, out);
+            if (tokens <= most && w->rht_block == 0)
+                return {ufp4_mxfp4_linear(x->data_ptr(), tokens, x->stride(0), w, out.data_ptr(), out.stride(0), code_of(out), stream),
+                        "ufp4_mxfp4_linear"};
+            ufp4_qtensor d;  // x as W was rotated
+            at::Tensor codes, scales;
+            Done done = new_operand(*x, tokens, red, d, codes, scales);
+            if (done.status != UFP4_OK) return done;
+            done = {ufp4_mxfp4_quantize(x->data_ptr(), tokens, red, x->stride(0), 0, w->rht_block != 0, w->rht_block ? w->sign_words[0] : 0,
+                                        UFP4_ROUND_RTNE, 0, 0, &d, stream), "ufp4_mxfp4_quantize"};
+            if (done.status != UFP4_OK) return done;
+            return {ufp4_mxfp4_gemm_fwd_y(&d, w, out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_mxfp4_gemm_fwd_y"};
+        }))
         return nullptr;
     return THPVariable_Wrap(out);
 END_CALL

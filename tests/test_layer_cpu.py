@@ -4,6 +4,8 @@ oracle's microscaled 4-bit quantizer against exact arithmetic."""
 
 import ctypes
 import os
+import shutil
+import subprocess
 import sys
 from fractions import Fraction
 
@@ -387,3 +389,46 @@ def test_host_module_refuses_grouped_calls_before_the_library(lib):
         dw(off)
     with pytest.raises(RuntimeError):
         y(off, rows=-1)
+
+
+STAND_IN = """
+int PyGILState_Check(void);
+static int calls, held;
+static int called(void) { ++calls; held += PyGILState_Check(); return 0; }
+int call_count(void) { return calls; }
+int held_count(void) { return held; }
+"""
+STAND_IN_RUN = """
+import ctypes, sys
+import torch
+sys.path.insert(0, sys.argv[2])
+s = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)  # found before the library
+from paper_2606_20381_amd import _host as h, ufp4 as U
+codes, off = torch.zeros(1, 2048, dtype=torch.uint8), torch.zeros(3, dtype=torch.int64)
+d = U.QDesc(codes=1 << 20, scales=1 << 20, code_panel_ld=2048, scale_panel_ld=512, panels=1, rows=2, red=32, format=U.E2M1_MX32)
+a = ctypes.addressof(d)
+for out in (None, torch.zeros(2, 2)):
+    for f in (h.mxfp4_gemm_fwd_y, h.mxfp4_gemm_bwd_dx, h.mxfp4_gemm_bwd_dw):
+        assert f(codes, a, a, U.OUT_F32, out, 0).shape == (2, 2)
+h.mxfp4_dequantize(codes, a, None, 0)
+h.mxfp4_gemm_fwd_y_grouped(codes, a, a, off, 7, U.OUT_BF16, None, 0)
+h.mxfp4_gemm_bwd_dx_grouped(codes, a, a, off, 7, U.OUT_BF16, None, 0)
+h.mxfp4_gemm_bwd_dw_grouped(codes, a, a, off, U.OUT_F32, None, 0)
+print("calls", s.call_count(), "held", s.held_count())
+"""
+
+
+def test_host_module_calls_the_library_without_the_interpreter_lock(lib, tmp_path):
+    """A launch can wait (a full queue, work that another Python thread has still to issue), so other threads run meanwhile. The library's
+    functions are replaced by ones that note whether the caller holds the lock."""
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if not cc:
+        pytest.skip("no C compiler")
+    names = ["ufp4_mxfp4_dequantize"] + [f"ufp4_mxfp4_gemm_{p}{g}" for p in ("fwd_y", "bwd_dx", "bwd_dw") for g in ("", "_grouped")]
+    src, so = tmp_path / "standin.c", tmp_path / "standin.so"
+    src.write_text(STAND_IN + "".join(f"int {n}() {{ return called(); }}\n" for n in names))
+    subprocess.run([cc, "-shared", "-fPIC", "-o", str(so), str(src)], check=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", STAND_IN_RUN, str(so), root], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert r.stdout.split() == ["calls", "10", "held", "0"]
