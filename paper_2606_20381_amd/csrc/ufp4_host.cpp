@@ -687,6 +687,20 @@ CALL(mxfp4_linear, 6)
     return THPVariable_Wrap(out);
 END_CALL
 
+// (x or codes, codes): refuses two that are not on one GPU. A descriptor holds addresses, which the calls above cannot tell apart, so the
+// binding asks this of an operand's tensor first.
+CALL(on_one_gpu, 2)
+    const at::Tensor* const x = tensor(a[0], "x");
+    const at::Tensor* const codes = x ? tensor(a[1], "the operand's codes") : nullptr;
+    if (!codes) return nullptr;
+    if (!codes->is_cuda() || x->device() != codes->device()) {
+        PyErr_Format(PyExc_ValueError, "the operand (%s) and the tensor or operand beside it (%s) must be on one CUDA device",
+                     codes->device().str().c_str(), x->device().str().c_str());
+        return nullptr;
+    }
+    Py_RETURN_NONE;
+END_CALL
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XDECREF(g_error);
@@ -700,7 +714,7 @@ PyMethodDef kMethods[] = {METHOD(layer_norm),   METHOD(layer_norm_bwd), METHOD(m
                           METHOD(mxfp4_quantize), METHOD(mxfp4_dequantize), METHOD(mxfp4_gemm_fwd_y),
                           METHOD(mxfp4_gemm_bwd_dx), METHOD(mxfp4_gemm_bwd_dw), METHOD(mxfp4_linear),
                           METHOD(mxfp4_quantize_dual), METHOD(mxfp4_quantize_grouped), METHOD(mxfp4_gemm_fwd_y_grouped),
-                          METHOD(mxfp4_gemm_bwd_dx_grouped), METHOD(mxfp4_gemm_bwd_dw_grouped),
+                          METHOD(mxfp4_gemm_bwd_dx_grouped), METHOD(mxfp4_gemm_bwd_dw_grouped), METHOD(on_one_gpu),
                           {"set_error", set_error, METH_O, nullptr},    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", "Host side of the short calls of ufp4.py", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

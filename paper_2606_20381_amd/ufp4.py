@@ -656,6 +656,7 @@ def mxfp4_quantize(x: torch.Tensor, *, transpose: bool = False, rht: bool = Fals
     """Microscaled 4-bit quantization, after an optional block-16 RHT (ufp4_mxfp4_quantize)."""
     h = _host_module or _host()
     if out is not None:
+        h.on_one_gpu(x, out.codes)
         h.mxfp4_quantize(x, transpose, rht, sign_mask, rounding, seed, stream_id, _addressof(out.desc), False, _stream())
         return out
     desc = QDesc()
@@ -669,9 +670,13 @@ def mxfp4_quantize_dual(x: torch.Tensor, *, rht_rows: bool = False, rht_cols: bo
                         out_cols: QTensor | None = None) -> tuple[QTensor, QTensor]:
     """Both microscaled operands of x [rows, cols] (ufp4_mxfp4_quantize_dual): (Q_r [rows, cols] along cols, Q_c [cols, rows]
     along rows)."""
+    h = _host_module or _host()
+    for q in (out_rows, out_cols):
+        if q is not None:
+            h.on_one_gpu(x, q.codes)
     dr = out_rows.desc if out_rows is not None else QDesc()
     dc = out_cols.desc if out_cols is not None else QDesc()
-    cr, sr, cc, sc = (_host_module or _host()).mxfp4_quantize_dual(
+    cr, sr, cc, sc = h.mxfp4_quantize_dual(
         x, rht_rows, rht_cols, sign_mask_rows, sign_mask_cols, rounding, seed, stream_rows, stream_cols, _addressof(dr), out_rows is None,
         _addressof(dc), out_cols is None, _stream())
     return (out_rows if out_rows is not None else QTensor(cr, sr, dr)), (out_cols if out_cols is not None else QTensor(cc, sc, dc))
@@ -684,6 +689,7 @@ def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total:
     transpose False, 32 for True)."""
     h = _host_module or _host()
     if out is not None:
+        h.on_one_gpu(x, out.codes)
         h.mxfp4_quantize_grouped(x, offsets, padded_total, transpose, rht, sign_mask, rounding, seed, stream_id, _addressof(out.desc), False,
                                  _stream())
         return out
@@ -695,43 +701,57 @@ def mxfp4_quantize_grouped(x: torch.Tensor, offsets: torch.Tensor, padded_total:
 
 def mxfp4_dequantize(q: QTensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """The operand's values as bf16 [rows, red] (ufp4_mxfp4_dequantize), exact."""
-    return (_host_module or _host()).mxfp4_dequantize(q.codes, _addressof(q.desc), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(q.codes, q.scales)
+    return h.mxfp4_dequantize(q.codes, _addressof(q.desc), out, _stream())
 
 
 def mxfp4_gemm_fwd_y(xq: QTensor, wq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """Y [M, N] = Q(X) Q(W)^T on microscaled operands (ufp4_mxfp4_gemm_fwd_y)."""
-    return (_host_module or _host()).mxfp4_gemm_fwd_y(xq.codes, _addressof(xq.desc), _addressof(wq.desc), _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(xq.codes, wq.codes)
+    return h.mxfp4_gemm_fwd_y(xq.codes, _addressof(xq.desc), _addressof(wq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dx(dyq: QTensor, wtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """dX [M, K] = Q(dY) Q(W^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dx)."""
-    return (_host_module or _host()).mxfp4_gemm_bwd_dx(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(dyq.codes, wtq.codes)
+    return h.mxfp4_gemm_bwd_dx(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dw(dytq: QTensor, xtq: QTensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
     """dW [N, K] = Q(dY^T) Q(X^T)^T on microscaled operands (ufp4_mxfp4_gemm_bwd_dw)."""
-    return (_host_module or _host()).mxfp4_gemm_bwd_dw(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(dytq.codes, xtq.codes)
+    return h.mxfp4_gemm_bwd_dw(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_fwd_y_grouped(xq: QTensor, wq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
                              out=None) -> torch.Tensor:
     """Y [m_total, N] per group from the grouped-rows X and W [G*N, K] (ufp4_mxfp4_gemm_fwd_y_grouped)."""
-    return (_host_module or _host()).mxfp4_gemm_fwd_y_grouped(xq.codes, _addressof(xq.desc), _addressof(wq.desc), offsets, m_total,
-                                                              _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(xq.codes, wq.codes)
+    return h.mxfp4_gemm_fwd_y_grouped(xq.codes, _addressof(xq.desc), _addressof(wq.desc), offsets, m_total,
+                                      _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dx_grouped(dyq: QTensor, wtq: QTensor, offsets: torch.Tensor, m_total: int, out_dtype=torch.float32,
                               out=None) -> torch.Tensor:
     """dX [m_total, K] per group from the grouped-rows dY and W^T [K, G*N] (ufp4_mxfp4_gemm_bwd_dx_grouped)."""
-    return (_host_module or _host()).mxfp4_gemm_bwd_dx_grouped(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), offsets, m_total,
-                                                               _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(dyq.codes, wtq.codes)
+    return h.mxfp4_gemm_bwd_dx_grouped(dyq.codes, _addressof(dyq.desc), _addressof(wtq.desc), offsets, m_total,
+                                       _code_of(out_dtype), out, _stream())
 
 
 def mxfp4_gemm_bwd_dw_grouped(dytq: QTensor, xtq: QTensor, offsets: torch.Tensor, out_dtype=torch.float32,
                               out=None) -> torch.Tensor:
     """dW [G, N, K] from the grouped-reduction dY^T and X^T (ufp4_mxfp4_gemm_bwd_dw_grouped)."""
-    return (_host_module or _host()).mxfp4_gemm_bwd_dw_grouped(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), offsets,
-                                                               _code_of(out_dtype), out, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(dytq.codes, xtq.codes)
+    return h.mxfp4_gemm_bwd_dw_grouped(dytq.codes, _addressof(dytq.desc), _addressof(xtq.desc), offsets,
+                                       _code_of(out_dtype), out, _stream())
 
 
 LINEAR_TOKENS = 16  # tokens up to which ufp4_mxfp4_linear takes a product
@@ -740,7 +760,9 @@ LINEAR_TOKENS = 16  # tokens up to which ufp4_mxfp4_linear takes a product
 def mxfp4_linear(x: torch.Tensor, wq: QTensor, out_dtype=torch.bfloat16, out=None) -> torch.Tensor:
     """Y [tokens, N] = Q(x) W^T with bf16 x and W kept microscaled: a decode step's few tokens in one launch
     (ufp4_mxfp4_linear), more (or a rotated W) by quantizing x and one GEMM."""
-    return (_host_module or _host()).mxfp4_linear(x, _addressof(wq.desc), _code_of(out_dtype), out, LINEAR_TOKENS, _stream())
+    h = _host_module or _host()
+    h.on_one_gpu(x, wq.codes)
+    return h.mxfp4_linear(x, _addressof(wq.desc), _code_of(out_dtype), out, LINEAR_TOKENS, _stream())
 
 
 # ---------------------------------------------------------------------------------------------------

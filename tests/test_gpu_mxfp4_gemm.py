@@ -374,3 +374,23 @@ def test_linear_refuses_a_grouped_weight(tokens):
         with pytest.raises(U.UFP4Error) as e:
             U.mxfp4_linear(x, w)
         assert e.value.status == 4
+
+
+def test_operands_of_another_device_are_refused():
+    """One operand on the GPU, the one beside it in host memory."""
+    a, x, off = _operand(32, 32, 1), torch.randn(32, 32, device="cuda").to(BF), torch.tensor([0, 32], device="cuda")
+    b = U.empty_qtensor(32, 32, U.E2M1_MX32, device="cpu")
+    for p, q in ((a, b), (b, a)):
+        for f in (U.mxfp4_gemm_fwd_y, U.mxfp4_gemm_bwd_dx, U.mxfp4_gemm_bwd_dw):
+            with pytest.raises(ValueError):
+                f(p, q)
+        for f in (U.mxfp4_gemm_fwd_y_grouped, U.mxfp4_gemm_bwd_dx_grouped):
+            with pytest.raises(ValueError):
+                f(p, q, off, 32)
+        with pytest.raises(ValueError):
+            U.mxfp4_gemm_bwd_dw_grouped(p, q, off)
+    for call in (lambda: U.mxfp4_linear(x, b), lambda: U.mxfp4_linear(x.cpu(), a), lambda: U.mxfp4_quantize(x, out=b),
+                 lambda: U.mxfp4_quantize_dual(x, out_rows=b), lambda: U.mxfp4_quantize_dual(x, out_rows=a, out_cols=b),
+                 lambda: U.mxfp4_quantize_grouped(x, off, 32, transpose=True, out=b), lambda: U.mxfp4_dequantize(b)):
+        with pytest.raises(ValueError):
+            call()

@@ -432,3 +432,20 @@ def test_host_module_calls_the_library_without_the_interpreter_lock(lib, tmp_pat
     r = subprocess.run([sys.executable, "-c", STAND_IN_RUN, str(so), root], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     assert r.stdout.split() == ["calls", "10", "held", "0"]
+
+
+def test_operands_off_the_gpu_are_refused(lib):
+    """A descriptor holds addresses only: operands in host memory are refused before a kernel could read them."""
+    q, x = U.empty_qtensor(32, 32, U.E2M1_MX32, device="cpu"), torch.zeros(32, 32, dtype=torch.bfloat16)
+    off = torch.zeros(2, dtype=torch.int64)
+    calls = [lambda f=f: f(q, q) for f in (U.mxfp4_gemm_fwd_y, U.mxfp4_gemm_bwd_dx, U.mxfp4_gemm_bwd_dw)]
+    calls += [lambda f=f: f(q, q, off, 32) for f in (U.mxfp4_gemm_fwd_y_grouped, U.mxfp4_gemm_bwd_dx_grouped)]
+    calls += [lambda: U.mxfp4_gemm_bwd_dw_grouped(q, q, off), lambda: U.mxfp4_dequantize(q), lambda: U.mxfp4_linear(x, q),
+              lambda: U.mxfp4_quantize(x, out=q), lambda: U.mxfp4_quantize_dual(x, out_rows=q), lambda: U.mxfp4_quantize_dual(x, out_cols=q),
+              lambda: U.mxfp4_quantize_grouped(x, off, 32, transpose=True, out=q)]
+    for call in calls:
+        with pytest.raises(ValueError, match="CUDA device"):
+            call()
+    for call in (lambda: U.mxfp4_linear(3, q), lambda: U.mxfp4_quantize(3, out=q)):
+        with pytest.raises(TypeError, match="tensor"):
+            call()
