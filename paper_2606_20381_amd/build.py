@@ -62,9 +62,12 @@ def _run(cmd, verbose):
     return r
 
 
-def _host_object(cc: str) -> tuple[list, str, str]:
-    """(command that compiles the host module, its object file, torch's library folder)."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+def _host_object(cc: str) -> tuple[list, str, str] | None:
+    """(command that compiles the host module, its object file, torch's library folder), None where there is no torch."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    torch = os.path.dirname(spec.origin)
     inc = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include")]
     obj = os.path.join(BUILD, "ufp4_host.o")
     return ([cc, "-x", "c++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{INCLUDE}",
@@ -73,7 +76,8 @@ def _host_object(cc: str) -> tuple[list, str, str]:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source and link the shared library and the host module; always rebuilds. Returns the library path."""
+    """Compile every source and link the shared library and the host module; always rebuilds. Returns the library path. The library needs
+    no torch: without one (or where the host module does not compile, which raises) it is built all the same."""
     os.makedirs(BUILD, exist_ok=True)
     cc = hipcc()
     objs = []
@@ -84,13 +88,18 @@ def build(verbose: bool = False) -> str:
         form = [] if src in AGPR_SOURCES else VGPR_FORM
         cmds.append([cc, *FLAGS, *form, f"-I{INCLUDE}", *lang, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    host_cmd, host_obj, torch_lib = _host_object(cc)
-    cmds.append(host_cmd)
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
+    host = _host_object(cc)
+    with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
+        host_done = ex.submit(_run, host[0], verbose) if host else None
         list(ex.map(lambda c: _run(c, verbose), cmds))
     tmp = LIB + ".tmp"
     _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB)
+    if host is None:
+        print("no torch: the binding's host module is not built", file=sys.stderr)
+        return LIB
+    host_done.result()
+    _, host_obj, torch_lib = host
     tmp = HOST + ".tmp"  # torch's libraries are loaded by the time the module is
     _run([cc, "-shared", "-fPIC", "-o", tmp, host_obj, f"-L{PKG}", "-l:libufp4.so", "-Wl,-rpath,$ORIGIN", f"-L{torch_lib}",
           "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)

@@ -449,3 +449,32 @@ def test_operands_off_the_gpu_are_refused(lib):
     for call in (lambda: U.mxfp4_linear(3, q), lambda: U.mxfp4_quantize(3, out=q)):
         with pytest.raises(TypeError, match="tensor"):
             call()
+
+
+# ------------------------------------------------------------------------------------------------
+# the build
+# ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("torch_is", ["there", "missing", "of another kind"])
+def test_the_library_is_built_without_the_host_module(monkeypatch, tmp_path, torch_is):
+    """The C interface needs no torch: a missing one, or headers that the host module does not compile with, leave a library."""
+    from paper_2606_20381_amd import build as B
+
+    for name, path in (("LIB", "lib.so"), ("HOST", "host.so"), ("BUILD", "objects")):
+        monkeypatch.setattr(B, name, str(tmp_path / path))
+    find = B.importlib.util.find_spec
+    if torch_is == "missing":
+        monkeypatch.setattr(B.importlib.util, "find_spec", lambda name: None if name == "torch" else find(name))
+
+    def run(cmd, verbose):
+        if torch_is == "of another kind" and any(a.endswith("ufp4_host.cpp") for a in cmd):
+            raise RuntimeError("host module")
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    monkeypatch.setattr(B, "_run", run)
+    if torch_is == "of another kind":
+        with pytest.raises(RuntimeError, match="host module"):
+            B.build()
+    else:
+        assert B.build() == B.LIB
+    assert os.path.exists(B.LIB) and os.path.exists(B.HOST) == (torch_is == "there")
