@@ -394,3 +394,46 @@ def test_operands_of_another_device_are_refused():
                  lambda: U.mxfp4_quantize_grouped(x, off, 32, transpose=True, out=b), lambda: U.mxfp4_dequantize(b)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("counts,N,K", [([8100, 0, 12001, 12600], 256, 256), ([33, 20000, 0, 12000], 200, 136), ([70, 32000, 1], 64, 256)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_weight_gradients_by_four_teams(counts, N, K, dt):
+    """Few tiles of long reductions: groups that begin and end inside four blocks, empty ones, and one shorter than the teams' first
+    stages, in small integers, so that the fp32 sums are exact."""
+    G, total = len(counts), sum(counts)
+    off, p32 = U.group_offsets(counts, block=32)
+    assert _plan(N, K, p32, 2, G, N) == 3
+    x, dy = _small(total, K, 1, False), _small(total, N, 2, False)
+    for s in _groups(counts, total):
+        x[s][::32], dy[s][::32] = 4, 4
+    q = [U.mxfp4_quantize_grouped(t, off, p32, transpose=True) for t in (dy, x)]
+    dw = U.mxfp4_gemm_bwd_dw_grouped(*q, off, dt)
+    for e, s in enumerate(_groups(counts, total)):
+        assert torch.equal(dw[e], (dy[s].double().t().contiguous() @ x[s].double()).to(dt))
+
+
+@pytest.mark.parametrize("counts,N,K", [([100, 0, 150, 50], 8192, 256), ([1, 130], 8192, 248)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_input_gradients_by_four_teams(counts, N, K, dt):
+    """Few tokens and a long N: the grouped input gradient (N its reduction, K its columns)."""
+    G, total = len(counts), sum(counts)
+    off, p128 = U.group_offsets(counts, block=128)
+    assert _plan(total, K, N, 1, G, p128) == 3
+    dy, w = _small(total, N, 1, True), _small(G * N, K, 2, False)
+    dx = U.mxfp4_gemm_bwd_dx_grouped(U.mxfp4_quantize_grouped(dy, off, p128, transpose=False), U.mxfp4_quantize(w, transpose=True), off,
+                                     total, dt)
+    for e, s in enumerate(_groups(counts, total)):
+        assert torch.equal(dx[s], (dy[s].double() @ w[e * N : (e + 1) * N].double()).to(dt))
+
+
+def test_large_outputs_of_the_64_row_tiles():
+    """256 MiB and more of many small weight gradients: stored plainly, as the 64-row tiles store everything."""
+    counts, N, K = [64] * 256, 192, 2048
+    total, G = sum(counts), len(counts)
+    off, p32 = U.group_offsets(counts, block=32)
+    assert _plan(N, K, p32, 2, G, N) == 2 and G * N * K * 4 >= 1 << 28
+    x, dy = _small(total, K, 1, False), _small(total, N, 2, False)
+    dw = U.mxfp4_gemm_bwd_dw_grouped(*(U.mxfp4_quantize_grouped(t, off, p32, transpose=True) for t in (dy, x)), off)
+    for e, s in enumerate(_groups(counts, total)):
+        assert torch.equal(dw[e].double(), dy[s].double().t().contiguous() @ x[s].double())

@@ -7,6 +7,8 @@ longer than the registers hold add up to cols / 8192 more terms per thread. An o
 of its value (bf16: half an ulp of 8 bits).
 """
 
+import ctypes
+
 import pytest
 import torch
 
@@ -307,3 +309,36 @@ def test_rows_without_columns(dt, rows):
         assert torch.isnan(mean).all() and torch.isnan(rstd).all()
     dx, dgamma, dbeta = U.layer_norm_bwd(y, y, None, mean, rstd)
     assert dx.shape == (rows, 0) and dgamma.shape == dbeta.shape == (0,)
+
+
+# a row's threads and pieces: 8 to 64 x 1, 64 x 2, 256 x 1 .. 3, 1024 x 1 .. 4, and past them the columns' own kernel; the last three
+# tensors are stored nontemporally
+MANY_ROWS = [(40000, 33, BF), (20000, 100, BF), (20000, 250, BF), (9000, 500, BF), (7000, 1000, BF), (8192, 2048, BF), (4099, 1411, F32),
+             (2500, 4000, BF), (1500, 5120, BF), (1500, 7000, BF), (1500, 7000, F32), (700, 16384, F32), (700, 16384, BF), (300, 20000, BF),
+             (300, 33000, F32), (4100, 16392, BF), (30011, 2304, BF), (20000, 1411, F32), (6000, 16384, BF)]
+
+
+@pytest.mark.parametrize("rows,cols,dt", MANY_ROWS)
+def test_weight_gradients_of_many_rows(rows, cols, dt):
+    """dgamma and dbeta where every workgroup adds up several rows. A workgroup has at most ceil(rows / parts) rows: a thread adds every
+    kRows-th of them and the kRows sums are added in turn (together at most that many additions and one more; rows that share a wave have
+    16 waves' sums, and three shuffles); then the parts' sums, ceil(parts / 16) in each of 16 waves and 16 more."""
+    need = ctypes.c_size_t()
+    assert U.lib().ufp4_layer_norm_bwd_workspace(U.OUT_BF16 if dt == BF else U.OUT_F32, rows, cols, ctypes.byref(need)) == 0
+    parts = need.value // (8 * cols)
+    assert parts > 1 and rows > 2 * parts
+    x, dy = _tensor(rows, cols, dt, rows + cols), _tensor(rows, cols, dt, rows + 2 * cols, mean=0.1)
+    gamma, _ = _weights(cols, F32, cols)
+    _, mean, rstd = U.layer_norm(x, gamma, None)
+    _, dgamma, dbeta = U.layer_norm_bwd(dy, x, gamma, mean, rstd)
+    sums = torch.zeros(5, cols, dtype=torch.float64, device="cuda")
+    for a in range(0, rows, 4096):
+        s = slice(a, min(rows, a + 4096))
+        d, v, m, r = dy[s].double(), x[s].double(), mean[s].double()[:, None], rstd[s].double()[:, None]
+        t = d * ((v - m) * r)
+        # h itself: one subtraction and one product of rounded numbers, relative to |x| + |mu|
+        off = 2.0**-22 * d.abs() * (v.abs() + m.abs()) * r
+        sums += torch.stack([q.sum(0) for q in (t, t.abs(), off, d, d.abs())])
+    k = 2.0**-24 * (-(-rows // parts) + 1 + 16 + 3 + -(-parts // 16) + 16)
+    _within("dgamma", dgamma, sums[0], k * sums[1] + 2 * sums[2])
+    _within("dbeta", dbeta, sums[3], k * sums[4])
