@@ -3,13 +3,14 @@
 //
 // A lane of the instruction holds the 32 codes of one row and one 32-block: 16 bytes, one LDS read. K advances 128 (four
 // blocks) per stage; a panel's stage is 8 KiB of codes and 512 bytes of scales, both contiguous, copied unchanged into a
-// three-deep LDS ring by direct-to-LDS loads (a fourth slot measured the same). Each wave keeps two sets of operands in registers: while the matrix core works
-// on one half of a stage, the other half (or, past the barrier, the next stage's first half) is read from LDS, so that
-// neither the barrier nor the LDS latency stands between two matrix instructions.
+// three-deep LDS ring by direct-to-LDS loads (a fourth slot measured the same at 16384^3). Each wave keeps two sets of operands
+// in registers: while the matrix core works on one half of a stage, the other half (or, past the barrier, the next stage's first
+// half) is read from LDS, so that neither the barrier nor the LDS latency stands between two matrix instructions.
 //
-// Bound by the matrix cores' power where the reduction is long: the instruction alone, on registers, reaches 5.5 PFLOP/s (the
-// clock falls to 1.4 GHz), 16384^3 with bf16 output takes 1.75-1.84 ms = 4.8-5.0 (matrix cores busy 75% of the time at 1.45 GHz). Where it is short, by the stores, which take the memory
-// system from the loads: 16384 x 16384 x 2048 takes 0.29 ms = 3.8 PFLOP/s, without its stores 0.235 ms.
+// Bound by the matrix cores and their power where the reduction is long: the instruction alone, on registers, reaches 6.3 PFLOP/s
+// on codes of normal numbers (9.8 on zeros: power takes the clock to 1.5 GHz), 16384^3 with bf16 output takes 1.75-1.87 ms = 4.7-5.0
+// (matrix cores busy 73% of the time at 1.5 GHz). Where it is short, by the stores, which take the memory system from the loads:
+// 16384 x 16384 x 2048 takes 0.29 ms = 3.8 PFLOP/s, without its stores 0.235 ms.
 
 #include "ufp4_internal.h"
 #include "ufp4_mxfp4.h"
@@ -667,11 +668,12 @@ hipError_t launch_tile(const MxGemmJob& j, hipStream_t s) {
 // in the L2's recency order they push the operands out. Measured, us, nontemporal / plain: 16384 x 16384 x 2048 bf16 311 / 398,
 // fp32 393 / 602 (190 MB read instead of 425), x 512 bf16 150 / 205, 64 experts' 98304 x 1408 x 2048 forward 200 / 251 and weight
 // gradient 259 / 322; at 256 MiB 8192 x 8192 fp32 of 1024 74 / 97, of 2048 107 / 99, of 8192 254 / 267; below, 8192 x 8192 x 2048
-// bf16 83 / 77. The 64-row tiles are not taken for outputs of that size.
+// bf16 83 / 77. The 64-row tiles store everything plainly: outputs of that size are theirs only where one side is narrow (up to about
+// 320 rows or columns, of weight gradients 570: 64 x 2^20 x 128, 256 experts of 192 x 2048 over 64 tokens each).
 // A weights' gradient is read when the whole step's have been computed, hundreds of MB later, so it is stored so from 64 MiB on. Whole
 // steps (quantizers and the three products), us, nontemporal / plain: 16 experts 4823 x 1920 x 1600 (188 MiB of gradients) 132 / 150, 8
 // experts 1602 x 3456 x 1600 (169) 106 / 119, 16508 x 4736 x 1344 (194) 403 / 418, 16 experts 2069 x 7552 x 256 (118) 102 / 106, dense
-// 5120 x 6016 x 2976 (68) 202 / 208-214; below 32 MiB the same within 1%. (Where 64-row tiles take such a gradient they store plainly.)
+// 5120 x 6016 x 2976 (68) 202 / 208-214; below 32 MiB the same within 1%. (The 64-row tiles: as above.)
 constexpr int64_t kStreamGradBytes = int64_t(64) << 20;
 bool streams(const MxGemmJob& j) {
     return j.M * j.N * (j.mode == kGemmRaggedK ? j.G : 1) * (j.out_dtype == kOutF32 ? 4 : 2) >= (j.weight_grad ? kStreamGradBytes : kStreamBytes);

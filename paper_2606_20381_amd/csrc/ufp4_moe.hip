@@ -11,8 +11,8 @@
 //   longer rows (more than a segment) takes a workgroup per token, of few tokens one per slot.
 //
 // Measured, 16384 tokens to 6 of 64 experts, 2048 bf16 columns: sort 4.7 + 7.7 us (two launches of 24 workgroups, bound by their
-// own latency), dispatch 79 us and combine 80 us (470 MB each: 5.9 TB/s; a copy of 1 GiB runs at 5.1), combine_bwd 173 us (873 MB:
-// 5.0 TB/s; 5003 x 2 x 5120 fp32 92 us, 512 MB: 5.6 TB/s).
+// own latency), dispatch 78 us and combine 80 us (470 MB each: 5.9 TB/s; a copy of 1 GiB runs at 5.1), combine_bwd 172 us (873 MB:
+// 5.1 TB/s; among a layer step's other kernels 189; 5003 x 2 x 5120 fp32 91 us, 512 MB: 5.6 TB/s).
 
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"

@@ -10,10 +10,12 @@
 // four blocks (128 of the reduction) lie together. Scale bytes of the blocks that fill up the last four are 0.
 //
 // HBM bound: 2 bytes read and 17/32 written per value. amax is a packed 16-bit integer maximum of the bf16 patterns (their
-// order is that of the magnitudes) and the conversion one instruction per two values, so the plain form has little to compute;
-// rotated (fp64 sums, as the other quantizers) or stochastic (Philox) it is bound by vector issue. Measured, 32768 x 16384 (1 GiB),
-// us: rowwise 230 (5.9 TB/s), transposed 256 (5.3), both 306 (5.4), rowwise / transposed rotated 244 / 316, stochastic 380 / 411,
-// back to bf16 243 (5.6).
+// order is that of the magnitudes) and the conversion one instruction per two values, so the plain form has little to compute (4
+// vector instructions a value). Stochastic it has 27 (28 transposed) and is bound by their issue; Philox's draws are part of them, but
+// the quantizer of the uniform grid, with the same draws and a rotation, has 24 (21): the rest goes into two ranges of every value
+// (fp4_sr) and into codes merged one at a time. Rotated (fp64 sums, as the other quantizers) and stochastic it has 35 (36).
+// Measured, 32768 x 16384 (1 GiB), us: rowwise 230 (5.9 TB/s), transposed 256 (5.3), both 306 (5.4), rowwise / transposed rotated
+// 230-244 / 315, stochastic 350-380 / 404-411, both of these 453 / 526, back to bf16 243-251 (5.6).
 
 #include "ufp4_internal.h"
 #include "ufp4_device.h"
