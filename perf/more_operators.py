@@ -172,6 +172,11 @@ def _eight(x):
     return torch.ldexp(v, e).view(x.shape[0], -1)[:, :cols]
 
 
+def _eight_parts(u, kind):
+    """A gated activation's input has two halves, each in blocks of its own."""
+    return _eight(u) if kind == "relu2" else torch.cat([_eight(p) for p in u.chunk(2, 1)], 1)
+
+
 def _act(u, kind):
     if kind == "relu2":
         return u.clamp(min=0).square()
@@ -192,7 +197,7 @@ def _run_plain(s):
     if op == "save":
         return _eight(s["x"]).to(s["dt"])
     if op == "act":
-        kept, da = _eight(s["u"]), s["da"].float()
+        kept, da = _eight_parts(s["u"], s["kind"]), s["da"].float()
         return {"a": _act(s["u"].float(), s["kind"]).to(s["dt"]), "du": _act_grad(da, kept, s["kind"]).to(s["dt"]),
                 "again": _act(kept, s["kind"]).to(s["dt"])}
     if op == "saved":
@@ -272,11 +277,13 @@ def exact(case, seed):
     if op == "save":
         return _eight64(s["x"])
     if op == "act":
-        u, kept, da = s["u"].double(), _eight64(s["u"]), s["da"].double()
+        n, u, da = case["cols"], s["u"].double(), s["da"].double()
+        kept = torch.empty_like(u)
+        for at in range(0, u.shape[1], n):
+            kept[:, at : at + n] = _eight64(s["u"][:, at : at + n])
         if case["kind"] == "relu2":
             up, kp = torch.relu(u), torch.relu(kept)
             return {"a": up * up, "du": kp * da * 2.0, "again": kp * kp}
-        n = case["cols"]
         f, slope = _silu64(kept[:, :n])
         du = torch.empty_like(kept)
         du[:, :n] = slope * kept[:, n:] * da
