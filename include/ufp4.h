@@ -584,6 +584,71 @@ int ufp4_moe_combine_bwd(int dtype, const void *dout_dev, int64_t tokens, int64_
                          int32_t experts, const float *weights_dev, void *dy_dev, int64_t lddy, float *dweights_dev,
                          void *stream);
 
+/*
+ * Products of bf16 rows in groups (an MoE layer's experts kept in 16 bits), W as it is stored:
+ *
+ *   ufp4_bf16_gemm_fwd_y_grouped : Y_g  [m_g, N] = X_g  [m_g, K] W_g [N, K]^T
+ *   ufp4_bf16_gemm_bwd_dx_grouped: dX_g [m_g, K] = dY_g [m_g, N] W_g [N, K]
+ *   ufp4_bf16_gemm_bwd_dw_grouped: dW_g [N, K]   = dY_g [m_g, N]^T X_g [m_g, K]
+ *   ufp4_bf16_gemm_bwd_dw_grouped_ckpt8: the same with X an 8-bit checkpoint (ufp4_ckpt8_save), read as it is
+ *
+ * Group g has the rows offsets[g] .. offsets[g + 1] - 1 of the `tokens` rows of x, dy, y and dx (offsets int64 [num_groups + 1] on the
+ * device, as ufp4_moe_sort writes them; cut to 0 .. tokens; a group whose end is not past its start has no rows), w is
+ * [num_groups * N, K], dw [num_groups, N, K] with rows ldc apart and groups N rows apart. Rows of y and dx outside the groups are left
+ * as they were; dw of a group without rows is zero. Any sizes, leading dimensions (elements, at least the row's) and alignment of a whole
+ * element; rows of 16-byte aligned pieces (sizes and leading dimensions multiples of 8, bases 16-byte aligned) are faster.
+ * fp32 sums, in an order that follows the sizes (not the values, nor the run); out_dtype UFP4_OUT_F32 or UFP4_OUT_BF16 (one
+ * rounding). num_groups 1 .. 1024, tokens below 2^31, N and K up to 2^30, fewer than 2^24 tiles of 16 x 64 outputs at worst (else
+ * UFP4_ERR_UNSUPPORTED). Outputs must not overlap inputs.
+ */
+int ufp4_bf16_gemm_fwd_y_grouped(const void *x_dev, int64_t tokens, int64_t K, int64_t ldx, const void *w_dev, int64_t N, int64_t ldw,
+                                 const int64_t *group_offsets_dev, int32_t num_groups, void *y_dev, int64_t ldc, int out_dtype,
+                                 void *stream);
+int ufp4_bf16_gemm_bwd_dx_grouped(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void *w_dev, int64_t K, int64_t ldw,
+                                  const int64_t *group_offsets_dev, int32_t num_groups, void *dx_dev, int64_t ldc, int out_dtype,
+                                  void *stream);
+int ufp4_bf16_gemm_bwd_dw_grouped(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void *x_dev, int64_t K, int64_t ldx,
+                                  const int64_t *group_offsets_dev, int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype,
+                                  void *stream);
+int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const uint8_t *codes_dev,
+                                        int64_t code_ld, const uint8_t *scales_dev, int64_t scale_ld, int64_t K,
+                                        const int64_t *group_offsets_dev, int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype,
+                                        void *stream);
+
+/*
+ * Activations kept in 8 bits between the forward and the backward pass. Per 32 values of a row one scale 2^e, stored as the byte
+ * e + 127: e is the smallest integer >= -124 with |x| <= 448 2^e for every finite x of the block; and per value the E4M3 number (OCP, one
+ * byte, no infinity) nearest to x 2^-e, ties to the even code. A value is off by at most 2^-4 of itself or half of 2^(e - 9), where
+ * that is more (magnitudes from 1.9375 2^127 on are kept as 1.875 2^127, the next level being no fp32 number); an infinity or NaN is kept as NaN and leaves its block's other values alone. Every kept value is a bf16 number.
+ * A row of `cols` values has ceil(cols / 32) scales and 32 ceil(cols / 32) codes, those past `cols` 0.
+ *
+ * ufp4_ckpt8_ld -- the smallest leading dimensions (bytes) of codes and scales of a row in `parts` parts of `cols` values each, every
+ *   part in blocks of its own (parts 1; 2 for the input of a gated activation).
+ * ufp4_ckpt8_save, ufp4_ckpt8_load -- a tensor [rows, cols] of type `dtype` to codes and scales, and back. Codes 16-byte aligned with
+ *   code_ld % 16 == 0.
+ */
+int ufp4_ckpt8_ld(int64_t cols, int parts, int64_t *code_ld, int64_t *scale_ld);
+int ufp4_ckpt8_save(int dtype, const void *x_dev, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes_dev, int64_t code_ld,
+                    uint8_t *scales_dev, int64_t scale_ld, void *stream);
+int ufp4_ckpt8_load(int dtype, const uint8_t *codes_dev, int64_t code_ld, const uint8_t *scales_dev, int64_t scale_ld, int64_t rows,
+                    int64_t cols, void *y_dev, int64_t ldy, void *stream);
+
+/*
+ * The experts' activation and its gradient, arithmetic in fp32, one rounding to `dtype`:
+ *   UFP4_ACT_RELU2  a [rows, cols] = max(u, 0)^2, u [rows, cols];  du = 2 max(u, 0) da
+ *   UFP4_ACT_SWIGLU a [rows, cols] = silu(g) v, u [rows, 2 cols] = (g, v), silu(g) = g / (1 + e^-g);
+ *                   du = (da v silu'(g), da silu(g))
+ * ufp4_activation -- a, and with codes_dev u's checkpoint from the same read (parts 1 or, of the gated one, 2).
+ * ufp4_activation_bwd -- du from da and u, or (u_dev NULL) u's checkpoint; with a_dev also a of that u, which the weights' gradient of
+ *   the next product needs. Outputs must not overlap inputs.
+ */
+typedef enum { UFP4_ACT_RELU2 = 0, UFP4_ACT_SWIGLU = 1 } ufp4_act_t;
+int ufp4_activation(int kind, int dtype, const void *u_dev, int64_t rows, int64_t cols, int64_t ldu, void *a_dev, int64_t lda,
+                    uint8_t *codes_dev, int64_t code_ld, uint8_t *scales_dev, int64_t scale_ld, void *stream);
+int ufp4_activation_bwd(int kind, int dtype, const void *da_dev, int64_t rows, int64_t cols, int64_t ldda, const void *u_dev, int64_t ldu,
+                        const uint8_t *codes_dev, int64_t code_ld, const uint8_t *scales_dev, int64_t scale_ld, void *du_dev,
+                        int64_t lddu, void *a_dev, int64_t lda, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,8 @@ HOST = os.path.join(PKG, "_host.so")  # a Python module: the host side of short 
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
 SOURCES = ["ufp4_quant.hip", "ufp4_gemm.hip", "ufp4_gemm_mx.hip", "ufp4_mxfp4.hip", "ufp4_gemm_mxfp4.hip",
-           "ufp4_linear_mxfp4.hip", "ufp4_norm.hip", "ufp4_moe.hip", "ufp4_api.cpp", "ufp4_api_layer.cpp"]
+           "ufp4_linear_mxfp4.hip", "ufp4_norm.hip", "ufp4_moe.hip", "ufp4_gemm_bf16.hip", "ufp4_ckpt8.hip", "ufp4_api.cpp",
+           "ufp4_api_layer.cpp", "ufp4_api_bf16.cpp"]
 
 ARCH = "gfx950"
 FLAGS = [

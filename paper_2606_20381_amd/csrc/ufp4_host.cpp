@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -701,6 +702,257 @@ CALL(on_one_gpu, 2)
     Py_RETURN_NONE;
 END_CALL
 
+// ------------------------------------------------------------------------------------------------
+// bf16 products in groups, 8-bit checkpoints, activation
+// ------------------------------------------------------------------------------------------------
+
+// Whether a tensor on the GPU is on the current device, whose stream the call gets.
+bool on_current(const at::Tensor& t, const char* what) {
+    const at::Device now = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice();
+    if (t.device().index() == now.index()) return true;
+    PyErr_Format(PyExc_ValueError, "%s is on %s, the current device is %s", what, t.device().str().c_str(), now.str().c_str());
+    return false;
+}
+
+bool input_of(PyObject* o, const char* what, Rows& r) { return rows_of(o, what, r) && on_current(*r.t, what); }
+
+bool bf16_rows(PyObject* o, const char* what, Rows& r) {
+    if (!input_of(o, what, r)) return false;
+    return r.code == UFP4_OUT_BF16 || refuse(what, "bfloat16");
+}
+
+bool same_device(const at::Tensor& t, const at::Tensor& like, const char* what) {
+    return t.device() == like.device() || refuse(what, "on the device of the tensor beside it");
+}
+
+// A checkpoint's codes [rows, at least the blocks' bytes] and scales, of `parts` parts of `cols` values.
+struct Kept {
+    uint8_t *codes = nullptr, *scales = nullptr;
+    int64_t rows = 0, code_ld = 0, scale_ld = 0;
+};
+
+bool bytes_of(PyObject* o, const char* what, int64_t cols, const at::Tensor*& t, int64_t& ld) {
+    t = tensor(o, what);
+    if (!t) return false;
+    if (t->scalar_type() != at::kByte || !t->is_cuda() || t->dim() != 2 || t->size(1) < cols || (t->size(1) > 1 && t->stride(1) != 1))
+        return refuse(what, "a row-major uint8 CUDA tensor of the checkpoint's width");
+    ld = t->size(0) > 1 ? t->stride(0) : t->size(1);
+    return true;
+}
+
+bool kept_of(PyObject* codes, PyObject* scales, int64_t cols, int parts, Kept& k, const at::Tensor*& t) {
+    int64_t cld, sld;
+    if (!check(ufp4_ckpt8_ld(cols, parts, &cld, &sld), "ufp4_ckpt8_ld")) return false;
+    const at::Tensor* s;
+    if (!bytes_of(codes, "codes", cld, t, k.code_ld) || !bytes_of(scales, "scales", sld, s, k.scale_ld)) return false;
+    if (s->size(0) != t->size(0)) return refuse("scales", "of the rows of codes");
+    if (!same_device(*s, *t, "scales")) return false;
+    k.rows = t->size(0);
+    k.codes = static_cast<uint8_t*>(t->data_ptr());
+    k.scales = static_cast<uint8_t*>(s->data_ptr());
+    return true;
+}
+
+// Buffers for a checkpoint of [rows, parts * cols].
+Done new_kept(const at::Tensor& like, int64_t rows, int64_t cols, int parts, at::Tensor& codes, at::Tensor& scales, Kept& k) {
+    const Done done{ufp4_ckpt8_ld(cols, parts, &k.code_ld, &k.scale_ld), "ufp4_ckpt8_ld"};
+    if (done.status != UFP4_OK) return done;
+    const auto bytes = like.options().dtype(at::kByte);
+    codes = at::empty({rows, k.code_ld}, bytes);
+    scales = at::empty({rows, k.scale_ld}, bytes);
+    k.rows = rows;
+    k.codes = static_cast<uint8_t*>(codes.data_ptr());
+    k.scales = static_cast<uint8_t*>(scales.data_ptr());
+    return done;
+}
+
+// (x, w, offsets, out type, out, stream) -> y [tokens, N] of x [tokens, K] (BACK: of dy [tokens, N] -> dx [tokens, K])
+template <bool BACK>
+PyObject* bf16_rows_product(PyObject* const* a, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    if (!arguments(n_args, 6)) return nullptr;
+    Rows x, w;
+    void* offsets;
+    int64_t groups;
+    if (!bf16_rows(a[0], BACK ? "dy" : "x", x) || !bf16_rows(a[1], "w", w) || !same_device(*w.t, *x.t, "w") ||
+        !offsets_of(a[2], x.t->device(), offsets, groups))
+        return nullptr;
+    const int code = (int)PyLong_AsLong(a[3]);
+    void* const stream = pointer(a[5]);
+    if (PyErr_Occurred()) return nullptr;
+    if (groups < 1) return refuse("offsets", "of at least one group"), nullptr;
+    const int64_t n = w.rows / groups;
+    if (n * groups != w.rows || x.cols != (BACK ? n : w.cols)) {
+        PyErr_Format(PyExc_ValueError, BACK ? "dy must have %lld columns, a %lld-th of w's rows" : "x must have %lld columns, and w's rows be a multiple of %lld",
+                     (long long)(BACK ? n : w.cols), (long long)groups);
+        return nullptr;
+    }
+    at::Tensor out;
+    const Shape shape{{0, x.rows, BACK ? w.cols : n}};
+    if (!product_out(a[4], *x.t, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*x.t, shape, code, out);
+            const int32_t g = groups > INT32_MAX ? INT32_MAX : (int32_t)groups;
+            if (BACK)
+                return {ufp4_bf16_gemm_bwd_dx_grouped(x.data(), x.rows, n, x.ld, w.data(), w.cols, w.ld, static_cast<int64_t*>(offsets), g,
+                                                      out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_bf16_gemm_bwd_dx_grouped"};
+            return {ufp4_bf16_gemm_fwd_y_grouped(x.data(), x.rows, x.cols, x.ld, w.data(), n, w.ld, static_cast<int64_t*>(offsets), g,
+                                                 out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_bf16_gemm_fwd_y_grouped"};
+        }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* bf16_gemm_fwd_y_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) { return bf16_rows_product<false>(a, n); }
+PyObject* bf16_gemm_bwd_dx_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) { return bf16_rows_product<true>(a, n); }
+
+// (dy, x or None, codes, scales, columns of a checkpoint, offsets, out type, out, stream) -> dw [groups, N, K]
+CALL(bf16_gemm_bwd_dw_grouped, 9)
+    Rows dy, x;
+    Kept k;
+    void* offsets;
+    int64_t groups;
+    const bool saved = a[1] == Py_None;
+    int64_t cols = PyLong_AsLongLong(a[4]);
+    const int code = (int)PyLong_AsLong(a[6]);
+    void* const stream = pointer(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!bf16_rows(a[0], "dy", dy)) return nullptr;
+    const at::Tensor* codes = nullptr;
+    if (saved) {
+        if (!kept_of(a[2], a[3], cols, 1, k, codes) || !same_device(*codes, *dy.t, "x")) return nullptr;
+        x.rows = k.rows;
+    } else {
+        if (!bf16_rows(a[1], "x", x) || !same_device(*x.t, *dy.t, "x")) return nullptr;
+        cols = x.cols;
+    }
+    if (!offsets_of(a[5], dy.t->device(), offsets, groups)) return nullptr;
+    if (groups < 1) return refuse("offsets", "of at least one group"), nullptr;
+    if (x.rows != dy.rows) return refuse("x", "of the rows of dy"), nullptr;
+    at::Tensor out;
+    const Shape shape{{groups, dy.cols, cols}};
+    if (!product_out(a[7], *dy.t, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*dy.t, shape, code, out);
+            const int32_t g = groups > INT32_MAX ? INT32_MAX : (int32_t)groups;
+            int64_t* const off = static_cast<int64_t*>(offsets);
+            if (saved)
+                return {ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(dy.data(), dy.rows, dy.cols, dy.ld, k.codes, k.code_ld, k.scales, k.scale_ld, cols,
+                                                            off, g, out.data_ptr(), out.stride(1), code_of(out), stream),
+                        "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8"};
+            return {ufp4_bf16_gemm_bwd_dw_grouped(dy.data(), dy.rows, dy.cols, dy.ld, x.data(), cols, x.ld, off, g, out.data_ptr(),
+                                                  out.stride(1), code_of(out), stream), "ufp4_bf16_gemm_bwd_dw_grouped"};
+        }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+END_CALL
+
+// (x, codes or None, scales, stream) -> (codes, scales)
+CALL(checkpoint8_save, 4)
+    Rows x;
+    void* const stream = pointer(a[3]);
+    if (PyErr_Occurred() || !input_of(a[0], "x", x)) return nullptr;
+    Kept k;
+    at::Tensor codes, scales;
+    const bool fresh = a[1] == Py_None;
+    if (!fresh) {
+        const at::Tensor* t;
+        if (!kept_of(a[1], a[2], x.cols, 1, k, t) || !same_device(*t, *x.t, "out")) return nullptr;
+        if (k.rows != x.rows) return refuse("out", "a checkpoint of x's shape"), nullptr;
+        codes = *t;
+        scales = THPVariable_Unpack(a[2]);
+    }
+    if (!unlocked([&]() -> Done {
+            if (fresh) {
+                const Done made = new_kept(*x.t, x.rows, x.cols, 1, codes, scales, k);
+                if (made.status != UFP4_OK) return made;
+            }
+            return {ufp4_ckpt8_save(x.code, x.data(), x.rows, x.cols, x.ld, k.codes, k.code_ld, k.scales, k.scale_ld, stream),
+                    "ufp4_ckpt8_save"};
+        }))
+        return nullptr;
+    return pair(codes, THPVariable_Wrap(scales));
+END_CALL
+
+// (codes, scales, columns of a part, parts, out type, out, stream) -> out [rows, parts * columns]
+CALL(checkpoint8_load, 7)
+    const int64_t cols = PyLong_AsLongLong(a[2]);
+    const int parts = (int)PyLong_AsLong(a[3]), code = (int)PyLong_AsLong(a[4]);
+    void* const stream = pointer(a[6]);
+    if (PyErr_Occurred()) return nullptr;
+    Kept k;
+    const at::Tensor* codes;
+    if (!kept_of(a[0], a[1], cols, parts, k, codes) || !on_current(*codes, "the checkpoint")) return nullptr;
+    at::Tensor out;
+    const Shape shape{{0, k.rows, parts * cols}};
+    if (!product_out(a[5], *codes, shape, code, out)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            product_new(*codes, shape, code, out);
+            int64_t cld = 0, sld = 0;
+            ufp4_ckpt8_ld(cols, 1, &cld, &sld);
+            for (int p = 0; p < parts; ++p) {
+                const int st = ufp4_ckpt8_load(code_of(out), k.codes + p * cld, k.code_ld, k.scales + p * sld, k.scale_ld, k.rows, cols,
+                                               static_cast<uint8_t*>(out.data_ptr()) + p * cols * out.element_size(), out.stride(0), stream);
+                if (st != UFP4_OK) return {st, "ufp4_ckpt8_load"};
+            }
+            return {UFP4_OK, nullptr};
+        }))
+        return nullptr;
+    return THPVariable_Wrap(out);
+END_CALL
+
+// (u, kind, parts, save, out, stream) -> (a, codes, scales), None for those where nothing is saved
+CALL(activation, 6)
+    Rows u, y;
+    const int kind = (int)PyLong_AsLong(a[1]), parts = (int)PyLong_AsLong(a[2]), save = PyObject_IsTrue(a[3]);
+    void* const stream = pointer(a[5]);
+    if (PyErr_Occurred() || !input_of(a[0], "u", u)) return nullptr;
+    if (u.cols % parts) return refuse("u", "of two halves"), nullptr;
+    const int64_t cols = u.cols / parts;
+    at::Tensor out, codes, scales;
+    if (!rows_out(a[4], u, u.rows, cols, out, y)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            rows_new(u, out, y);
+            Kept k;
+            if (save) {
+                const Done made = new_kept(*u.t, u.rows, cols, parts, codes, scales, k);
+                if (made.status != UFP4_OK) return made;
+            }
+            return {ufp4_activation(kind, u.code, u.data(), u.rows, cols, u.ld, y.data(), y.ld, k.codes, k.code_ld, k.scales, k.scale_ld,
+                                    stream), "ufp4_activation"};
+        }))
+        return nullptr;
+    return triple(out, codes, scales);
+END_CALL
+
+// (da, u or None, codes, scales, kind, parts, whether a is wanted, out, stream) -> (du, a), None for an a that is not
+CALL(activation_bwd, 9)
+    Rows da, u, du;
+    Kept k;
+    const bool saved = a[1] == Py_None;
+    const int kind = (int)PyLong_AsLong(a[4]), parts = (int)PyLong_AsLong(a[5]), again = PyObject_IsTrue(a[6]);
+    void* const stream = pointer(a[8]);
+    if (PyErr_Occurred() || !input_of(a[0], "da", da)) return nullptr;
+    if (saved) {
+        const at::Tensor* codes;
+        if (!kept_of(a[2], a[3], da.cols, parts, k, codes) || !same_device(*codes, *da.t, "the checkpoint")) return nullptr;
+        if (k.rows != da.rows) return refuse("the checkpoint", "of the rows of da"), nullptr;
+    } else if (!rows_like(a[1], "u", da, da.rows, parts * da.cols, u)) {
+        return nullptr;
+    }
+    at::Tensor out, y;
+    if (!rows_out(a[7], da, da.rows, parts * da.cols, out, du)) return nullptr;
+    if (!unlocked([&]() -> Done {
+            rows_new(da, out, du);
+            if (again) y = at::empty({da.rows, da.cols}, da.t->options());
+            return {ufp4_activation_bwd(kind, da.code, da.data(), da.rows, da.cols, da.ld, saved ? nullptr : u.data(), u.ld, k.codes, k.code_ld,
+                                        k.scales, k.scale_ld, du.data(), du.ld, again ? y.data_ptr() : nullptr, da.cols, stream),
+                    "ufp4_activation_bwd"};
+        }))
+        return nullptr;
+    return pair(out, THPVariable_Wrap(y));
+END_CALL
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XDECREF(g_error);
@@ -715,6 +967,8 @@ PyMethodDef kMethods[] = {METHOD(layer_norm),   METHOD(layer_norm_bwd), METHOD(m
                           METHOD(mxfp4_gemm_bwd_dx), METHOD(mxfp4_gemm_bwd_dw), METHOD(mxfp4_linear),
                           METHOD(mxfp4_quantize_dual), METHOD(mxfp4_quantize_grouped), METHOD(mxfp4_gemm_fwd_y_grouped),
                           METHOD(mxfp4_gemm_bwd_dx_grouped), METHOD(mxfp4_gemm_bwd_dw_grouped), METHOD(on_one_gpu),
+                          METHOD(bf16_gemm_fwd_y_grouped), METHOD(bf16_gemm_bwd_dx_grouped), METHOD(bf16_gemm_bwd_dw_grouped),
+                          METHOD(checkpoint8_save), METHOD(checkpoint8_load), METHOD(activation), METHOD(activation_bwd),
                           {"set_error", set_error, METH_O, nullptr},    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", "Host side of the short calls of ufp4.py", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

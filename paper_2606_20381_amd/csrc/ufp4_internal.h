@@ -308,6 +308,65 @@ struct MoeBwdJob {
 };
 hipError_t launch_moe_combine_bwd(const MoeBwdJob& job, hipStream_t stream);
 
+// Products of bf16 rows in groups. A's rows are the output's rows, B's its columns:
+//   fwd_y  A = x [tokens, red], B = w [G * N, red];  bwd_dx  A = dy [tokens, red], B = w [G * red, N], read across
+//   bwd_dw A = dy [tokens, M], B = x [tokens, N], both read across; one [M, N] per group
+enum { kBf16FwdY = 0, kBf16BwdDx = 1, kBf16BwdDw = 2 };
+constexpr int kBf16Groups = 1024;
+struct Bf16GemmJob {
+    int pass, out_dtype;
+    const uint16_t* a;
+    int64_t lda;
+    const uint16_t* b;
+    int64_t ldb;        // of b or b8
+    const uint8_t* b8;  // bwd_dw: x as an 8-bit checkpoint, b is null
+    const uint8_t* bs;
+    int64_t ldbs;
+    int64_t tokens, M, N, red;  // M of bwd_dw; red of the others
+    void* c;
+    int64_t ldc;
+    const int64_t* offsets;
+    int32_t G;
+};
+hipError_t launch_gemm_bf16(const Bf16GemmJob& job, hipStream_t stream);
+bool bf16_gemm_fits(const Bf16GemmJob& job);  // the grid of every kernel that may take it
+
+// Checkpoints in 8 bits (format in ufp4_ckpt8.h): codes [rows][ldc], scales [rows][lds].
+struct Ckpt8Job {
+    int bf16;
+    const void* x;  // save
+    void* out;      // load
+    int64_t ldx;    // of either
+    int64_t rows, cols;
+    uint8_t* codes;
+    int64_t ldc;
+    uint8_t* scales;
+    int64_t lds;
+};
+hipError_t launch_ckpt8_save(const Ckpt8Job& job, hipStream_t stream);
+hipError_t launch_ckpt8_load(const Ckpt8Job& job, hipStream_t stream);
+int64_t ckpt8_units(int64_t rows, int64_t cols);  // threads at most
+
+enum { kActRelu2 = 0, kActSwiglu = 1 };
+struct ActJob {
+    int bf16, kind;
+    const void* u;  // bwd: null where the checkpoint takes its place
+    int64_t ldu;
+    void* a;  // bwd: may be null
+    int64_t lda;
+    const void* da;
+    int64_t ldda;
+    void* du;
+    int64_t lddu;
+    int64_t rows, cols;  // of a
+    uint8_t* codes;      // forward: null for no checkpoint
+    int64_t ldc;
+    uint8_t* scales;
+    int64_t lds;
+};
+hipError_t launch_act(const ActJob& job, hipStream_t stream);
+hipError_t launch_act_bwd(const ActJob& job, hipStream_t stream);
+
 }  // namespace ufp4
 
 // The size rules asked from the host: exported for the tests, not part of the interface in include/ufp4.h.

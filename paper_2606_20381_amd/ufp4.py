@@ -63,6 +63,7 @@ _M = ctypes.POINTER(Metrics)
 _QUANT_ARGS = [_P, _I64, _I64, _I64, _INT, _INT, _U32, _INT, _U64, _U32, _Q, _P]
 _GEMM_ARGS = [_Q, _Q, _P, _I64, _INT, _P]
 _GEMM_G_ARGS = [_Q, _Q, _P, _I32, _P, _I64, _INT, _P]
+_BF16_GEMM_ARGS = [_P, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P]
 SIGNATURES = {
     "ufp4_status_string": ([_INT], ctypes.c_char_p),
     "ufp4_version": ([], ctypes.c_char_p),
@@ -118,6 +119,15 @@ SIGNATURES = {
     "ufp4_moe_sort": ([_P, _INT, _I64, _I32, _I32, _P, _P, _P, _P, _SZ, _P], _INT),
     "ufp4_moe_dispatch": ([_INT, _P, _I64, _I64, _I64, _P, _I32, _P, _I32, _P, _P, _I64, _I64, _P], _INT),
     "ufp4_moe_combine": ([_INT, _P, _I64, _I64, _I64, _P, _I64, _I32, _P, _P, _I64, _P], _INT),
+    "ufp4_bf16_gemm_fwd_y_grouped": (_BF16_GEMM_ARGS, _INT),
+    "ufp4_bf16_gemm_bwd_dx_grouped": (_BF16_GEMM_ARGS, _INT),
+    "ufp4_bf16_gemm_bwd_dw_grouped": (_BF16_GEMM_ARGS, _INT),
+    "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8": ([_P, _I64, _I64, _I64, _P, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P], _INT),
+    "ufp4_ckpt8_ld": ([_I64, _INT, _P, _P], _INT),
+    "ufp4_ckpt8_save": ([_INT, _P, _I64, _I64, _I64, _P, _I64, _P, _I64, _P], _INT),
+    "ufp4_ckpt8_load": ([_INT, _P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P], _INT),
+    "ufp4_activation": ([_INT, _INT, _P, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _P], _INT),
+    "ufp4_activation_bwd": ([_INT, _INT, _P, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P], _INT),
     "ufp4_moe_combine_bwd": ([_INT, _P, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _P, _I32, _P, _P, _I64, _P, _P], _INT),
 }
 
@@ -809,3 +819,96 @@ def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, rows: torch.Tensor, off
                     weights: torch.Tensor | None = None, *, out: torch.Tensor | None = None):
     """(dy, dweights) of moe_combine (ufp4_moe_combine_bwd); dweights is fp32 [tokens, k]."""
     return (_host_module or _host()).moe_combine_bwd(dout, y, rows, offsets, weights, out, _stream())
+
+
+# ---------------------------------------------------------------------------------------------------
+# activations kept in 8 bits
+# ---------------------------------------------------------------------------------------------------
+
+class Checkpoint8:
+    """A tensor [rows, cols] kept in 8 bits (ufp4_ckpt8_save): E4M3 `codes`, uint8 [rows, whole blocks], and one power of two per 32
+    values of a row, uint8 `scales`. `parts` 2 (the input of a gated activation): the two halves of a row are kept each in blocks of
+    its own."""
+
+    __slots__ = ("codes", "scales", "cols", "parts")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, parts: int = 1):
+        self.codes, self.scales, self.cols, self.parts = codes, scales, cols, parts
+
+    rows = property(lambda self: self.codes.shape[0])
+    shape = property(lambda self: (self.codes.shape[0], self.cols))
+
+
+def checkpoint8_save(x: torch.Tensor, *, out: Checkpoint8 | None = None) -> Checkpoint8:
+    """x [rows, cols] bf16 or fp32 kept in 8 bits (ufp4_ckpt8_save)."""
+    h = _host_module or _host()
+    if out is not None:
+        if out.parts != 1 or out.cols != x.shape[-1]:
+            raise ValueError("out must be a checkpoint of x's shape, in one part")
+        h.checkpoint8_save(x, out.codes, out.scales, _stream())
+        return out
+    codes, scales = h.checkpoint8_save(x, None, None, _stream())
+    return Checkpoint8(codes, scales, x.shape[1])
+
+
+def checkpoint8_load(c: Checkpoint8, dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The kept values as bf16 or fp32 [rows, cols] (ufp4_ckpt8_load), exact in either."""
+    return (_host_module or _host()).checkpoint8_load(c.codes, c.scales, c.cols // c.parts, c.parts, _code_of(dtype), out, _stream())
+
+
+_ACTIVATIONS = {"relu2": (0, 1), "swiglu": (1, 2)}  # UFP4_ACT_*, parts of u
+
+
+def _activation(kind: str) -> tuple[int, int]:
+    if kind not in _ACTIVATIONS:
+        raise ValueError(f"kind must be one of {', '.join(_ACTIVATIONS)}")
+    return _ACTIVATIONS[kind]
+
+
+def activation(u: torch.Tensor, kind: str = "relu2", *, save: bool = False, out: torch.Tensor | None = None):
+    """(a, checkpoint) of the experts' activation (ufp4_activation): "relu2" a = max(u, 0)^2, "swiglu" a = silu(g) v of u = (g, v).
+    With save u is kept in 8 bits from the same read, otherwise the checkpoint is None."""
+    code, parts = _activation(kind)
+    a, codes, scales = (_host_module or _host()).activation(u, code, parts, save, out, _stream())
+    return a, Checkpoint8(codes, scales, u.shape[1], parts) if save else None
+
+
+def activation_bwd(da: torch.Tensor, u: torch.Tensor | Checkpoint8, kind: str = "relu2", *, again: bool = True,
+                   out: torch.Tensor | None = None):
+    """(du, a) of activation from u or its checkpoint (ufp4_activation_bwd): the gradient, and a of that u once more, which the weights'
+    gradient of the product after it reads (None with again False)."""
+    code, parts = _activation(kind)
+    h = _host_module or _host()
+    if isinstance(u, Checkpoint8):
+        if u.parts != parts or u.cols != parts * da.shape[-1]:
+            raise ValueError(f"the checkpoint must be of [rows, {parts * da.shape[-1]}] in {parts} part{'s' if parts > 1 else ''}")
+        return h.activation_bwd(da, None, u.codes, u.scales, code, parts, again, out, _stream())
+    return h.activation_bwd(da, u, None, None, code, parts, again, out, _stream())
+
+
+# ---------------------------------------------------------------------------------------------------
+# bf16 products in groups
+# ---------------------------------------------------------------------------------------------------
+
+def bf16_gemm_fwd_y_grouped(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
+    """Y [tokens, N] with Y_g = X_g W_g^T, x [tokens, K] and w [G*N, K] bf16 (ufp4_bf16_gemm_fwd_y_grouped). Rows in no group are not
+    written."""
+    return (_host_module or _host()).bf16_gemm_fwd_y_grouped(x, w, offsets, _code_of(out_dtype), out, _stream())
+
+
+def bf16_gemm_bwd_dx_grouped(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, out_dtype=torch.float32, out=None) -> torch.Tensor:
+    """dX [tokens, K] with dX_g = dY_g W_g, dy [tokens, N] and w [G*N, K] bf16 (ufp4_bf16_gemm_bwd_dx_grouped). Rows in no group are
+    not written."""
+    return (_host_module or _host()).bf16_gemm_bwd_dx_grouped(dy, w, offsets, _code_of(out_dtype), out, _stream())
+
+
+def bf16_gemm_bwd_dw_grouped(dy: torch.Tensor, x: torch.Tensor | Checkpoint8, offsets: torch.Tensor, out_dtype=torch.float32,
+                             out=None) -> torch.Tensor:
+    """dW [G, N, K] with dW_g = dY_g^T X_g, dy [tokens, N] bf16 and x [tokens, K] bf16 (ufp4_bf16_gemm_bwd_dw_grouped) or kept in 8 bits
+    (ufp4_bf16_gemm_bwd_dw_grouped_ckpt8)."""
+    h = _host_module or _host()
+    if isinstance(x, Checkpoint8):
+        if x.parts != 1:
+            raise ValueError("x must be kept in one part")
+        return h.bf16_gemm_bwd_dw_grouped(dy, None, x.codes, x.scales, x.cols, offsets, _code_of(out_dtype), out, _stream())
+    return h.bf16_gemm_bwd_dw_grouped(dy, x, None, None, 0, offsets, _code_of(out_dtype), out, _stream())
