@@ -20,7 +20,6 @@ namespace ufp4 {
 
 namespace {
 
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
@@ -36,9 +35,8 @@ template <int ROWS, bool ACROSS>
 struct Stage {
     static constexpr uint32_t kSize = ROWS * kStageK * 2;
     static constexpr int kPieces = ROWS * kStageK / 8;  // 16 bytes each
-    static_assert(ROWS >= 128 || !ACROSS, "eight segments to choose from");
     static __device__ __forceinline__ uint32_t turn_row(uint32_t r) { return ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2); }
-    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return (k & 3) | (k >> 1 & 4); }
+    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return ROWS < 128 ? k & 3 : (k & 3) | (k >> 1 & 4); }
 
     // Byte address of the piece of row r with places 8 p .. of the reduction.
     static __device__ __forceinline__ uint32_t along(uint32_t r, uint32_t p) { return r * 64 + (p ^ turn_row(r)) * 16; }
@@ -260,6 +258,309 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     }
 }
 
+// ------------------------------------------------------------------------------------------------
+// Rows of whole 16-byte pieces: memory to LDS without registers between.
+// ------------------------------------------------------------------------------------------------
+
+// WM x WN waves, each with WTM x WTN matrix tiles of 32 x 32 outputs; RING stages in LDS; PER_CU workgroups on a CU.
+template <int WTM_, int WTN_, int WM_, int WN_, int RING_, int PER_CU>
+struct Tile {
+    static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, kRing = RING_;
+    static constexpr int BM = 32 * WTM * WM, BN = 32 * WTN * WN;
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int kResident = 256 * PER_CU;    // workgroups on 256 CUs
+    static constexpr int kPerEU = PER_CU * kWaves / 4;  // waves per SIMD that the registers have to allow
+    static constexpr int kLoadsA = BM / 16 / kWaves, kLoadsB = BN / 16 / kWaves;  // 1 KiB loads of a stage, a wave
+    static constexpr int kWaveLoads = kLoadsA + kLoadsB;
+    static_assert(kLoadsA * 16 * kWaves == BM && kLoadsB * 16 * kWaves == BN, "every wave issues the same loads");
+    static_assert(kWaveLoads * (kRing - 1) + 32 < 64, "vmcnt has six bits");
+};
+
+// The pipeline: a ring of stages in LDS, filled kRing - 1 ahead by direct-to-LDS loads; each wave keeps two sets of operands in
+// registers: while the matrix core works on one half of a stage, the other half (or, past the barrier, the next stage's first
+// half) is read from LDS. A reduction's last places that make no whole stage are multiplied first, by operands that the wave loads from
+// memory itself while the ring fills.
+template <int OUT, class C, int PASS, bool STREAM>
+__global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16GemmJob j) {
+    using P = Pass<PASS>;
+    constexpr int BM = C::BM, BN = C::BN, WTM = C::WTM, WTN = C::WTN, kRing = C::kRing;
+    using SA = Stage<BM, P::kAcrossA>;
+    using SB = Stage<BN, P::kAcrossB>;
+    constexpr uint32_t kSlot = SA::kSize + SB::kSize;
+    __shared__ __align__(16) uint8_t ring[kRing * kSlot];
+    __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int wm = (int)((unsigned)wave / C::WN), wn = (int)((unsigned)wave % C::WN), h = lane >> 5, l32 = lane & 31;
+    const uint32_t gx = (uint32_t)((j.N + BN - 1) / BN);
+    uint32_t gy, total;
+    if constexpr (P::kRagged) {
+        if (tid < 64) groups.build(j);
+        __syncthreads();
+        const uint32_t bound = (uint32_t)((j.tokens + BM - 1) / BM + j.G), have = (uint32_t)uniform(groups.tile[j.G]);
+        gy = have < bound ? have : bound;
+        total = gx * gy;
+    } else {
+        gy = (uint32_t)((j.M + BM - 1) / BM);
+        total = gx * gy * (uint32_t)j.G;
+    }
+
+    // One output tile: its operands' places of stage 0 (with a rest: a stage before the first place, where nothing is read), this lane's
+    // pieces of a stage, and where the results go.
+    struct Work {
+        const uint8_t *a, *b;
+        uint32_t va[C::kLoadsA], vb[C::kLoadsB];
+        int nst, rest;  // stages of the reduction; places of it that make no whole one, which are then stage 0
+        int row0, rows, col0;
+        int64_t c_base;
+    };
+    const uint32_t stepA = P::kAcrossA ? (uint32_t)(kStageK * 2 * j.lda) : kStageK * 2, stepB = P::kAcrossB ? (uint32_t)(kStageK * 2 * j.ldb) : kStageK * 2;
+    // Lane's piece of load q (unit wave * loads + q of the stage: 64 pieces in the LDS's order), as an offset from the operand's first
+    // row and place. Rows past the last one are replaced by it: they only feed outputs that are not stored.
+    auto offset = [&](auto stage, bool across, int unit, int64_t ld, int64_t have) INLINE {
+        using S = decltype(stage);
+        constexpr uint32_t kRow = S::kSize / kStageK / 2;  // rows of the operand's tile
+        if (across) {
+            constexpr uint32_t kEach = kRow / 8;  // pieces of a place
+            const uint32_t i = (uint32_t)unit * 64 + lane, k = i / kEach, at = i % kEach;
+            uint32_t r = ((at >> 1 ^ S::turn_k(k)) * 2 + (at & 1)) * 8;
+            r = r < have ? r : (uint32_t)have - 8;
+            return (uint32_t)(k * (uint32_t)ld + r) * 2;
+        }
+        const uint32_t r = (uint32_t)unit * 16 + (lane >> 2), p = (lane & 3) ^ S::turn_row(r);
+        return (uint32_t)((r < have ? r : (uint32_t)have - 1) * (uint32_t)ld + p * 8) * 2;
+    };
+    auto locate = [&](uint32_t L, Work& w) INLINE {
+        int tm, tn;
+        int64_t k0 = 0, k1 = j.red, row0, rows;
+        const uint16_t* b = j.b;
+        w.c_base = 0;
+        if constexpr (P::kRagged) {
+            tile_at(L, gy, gx, tm, tn);
+            const int g = groups.of(j.G, tm), lt = tm - uniform(groups.tile[g]);
+            row0 = (int64_t)uniform(groups.start[g]) + (int64_t)lt * BM;
+            rows = uniform(groups.rows[g]) - (int64_t)lt * BM;
+            b += (int64_t)g * (PASS == kBf16FwdY ? j.N : j.red) * j.ldb;
+        } else {
+            const uint32_t g = L / (gx * gy);
+            tile_at(L - g * (gx * gy), gy, gx, tm, tn);
+            row0 = (int64_t)tm * BM;
+            rows = j.M - row0;
+            k0 = uniform64(clamped(j.offsets[g], j.tokens));
+            k1 = uniform64(clamped(j.offsets[g + 1], j.tokens));
+            if (k1 < k0) k1 = k0;
+            w.c_base = (int64_t)g * j.M * j.ldc;
+        }
+        w.row0 = (int)row0;
+        w.rows = rows < BM ? (int)rows : BM;
+        w.col0 = tn * BN;
+        const int whole = (int)((k1 - k0) / kStageK);
+        w.rest = (int)(k1 - k0) % kStageK;
+        w.nst = whole + (w.rest ? 1 : 0);
+        const int64_t cols = j.N - w.col0;
+        const int64_t a0 = (P::kAcrossA ? k0 * j.lda + row0 : row0 * j.lda + k0) * 2 - (w.rest ? stepA : 0);
+        const int64_t b0 = (P::kAcrossB ? k0 * j.ldb + w.col0 : w.col0 * j.ldb + k0) * 2 - (w.rest ? stepB : 0);
+        w.a = reinterpret_cast<const uint8_t*>(j.a) + uniform64(a0);
+        w.b = reinterpret_cast<const uint8_t*>(b) + uniform64(b0);
+#pragma unroll
+        for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset(SA{}, P::kAcrossA, wave * C::kLoadsA + q, j.lda, w.rows);
+#pragma unroll
+        for (int q = 0; q < C::kLoadsB; ++q) w.vb[q] = offset(SB{}, P::kAcrossB, wave * C::kLoadsB + q, j.ldb, cols);
+    };
+    // Load q of this wave for stage i into the slot at `slot`.
+    auto issue_one = [&](const Work& w, int q, int i, uint32_t slot) INLINE {
+        // the address in scalar registers whatever the compiler took it for
+        if (q < C::kLoadsA)
+            to_lds16(w.va[q], reinterpret_cast<const void*>(uniform64((int64_t)w.a + (int64_t)i * stepA)), ring + slot + (wave * C::kLoadsA + q) * 1024);
+        else
+            to_lds16(w.vb[q - C::kLoadsA], reinterpret_cast<const void*>(uniform64((int64_t)w.b + (int64_t)i * stepB)), ring + slot + SA::kSize + (wave * C::kLoadsB + q - C::kLoadsA) * 1024);
+    };
+    // The first stages. Places that make no whole stage are stage 0, through registers, zeros behind them: every piece (of an operand
+    // along the reduction: 8 places, a divisor of its length) is inside or outside.
+    auto fill = [&](const Work& w) INLINE {
+        for (int i = w.rest ? 1 : 0; i < kRing && i < w.nst; ++i)
+#pragma unroll
+            for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, i, i * kSlot);
+        if (!w.rest) return;
+        auto partial = [&](auto stage, bool across, const uint8_t* from, uint32_t v, int unit, uint8_t* to) INLINE {
+            using S = decltype(stage);
+            const uint32_t r = (uint32_t)unit * 16 + (lane >> 2);
+            const uint32_t k = across ? ((uint32_t)unit * 64 + lane) / (S::kSize / kStageK / 16) : ((lane & 3) ^ S::turn_row(r)) * 8;
+            u32x4_any x = {0, 0, 0, 0};
+            if (k < (uint32_t)w.rest) x = *reinterpret_cast<const u32x4_any*>(from + v);
+            *reinterpret_cast<u32x4_any*>(to + unit * 1024 + lane * 16) = x;
+        };
+        const uint8_t* const ra = w.a + (int64_t)w.nst * stepA;
+        const uint8_t* const rb = w.b + (int64_t)w.nst * stepB;
+#pragma unroll
+        for (int q = 0; q < C::kLoadsA; ++q) partial(SA{}, P::kAcrossA, ra, w.va[q], wave * C::kLoadsA + q, ring);
+#pragma unroll
+        for (int q = 0; q < C::kLoadsB; ++q) partial(SB{}, P::kAcrossB, rb, w.vb[q], wave * C::kLoadsB + q, ring + SA::kSize);
+    };
+
+    constexpr int kTiles = WTM * WTN, kOps = WTM + WTN;  // B's WTN operands, then A's WTM
+    struct Operands {
+        v8b v[kOps];
+    };
+    const uint32_t arow = (uint32_t)wm * WTM * 32, bcol = (uint32_t)wn * WTN * 32;
+    auto read_one = [&](int t, uint32_t slot, int ks, Operands& f) INLINE {
+        f.v[t] = t < WTN ? SB::read(ring + slot + SA::kSize, bcol + t * 32, ks) : SA::read(ring + slot, arow + (t - WTN) * 32, ks);
+    };
+    // B's rows are the instruction's rows, so that a lane gets runs of consecutive columns of one row of C.
+    v16f acc[WTM][WTN];
+    auto multiply_one = [&](int k, const Operands& f) INLINE {
+        const int a = k / WTN, b = k % WTN;
+        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v[b], f.v[WTN + a], acc[a][b], 0, 0, 0);
+    };
+    // Waits until at most OUTSTANDING of this wave's memory operations are in flight and its LDS reads are done, then for every
+    // wave: what all have waited for is then visible to all, and nobody reads the stage before any more.
+    auto arrive = [&](auto outstanding) INLINE {
+        asm volatile("" ::: "memory");
+        wait_loads<decltype(outstanding)::value>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // A stage: the first half's products while the second half's operands are read; then, past the barrier that lets the next
+    // stage be read and this one be overwritten, the second half's products while the next stage's first half is read and the
+    // stage kRing ahead (stage li of tile lw, if `loads`) is loaded. The order is pinned: one product, then what its 32 cycles cover.
+    constexpr int kOpsPer = (kOps + kTiles - 1) / kTiles, kLoadsPer = (C::kWaveLoads + kTiles - 1) / kTiles;
+    Operands f0, f1;
+    auto stage = [&](uint32_t cur, uint32_t next, auto outstanding, const Work& lw, int li, auto loads) INLINE {
+        constexpr bool kMore = decltype(outstanding)::value >= 0, kLoads = decltype(loads)::value;
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k) {
+            multiply_one(k, f0);
+#pragma unroll
+            for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t) read_one(t, cur, 1, f1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (kMore) arrive(outstanding);
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k) {
+            multiply_one(k, f1);
+            if constexpr (kMore) {
+#pragma unroll
+                for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t) read_one(t, next, 0, f0);
+            }
+            if constexpr (kLoads) {
+#pragma unroll
+                for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    constexpr int kStores = Stored<OUT, WTM, WTN>::kStores;
+    auto store = [&](const Work& w, auto inside) INLINE {
+        store_tile<OUT, WTM, WTN, STREAM, decltype(inside)::value>(acc, j.c, w.c_base, w.row0, w.col0, j.ldc, w.rows, j.N, wm, wn);
+    };
+    auto clear = [&] INLINE {
+#pragma unroll
+        for (int a = 0; a < WTM; ++a)
+#pragma unroll
+            for (int b = 0; b < WTN; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    };
+    auto is_inside = [&](const Work& w) INLINE { return w.rows == BM && (int64_t)w.col0 + BN <= j.N; };
+    constexpr int L1 = C::kWaveLoads;
+    uint32_t L = blockIdx.x;
+    if (L >= total) return;
+    Work w;
+    locate(L, w);
+    fill(w);
+    uint32_t cur = 0, next = kSlot;
+    auto advance = [&] INLINE {
+        cur = next;
+        next = next == (kRing - 1) * kSlot ? 0 : next + kSlot;
+    };
+    auto begin = [&] INLINE {
+#pragma unroll
+        for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, f0);
+    };
+    using std::integral_constant;
+
+    // The workgroup's tiles, all of as many stages: those of one tile follow those of the one before without a gap. Its last kRing
+    // stages load the next tile's first ones (after the last tile its own first ones again, which nobody reads: a branch here
+    // makes the compiler spill the sums), and the last reads the first's operands. A tile's stores are then younger than those
+    // loads, and memory operations complete in order, so the next tile's first waits count them in instead of waiting for them.
+    if constexpr (P::kRagged) {
+        if (w.nst >= 2 * kRing && w.rest == 0) {
+            arrive(integral_constant<int, (kRing - 1) * L1>{});
+            begin();
+            bool behind = false;  // kStores stores were issued after the loads
+            while (true) {
+                clear();
+                L += gridDim.x;
+                const bool more = L < total;
+                Work n = w;
+                if (more) locate(L, n);
+                int i = 0;
+                if (behind) {
+                    for (; i < kRing - 1; ++i) {
+                        stage(cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, std::true_type{});
+                        advance();
+                    }
+                }
+                constexpr integral_constant<int, (kRing - 2) * L1> kept{};
+                for (; i + kRing < w.nst; ++i) {
+                    stage(cur, next, kept, w, i + kRing, std::true_type{});
+                    advance();
+                }
+#pragma unroll
+                for (int q = 0; q < kRing; ++q) {
+                    stage(cur, next, kept, n, q, std::true_type{});
+                    advance();
+                }
+                asm volatile("" ::: "memory");
+                behind = is_inside(w);
+                if (behind) store(w, std::true_type{});
+                else store(w, std::false_type{});
+                if (!more) {
+                    wait_loads<0>();  // the LDS must not be another workgroup's before they have landed
+                    return;
+                }
+                w = n;
+            }
+        }
+    }
+
+    // Tiles of different length, or of few stages: one after the other.
+    while (true) {
+        clear();
+        if (w.nst > 0) {
+            cur = 0, next = kSlot;
+            arrive(integral_constant<int, 0>{});
+            begin();
+            int i = 0;
+            for (; i + kRing < w.nst; ++i) {
+                stage(cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
+                advance();
+            }
+            for (; i + 1 < w.nst; ++i) {  // the loads are on their way: wait for all of them
+                stage(cur, next, integral_constant<int, 0>{}, w, 0, std::false_type{});
+                advance();
+            }
+            stage(cur, next, integral_constant<int, -1>{}, w, 0, std::false_type{});
+        }
+        L += gridDim.x;
+        const bool more = L < total;
+        const Work done = w;
+        if (more) {
+            locate(L, w);
+            __syncthreads();  // every wave has read the last stage
+            fill(w);
+        }
+        asm volatile("" ::: "memory");
+        if (is_inside(done)) store(done, std::true_type{});
+        else store(done, std::false_type{});
+        if (!more) return;
+    }
+}
+
+using Tile256 = Tile<4, 2, 2, 4, 4, 1>;  // 256 x 256: 8 waves of 128 x 64, two per SIMD
+using Tile128 = Tile<2, 2, 2, 2, 4, 2>;  // 128 x 128: 4 waves of 64 x 64, two workgroups per CU
+
 // Tile rows that a launch provides for; ragged rows: every group may end in a partial tile.
 int64_t tile_rows(const Bf16GemmJob& j, int bm) {
     return j.pass != kBf16BwdDw ? (j.tokens + bm - 1) / bm + j.G : (j.M + bm - 1) / bm;
@@ -268,11 +569,32 @@ int64_t grid_tiles(const Bf16GemmJob& j, int bm, int bn) {
     return tile_rows(j, bm) * ((j.N + bn - 1) / bn) * (j.pass == kBf16BwdDw ? j.G : 1);
 }
 
-template <int OUT>
-hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
-    const int64_t tiles = grid_tiles(j, kAnyTile, kAnyTile);
-    if (tiles == 0) return hipSuccess;
+// Whether every row is whole 16-byte pieces, and a tile's rows (or a stage's) lie within 32 bits.
+bool pieces(const Bf16GemmJob& j) {
+    constexpr int64_t kMost = int64_t(1) << 22;
+    const int64_t wide_a = j.pass == kBf16BwdDw ? j.M : j.red, wide_b = j.pass == kBf16FwdY ? j.red : j.N;
+    return !j.b8 && wide_a % 8 == 0 && wide_b % 8 == 0 && j.lda % 8 == 0 && j.ldb % 8 == 0 && j.lda <= kMost && j.ldb <= kMost &&
+           reinterpret_cast<uintptr_t>(j.a) % 16 == 0 && reinterpret_cast<uintptr_t>(j.b) % 16 == 0;
+}
+
+template <int OUT, class C, bool STREAM>
+hipError_t launch_tile(const Bf16GemmJob& j, hipStream_t s) {
+    int64_t tiles = grid_tiles(j, C::BM, C::BN);
+    // One workgroup per tile where tiles differ in length (ragged reduction: the next free CU takes the next one); otherwise the
+    // workgroups that are resident take the tiles in turn.
+    if (j.pass != kBf16BwdDw && tiles > C::kResident) tiles = C::kResident;
     const unsigned n = (unsigned)tiles;
+    switch (j.pass) {
+        case kBf16FwdY: gemm_bf16_kernel<OUT, C, kBf16FwdY, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
+        case kBf16BwdDx: gemm_bf16_kernel<OUT, C, kBf16BwdDx, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
+        default: gemm_bf16_kernel<OUT, C, kBf16BwdDw, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
+    }
+    return hipGetLastError();
+}
+
+template <int OUT>
+hipError_t launch_any(const Bf16GemmJob& j, hipStream_t s) {
+    const unsigned n = (unsigned)grid_tiles(j, kAnyTile, kAnyTile);
     switch (j.pass) {
         case kBf16FwdY: gemm_bf16_any_kernel<OUT, kBf16FwdY, false><<<n, kAnyThreads, 0, s>>>(j); break;
         case kBf16BwdDx: gemm_bf16_any_kernel<OUT, kBf16BwdDx, false><<<n, kAnyThreads, 0, s>>>(j); break;
@@ -281,6 +603,15 @@ hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
             else gemm_bf16_any_kernel<OUT, kBf16BwdDw, false><<<n, kAnyThreads, 0, s>>>(j);
     }
     return hipGetLastError();
+}
+
+template <int OUT>
+hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
+    if (grid_tiles(j, kAnyTile, kAnyTile) == 0) return hipSuccess;
+    if (!pieces(j)) return launch_any<OUT>(j, s);
+    // The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
+    // us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
+    return grid_tiles(j, Tile256::BM, Tile256::BN) >= 256 ? launch_tile<OUT, Tile256, false>(j, s) : launch_tile<OUT, Tile128, false>(j, s);
 }
 
 }  // namespace

@@ -25,7 +25,6 @@ namespace ufp4 {
 
 namespace {
 
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 
@@ -361,99 +360,9 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_mxfp4_kernel(MxGe
         }
     };
 
-    // A lane holds columns 8q + 4h .. + 3 (q < 4) of row l32 of each 32 x 32 tile. Lanes trade until a store of 16 bytes a lane
-    // writes whole 128-byte lines (8 rows of them; pieces of 32 or 64 bytes cost the memory system up to 1.6 times as long):
-    //   bf16: the halves of the wave, so that a lane has eight consecutive columns; then the 16-lane rows of the wave (16 rows x
-    //   64 bytes), then the 8-lane halves of those with the neighbouring tile; fp32: the same without the first step, the
-    //   neighbour being the tile's other 16 columns. kStores stores a wave for a tile inside the output.
-    constexpr int kElems = OUT == kOutF32 ? 4 : 8, kStores = kTiles * 32 / kElems / 2;
-    constexpr bool kLine = OUT == kOutF32 || WTN % 2 == 0;  // a lone bf16 tile stays at 64 bytes
+    constexpr int kStores = Stored<OUT, WTM, WTN>::kStores;
     auto store = [&](const Work& w, auto inside) INLINE {
-        const int64_t N = j.N;
-        // one store: v, at row lr and column col of the tile; at the output's right edge the pieces that are inside are still whole
-        auto put = [&](const uint32_t (&v)[4], int lr, int col) INLINE {
-            const int64_t off = w.c_base + (int64_t)(w.row0 + lr) * j.ldc + w.col0 + col;
-            const int64_t left = N - w.col0 - col;  // columns from this lane's first
-            if (decltype(inside)::value || (lr < w.rows && left >= kElems)) {
-                const u32x4_any x = {v[0], v[1], v[2], v[3]};
-                u32x4_any* const to = reinterpret_cast<u32x4_any*>(static_cast<uint8_t*>(j.c) + off * (OUT == kOutF32 ? 4 : 2));
-                if constexpr (STREAM) __builtin_nontemporal_store(x, to);
-                else *to = x;
-            } else if (lr < w.rows) {
-#pragma unroll
-                for (int e = 0; e < kElems; ++e) {
-                    if (e >= left) continue;
-                    if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[off + e] = __uint_as_float(v[e]);
-                    else static_cast<uint16_t*>(j.c)[off + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-                }
-            }
-        };
-        // 16 rows x 64 bytes: u = 0, 1 the tile's rows 16u ..; the wave's 16-lane rows hold the pieces 0, 2, 1, 3 of the 64 bytes
-        // (fp32: half `part` of the tile's columns)
-        auto quarter = [&](const v16f& c, int part, uint32_t (&v)[2][4]) INLINE {
-            uint32_t x[4], y[4];
-            if constexpr (OUT == kOutF32) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    x[t] = __float_as_uint(c[8 * part + t]);
-                    y[t] = __float_as_uint(c[8 * part + 4 + t]);
-                }
-            } else {
-                auto pair = [&](int i) INLINE {
-                    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)c[i]) |
-                           (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)c[i + 1]) << 16;
-                };
-                const auto e = __builtin_amdgcn_permlane32_swap(pair(0), pair(4), false, false);
-                const auto f = __builtin_amdgcn_permlane32_swap(pair(2), pair(6), false, false);
-                const auto g = __builtin_amdgcn_permlane32_swap(pair(8), pair(12), false, false);
-                const auto k = __builtin_amdgcn_permlane32_swap(pair(10), pair(14), false, false);
-                x[0] = e[0], x[1] = f[0], x[2] = e[1], x[3] = f[1];
-                y[0] = g[0], y[1] = k[0], y[2] = g[1], y[3] = k[1];
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const auto r = __builtin_amdgcn_permlane16_swap(x[t], y[t], false, false);
-                v[0][t] = r[0];
-                v[1][t] = r[1];
-            }
-        };
-        const int piece = ((lane >> 4) & 1) * 2 + (lane >> 5);  // of 64 bytes
-        constexpr int kSteps = kLine ? (OUT == kOutF32 ? WTN : WTN / 2) : WTN;
-#pragma unroll
-        for (int a = 0; a < WTM; ++a) {
-            const int lr = (wm * WTM + a) * 32;
-#pragma unroll
-            for (int b = 0; b < kSteps; ++b) {
-                uint32_t v[2][4];
-                if constexpr (kLine) {
-                    uint32_t n[2][4];
-                    if constexpr (OUT == kOutF32) {
-                        quarter(acc[a][b], 0, v);
-                        quarter(acc[a][b], 1, n);
-                    } else {
-                        quarter(acc[a][2 * b], 0, v);
-                        quarter(acc[a][2 * b + 1], 0, n);
-                    }
-                    const int col = (wn * WTN + (OUT == kOutF32 ? b : 2 * b)) * 32 + (lane & 8) / 8 * 4 * kElems + piece * kElems;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        uint32_t lo[4], hi[4];  // rows 0-7 and 8-15 of the sixteen: lanes 8-15 of each sixteen have the neighbour's
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            constexpr int kRor8 = 0x128;  // rotate each sixteen lanes by eight
-                            lo[t] = __builtin_amdgcn_update_dpp(v[u][t], n[u][t], kRor8, 0xF, 0xC, false);
-                            hi[t] = __builtin_amdgcn_update_dpp(n[u][t], v[u][t], kRor8, 0xF, 0x3, false);
-                        }
-                        put(lo, lr + u * 16 + (lane & 7), col);
-                        put(hi, lr + u * 16 + 8 + (lane & 7), col);
-                    }
-                } else {
-                    quarter(acc[a][b], 0, v);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) put(v[u], lr + u * 16 + (lane & 15), (wn * WTN + b) * 32 + piece * kElems);
-                }
-            }
-        }
+        store_tile<OUT, WTM, WTN, STREAM, decltype(inside)::value>(acc, j.c, w.c_base, w.row0, w.col0, j.ldc, w.rows, j.N, wm, wn);
     };
 
     auto clear = [&] INLINE {
