@@ -25,24 +25,40 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 
 #define INLINE __attribute__((always_inline))
 
-constexpr int kStageK = 32;  // of the reduction per stage: two matrix instructions
-
-// One stage of an operand in LDS: ROWS x kStageK values.
-//   along the reduction: row r has 64 bytes, its 16-byte piece p (8 places of the reduction) at piece p ^ f(r);
-//   across it: place k of the reduction has 2 ROWS bytes, their 32-byte segment s (16 rows) at segment s ^ f(k).
-// Both f make what the lanes of one read touch at a time lie in different banks, whether 128 or 256 bytes are served together.
-template <int ROWS, bool ACROSS>
+// One stage of an operand in LDS: ROWS x K values, K places of the reduction (16 a matrix instruction).
+//   along the reduction: row r has 2 K bytes, its 16-byte piece p (8 places of the reduction) at piece p ^ turn_row(r);
+//   across it: place k of the reduction has 2 ROWS bytes, their 32-byte segment s (16 rows) at segment s ^ turn_k(k).
+// Both turns make what the lanes of one read touch at a time lie in different banks, whether 128 or 256 bytes are served together
+// (measured: no conflict).
+template <int ROWS_, int K_, bool ACROSS>
 struct Stage {
-    static constexpr uint32_t kSize = ROWS * kStageK * 2;
-    static constexpr int kPieces = ROWS * kStageK / 8;  // 16 bytes each
-    static __device__ __forceinline__ uint32_t turn_row(uint32_t r) { return ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2); }
-    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return ROWS < 128 ? k & 3 : (k & 3) | (k >> 1 & 4); }
+    static constexpr int ROWS = ROWS_, K = K_;
+    static constexpr bool kAcross = ACROSS;
+    static constexpr uint32_t kSize = ROWS * K * 2;
+    static constexpr uint32_t kRowPieces = K / 8, kPlacePieces = ROWS / 8;
+    static __device__ __forceinline__ uint32_t turn_row(uint32_t r) {
+        static_assert(K == 32 || K == 64, "");
+        return K == 32 ? ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2) : (r ^ r >> 3) & 7;
+    }
+    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return ROWS < 128 ? k & 2 : (k << 1 & 6) | (k >> 1 & 1); }
 
     // Byte address of the piece of row r with places 8 p .. of the reduction.
-    static __device__ __forceinline__ uint32_t along(uint32_t r, uint32_t p) { return r * 64 + (p ^ turn_row(r)) * 16; }
+    static __device__ __forceinline__ uint32_t along(uint32_t r, uint32_t p) { return r * (K * 2) + (p ^ turn_row(r)) * 16; }
     // Byte address of rows 8 s .. + 7 at place k.
     static __device__ __forceinline__ uint32_t across(uint32_t k, uint32_t s) {
         return k * (ROWS * 2) + ((s >> 1 ^ turn_k(k)) * 2 + (s & 1)) * 16;
+    }
+
+    // What the i-th 16 bytes of the stage hold: rows from `row` at place `k` (one row and 8 places, or 8 rows and one place).
+    static __device__ __forceinline__ void piece(uint32_t i, uint32_t& row, uint32_t& k) {
+        if constexpr (ACROSS) {
+            k = i / kPlacePieces;
+            const uint32_t at = i % kPlacePieces;
+            row = ((at >> 1 ^ turn_k(k)) * 2 + (at & 1)) * 8;
+        } else {
+            row = i / kRowPieces;
+            k = (i % kRowPieces ^ turn_row(row)) * 8;
+        }
     }
 
     // The operand of 32 rows from row0 at places 16 ks .. + 15: lane l has row l % 32 and places 8 (l / 32) .. of those.
@@ -117,14 +133,14 @@ struct Pass {
 // ------------------------------------------------------------------------------------------------
 // Any size, stride and alignment: pieces go through registers, where what lies outside is zeroed.
 // ------------------------------------------------------------------------------------------------
-constexpr int kAnyTile = 128, kAnyThreads = 256;
+constexpr int kAnyTile = 128, kAnyThreads = 256, kAnyK = 32;
 
 template <int OUT, int PASS, bool SAVED>
 __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJob j) {
     using P = Pass<PASS>;
     constexpr int BM = kAnyTile, BN = kAnyTile;
-    using SA = Stage<BM, P::kAcrossA>;
-    using SB = Stage<BN, P::kAcrossB>;
+    using SA = Stage<BM, kAnyK, P::kAcrossA>;
+    using SB = Stage<BN, kAnyK, P::kAcrossB>;
     constexpr uint32_t kSlot = SA::kSize + SB::kSize;
     __shared__ __align__(16) uint8_t ring[2 * kSlot];
     __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
@@ -159,8 +175,8 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     const int64_t col0 = (int64_t)tn * BN, cols = j.N - col0;
 
     // Piece q of this thread: 16 bytes of operand A (B) of the stage from place k on; zero outside.
-    constexpr int kEach = SA::kPieces / kAnyThreads;
-    static_assert(SA::kPieces == SB::kPieces, "");
+    constexpr int kEach = SA::kSize / 16 / kAnyThreads;
+    static_assert(SA::kSize == SB::kSize, "");
     auto fetch = [&](const uint16_t* p, int64_t ld, bool across, int64_t first, int64_t have, int64_t k, int q) INLINE {
         const int i = q * kAnyThreads + tid;
         u32x4_any zero = {0, 0, 0, 0};
@@ -208,7 +224,7 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     };
     if (k0 < k1) load(k0);
     uint32_t slot = 0;
-    for (int64_t k = k0; k < k1; k += kStageK) {
+    for (int64_t k = k0; k < k1; k += kAnyK) {
         uint8_t* const sa = ring + slot;
         uint8_t* const sb = sa + SA::kSize;
 #pragma unroll
@@ -223,7 +239,7 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
             for (int q = 0; q < kEach; ++q) *reinterpret_cast<u32x4_any*>(sb + place(P::kAcrossB, q)) = rb[q];
         }
         __syncthreads();  // two slots: the next stage is written to the other one, which everyone has read
-        if (k + kStageK < k1) load(k + kStageK);
+        if (k + kAnyK < k1) load(k + kAnyK);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             v8b fa[2], fb[2];
@@ -262,35 +278,75 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
 // Rows of whole 16-byte pieces: memory to LDS without registers between.
 // ------------------------------------------------------------------------------------------------
 
-// WM x WN waves, each with WTM x WTN matrix tiles of 32 x 32 outputs; RING stages in LDS; PER_CU workgroups on a CU.
-template <int WTM_, int WTN_, int WM_, int WN_, int RING_, int PER_CU>
+// WM x WN waves, each with WTM x WTN matrix tiles of 32 x 32 outputs; RING stages of K places in LDS; PER_CU workgroups on a CU.
+template <int WTM_, int WTN_, int WM_, int WN_, int K_, int RING_, int PER_CU>
 struct Tile {
-    static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, kRing = RING_;
+    static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, K = K_, kRing = RING_;
     static constexpr int BM = 32 * WTM * WM, BN = 32 * WTN * WN;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int kResident = 256 * PER_CU;    // workgroups on 256 CUs
     static constexpr int kPerEU = PER_CU * kWaves / 4;  // waves per SIMD that the registers have to allow
-    static constexpr int kLoadsA = BM / 16 / kWaves, kLoadsB = BN / 16 / kWaves;  // 1 KiB loads of a stage, a wave
+    static constexpr int kLoadsA = BM * K / 512 / kWaves, kLoadsB = BN * K / 512 / kWaves;  // 1 KiB loads of a stage, a wave
     static constexpr int kWaveLoads = kLoadsA + kLoadsB;
-    static_assert(kLoadsA * 16 * kWaves == BM && kLoadsB * 16 * kWaves == BN, "every wave issues the same loads");
+    static_assert(kLoadsA * 512 * kWaves == BM * K && kLoadsB * 512 * kWaves == BN * K, "every wave issues the same loads");
     static_assert(kWaveLoads * (kRing - 1) + 32 < 64, "vmcnt has six bits");
 };
 
-// The pipeline: a ring of stages in LDS, filled kRing - 1 ahead by direct-to-LDS loads; each wave keeps two sets of operands in
-// registers: while the matrix core works on one half of a stage, the other half (or, past the barrier, the next stage's first
-// half) is read from LDS. A reduction's last places that make no whole stage are multiplied first, by operands that the wave loads from
-// memory itself while the ring fills.
+// The group with the `rank`-th longest reduction (of equally long ones the lower first): long tiles that begin last would run alone at
+// the end. By every wave for itself: the length by its bits, from counts of groups at least as long, then the place among equals.
+__device__ __forceinline__ int by_length(const Bf16GemmJob& j, uint32_t rank) {
+    const int lane = threadIdx.x & 63, rounds = (j.G + 63) / 64;
+    auto length = [&](int g) -> int64_t {
+        if (g >= j.G) return -1;
+        const int64_t n = clamped(j.offsets[g + 1], j.tokens) - clamped(j.offsets[g], j.tokens);
+        return n < 0 ? 0 : n;
+    };
+    const int64_t mine = length(lane);  // of the first 64 groups; the others' are read again each time
+    auto count = [&](int64_t least) {   // groups of at least this length
+        int n = __popcll(__ballot(mine >= least));
+        for (int r = 1; r < rounds; ++r) n += __popcll(__ballot(length(r * 64 + lane) >= least));
+        return (uint32_t)n;
+    };
+    int64_t v = 0;  // the largest length that more than `rank` groups reach
+    for (int b = 31 - __builtin_clz((uint32_t)j.tokens | 1); b >= 0; --b)
+        if (count(v + (int64_t(1) << b)) > rank) v += int64_t(1) << b;
+    uint32_t place = rank - count(v + 1);  // among the groups of length v
+    for (int r = 0; r < rounds; ++r) {
+        uint64_t same = __ballot((r == 0 ? mine : length(r * 64 + lane)) == v);
+        const uint32_t n = (uint32_t)__popcll(same);
+        if (place >= n) {
+            place -= n;
+            continue;
+        }
+        for (; place > 0; --place) same &= same - 1;
+        return uniform(r * 64 + __builtin_ctzll(same));
+    }
+    return 0;
+}
+
+// The pipeline: a ring of stages in LDS, filled by direct-to-LDS loads; each wave keeps two sets of operands in registers: while the
+// matrix core works on one step of a stage, the next step's operands (past the barrier, the next stage's first) are read from LDS.
 template <int OUT, class C, int PASS, bool STREAM>
 __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16GemmJob j) {
     using P = Pass<PASS>;
     constexpr int BM = C::BM, BN = C::BN, WTM = C::WTM, WTN = C::WTN, kRing = C::kRing;
-    using SA = Stage<BM, P::kAcrossA>;
-    using SB = Stage<BN, P::kAcrossB>;
+    using SA = Stage<BM, C::K, P::kAcrossA>;
+    using SB = Stage<BN, C::K, P::kAcrossB>;
     constexpr uint32_t kSlot = SA::kSize + SB::kSize;
     __shared__ __align__(16) uint8_t ring[kRing * kSlot];
     __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int wm = (int)((unsigned)wave / C::WN), wn = (int)((unsigned)wave % C::WN), h = lane >> 5, l32 = lane & 31;
+    // Where a SIMD has two waves of eight (w and w + 4), they differ in both halves of the tile, so that a tile which lies half outside
+    // of the output leaves each SIMD one wave with work.
+    int wm, wn;
+    if constexpr (C::kWaves == 8) {
+        static_assert(C::kWaves != 8 || (C::WM == 2 && C::WN == 4), "");
+        wm = (wave >> 1 ^ wave >> 2) & 1;
+        wn = (wave & 1) | (wave >> 1 & 2);
+    } else {
+        wm = (int)((unsigned)wave / C::WN);
+        wn = (int)((unsigned)wave % C::WN);
+    }
     const uint32_t gx = (uint32_t)((j.N + BN - 1) / BN);
     uint32_t gy, total;
     if constexpr (P::kRagged) {
@@ -312,22 +368,17 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         int nst, rest;  // stages of the reduction; places of it that make no whole one, which are then stage 0
         int row0, rows, col0;
         int64_t c_base;
+        bool idle;  // this wave's part is outside of the output: it loads with the others, and multiplies nothing
     };
-    const uint32_t stepA = P::kAcrossA ? (uint32_t)(kStageK * 2 * j.lda) : kStageK * 2, stepB = P::kAcrossB ? (uint32_t)(kStageK * 2 * j.ldb) : kStageK * 2;
+    const uint32_t stepA = P::kAcrossA ? (uint32_t)(C::K * 2 * j.lda) : C::K * 2, stepB = P::kAcrossB ? (uint32_t)(C::K * 2 * j.ldb) : C::K * 2;
     // Lane's piece of load q (unit wave * loads + q of the stage: 64 pieces in the LDS's order), as an offset from the operand's first
     // row and place. Rows past the last one are replaced by it: they only feed outputs that are not stored.
-    auto offset = [&](auto stage, bool across, int unit, int64_t ld, int64_t have) INLINE {
+    auto offset = [&](auto stage, int unit, int64_t ld, int64_t have) INLINE {
         using S = decltype(stage);
-        constexpr uint32_t kRow = S::kSize / kStageK / 2;  // rows of the operand's tile
-        if (across) {
-            constexpr uint32_t kEach = kRow / 8;  // pieces of a place
-            const uint32_t i = (uint32_t)unit * 64 + lane, k = i / kEach, at = i % kEach;
-            uint32_t r = ((at >> 1 ^ S::turn_k(k)) * 2 + (at & 1)) * 8;
-            r = r < have ? r : (uint32_t)have - 8;
-            return (uint32_t)(k * (uint32_t)ld + r) * 2;
-        }
-        const uint32_t r = (uint32_t)unit * 16 + (lane >> 2), p = (lane & 3) ^ S::turn_row(r);
-        return (uint32_t)((r < have ? r : (uint32_t)have - 1) * (uint32_t)ld + p * 8) * 2;
+        uint32_t r, k;
+        S::piece((uint32_t)unit * 64 + lane, r, k);
+        if (S::kAcross) return (k * (uint32_t)ld + (r < have ? r : (uint32_t)have - 8)) * 2;
+        return ((r < have ? r : (uint32_t)have - 1) * (uint32_t)ld + k) * 2;
     };
     auto locate = [&](uint32_t L, Work& w) INLINE {
         int tm, tn;
@@ -341,8 +392,8 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
             rows = uniform(groups.rows[g]) - (int64_t)lt * BM;
             b += (int64_t)g * (PASS == kBf16FwdY ? j.N : j.red) * j.ldb;
         } else {
-            const uint32_t g = L / (gx * gy);
-            tile_at(L - g * (gx * gy), gy, gx, tm, tn);
+            const uint32_t rank = L / (gx * gy), g = by_length(j, rank);
+            tile_at(L - rank * (gx * gy), gy, gx, tm, tn);
             row0 = (int64_t)tm * BM;
             rows = j.M - row0;
             k0 = uniform64(clamped(j.offsets[g], j.tokens));
@@ -353,18 +404,19 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         w.row0 = (int)row0;
         w.rows = rows < BM ? (int)rows : BM;
         w.col0 = tn * BN;
-        const int whole = (int)((k1 - k0) / kStageK);
-        w.rest = (int)(k1 - k0) % kStageK;
+        const int whole = (int)((k1 - k0) / C::K);
+        w.rest = (int)(k1 - k0) % C::K;
         w.nst = whole + (w.rest ? 1 : 0);
         const int64_t cols = j.N - w.col0;
+        w.idle = wm * WTM * 32 >= rows || wn * WTN * 32 >= cols;
         const int64_t a0 = (P::kAcrossA ? k0 * j.lda + row0 : row0 * j.lda + k0) * 2 - (w.rest ? stepA : 0);
         const int64_t b0 = (P::kAcrossB ? k0 * j.ldb + w.col0 : w.col0 * j.ldb + k0) * 2 - (w.rest ? stepB : 0);
         w.a = reinterpret_cast<const uint8_t*>(j.a) + uniform64(a0);
         w.b = reinterpret_cast<const uint8_t*>(b) + uniform64(b0);
 #pragma unroll
-        for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset(SA{}, P::kAcrossA, wave * C::kLoadsA + q, j.lda, w.rows);
+        for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset(SA{}, wave * C::kLoadsA + q, j.lda, w.rows);
 #pragma unroll
-        for (int q = 0; q < C::kLoadsB; ++q) w.vb[q] = offset(SB{}, P::kAcrossB, wave * C::kLoadsB + q, j.ldb, cols);
+        for (int q = 0; q < C::kLoadsB; ++q) w.vb[q] = offset(SB{}, wave * C::kLoadsB + q, j.ldb, cols);
     };
     // Load q of this wave for stage i into the slot at `slot`.
     auto issue_one = [&](const Work& w, int q, int i, uint32_t slot) INLINE {
@@ -381,10 +433,9 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
 #pragma unroll
             for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, i, i * kSlot);
         if (!w.rest) return;
-        auto partial = [&](auto stage, bool across, const uint8_t* from, uint32_t v, int unit, uint8_t* to) INLINE {
-            using S = decltype(stage);
-            const uint32_t r = (uint32_t)unit * 16 + (lane >> 2);
-            const uint32_t k = across ? ((uint32_t)unit * 64 + lane) / (S::kSize / kStageK / 16) : ((lane & 3) ^ S::turn_row(r)) * 8;
+        auto partial = [&](auto stage, const uint8_t* from, uint32_t v, int unit, uint8_t* to) INLINE {
+            uint32_t r, k;
+            decltype(stage)::piece((uint32_t)unit * 64 + lane, r, k);
             u32x4_any x = {0, 0, 0, 0};
             if (k < (uint32_t)w.rest) x = *reinterpret_cast<const u32x4_any*>(from + v);
             *reinterpret_cast<u32x4_any*>(to + unit * 1024 + lane * 16) = x;
@@ -392,9 +443,9 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         const uint8_t* const ra = w.a + (int64_t)w.nst * stepA;
         const uint8_t* const rb = w.b + (int64_t)w.nst * stepB;
 #pragma unroll
-        for (int q = 0; q < C::kLoadsA; ++q) partial(SA{}, P::kAcrossA, ra, w.va[q], wave * C::kLoadsA + q, ring);
+        for (int q = 0; q < C::kLoadsA; ++q) partial(SA{}, ra, w.va[q], wave * C::kLoadsA + q, ring);
 #pragma unroll
-        for (int q = 0; q < C::kLoadsB; ++q) partial(SB{}, P::kAcrossB, rb, w.vb[q], wave * C::kLoadsB + q, ring + SA::kSize);
+        for (int q = 0; q < C::kLoadsB; ++q) partial(SB{}, rb, w.vb[q], wave * C::kLoadsB + q, ring + SA::kSize);
     };
 
     constexpr int kTiles = WTM * WTN, kOps = WTM + WTN;  // B's WTN operands, then A's WTM
@@ -420,33 +471,35 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         asm volatile("" ::: "memory");
     };
 
-    // A stage: the first half's products while the second half's operands are read; then, past the barrier that lets the next
-    // stage be read and this one be overwritten, the second half's products while the next stage's first half is read and the
-    // stage kRing ahead (stage li of tile lw, if `loads`) is loaded. The order is pinned: one product, then what its 32 cycles cover.
+    // A stage, K / 16 steps: the products of one step while the next step's operands are read. Before the last step's products comes the
+    // barrier that lets the next stage be read and this one be overwritten: they cover the reads of the next stage's first operands and
+    // the loads of the stage kRing ahead (stage li of tile lw, if `loads`). The order is pinned: one product, then what its 32 cycles
+    // cover. OUTSTANDING: as of arrive() for the next stage, -1 if there is none.
+    constexpr int kSteps = C::K / 16;
     constexpr int kOpsPer = (kOps + kTiles - 1) / kTiles, kLoadsPer = (C::kWaveLoads + kTiles - 1) / kTiles;
-    Operands f0, f1;
-    auto stage = [&](uint32_t cur, uint32_t next, auto outstanding, const Work& lw, int li, auto loads) INLINE {
+    Operands f[2];
+    auto stage = [&](auto idle, uint32_t cur, uint32_t next, auto outstanding, const Work& lw, int li, auto loads) INLINE {
         constexpr bool kMore = decltype(outstanding)::value >= 0, kLoads = decltype(loads)::value;
 #pragma unroll
-        for (int k = 0; k < kTiles; ++k) {
-            multiply_one(k, f0);
+        for (int ks = 0; ks < kSteps; ++ks) {
+            const bool last = ks == kSteps - 1;
+            if constexpr (kMore)
+                if (last) arrive(outstanding);
 #pragma unroll
-            for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t) read_one(t, cur, 1, f1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (kMore) arrive(outstanding);
+            for (int k = 0; k < kTiles; ++k) {
+                if constexpr (!decltype(idle)::value) multiply_one(k, f[ks & 1]);
+                if (last ? kMore : !decltype(idle)::value) {
 #pragma unroll
-        for (int k = 0; k < kTiles; ++k) {
-            multiply_one(k, f1);
-            if constexpr (kMore) {
+                    for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t)
+                        read_one(t, last ? next : cur, last ? 0 : ks + 1, f[(ks + 1) & 1]);
+                }
+                if constexpr (kLoads) {
+                    if (last)
 #pragma unroll
-                for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t) read_one(t, next, 0, f0);
+                        for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (kLoads) {
-#pragma unroll
-                for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur);
-            }
-            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -476,7 +529,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     };
     auto begin = [&] INLINE {
 #pragma unroll
-        for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, f0);
+        for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, f[0]);
     };
     using std::integral_constant;
 
@@ -496,22 +549,26 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
                 Work n = w;
                 if (more) locate(L, n);
                 int i = 0;
-                if (behind) {
-                    for (; i < kRing - 1; ++i) {
-                        stage(cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, std::true_type{});
+                auto run = [&](auto idle) INLINE {
+                    if (behind) {
+                        for (; i < kRing - 1; ++i) {
+                            stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, std::true_type{});
+                            advance();
+                        }
+                    }
+                    constexpr integral_constant<int, (kRing - 2) * L1> kept{};
+                    for (; i + kRing < w.nst; ++i) {
+                        stage(idle, cur, next, kept, w, i + kRing, std::true_type{});
                         advance();
                     }
-                }
-                constexpr integral_constant<int, (kRing - 2) * L1> kept{};
-                for (; i + kRing < w.nst; ++i) {
-                    stage(cur, next, kept, w, i + kRing, std::true_type{});
-                    advance();
-                }
 #pragma unroll
-                for (int q = 0; q < kRing; ++q) {
-                    stage(cur, next, kept, n, q, std::true_type{});
-                    advance();
-                }
+                    for (int q = 0; q < kRing; ++q) {
+                        stage(idle, cur, next, kept, n, q, std::true_type{});
+                        advance();
+                    }
+                };
+                if (w.idle) run(std::true_type{});
+                else run(std::false_type{});
                 asm volatile("" ::: "memory");
                 behind = is_inside(w);
                 if (behind) store(w, std::true_type{});
@@ -532,16 +589,20 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
             cur = 0, next = kSlot;
             arrive(integral_constant<int, 0>{});
             begin();
-            int i = 0;
-            for (; i + kRing < w.nst; ++i) {
-                stage(cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
-                advance();
-            }
-            for (; i + 1 < w.nst; ++i) {  // the loads are on their way: wait for all of them
-                stage(cur, next, integral_constant<int, 0>{}, w, 0, std::false_type{});
-                advance();
-            }
-            stage(cur, next, integral_constant<int, -1>{}, w, 0, std::false_type{});
+            auto run = [&](auto idle) INLINE {
+                int i = 0;
+                for (; i + kRing < w.nst; ++i) {
+                    stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
+                    advance();
+                }
+                for (; i + 1 < w.nst; ++i) {  // the loads are on their way: wait for all of them
+                    stage(idle, cur, next, integral_constant<int, 0>{}, w, 0, std::false_type{});
+                    advance();
+                }
+                stage(idle, cur, next, integral_constant<int, -1>{}, w, 0, std::false_type{});
+            };
+            if (w.idle) run(std::true_type{});
+            else run(std::false_type{});
         }
         L += gridDim.x;
         const bool more = L < total;
@@ -558,8 +619,17 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     }
 }
 
-using Tile256 = Tile<4, 2, 2, 4, 4, 1>;  // 256 x 256: 8 waves of 128 x 64, two per SIMD
-using Tile128 = Tile<2, 2, 2, 2, 4, 2>;  // 128 x 128: 4 waves of 64 x 64, two workgroups per CU
+// Two stages of 64 places, 128 bytes of a row, or four of 32: an operand along the reduction is read in whole lines by the former (8192^3
+// forward 910 -> 851 us), one across it has whole lines in both, and more loads on the way in the latter (64 experts' weight gradient of
+// 98304 x 1408 x 2048 751 -> 709).
+template <int PASS>
+struct Depth {
+    static constexpr int K = PASS == kBf16BwdDw ? 32 : 64, kRing = 128 / K;
+};
+template <int PASS>
+using Tile256 = Tile<4, 2, 2, 4, Depth<PASS>::K, Depth<PASS>::kRing, 1>;  // 256 x 256: 8 waves of 128 x 64, two per SIMD
+template <int PASS>
+using Tile128 = Tile<2, 2, 2, 2, Depth<PASS>::K, Depth<PASS>::kRing, 2>;  // 128 x 128: 4 waves of 64 x 64, two workgroups per CU
 
 // Tile rows that a launch provides for; ragged rows: every group may end in a partial tile.
 int64_t tile_rows(const Bf16GemmJob& j, int bm) {
@@ -577,19 +647,21 @@ bool pieces(const Bf16GemmJob& j) {
            reinterpret_cast<uintptr_t>(j.a) % 16 == 0 && reinterpret_cast<uintptr_t>(j.b) % 16 == 0;
 }
 
-template <int OUT, class C, bool STREAM>
+template <int OUT, class C, int PASS>
 hipError_t launch_tile(const Bf16GemmJob& j, hipStream_t s) {
     int64_t tiles = grid_tiles(j, C::BM, C::BN);
     // One workgroup per tile where tiles differ in length (ragged reduction: the next free CU takes the next one); otherwise the
     // workgroups that are resident take the tiles in turn.
-    if (j.pass != kBf16BwdDw && tiles > C::kResident) tiles = C::kResident;
-    const unsigned n = (unsigned)tiles;
-    switch (j.pass) {
-        case kBf16FwdY: gemm_bf16_kernel<OUT, C, kBf16FwdY, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
-        case kBf16BwdDx: gemm_bf16_kernel<OUT, C, kBf16BwdDx, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
-        default: gemm_bf16_kernel<OUT, C, kBf16BwdDw, STREAM><<<n, C::kThreads, 0, s>>>(j); break;
-    }
+    if (PASS != kBf16BwdDw && tiles > C::kResident) tiles = C::kResident;
+    gemm_bf16_kernel<OUT, C, PASS, false><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
     return hipGetLastError();
+}
+
+template <int OUT, int PASS>
+hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
+    // The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
+    // us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
+    return grid_tiles(j, 256, 256) >= 256 ? launch_tile<OUT, Tile256<PASS>, PASS>(j, s) : launch_tile<OUT, Tile128<PASS>, PASS>(j, s);
 }
 
 template <int OUT>
@@ -609,9 +681,11 @@ template <int OUT>
 hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
     if (grid_tiles(j, kAnyTile, kAnyTile) == 0) return hipSuccess;
     if (!pieces(j)) return launch_any<OUT>(j, s);
-    // The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
-    // us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
-    return grid_tiles(j, Tile256::BM, Tile256::BN) >= 256 ? launch_tile<OUT, Tile256, false>(j, s) : launch_tile<OUT, Tile128, false>(j, s);
+    switch (j.pass) {
+        case kBf16FwdY: return launch_pass<OUT, kBf16FwdY>(j, s);
+        case kBf16BwdDx: return launch_pass<OUT, kBf16BwdDx>(j, s);
+        default: return launch_pass<OUT, kBf16BwdDw>(j, s);
+    }
 }
 
 }  // namespace
