@@ -600,20 +600,25 @@ int ufp4_moe_combine_bwd(int dtype, const void *dout_dev, int64_t tokens, int64_
  * fp32 sums, in an order that follows the sizes (not the values, nor the run); out_dtype UFP4_OUT_F32 or UFP4_OUT_BF16 (one
  * rounding). num_groups 1 .. 1024, tokens below 2^31, N and K up to 2^30, fewer than 2^24 tiles of 16 x 64 outputs at worst (else
  * UFP4_ERR_UNSUPPORTED). Outputs must not overlap inputs.
+ * ufp4_bf16_gemm_grouped_workspace -- the scratch memory (4-byte aligned, contents of no account) that a product of these sizes takes,
+ *   0 for small ones (workspace_dev may then be NULL): from it the workgroups take the next tile. Two calls that may run at the same time
+ *   need one each.
  */
+typedef enum { UFP4_PASS_FWD_Y = 0, UFP4_PASS_BWD_DX = 1, UFP4_PASS_BWD_DW = 2 } ufp4_pass_t;
+int ufp4_bf16_gemm_grouped_workspace(int pass, int64_t tokens, int64_t N, int64_t K, int32_t num_groups, size_t *bytes);
 int ufp4_bf16_gemm_fwd_y_grouped(const void *x_dev, int64_t tokens, int64_t K, int64_t ldx, const void *w_dev, int64_t N, int64_t ldw,
                                  const int64_t *group_offsets_dev, int32_t num_groups, void *y_dev, int64_t ldc, int out_dtype,
-                                 void *stream);
+                                 void *workspace_dev, size_t workspace_bytes, void *stream);
 int ufp4_bf16_gemm_bwd_dx_grouped(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void *w_dev, int64_t K, int64_t ldw,
                                   const int64_t *group_offsets_dev, int32_t num_groups, void *dx_dev, int64_t ldc, int out_dtype,
-                                  void *stream);
+                                  void *workspace_dev, size_t workspace_bytes, void *stream);
 int ufp4_bf16_gemm_bwd_dw_grouped(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void *x_dev, int64_t K, int64_t ldx,
                                   const int64_t *group_offsets_dev, int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype,
-                                  void *stream);
+                                  void *workspace_dev, size_t workspace_bytes, void *stream);
 int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void *dy_dev, int64_t tokens, int64_t N, int64_t lddy, const uint8_t *codes_dev,
                                         int64_t code_ld, const uint8_t *scales_dev, int64_t scale_ld, int64_t K,
                                         const int64_t *group_offsets_dev, int32_t num_groups, void *dw_dev, int64_t ldc, int out_dtype,
-                                        void *stream);
+                                        void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Activations kept in 8 bits between the forward and the backward pass. Per 32 values of a row one scale 2^e, stored as the byte

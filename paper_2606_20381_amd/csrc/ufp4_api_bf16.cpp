@@ -57,8 +57,12 @@ int check_gemm(int64_t tokens, int64_t N, int64_t K, const int64_t* offsets, int
     return check_rows(out_dtype, c, out_rows, out_cols, ldc);
 }
 
-int run(const Bf16GemmJob& j, void* stream) {
+int run(const Bf16GemmJob& j, size_t workspace_bytes, void* stream) {
     if (!bf16_gemm_fits(j)) return UFP4_ERR_UNSUPPORTED;
+    const size_t need = (size_t)bf16_gemm_workspace(j);
+    if (need && !j.counters) return UFP4_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return UFP4_ERR_SHAPE;
+    if (need && !aligned(j.counters, 4)) return UFP4_ERR_ALIGN;
     return status_of(launch_gemm_bf16(j, static_cast<hipStream_t>(stream)));
 }
 
@@ -66,42 +70,56 @@ int run(const Bf16GemmJob& j, void* stream) {
 
 extern "C" {
 
+int ufp4_bf16_gemm_grouped_workspace(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, size_t* bytes) {
+    if (pass < UFP4_PASS_FWD_Y || pass > UFP4_PASS_BWD_DW || tokens < 0 || N < 0 || K < 0 || G < 1 || !bytes) return UFP4_ERR_INVALID_ARG;
+    if (G > kBf16Groups || tokens > INT32_MAX || N > kMostCols || K > kMostCols) return UFP4_ERR_UNSUPPORTED;
+    Bf16GemmJob j{};
+    j.pass = pass;
+    j.tokens = tokens;
+    j.M = pass == UFP4_PASS_BWD_DW ? N : 0;
+    j.N = pass == UFP4_PASS_FWD_Y ? N : K;
+    j.G = G;
+    if (!bf16_gemm_fits(j)) return UFP4_ERR_UNSUPPORTED;
+    *bytes = (size_t)bf16_gemm_workspace(j);
+    return UFP4_OK;
+}
+
 int ufp4_bf16_gemm_fwd_y_grouped(const void* x_dev, int64_t tokens, int64_t K, int64_t ldx, const void* w_dev, int64_t N, int64_t ldw,
-                                 const int64_t* offsets_dev, int32_t G, void* y_dev, int64_t ldc, int out_dtype, void* stream) {
+                                 const int64_t* offsets_dev, int32_t G, void* y_dev, int64_t ldc, int out_dtype, void* workspace_dev, size_t workspace_bytes, void* stream) {
     const int st = first(check_gemm(tokens, N, K, offsets_dev, G, y_dev, tokens, N, ldc, out_dtype),
                          first(check_rows(UFP4_OUT_BF16, x_dev, tokens, K, ldx), check_rows(UFP4_OUT_BF16, w_dev, N, K, ldw)));
     if (st != UFP4_OK) return st;
     if (tokens == 0 || N == 0) return UFP4_OK;
     const Bf16GemmJob j{kBf16FwdY, out_dtype, static_cast<const uint16_t*>(x_dev), ldx, static_cast<const uint16_t*>(w_dev), ldw, nullptr,
-                        nullptr, 0, tokens, 0, N, K, y_dev, ldc, offsets_dev, G};
-    return run(j, stream);
+                        nullptr, 0, tokens, 0, N, K, y_dev, ldc, offsets_dev, G, static_cast<uint32_t*>(workspace_dev)};
+    return run(j, workspace_bytes, stream);
 }
 
 int ufp4_bf16_gemm_bwd_dx_grouped(const void* dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void* w_dev, int64_t K, int64_t ldw,
-                                  const int64_t* offsets_dev, int32_t G, void* dx_dev, int64_t ldc, int out_dtype, void* stream) {
+                                  const int64_t* offsets_dev, int32_t G, void* dx_dev, int64_t ldc, int out_dtype, void* workspace_dev, size_t workspace_bytes, void* stream) {
     const int st = first(check_gemm(tokens, N, K, offsets_dev, G, dx_dev, tokens, K, ldc, out_dtype),
                          first(check_rows(UFP4_OUT_BF16, dy_dev, tokens, N, lddy), check_rows(UFP4_OUT_BF16, w_dev, N, K, ldw)));
     if (st != UFP4_OK) return st;
     if (tokens == 0 || K == 0) return UFP4_OK;
     const Bf16GemmJob j{kBf16BwdDx, out_dtype, static_cast<const uint16_t*>(dy_dev), lddy, static_cast<const uint16_t*>(w_dev), ldw, nullptr,
-                        nullptr, 0, tokens, 0, K, N, dx_dev, ldc, offsets_dev, G};
-    return run(j, stream);
+                        nullptr, 0, tokens, 0, K, N, dx_dev, ldc, offsets_dev, G, static_cast<uint32_t*>(workspace_dev)};
+    return run(j, workspace_bytes, stream);
 }
 
 int ufp4_bf16_gemm_bwd_dw_grouped(const void* dy_dev, int64_t tokens, int64_t N, int64_t lddy, const void* x_dev, int64_t K, int64_t ldx,
-                                  const int64_t* offsets_dev, int32_t G, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
+                                  const int64_t* offsets_dev, int32_t G, void* dw_dev, int64_t ldc, int out_dtype, void* workspace_dev, size_t workspace_bytes, void* stream) {
     const int st = first(check_gemm(tokens, N, K, offsets_dev, G, dw_dev, N, K, ldc, out_dtype),
                          first(check_rows(UFP4_OUT_BF16, dy_dev, tokens, N, lddy), check_rows(UFP4_OUT_BF16, x_dev, tokens, K, ldx)));
     if (st != UFP4_OK) return st;
     if (N == 0 || K == 0) return UFP4_OK;
     const Bf16GemmJob j{kBf16BwdDw, out_dtype, static_cast<const uint16_t*>(dy_dev), lddy, static_cast<const uint16_t*>(x_dev), ldx, nullptr,
-                        nullptr, 0, tokens, N, K, 0, dw_dev, ldc, offsets_dev, G};
-    return run(j, stream);
+                        nullptr, 0, tokens, N, K, 0, dw_dev, ldc, offsets_dev, G, static_cast<uint32_t*>(workspace_dev)};
+    return run(j, workspace_bytes, stream);
 }
 
 int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void* dy_dev, int64_t tokens, int64_t N, int64_t lddy, const uint8_t* codes_dev,
                                         int64_t code_ld, const uint8_t* scales_dev, int64_t scale_ld, int64_t K, const int64_t* offsets_dev,
-                                        int32_t G, void* dw_dev, int64_t ldc, int out_dtype, void* stream) {
+                                        int32_t G, void* dw_dev, int64_t ldc, int out_dtype, void* workspace_dev, size_t workspace_bytes, void* stream) {
     const int st = first(check_gemm(tokens, N, K, offsets_dev, G, dw_dev, N, K, ldc, out_dtype),
                          first(check_rows(UFP4_OUT_BF16, dy_dev, tokens, N, lddy),
                                check_codes(codes_dev, code_ld, scales_dev, scale_ld, tokens, K, 1)));
@@ -109,8 +127,8 @@ int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void* dy_dev, int64_t tokens, int6
     if (N == 0 || K == 0) return UFP4_OK;
     static const uint8_t none = 0;  // never read: a checkpoint of no tokens may have no codes
     const Bf16GemmJob j{kBf16BwdDw, out_dtype, static_cast<const uint16_t*>(dy_dev), lddy, nullptr, code_ld, codes_dev ? codes_dev : &none,
-                        scales_dev, scale_ld, tokens, N, K, 0, dw_dev, ldc, offsets_dev, G};
-    return run(j, stream);
+                        scales_dev, scale_ld, tokens, N, K, 0, dw_dev, ldc, offsets_dev, G, static_cast<uint32_t*>(workspace_dev)};
+    return run(j, workspace_bytes, stream);
 }
 
 int ufp4_ckpt8_ld(int64_t cols, int parts, int64_t* code_ld, int64_t* scale_ld) {

@@ -38,7 +38,7 @@ struct Stage {
     static constexpr uint32_t kRowPieces = K / 8, kPlacePieces = ROWS / 8;
     static __device__ __forceinline__ uint32_t turn_row(uint32_t r) {
         static_assert(K == 32 || K == 64, "");
-        return K == 32 ? ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2) : (r ^ r >> 3) & 7;
+        return K == 32 ? ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2) : (r ^ (r >> 3 & 3)) & 7;
     }
     static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return ROWS < 128 ? k & 2 : (k << 1 & 6) | (k >> 1 & 1); }
 
@@ -292,37 +292,59 @@ struct Tile {
     static_assert(kWaveLoads * (kRing - 1) + 32 < 64, "vmcnt has six bits");
 };
 
-// The group with the `rank`-th longest reduction (of equally long ones the lower first): long tiles that begin last would run alone at
-// the end. By every wave for itself: the length by its bits, from counts of groups at least as long, then the place among equals.
-__device__ __forceinline__ int by_length(const Bf16GemmJob& j, uint32_t rank) {
-    const int lane = threadIdx.x & 63, rounds = (j.G + 63) / 64;
-    auto length = [&](int g) -> int64_t {
-        if (g >= j.G) return -1;
-        const int64_t n = clamped(j.offsets[g + 1], j.tokens) - clamped(j.offsets[g], j.tokens);
-        return n < 0 ? 0 : n;
-    };
-    const int64_t mine = length(lane);  // of the first 64 groups; the others' are read again each time
-    auto count = [&](int64_t least) {   // groups of at least this length
-        int n = __popcll(__ballot(mine >= least));
-        for (int r = 1; r < rounds; ++r) n += __popcll(__ballot(length(r * 64 + lane) >= least));
-        return (uint32_t)n;
-    };
-    int64_t v = 0;  // the largest length that more than `rank` groups reach
-    for (int b = 31 - __builtin_clz((uint32_t)j.tokens | 1); b >= 0; --b)
-        if (count(v + (int64_t(1) << b)) > rank) v += int64_t(1) << b;
-    uint32_t place = rank - count(v + 1);  // among the groups of length v
-    for (int r = 0; r < rounds; ++r) {
-        uint64_t same = __ballot((r == 0 ? mine : length(r * 64 + lane)) == v);
-        const uint32_t n = (uint32_t)__popcll(same);
-        if (place >= n) {
-            place -= n;
-            continue;
-        }
-        for (; place > 0; --place) same &= same - 1;
-        return uniform(r * 64 + __builtin_ctzll(same));
+// Ragged reductions by length, the longest first (of equally long ones the lower group): long tiles that begin last would run alone at
+// the end. By every wave for itself.
+struct Lengths {
+    int start, len;  // of the lane's group among the first 64; the others' are read again each time
+
+    __device__ __forceinline__ static void span(const Bf16GemmJob& j, int g, int& start, int& len) {
+        start = 0;
+        len = -1;
+        if (g >= j.G) return;
+        start = (int)clamped(j.offsets[g], j.tokens);
+        len = (int)clamped(j.offsets[g + 1], j.tokens) - start;
+        if (len < 0) len = 0;
     }
-    return 0;
-}
+    __device__ __forceinline__ void load(const Bf16GemmJob& j) { span(j, threadIdx.x & 63, start, len); }
+    // The group of this rank and its reduction: the length bit by bit, from counts of groups at least as long, then the place among equals.
+    __device__ __forceinline__ int ranked(const Bf16GemmJob& j, uint32_t rank, int64_t& from, int64_t& to) const {
+        const int lane = threadIdx.x & 63, rounds = (j.G + 63) / 64;
+        auto count = [&](int64_t least) {  // groups of at least this length
+            int n = __popcll(__ballot(len >= least));
+            for (int r = 1; r < rounds; ++r) {
+                int s, l;
+                span(j, r * 64 + lane, s, l);
+                n += __popcll(__ballot(l >= least));
+            }
+            return (uint32_t)uniform(n);
+        };
+        int64_t v = 0;  // the largest length that more than `rank` groups reach
+        for (int b = 31 - __builtin_clz((uint32_t)j.tokens | 1); b >= 0; --b)
+            if (count(v + (int64_t(1) << b)) > rank) v += int64_t(1) << b;
+        uint32_t place = rank - count(v + 1);  // among the groups of length v
+        for (int r = 0; r < rounds; ++r) {
+            int s = start, l = len;
+            if (r > 0) span(j, r * 64 + lane, s, l);
+            uint64_t same = __ballot(l == v);
+            const uint32_t n = (uint32_t)__popcll(same);
+            if (place >= n) {
+                place -= n;
+                continue;
+            }
+            for (; place > 0; --place) same &= same - 1;
+            const int at = uniform(__builtin_ctzll(same));
+            from = __builtin_amdgcn_readlane(s, at);
+            to = from + v;
+            return r * 64 + at;
+        }
+        from = to = 0;
+        return 0;
+    }
+};
+
+constexpr int kCounterStride = 16;  // of 4 bytes: each XCD's counter has a line of its own
+
+__global__ void clear_counters_kernel(uint32_t* counters) { counters[threadIdx.x] = 0; }
 
 // The pipeline: a ring of stages in LDS, filled by direct-to-LDS loads; each wave keeps two sets of operands in registers: while the
 // matrix core works on one step of a stage, the next step's operands (past the barrier, the next stage's first) are read from LDS.
@@ -335,6 +357,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     constexpr uint32_t kSlot = SA::kSize + SB::kSize;
     __shared__ __align__(16) uint8_t ring[kRing * kSlot];
     __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
+    __shared__ uint32_t s_next;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     // Where a SIMD has two waves of eight (w and w + 4), they differ in both halves of the tile, so that a tile which lies half outside
     // of the output leaves each SIMD one wave with work.
@@ -359,27 +382,33 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         gy = (uint32_t)((j.M + BM - 1) / BM);
         total = gx * gy * (uint32_t)j.G;
     }
+    Lengths lengths;
+    if constexpr (!P::kRagged) lengths.load(j);
 
-    // One output tile: its operands' places of stage 0 (with a rest: a stage before the first place, where nothing is read), this lane's
-    // pieces of a stage, and where the results go.
+    // One output tile: its operands' places of stage 0, this lane's pieces of a stage, and where the results go. A reduction of no whole
+    // stages begins inside stage 0: its first `gap` places are zeroed in LDS (memory is read from the first place on).
     struct Work {
         const uint8_t *a, *b;
         uint32_t va[C::kLoadsA], vb[C::kLoadsB];
-        int nst, rest;  // stages of the reduction; places of it that make no whole one, which are then stage 0
+        int nst, gap;
         int row0, rows, col0;
         int64_t c_base;
         bool idle;  // this wave's part is outside of the output: it loads with the others, and multiplies nothing
     };
     const uint32_t stepA = P::kAcrossA ? (uint32_t)(C::K * 2 * j.lda) : C::K * 2, stepB = P::kAcrossB ? (uint32_t)(C::K * 2 * j.ldb) : C::K * 2;
     // Lane's piece of load q (unit wave * loads + q of the stage: 64 pieces in the LDS's order), as an offset from the operand's first
-    // row and place. Rows past the last one are replaced by it: they only feed outputs that are not stored.
-    auto offset = [&](auto stage, int unit, int64_t ld, int64_t have) INLINE {
+    // row and place. Rows past the last one are replaced by it: they only feed outputs that are not stored. Places before `gap` (a
+    // multiple of 8 along the reduction) are replaced by that one.
+    auto offset = [&](auto stage, int unit, int64_t ld, int64_t have, int gap) INLINE {
         using S = decltype(stage);
         uint32_t r, k;
         S::piece((uint32_t)unit * 64 + lane, r, k);
+        k = k < (uint32_t)gap ? (uint32_t)gap : k;
         if (S::kAcross) return (k * (uint32_t)ld + (r < have ? r : (uint32_t)have - 8)) * 2;
         return ((r < have ? r : (uint32_t)have - 1) * (uint32_t)ld + k) * 2;
     };
+    auto offset_a = [&](const Work& w, int q, int gap) INLINE { return offset(SA{}, wave * C::kLoadsA + q, j.lda, w.rows, gap); };
+    auto offset_b = [&](const Work& w, int q, int gap) INLINE { return offset(SB{}, wave * C::kLoadsB + q, j.ldb, j.N - w.col0, gap); };
     auto locate = [&](uint32_t L, Work& w) INLINE {
         int tm, tn;
         int64_t k0 = 0, k1 = j.red, row0, rows;
@@ -392,60 +421,59 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
             rows = uniform(groups.rows[g]) - (int64_t)lt * BM;
             b += (int64_t)g * (PASS == kBf16FwdY ? j.N : j.red) * j.ldb;
         } else {
-            const uint32_t rank = L / (gx * gy), g = by_length(j, rank);
+            const uint32_t rank = L / (gx * gy);
+            const int g = lengths.ranked(j, rank, k0, k1);
             tile_at(L - rank * (gx * gy), gy, gx, tm, tn);
             row0 = (int64_t)tm * BM;
             rows = j.M - row0;
-            k0 = uniform64(clamped(j.offsets[g], j.tokens));
-            k1 = uniform64(clamped(j.offsets[g + 1], j.tokens));
-            if (k1 < k0) k1 = k0;
             w.c_base = (int64_t)g * j.M * j.ldc;
         }
         w.row0 = (int)row0;
         w.rows = rows < BM ? (int)rows : BM;
         w.col0 = tn * BN;
-        const int whole = (int)((k1 - k0) / C::K);
-        w.rest = (int)(k1 - k0) % C::K;
-        w.nst = whole + (w.rest ? 1 : 0);
-        const int64_t cols = j.N - w.col0;
-        w.idle = wm * WTM * 32 >= rows || wn * WTN * 32 >= cols;
-        const int64_t a0 = (P::kAcrossA ? k0 * j.lda + row0 : row0 * j.lda + k0) * 2 - (w.rest ? stepA : 0);
-        const int64_t b0 = (P::kAcrossB ? k0 * j.ldb + w.col0 : w.col0 * j.ldb + k0) * 2 - (w.rest ? stepB : 0);
-        w.a = reinterpret_cast<const uint8_t*>(j.a) + uniform64(a0);
-        w.b = reinterpret_cast<const uint8_t*>(b) + uniform64(b0);
+        w.nst = (int)((k1 - k0 + C::K - 1) / C::K);
+        w.gap = w.nst * C::K - (int)(k1 - k0);
+        w.idle = wm * WTM * 32 >= rows || wn * WTN * 32 >= j.N - w.col0;
+        const int64_t k = k0 - w.gap;
+        w.a = reinterpret_cast<const uint8_t*>(j.a) + uniform64((P::kAcrossA ? k * j.lda + row0 : row0 * j.lda + k) * 2);
+        w.b = reinterpret_cast<const uint8_t*>(b) + uniform64((P::kAcrossB ? k * j.ldb + w.col0 : w.col0 * j.ldb + k) * 2);
 #pragma unroll
-        for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset(SA{}, wave * C::kLoadsA + q, j.lda, w.rows);
+        for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset_a(w, q, 0);
 #pragma unroll
-        for (int q = 0; q < C::kLoadsB; ++q) w.vb[q] = offset(SB{}, wave * C::kLoadsB + q, j.ldb, cols);
+        for (int q = 0; q < C::kLoadsB; ++q) w.vb[q] = offset_b(w, q, 0);
     };
-    // Load q of this wave for stage i into the slot at `slot`.
-    auto issue_one = [&](const Work& w, int q, int i, uint32_t slot) INLINE {
+    // Load q of this wave for stage i (`first`: which is stage 0) into the slot at `slot`.
+    auto issue_one = [&](const Work& w, int q, int i, uint32_t slot, auto first) INLINE {
+        const bool is_a = q < C::kLoadsA;
+        const int u = is_a ? q : q - C::kLoadsA;
+        uint32_t v;
+        if constexpr (decltype(first)::value) v = is_a ? offset_a(w, u, w.gap) : offset_b(w, u, w.gap);
+        else v = is_a ? w.va[u] : w.vb[u];
         // the address in scalar registers whatever the compiler took it for
-        if (q < C::kLoadsA)
-            to_lds16(w.va[q], reinterpret_cast<const void*>(uniform64((int64_t)w.a + (int64_t)i * stepA)), ring + slot + (wave * C::kLoadsA + q) * 1024);
-        else
-            to_lds16(w.vb[q - C::kLoadsA], reinterpret_cast<const void*>(uniform64((int64_t)w.b + (int64_t)i * stepB)), ring + slot + SA::kSize + (wave * C::kLoadsB + q - C::kLoadsA) * 1024);
+        const int64_t base = uniform64(is_a ? (int64_t)w.a + (int64_t)i * stepA : (int64_t)w.b + (int64_t)i * stepB);
+        to_lds16(v, reinterpret_cast<const void*>(base), ring + slot + (is_a ? 0 : SA::kSize) + (wave * (is_a ? C::kLoadsA : C::kLoadsB) + u) * 1024);
     };
-    // The first stages. Places that make no whole stage are stage 0, through registers, zeros behind them: every piece (of an operand
-    // along the reduction: 8 places, a divisor of its length) is inside or outside.
-    auto fill = [&](const Work& w) INLINE {
-        for (int i = w.rest ? 1 : 0; i < kRing && i < w.nst; ++i)
+    auto fill = [&](const Work& w) INLINE {  // the first stages
+        if (w.nst > 0) {
 #pragma unroll
-            for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, i, i * kSlot);
-        if (!w.rest) return;
-        auto partial = [&](auto stage, const uint8_t* from, uint32_t v, int unit, uint8_t* to) INLINE {
+            for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, 0, 0, std::true_type{});
+        }
+        for (int i = 1; i < kRing && i < w.nst; ++i)
+#pragma unroll
+            for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, i, i * kSlot, std::false_type{});
+    };
+    // Zeros over the places before the gap's end, in what this wave has loaded of stage 0.
+    auto close_gap = [&](const Work& w, uint32_t slot) INLINE {
+        const u32x4_any zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < C::kWaveLoads; ++q) {
+            const bool is_a = q < C::kLoadsA;
+            const int unit = is_a ? wave * C::kLoadsA + q : wave * C::kLoadsB + q - C::kLoadsA;
             uint32_t r, k;
-            decltype(stage)::piece((uint32_t)unit * 64 + lane, r, k);
-            u32x4_any x = {0, 0, 0, 0};
-            if (k < (uint32_t)w.rest) x = *reinterpret_cast<const u32x4_any*>(from + v);
-            *reinterpret_cast<u32x4_any*>(to + unit * 1024 + lane * 16) = x;
-        };
-        const uint8_t* const ra = w.a + (int64_t)w.nst * stepA;
-        const uint8_t* const rb = w.b + (int64_t)w.nst * stepB;
-#pragma unroll
-        for (int q = 0; q < C::kLoadsA; ++q) partial(SA{}, ra, w.va[q], wave * C::kLoadsA + q, ring);
-#pragma unroll
-        for (int q = 0; q < C::kLoadsB; ++q) partial(SB{}, rb, w.vb[q], wave * C::kLoadsB + q, ring + SA::kSize);
+            if (is_a) SA::piece((uint32_t)unit * 64 + lane, r, k);
+            else SB::piece((uint32_t)unit * 64 + lane, r, k);
+            if (k < (uint32_t)w.gap) *reinterpret_cast<u32x4_any*>(ring + slot + (is_a ? 0 : SA::kSize) + unit * 1024 + lane * 16) = zero;
+        }
     };
 
     constexpr int kTiles = WTM * WTN, kOps = WTM + WTN;  // B's WTN operands, then A's WTM
@@ -463,28 +491,37 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v[b], f.v[WTN + a], acc[a][b], 0, 0, 0);
     };
     // Waits until at most OUTSTANDING of this wave's memory operations are in flight and its LDS reads are done, then for every
-    // wave: what all have waited for is then visible to all, and nobody reads the stage before any more.
-    auto arrive = [&](auto outstanding) INLINE {
+    // wave: what all have waited for is then visible to all, and nobody reads the stage before any more. `opens`: the stage that can be
+    // read now is stage 0 of tile w, in the slot at `slot`.
+    auto arrive = [&](auto outstanding, auto opens, const Work& w, uint32_t slot) INLINE {
         asm volatile("" ::: "memory");
         wait_loads<decltype(outstanding)::value>();
+        if constexpr (decltype(opens)::value) {
+            if (w.gap) {
+                asm volatile("" ::: "memory");
+                close_gap(w, slot);
+                asm volatile("" ::: "memory");
+                wait_loads<63>();
+            }
+        }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 
     // A stage, K / 16 steps: the products of one step while the next step's operands are read. Before the last step's products comes the
     // barrier that lets the next stage be read and this one be overwritten: they cover the reads of the next stage's first operands and
-    // the loads of the stage kRing ahead (stage li of tile lw, if `loads`). The order is pinned: one product, then what its 32 cycles
-    // cover. OUTSTANDING: as of arrive() for the next stage, -1 if there is none.
+    // the loads of the stage kRing ahead (stage li of tile lw, if `loads`; `first`: li is 0, `opens`: the next stage is stage 0 of lw).
+    // The order is pinned: one product, then what its 32 cycles cover. OUTSTANDING: as of arrive() for the next stage, -1 if there is none.
     constexpr int kSteps = C::K / 16;
     constexpr int kOpsPer = (kOps + kTiles - 1) / kTiles, kLoadsPer = (C::kWaveLoads + kTiles - 1) / kTiles;
     Operands f[2];
-    auto stage = [&](auto idle, uint32_t cur, uint32_t next, auto outstanding, const Work& lw, int li, auto loads) INLINE {
+    auto stage = [&](auto idle, uint32_t cur, uint32_t next, auto outstanding, const Work& lw, int li, auto loads, auto first, auto opens) INLINE {
         constexpr bool kMore = decltype(outstanding)::value >= 0, kLoads = decltype(loads)::value;
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) {
             const bool last = ks == kSteps - 1;
             if constexpr (kMore)
-                if (last) arrive(outstanding);
+                if (last) arrive(outstanding, opens, lw, next);
 #pragma unroll
             for (int k = 0; k < kTiles; ++k) {
                 if constexpr (!decltype(idle)::value) multiply_one(k, f[ks & 1]);
@@ -496,7 +533,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
                 if constexpr (kLoads) {
                     if (last)
 #pragma unroll
-                        for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur);
+                        for (int q = k * kLoadsPer; q < (k + 1) * kLoadsPer && q < C::kWaveLoads; ++q) issue_one(lw, q, li, cur, first);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -516,7 +553,14 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
                 for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
     };
     auto is_inside = [&](const Work& w) INLINE { return w.rows == BM && (int64_t)w.col0 + BN <= j.N; };
-    constexpr int L1 = C::kWaveLoads;
+
+    // The workgroup's first tile is its own place in the order of tiles, the next one the first that no other has: one counter for each of
+    // the 8 XCDs, whose workgroups and tiles are those of one remainder modulo 8. Without counters every workgroup has one tile.
+    auto take = [&] INLINE {  // by the first thread
+        if (!j.counters) return total;
+        const uint32_t x = blockIdx.x % 8;
+        return (gridDim.x / 8 + atomicAdd(j.counters + x * kCounterStride, 1u)) * 8 + x;
+    };
     uint32_t L = blockIdx.x;
     if (L >= total) return;
     Work w;
@@ -532,99 +576,116 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, f[0]);
     };
     using std::integral_constant;
+    constexpr int L1 = C::kWaveLoads;
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
 
-    // The workgroup's tiles, all of as many stages: those of one tile follow those of the one before without a gap. Its last kRing
-    // stages load the next tile's first ones (after the last tile its own first ones again, which nobody reads: a branch here
-    // makes the compiler spill the sums), and the last reads the first's operands. A tile's stores are then younger than those
-    // loads, and memory operations complete in order, so the next tile's first waits count them in instead of waiting for them.
-    if constexpr (P::kRagged) {
-        if (w.nst >= 2 * kRing && w.rest == 0) {
-            arrive(integral_constant<int, (kRing - 1) * L1>{});
-            begin();
-            bool behind = false;  // kStores stores were issued after the loads
-            while (true) {
-                clear();
-                L += gridDim.x;
-                const bool more = L < total;
-                Work n = w;
-                if (more) locate(L, n);
+    // Long tiles: the stages of one follow those of the one before without a gap. A tile's last kRing stages load the next one's first
+    // (after the last tile its own first ones again, which nobody reads: a branch here makes the compiler spill the sums), and the last
+    // reads the first's operands. A tile's stores are then younger than those loads, and memory operations complete in order, so the next
+    // tile's first waits count them in instead of waiting for them.
+    constexpr int kLong = 2 * kRing;
+    if (w.nst >= kLong) {
+        constexpr integral_constant<int, (kRing - 2) * L1> kept{};
+        arrive(integral_constant<int, (kRing - 1) * L1>{}, yes, w, cur);
+        begin();
+        bool behind = false;  // kStores stores were issued after the loads
+        while (true) {
+            clear();
+            uint32_t taken = 0;
+            if (tid == 0) taken = take();
+            Work n;
+            bool more, go;
+            auto run = [&](auto idle) INLINE {
                 int i = 0;
-                auto run = [&](auto idle) INLINE {
-                    if (behind) {
-                        for (; i < kRing - 1; ++i) {
-                            stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, std::true_type{});
-                            advance();
-                        }
-                    }
-                    constexpr integral_constant<int, (kRing - 2) * L1> kept{};
-                    for (; i + kRing < w.nst; ++i) {
-                        stage(idle, cur, next, kept, w, i + kRing, std::true_type{});
+                if (behind) {
+                    for (; i < kRing - 1; ++i) {
+                        stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, yes, no, no);
                         advance();
                     }
-#pragma unroll
-                    for (int q = 0; q < kRing; ++q) {
-                        stage(idle, cur, next, kept, n, q, std::true_type{});
-                        advance();
-                    }
-                };
-                if (w.idle) run(std::true_type{});
-                else run(std::false_type{});
-                asm volatile("" ::: "memory");
-                behind = is_inside(w);
-                if (behind) store(w, std::true_type{});
-                else store(w, std::false_type{});
-                if (!more) {
-                    wait_loads<0>();  // the LDS must not be another workgroup's before they have landed
-                    return;
                 }
-                w = n;
+                if (tid == 0) s_next = taken;  // a barrier lies between this and its reading: kLong
+                for (; i + kRing < w.nst; ++i) {
+                    stage(idle, cur, next, kept, w, i + kRing, yes, no, no);
+                    advance();
+                }
+                L = (uint32_t)uniform((int)s_next);
+                more = L < total;
+                n = w;
+                if (more) locate(L, n);
+                go = more && n.nst >= kLong;  // shorter ones, which come last where they differ, go the other way
+                if (!go) n = w;
+#pragma unroll
+                for (int q = 0; q < kRing; ++q) {
+                    if (q == 0) stage(idle, cur, next, kept, n, q, yes, yes, no);
+                    else if (q == kRing - 1) stage(idle, cur, next, kept, n, q, yes, no, yes);
+                    else stage(idle, cur, next, kept, n, q, yes, no, no);
+                    advance();
+                }
+            };
+            if (w.idle) run(yes);
+            else run(no);
+            asm volatile("" ::: "memory");
+            behind = is_inside(w);
+            if (behind) store(w, yes);
+            else store(w, no);
+            if (!go) {
+                wait_loads<0>();  // the LDS must not be another tile's or workgroup's before they have landed
+                if (!more) return;
+                break;
             }
+            w = n;
         }
+        __syncthreads();
+        locate(L, w);
+        fill(w);
     }
 
-    // Tiles of different length, or of few stages: one after the other.
+    // Short tiles: one after the other.
     while (true) {
         clear();
         if (w.nst > 0) {
             cur = 0, next = kSlot;
-            arrive(integral_constant<int, 0>{});
+            arrive(integral_constant<int, 0>{}, yes, w, cur);
             begin();
-            auto run = [&](auto idle) INLINE {
+            auto body = [&](auto idle) INLINE {
                 int i = 0;
                 for (; i + kRing < w.nst; ++i) {
-                    stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, std::true_type{});
+                    stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, yes, no, no);
                     advance();
                 }
                 for (; i + 1 < w.nst; ++i) {  // the loads are on their way: wait for all of them
-                    stage(idle, cur, next, integral_constant<int, 0>{}, w, 0, std::false_type{});
+                    stage(idle, cur, next, integral_constant<int, 0>{}, w, 0, no, no, no);
                     advance();
                 }
-                stage(idle, cur, next, integral_constant<int, -1>{}, w, 0, std::false_type{});
+                stage(idle, cur, next, integral_constant<int, -1>{}, w, 0, no, no, no);
             };
-            if (w.idle) run(std::true_type{});
-            else run(std::false_type{});
+            if (w.idle) body(yes);
+            else body(no);
         }
-        L += gridDim.x;
-        const bool more = L < total;
         const Work done = w;
+        if (tid == 0) s_next = take();
+        __syncthreads();  // every wave has read the last stage
+        L = (uint32_t)uniform((int)s_next);
+        const bool more = L < total;
         if (more) {
             locate(L, w);
-            __syncthreads();  // every wave has read the last stage
+            __syncthreads();  // and what was taken
             fill(w);
         }
         asm volatile("" ::: "memory");
-        if (is_inside(done)) store(done, std::true_type{});
-        else store(done, std::false_type{});
+        if (is_inside(done)) store(done, yes);
+        else store(done, no);
         if (!more) return;
     }
 }
 
-// Two stages of 64 places, 128 bytes of a row, or four of 32: an operand along the reduction is read in whole lines by the former (8192^3
-// forward 910 -> 851 us), one across it has whole lines in both, and more loads on the way in the latter (64 experts' weight gradient of
-// 98304 x 1408 x 2048 751 -> 709).
+// Two stages of 64 places, 128 bytes of a row, or four of 32: operands along the reduction are read in whole lines by the former (8192^3
+// forward 910 -> 851 us); one across it has whole lines in both, and more loads on the way in the latter (64 experts' 98304 x 1408 x
+// 2048, us, 64 / 32: weights' gradient 751 / 709, input's gradient 568 / 557).
 template <int PASS>
 struct Depth {
-    static constexpr int K = PASS == kBf16BwdDw ? 32 : 64, kRing = 128 / K;
+    static constexpr int K = PASS == kBf16FwdY ? 64 : 32, kRing = 128 / K;
 };
 template <int PASS>
 using Tile256 = Tile<4, 2, 2, 4, Depth<PASS>::K, Depth<PASS>::kRing, 1>;  // 256 x 256: 8 waves of 128 x 64, two per SIMD
@@ -647,21 +708,36 @@ bool pieces(const Bf16GemmJob& j) {
            reinterpret_cast<uintptr_t>(j.a) % 16 == 0 && reinterpret_cast<uintptr_t>(j.b) % 16 == 0;
 }
 
-template <int OUT, class C, int PASS>
-hipError_t launch_tile(const Bf16GemmJob& j, hipStream_t s) {
+constexpr int kCounters = 8 * kCounterStride;
+
+template <int OUT, class C, int PASS, bool STREAM>
+hipError_t launch_tile(Bf16GemmJob j, hipStream_t s) {
     int64_t tiles = grid_tiles(j, C::BM, C::BN);
-    // One workgroup per tile where tiles differ in length (ragged reduction: the next free CU takes the next one); otherwise the
-    // workgroups that are resident take the tiles in turn.
-    if (PASS != kBf16BwdDw && tiles > C::kResident) tiles = C::kResident;
-    gemm_bf16_kernel<OUT, C, PASS, false><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
+    if (tiles > C::kResident) {  // the workgroups that are resident take the tiles as they get done
+        tiles = C::kResident;
+        clear_counters_kernel<<<1, kCounters, 0, s>>>(j.counters);
+    } else {
+        j.counters = nullptr;
+    }
+    gemm_bf16_kernel<OUT, C, PASS, STREAM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
     return hipGetLastError();
+}
+
+// The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
+// us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
+bool large(const Bf16GemmJob& j) { return grid_tiles(j, 256, 256) >= 256; }
+
+// Outputs that no cache holds are stored nontemporally; weights' gradients, which are read when a step's have all been computed, from
+// 64 MiB on.
+bool streams(const Bf16GemmJob& j) {
+    const bool dw = j.pass == kBf16BwdDw;
+    return (dw ? j.M * j.G : j.tokens) * j.N * (j.out_dtype == kOutF32 ? 4 : 2) >= (dw ? int64_t(64) << 20 : kStreamBytes);
 }
 
 template <int OUT, int PASS>
 hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
-    // The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
-    // us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
-    return grid_tiles(j, 256, 256) >= 256 ? launch_tile<OUT, Tile256<PASS>, PASS>(j, s) : launch_tile<OUT, Tile128<PASS>, PASS>(j, s);
+    if (!large(j)) return launch_tile<OUT, Tile128<PASS>, PASS, false>(j, s);
+    return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false>(j, s);
 }
 
 template <int OUT>
@@ -689,6 +765,11 @@ hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
 }
 
 }  // namespace
+
+int64_t bf16_gemm_workspace(const Bf16GemmJob& j) {
+    const int tile = large(j) ? 256 : 128, resident = large(j) ? Tile256<kBf16FwdY>::kResident : Tile128<kBf16FwdY>::kResident;
+    return grid_tiles(j, tile, tile) > resident ? kCounters * 4 : 0;
+}
 
 bool bf16_gemm_fits(const Bf16GemmJob& j) { return grid_tiles(j, kAnyTile, kAnyTile) < int64_t(1) << 24; }
 

@@ -766,6 +766,16 @@ Done new_kept(const at::Tensor& like, int64_t rows, int64_t cols, int parts, at:
     return done;
 }
 
+// The scratch memory of a product, undefined where it needs none.
+Done product_workspace(int pass, const at::Tensor& like, int64_t tokens, int64_t n, int64_t k, int32_t groups, at::Tensor& ws, void*& p, size_t& bytes) {
+    const Done done{ufp4_bf16_gemm_grouped_workspace(pass, tokens, n, k, groups, &bytes), "ufp4_bf16_gemm_grouped_workspace"};
+    p = nullptr;
+    if (done.status != UFP4_OK || !bytes) return done;
+    ws = at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+    p = ws.data_ptr();
+    return done;
+}
+
 // (x, w, offsets, out type, out, stream) -> y [tokens, N] of x [tokens, K] (BACK: of dy [tokens, N] -> dx [tokens, K])
 template <bool BACK>
 PyObject* bf16_rows_product(PyObject* const* a, Py_ssize_t n_args) {
@@ -793,11 +803,16 @@ PyObject* bf16_rows_product(PyObject* const* a, Py_ssize_t n_args) {
     if (!unlocked([&]() -> Done {
             product_new(*x.t, shape, code, out);
             const int32_t g = groups > INT32_MAX ? INT32_MAX : (int32_t)groups;
+            at::Tensor ws;
+            void* scratch;
+            size_t bytes;
+            const Done done = product_workspace(BACK ? UFP4_PASS_BWD_DX : UFP4_PASS_FWD_Y, *x.t, x.rows, n, w.cols, g, ws, scratch, bytes);
+            if (done.status != UFP4_OK) return done;
             if (BACK)
                 return {ufp4_bf16_gemm_bwd_dx_grouped(x.data(), x.rows, n, x.ld, w.data(), w.cols, w.ld, static_cast<int64_t*>(offsets), g,
-                                                      out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_bf16_gemm_bwd_dx_grouped"};
+                                                      out.data_ptr(), out.stride(0), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dx_grouped"};
             return {ufp4_bf16_gemm_fwd_y_grouped(x.data(), x.rows, x.cols, x.ld, w.data(), n, w.ld, static_cast<int64_t*>(offsets), g,
-                                                 out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_bf16_gemm_fwd_y_grouped"};
+                                                 out.data_ptr(), out.stride(0), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_fwd_y_grouped"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -836,12 +851,17 @@ CALL(bf16_gemm_bwd_dw_grouped, 9)
             product_new(*dy.t, shape, code, out);
             const int32_t g = groups > INT32_MAX ? INT32_MAX : (int32_t)groups;
             int64_t* const off = static_cast<int64_t*>(offsets);
+            at::Tensor ws;
+            void* scratch;
+            size_t bytes;
+            const Done done = product_workspace(UFP4_PASS_BWD_DW, *dy.t, dy.rows, dy.cols, cols, g, ws, scratch, bytes);
+            if (done.status != UFP4_OK) return done;
             if (saved)
                 return {ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(dy.data(), dy.rows, dy.cols, dy.ld, k.codes, k.code_ld, k.scales, k.scale_ld, cols,
-                                                            off, g, out.data_ptr(), out.stride(1), code_of(out), stream),
+                                                            off, g, out.data_ptr(), out.stride(1), code_of(out), scratch, bytes, stream),
                         "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8"};
             return {ufp4_bf16_gemm_bwd_dw_grouped(dy.data(), dy.rows, dy.cols, dy.ld, x.data(), cols, x.ld, off, g, out.data_ptr(),
-                                                  out.stride(1), code_of(out), stream), "ufp4_bf16_gemm_bwd_dw_grouped"};
+                                                  out.stride(1), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dw_grouped"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);

@@ -327,7 +327,9 @@ struct Bf16GemmJob {
     int64_t ldc;
     const int64_t* offsets;
     int32_t G;
+    uint32_t* counters;  // bf16_gemm_workspace bytes, may be null for 0
 };
+int64_t bf16_gemm_workspace(const Bf16GemmJob& job);
 hipError_t launch_gemm_bf16(const Bf16GemmJob& job, hipStream_t stream);
 bool bf16_gemm_fits(const Bf16GemmJob& job);  // the grid of every kernel that may take it
 

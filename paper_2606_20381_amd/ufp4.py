@@ -63,7 +63,7 @@ _M = ctypes.POINTER(Metrics)
 _QUANT_ARGS = [_P, _I64, _I64, _I64, _INT, _INT, _U32, _INT, _U64, _U32, _Q, _P]
 _GEMM_ARGS = [_Q, _Q, _P, _I64, _INT, _P]
 _GEMM_G_ARGS = [_Q, _Q, _P, _I32, _P, _I64, _INT, _P]
-_BF16_GEMM_ARGS = [_P, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P]
+_BF16_GEMM_ARGS = [_P, _I64, _I64, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P, _SZ, _P]
 SIGNATURES = {
     "ufp4_status_string": ([_INT], ctypes.c_char_p),
     "ufp4_version": ([], ctypes.c_char_p),
@@ -122,7 +122,9 @@ SIGNATURES = {
     "ufp4_bf16_gemm_fwd_y_grouped": (_BF16_GEMM_ARGS, _INT),
     "ufp4_bf16_gemm_bwd_dx_grouped": (_BF16_GEMM_ARGS, _INT),
     "ufp4_bf16_gemm_bwd_dw_grouped": (_BF16_GEMM_ARGS, _INT),
-    "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8": ([_P, _I64, _I64, _I64, _P, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P], _INT),
+    "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8": ([_P, _I64, _I64, _I64, _P, _I64, _P, _I64, _I64, _P, _I32, _P, _I64, _INT, _P, _SZ, _P],
+                                            _INT),
+    "ufp4_bf16_gemm_grouped_workspace": ([_INT, _I64, _I64, _I64, _I32, _P], _INT),
     "ufp4_ckpt8_ld": ([_I64, _INT, _P, _P], _INT),
     "ufp4_ckpt8_save": ([_INT, _P, _I64, _I64, _I64, _P, _I64, _P, _I64, _P], _INT),
     "ufp4_ckpt8_load": ([_INT, _P, _I64, _P, _I64, _I64, _I64, _P, _I64, _P], _INT),

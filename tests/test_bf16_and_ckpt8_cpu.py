@@ -26,9 +26,9 @@ def lib():
 def test_product_refusals(lib, name):
     f = getattr(lib, f"ufp4_bf16_gemm_{name}_grouped")
 
-    def call(a=FAKE, tokens=4, ka=8, lda=8, b=FAKE, nb=16, ldb=16, off=FAKE, G=2, c=FAKE, ldc=16, dt=F32):
+    def call(a=FAKE, tokens=4, ka=8, lda=8, b=FAKE, nb=16, ldb=16, off=FAKE, G=2, c=FAKE, ldc=16, dt=F32, ws=FAKE, n=1 << 20):
         # fwd_y: x [4, 8], w [2 * 16, 8]; bwd_dx: dy [4, 8], w [2 * 8, 16]; bwd_dw: dy [4, 8], x [4, 16]
-        return f(a, tokens, ka, lda, b, nb, ldb, off, G, c, ldc, dt, None)
+        return f(a, tokens, ka, lda, b, nb, ldb, off, G, c, ldc, dt, ws, n, None)
 
     if name == "bwd_dw":
         assert call(tokens=0, a=None, b=None, c=None) == INVALID  # dw of no tokens is zero: it needs dw
@@ -48,13 +48,30 @@ def test_product_refusals(lib, name):
     assert call(ka=(1 << 30) + 1, lda=big, ldb=big, ldc=big) == UNSUPPORTED
     assert call(nb=(1 << 30) + 1, lda=big, ldb=big, ldc=big) == UNSUPPORTED
     assert call(lda=1 << 41) == UNSUPPORTED and call(ldb=1 << 41) == UNSUPPORTED and call(ldc=1 << 41) == UNSUPPORTED
+    # a product of many tiles needs its workspace
+    many = dict(tokens=100_000, ka=4096, nb=4096, lda=4096, ldb=4096, ldc=4096)
+    assert call(**many, ws=None) == INVALID and call(**many, n=511) == SHAPE and call(**many, ws=FAKE + 2) == ALIGN
     # tiles: outputs of 2^31 x 2^30
     assert call(tokens=big - 1, nb=1 << 30, ka=1 << 30, lda=big, ldb=big, ldc=big) == UNSUPPORTED
 
 
+def test_product_workspace(lib):
+    b, f = ctypes.c_size_t(7), lib.ufp4_bf16_gemm_grouped_workspace
+    for p in range(3):
+        assert f(p, 0, 0, 0, 1, R(b)) == OK and b.value == 0
+        assert f(p, 4, 128, 128, 2, R(b)) == OK and b.value == 0
+        assert f(p, 100_000, 4096, 4096, 64, R(b)) == OK and b.value == 512
+        for bad in ((-1, 8, 8, 1), (8, -1, 8, 1), (8, 8, -1, 1), (8, 8, 8, 0)):
+            assert f(p, *bad, R(b)) == INVALID
+        assert f(p, 8, 8, 8, 1, None) == INVALID
+        for big in ((1 << 31, 8, 8, 1), (8, (1 << 30) + 1, 8, 1), (8, 8, (1 << 30) + 1, 1), (8, 8, 8, 1025), ((1 << 31) - 1, 1 << 30, 1 << 30, 1)):
+            assert f(p, *big, R(b)) == UNSUPPORTED
+    assert f(3, 8, 8, 8, 1, R(b)) == INVALID and f(-1, 8, 8, 8, 1, R(b)) == INVALID
+
+
 def test_product_from_a_checkpoint_refusals(lib):
-    def call(dy=FAKE, tokens=4, N=8, lddy=8, codes=FAKE, cld=64, scales=FAKE, sld=2, K=40, off=FAKE, G=2, dw=FAKE, ldc=40, dt=F32):
-        return lib.ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(dy, tokens, N, lddy, codes, cld, scales, sld, K, off, G, dw, ldc, dt, None)
+    def call(dy=FAKE, tokens=4, N=8, lddy=8, codes=FAKE, cld=64, scales=FAKE, sld=2, K=40, off=FAKE, G=2, dw=FAKE, ldc=40, dt=F32, ws=FAKE, n=1 << 20):
+        return lib.ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(dy, tokens, N, lddy, codes, cld, scales, sld, K, off, G, dw, ldc, dt, ws, n, None)
 
     assert call(N=0, dy=None, dw=None) == OK and call(K=0, codes=None, scales=None, dw=None) == OK
     for k in ("dy", "codes", "scales", "off", "dw"):

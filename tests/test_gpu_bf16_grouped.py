@@ -119,6 +119,21 @@ def test_real_numbers(what, dtype, counts, N, K):
 
 
 @pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("counts,N,K", [([4000, 10, 3500, 0, 900, 1], 2568, 2056), ([300] * 40, 1032, 776), ([1, 20000], 640, 1024),
+                                        ([130] * 70 + [5000], 392, 1288), ([66, 65, 2, 700] * 25, 1160, 904)])
+def test_more_tiles_than_workgroups(what, dtype, counts, N, K):
+    """Tiles that workgroups take as they get done, long and short ones, in whole numbers; twice, since the order of taking is not fixed."""
+    g = _gen(N + K)
+    tokens, G = sum(counts) + 5, len(counts)
+    offsets, _ = U.group_offsets(counts)
+    x, dy, w = _whole(g, tokens, K), _whole(g, tokens, N), _whole(g, G * N, K)
+    ref, _ = _reference(what, x, dy, w, offsets, tokens, N, K)
+    for _ in range(2):
+        assert torch.equal(_call(what, x, dy, w, offsets, _out(what, tokens, N, K, G, dtype), dtype), ref.to(dtype))
+
+
+@pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
 @pytest.mark.parametrize("N,K", [(264, 72), (33, 35)])
 def test_offsets_that_lie(what, N, K):
     """Offsets past the rows, below zero or falling: cut to the rows; a group that ends before it starts has none."""
