@@ -593,13 +593,14 @@ int ufp4_moe_combine_bwd(int dtype, const void *dout_dev, int64_t tokens, int64_
  *   ufp4_bf16_gemm_bwd_dw_grouped_ckpt8: the same with X an 8-bit checkpoint (ufp4_ckpt8_save), read as it is
  *
  * Group g has the rows offsets[g] .. offsets[g + 1] - 1 of the `tokens` rows of x, dy, y and dx (offsets int64 [num_groups + 1] on the
- * device, as ufp4_moe_sort writes them; cut to 0 .. tokens; a group whose end is not past its start has no rows), w is
- * [num_groups * N, K], dw [num_groups, N, K] with rows ldc apart and groups N rows apart. Rows of y and dx outside the groups are left
- * as they were; dw of a group without rows is zero. Any sizes, leading dimensions (elements, at least the row's) and alignment of a whole
- * element; rows of 16-byte aligned pieces (sizes and leading dimensions multiples of 8, bases 16-byte aligned) are faster.
- * fp32 sums, in an order that follows the sizes (not the values, nor the run); out_dtype UFP4_OUT_F32 or UFP4_OUT_BF16 (one
- * rounding). num_groups 1 .. 1024, tokens below 2^31, N and K up to 2^30, fewer than 2^24 tiles of 16 x 64 outputs at worst (else
- * UFP4_ERR_UNSUPPORTED). Outputs must not overlap inputs.
+ * device, rising, as ufp4_moe_sort writes them; each is cut to 0 .. tokens, and a group whose end is not past its start has no rows; which
+ * result a row gets that falling offsets give to several groups is not defined). w is [num_groups * N, K], dw [num_groups, N, K] with rows
+ * ldc apart and groups N rows apart. Rows of y and dx outside the groups are left as they were; dw of a group without rows is zero.
+ * Any sizes, leading dimensions (elements, at least the row's) and alignment of a whole element; rows of 16-byte pieces (sizes and
+ * leading dimensions multiples of 8, bases 16-byte aligned) are faster. fp32 sums, in an order that follows the sizes and offsets, not
+ * the values nor the run; out_dtype UFP4_OUT_F32 or UFP4_OUT_BF16 (one rounding). num_groups 1 .. 1024, tokens below 2^31, N and K up to
+ * 2^30, fewer than 2^23 tiles of 128 x 128 outputs, of which every group may leave one row partial (else UFP4_ERR_UNSUPPORTED). Outputs
+ * must not overlap inputs.
  * ufp4_bf16_gemm_grouped_workspace -- the scratch memory (4-byte aligned, contents of no account) that a product of these sizes takes,
  *   0 for small ones (workspace_dev may then be NULL): from it the workgroups take the next tile. Two calls that may run at the same time
  *   need one each.

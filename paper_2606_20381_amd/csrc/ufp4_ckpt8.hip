@@ -4,62 +4,32 @@
 //   its gradient from the checkpoint (or from u): du = f'(u) da, and a once more, which the next product's weights need
 // Bound by memory: every tensor is read or written once, all arithmetic is on registers.
 //
-// A thread takes 16 values at a time (half a block: its codes are one 16-byte store), the other half's maximum comes from the
-// neighbouring lane.
+// A lane takes a 16-byte piece of a row at a time (8 bf16 or 4 fp32 values), so that every access of a wave is one run of memory; a block's
+// maximum comes from the 4 or 8 lanes that hold it.
 
 #include "ufp4_ckpt8.h"
 #include "ufp4_internal.h"
 #include "ufp4_rows.h"
 #include "ufp4_tiles.h"
 
+#include <type_traits>
+
 namespace ufp4 {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHalf = kCkpt8Block / 2;  // values of a thread's unit
 
-// 16 values of a row, in pieces of 16 bytes.
-template <typename T>
-struct Unit {
-    using P = Piece<T>;
-    static constexpr int kPieces = kHalf / P::V;
-    u32x4_any raw[kPieces];
-
-    __device__ __forceinline__ void load(const T* p, int64_t left) {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) raw[i] = P::load(p + i * P::V, left - i * P::V);
-    }
-    __device__ __forceinline__ void values(float (&f)[kHalf]) const {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            float v[P::V];
-            P::unpack(raw[i], v);
-#pragma unroll
-            for (int e = 0; e < P::V; ++e) f[i * P::V + e] = v[e];
-        }
-    }
-    template <bool STREAM>
-    static __device__ __forceinline__ void store(T* p, int64_t left, const float (&f)[kHalf]) {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            float v[P::V];
-#pragma unroll
-            for (int e = 0; e < P::V; ++e) v[e] = f[i * P::V + e];
-            P::template store<STREAM>(p + i * P::V, left - i * P::V, P::pack(v));
-        }
-    }
-};
-
-// Units [64 N w, 64 N (w + 1)) of wave w, N a lane: unit i of row i / per, values 16 (i % per) .. of it; `per` is even, so that a
-// block's halves are in neighbouring lanes.
-template <int N>
+// Pieces [64 N w, 64 N (w + 1)) of wave w, N a lane: piece i of row i / per, values V (i % per) .. of it. `per` is whole blocks, whose
+// lanes lie side by side.
+template <int N, int V>
 struct Where {
     int64_t row[N];
     int col[N];
     bool some[N];
 
-    __device__ __forceinline__ Where(int64_t rows, uint32_t per) {
+    __device__ __forceinline__ Where(int64_t rows, int64_t blocks) {
+        const uint32_t per = (uint32_t)blocks * (kCkpt8Block / V);
         const int64_t total = rows * per, base = ((int64_t)blockIdx.x * (kThreads / 64) + uniform(threadIdx.x >> 6)) * (64 * N);
         const int64_t row0 = total <= UINT32_MAX ? (int64_t)((uint32_t)base / per) : base / per;
         const uint32_t unit0 = (uint32_t)(base - row0 * per), lane = threadIdx.x & 63;
@@ -67,56 +37,77 @@ struct Where {
         for (int t = 0; t < N; ++t) {
             const uint32_t u = unit0 + t * 64 + lane, q = u / per;
             row[t] = row0 + q;
-            col[t] = (int)(u - q * per) * kHalf;
+            col[t] = (int)(u - q * per) * V;
             some[t] = base + t * 64 + lane < total;
         }
     }
 };
 
-// The scale byte of the block whose halves this lane and its neighbour hold.
-__device__ __forceinline__ uint32_t block_scale(const float (&f)[kHalf]) {
+__host__ __device__ inline int64_t blocks_of(int64_t cols) { return (cols + kCkpt8Block - 1) / kCkpt8Block; }
+
+// The scale byte of the block that this lane and its neighbours hold.
+template <int V>
+__device__ __forceinline__ uint32_t block_scale(const float (&f)[V]) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kHalf; ++i) {
+    for (int i = 0; i < V; ++i) {
         const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu;
         top = b < 0x7F800000u && b > top ? b : top;  // infinities and NaN do not set a scale
     }
-    const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false);  // lanes 1, 0, 3, 2
-    return ckpt8_scale(top > other ? top : other);
+    auto across = [&](auto control) {
+        const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, decltype(control)::value, 0xF, 0xF, false);
+        top = o > top ? o : top;
+    };
+    across(std::integral_constant<int, 0xB1>{});                          // lanes 1, 0, 3, 2
+    across(std::integral_constant<int, 0x4E>{});                          // lanes 2, 3, 0, 1
+    if constexpr (V == 4) across(std::integral_constant<int, 0x141>{});  // lanes 7 .. 0
+    return ckpt8_scale(top);
 }
 
-// A half block to its codes, and its scale from the block's first lane. Columns past the row are zeros, which the codes hold, too.
-template <bool STREAM>
-__device__ __forceinline__ void keep(float (&f)[kHalf], uint8_t* codes, uint8_t* scale, int col) {
+template <int V>
+struct CodeWord;
+template <>
+struct CodeWord<8> {
+    typedef uint32_t Type __attribute__((ext_vector_type(2)));
+};
+template <>
+struct CodeWord<4> {
+    typedef uint32_t Type __attribute__((ext_vector_type(1)));
+};
+
+// A piece of a block to its codes, and its scale from the block's first lane. Columns past the row are zeros, which the codes hold, too.
+template <bool STREAM, int V>
+__device__ __forceinline__ void keep(float (&f)[V], uint8_t* codes, uint8_t* scale, int col) {
     const uint32_t s = block_scale(f);
     if (s == kCkpt8MaxScale) {  // 1.9375 2^127 and more would become 2^128, which no load could give back: 1.875 2^127, the level below
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
+        for (int i = 0; i < V; ++i) {
             const uint32_t b = __float_as_uint(f[i]), m = b & 0x7FFFFFFFu;
             if (m >= 0x7F780000u && m < 0x7F800000u) f[i] = __uint_as_float((b & 0x80000000u) | 0x7F700000u);
         }
     }
     const float inverse = ckpt8_inverse(s);
-    u32x4_any c;
+    typename CodeWord<V>::Type c;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = ckpt8_encode(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], inverse);
-    u32x4_any* const to = reinterpret_cast<u32x4_any*>(codes + col);
+    for (int i = 0; i < V / 4; ++i) c[i] = ckpt8_encode(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], inverse);
+    auto* const to = reinterpret_cast<typename CodeWord<V>::Type*>(codes + col);
     if constexpr (STREAM) __builtin_nontemporal_store(c, to);
     else *to = c;
-    if (!(col & kHalf)) scale[col / kCkpt8Block] = (uint8_t)s;
+    if (!(col & (kCkpt8Block - 1))) scale[col / kCkpt8Block] = (uint8_t)s;
 }
 
+template <int V>
 struct Codes {
-    u32x4_any raw;
+    typename CodeWord<V>::Type raw;
     uint32_t scale;
     __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int col) {
-        raw = *reinterpret_cast<const u32x4_any*>(codes + col);
+        raw = *reinterpret_cast<const typename CodeWord<V>::Type*>(codes + col);
         scale = scales[col / kCkpt8Block];
     }
-    __device__ __forceinline__ void values(float (&f)[kHalf]) const {
+    __device__ __forceinline__ void values(float (&f)[V]) const {
         const float factor = ckpt8_factor(scale);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < V / 4; ++i) {
             float v[4];
             ckpt8_decode(raw[i], factor, v);
 #pragma unroll
@@ -127,33 +118,35 @@ struct Codes {
 
 template <typename T, int N, bool STREAM>
 __global__ __launch_bounds__(kThreads) void save_kernel(Ckpt8Job j) {
-    const Where<N> w(j.rows, (uint32_t)((j.cols + kCkpt8Block - 1) / kCkpt8Block * 2));
-    Unit<T> u[N];
+    using P = Piece<T>;
+    const Where<N, P::V> w(j.rows, blocks_of(j.cols));
+    u32x4_any u[N];
 #pragma unroll
     for (int t = 0; t < N; ++t)
-        if (w.some[t]) u[t].load(static_cast<const T*>(j.x) + w.row[t] * j.ldx + w.col[t], j.cols - w.col[t]);
+        if (w.some[t]) u[t] = P::load(static_cast<const T*>(j.x) + w.row[t] * j.ldx + w.col[t], j.cols - w.col[t]);
 #pragma unroll
     for (int t = 0; t < N; ++t) {
         if (!w.some[t]) continue;
-        float f[kHalf];
-        u[t].values(f);
+        float f[P::V];
+        P::unpack(u[t], f);
         keep<STREAM>(f, j.codes + w.row[t] * j.ldc, j.scales + w.row[t] * j.lds, w.col[t]);
     }
 }
 
 template <typename T, int N, bool STREAM>
 __global__ __launch_bounds__(kThreads) void load_kernel(Ckpt8Job j) {
-    const Where<N> w(j.rows, (uint32_t)((j.cols + kCkpt8Block - 1) / kCkpt8Block * 2));
-    Codes c[N];
+    using P = Piece<T>;
+    const Where<N, P::V> w(j.rows, blocks_of(j.cols));
+    Codes<P::V> c[N];
 #pragma unroll
     for (int t = 0; t < N; ++t)
         if (w.some[t]) c[t].load(j.codes + w.row[t] * j.ldc, j.scales + w.row[t] * j.lds, w.col[t]);
 #pragma unroll
     for (int t = 0; t < N; ++t) {
         if (!w.some[t]) continue;
-        float f[kHalf];
+        float f[P::V];
         c[t].values(f);
-        Unit<T>::template store<STREAM>(static_cast<T*>(j.out) + w.row[t] * j.ldx + w.col[t], j.cols - w.col[t], f);
+        P::template store<STREAM>(static_cast<T*>(j.out) + w.row[t] * j.ldx + w.col[t], j.cols - w.col[t], P::pack(f));
     }
 }
 
@@ -201,117 +194,107 @@ __device__ __forceinline__ float act_grad(const float (&u)[2], float da, float (
     }
 }
 
-template <typename T, int KIND, bool SAVE, int N, bool STREAM>
+// One piece a lane (two: 98304 x 1408 bf16 forward and back 280 us instead of 267).
+template <typename T, int KIND, bool SAVE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void act_kernel(ActJob j) {
-    constexpr int kParts = KIND == kActSwiglu ? 2 : 1;
-    const int64_t blocks = (j.cols + kCkpt8Block - 1) / kCkpt8Block;
-    const Where<N> w(j.rows, (uint32_t)(blocks * 2));
-    Unit<T> u[N][kParts];
+    using P = Piece<T>;
+    constexpr int kParts = KIND == kActSwiglu ? 2 : 1, V = P::V;
+    const int64_t blocks = blocks_of(j.cols);
+    const Where<1, V> w(j.rows, blocks);
+    if (!w.some[0]) return;
+    const int64_t row = w.row[0], left = j.cols - w.col[0];
+    const int col = w.col[0];
+    u32x4_any u[kParts];
 #pragma unroll
-    for (int t = 0; t < N; ++t)
+    for (int p = 0; p < kParts; ++p) u[p] = P::load(static_cast<const T*>(j.u) + row * j.ldu + p * j.cols + col, left);
+    float f[kParts][V], a[V];
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) P::unpack(u[p], f[p]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float v[2] = {f[0][i], f[kParts - 1][i]};
+        a[i] = act<KIND>(v);
+    }
+    P::template store<STREAM>(static_cast<T*>(j.a) + row * j.lda + col, left, P::pack(a));
+    if constexpr (SAVE)
 #pragma unroll
         for (int p = 0; p < kParts; ++p)
-            if (w.some[t]) u[t][p].load(static_cast<const T*>(j.u) + w.row[t] * j.ldu + p * j.cols + w.col[t], j.cols - w.col[t]);
-#pragma unroll
-    for (int t = 0; t < N; ++t) {
-        if (!w.some[t]) continue;
-        float f[kParts][kHalf], a[kHalf];
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) u[t][p].values(f[p]);
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            const float v[2] = {f[0][i], f[kParts - 1][i]};
-            a[i] = act<KIND>(v);
-        }
-        Unit<T>::template store<STREAM>(static_cast<T*>(j.a) + w.row[t] * j.lda + w.col[t], j.cols - w.col[t], a);
-        if constexpr (SAVE)
-#pragma unroll
-            for (int p = 0; p < kParts; ++p)
-                keep<STREAM>(f[p], j.codes + w.row[t] * j.ldc + p * blocks * kCkpt8Block, j.scales + w.row[t] * j.lds + p * blocks, w.col[t]);
-    }
+            keep<STREAM>(f[p], j.codes + row * j.ldc + p * blocks * kCkpt8Block, j.scales + row * j.lds + p * blocks, col);
 }
 
-template <typename T, int KIND, bool SAVED, int N, bool STREAM>
+template <typename T, int KIND, bool SAVED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(ActJob j) {
-    constexpr int kParts = KIND == kActSwiglu ? 2 : 1;
-    const int64_t blocks = (j.cols + kCkpt8Block - 1) / kCkpt8Block;
-    const Where<N> w(j.rows, (uint32_t)(blocks * 2));
-    Unit<T> d[N], u[N][kParts];
-    Codes c[N][kParts];
+    using P = Piece<T>;
+    constexpr int kParts = KIND == kActSwiglu ? 2 : 1, V = P::V;
+    const int64_t blocks = blocks_of(j.cols);
+    const Where<1, V> w(j.rows, blocks);
+    if (!w.some[0]) return;
+    const int64_t row = w.row[0], left = j.cols - w.col[0];
+    const int col = w.col[0];
+    const u32x4_any d = P::load(static_cast<const T*>(j.da) + row * j.ldda + col, left);
+    float f[kParts][V], da[V], du[kParts][V], a[V];
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-        if (!w.some[t]) continue;
-        d[t].load(static_cast<const T*>(j.da) + w.row[t] * j.ldda + w.col[t], j.cols - w.col[t]);
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            if constexpr (SAVED)
-                c[t][p].load(j.codes + w.row[t] * j.ldc + p * blocks * kCkpt8Block, j.scales + w.row[t] * j.lds + p * blocks, w.col[t]);
-            else
-                u[t][p].load(static_cast<const T*>(j.u) + w.row[t] * j.ldu + p * j.cols + w.col[t], j.cols - w.col[t]);
+    for (int p = 0; p < kParts; ++p) {
+        if constexpr (SAVED) {
+            Codes<V> c;
+            c.load(j.codes + row * j.ldc + p * blocks * kCkpt8Block, j.scales + row * j.lds + p * blocks, col);
+            c.values(f[p]);
+        } else {
+            P::unpack(P::load(static_cast<const T*>(j.u) + row * j.ldu + p * j.cols + col, left), f[p]);
         }
     }
+    P::unpack(d, da);
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-        if (!w.some[t]) continue;
-        float f[kParts][kHalf], da[kHalf], du[kParts][kHalf], a[kHalf];
-        d[t].values(da);
+    for (int i = 0; i < V; ++i) {
+        const float v[2] = {f[0][i], f[kParts - 1][i]};
+        float g[2];
+        a[i] = act_grad<KIND>(v, da[i], g);
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) {
-            if constexpr (SAVED) c[t][p].values(f[p]);
-            else u[t][p].values(f[p]);
-        }
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            const float v[2] = {f[0][i], f[kParts - 1][i]};
-            float g[2];
-            a[i] = act_grad<KIND>(v, da[i], g);
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) du[p][i] = g[p];
-        }
-#pragma unroll
-        for (int p = 0; p < kParts; ++p)
-            Unit<T>::template store<STREAM>(static_cast<T*>(j.du) + w.row[t] * j.lddu + p * j.cols + w.col[t], j.cols - w.col[t], du[p]);
-        if (j.a) Unit<T>::template store<STREAM>(static_cast<T*>(j.a) + w.row[t] * j.lda + w.col[t], j.cols - w.col[t], a);
+        for (int p = 0; p < kParts; ++p) du[p][i] = g[p];
     }
+#pragma unroll
+    for (int p = 0; p < kParts; ++p)
+        P::template store<STREAM>(static_cast<T*>(j.du) + row * j.lddu + p * j.cols + col, left, P::pack(du[p]));
+    if (j.a) P::template store<STREAM>(static_cast<T*>(j.a) + row * j.lda + col, left, P::pack(a));
 }
 
-int64_t units(int64_t rows, int64_t cols) { return rows * ((cols + kCkpt8Block - 1) / kCkpt8Block * 2); }
+int64_t pieces(int64_t rows, int64_t cols, bool bf16) { return rows * blocks_of(cols) * (kCkpt8Block / (bf16 ? 8 : 4)); }
 
 unsigned grid(int64_t n, int each) { return (unsigned)((n + kThreads * each - 1) / (kThreads * each)); }
 
-// Units a thread: several where the chip is full all the same.
-constexpr int64_t kManyUnits = int64_t(256) * 2048 * 4;
+// Two pieces a lane for tensors of 2^24 pieces and more (1 GiB of bf16 to 8 bits and back, us, one / two / four / eight a lane: 567 / 537 /
+// 539 / 554; 4099 x 1411 fp32 14.2 / 15.0).
+constexpr int kTwo = 2;
+constexpr int64_t kTwoPieces = int64_t(1) << 24;
 
 template <typename T, int N>
 void save_stream(const Ckpt8Job& j, bool stream, hipStream_t s) {
-    const unsigned n = grid(units(j.rows, j.cols), N);
+    const unsigned n = grid(pieces(j.rows, j.cols, j.bf16), N);
     if (stream) save_kernel<T, N, true><<<n, kThreads, 0, s>>>(j);
     else save_kernel<T, N, false><<<n, kThreads, 0, s>>>(j);
 }
 template <typename T, int N>
 void load_stream(const Ckpt8Job& j, bool stream, hipStream_t s) {
-    const unsigned n = grid(units(j.rows, j.cols), N);
+    const unsigned n = grid(pieces(j.rows, j.cols, j.bf16), N);
     if (stream) load_kernel<T, N, true><<<n, kThreads, 0, s>>>(j);
     else load_kernel<T, N, false><<<n, kThreads, 0, s>>>(j);
 }
 
-template <typename T, int KIND, bool SAVED, int N>
+template <typename T, int KIND, bool SAVED>
 void act_stream(const ActJob& j, bool bwd, bool stream, hipStream_t s) {
-    const unsigned n = grid(units(j.rows, j.cols), N);
+    const unsigned n = grid(pieces(j.rows, j.cols, j.bf16), 1);
     if (bwd) {
-        if (stream) act_bwd_kernel<T, KIND, SAVED, N, true><<<n, kThreads, 0, s>>>(j);
-        else act_bwd_kernel<T, KIND, SAVED, N, false><<<n, kThreads, 0, s>>>(j);
+        if (stream) act_bwd_kernel<T, KIND, SAVED, true><<<n, kThreads, 0, s>>>(j);
+        else act_bwd_kernel<T, KIND, SAVED, false><<<n, kThreads, 0, s>>>(j);
     } else {
-        if (stream) act_kernel<T, KIND, SAVED, N, true><<<n, kThreads, 0, s>>>(j);
-        else act_kernel<T, KIND, SAVED, N, false><<<n, kThreads, 0, s>>>(j);
+        if (stream) act_kernel<T, KIND, SAVED, true><<<n, kThreads, 0, s>>>(j);
+        else act_kernel<T, KIND, SAVED, false><<<n, kThreads, 0, s>>>(j);
     }
 }
 
 template <typename T, int KIND>
 void act_saved(const ActJob& j, bool bwd, bool stream, hipStream_t s) {
-    const bool many = units(j.rows, j.cols) >= kManyUnits;
-    if (j.codes) many ? act_stream<T, KIND, true, 2>(j, bwd, stream, s) : act_stream<T, KIND, true, 1>(j, bwd, stream, s);
-    else many ? act_stream<T, KIND, false, 2>(j, bwd, stream, s) : act_stream<T, KIND, false, 1>(j, bwd, stream, s);
+    j.codes ? act_stream<T, KIND, true>(j, bwd, stream, s) : act_stream<T, KIND, false>(j, bwd, stream, s);
 }
 
 hipError_t launch_any(const ActJob& j, bool bwd, hipStream_t s) {
@@ -324,24 +307,22 @@ hipError_t launch_any(const ActJob& j, bool bwd, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_ckpt8_save(const Ckpt8Job& j, hipStream_t s) {
-    const int64_t n = units(j.rows, j.cols);
-    const bool many = n >= kManyUnits, stream = n * kHalf >= kStreamBytes;
-    if (j.bf16) many ? save_stream<uint16_t, 4>(j, stream, s) : save_stream<uint16_t, 1>(j, stream, s);
-    else many ? save_stream<float, 2>(j, stream, s) : save_stream<float, 1>(j, stream, s);
+    const bool many = pieces(j.rows, j.cols, j.bf16) >= kTwoPieces, stream = j.rows * j.cols >= kStreamBytes;
+    if (j.bf16) many ? save_stream<uint16_t, kTwo>(j, stream, s) : save_stream<uint16_t, 1>(j, stream, s);
+    else many ? save_stream<float, kTwo>(j, stream, s) : save_stream<float, 1>(j, stream, s);
     return hipGetLastError();
 }
 
 hipError_t launch_ckpt8_load(const Ckpt8Job& j, hipStream_t s) {
-    const int64_t n = units(j.rows, j.cols);
-    const bool many = n >= kManyUnits, stream = n * kHalf * (j.bf16 ? 2 : 4) >= kStreamBytes;
-    if (j.bf16) many ? load_stream<uint16_t, 4>(j, stream, s) : load_stream<uint16_t, 1>(j, stream, s);
-    else many ? load_stream<float, 2>(j, stream, s) : load_stream<float, 1>(j, stream, s);
+    const bool many = pieces(j.rows, j.cols, j.bf16) >= kTwoPieces, stream = j.rows * j.cols * (j.bf16 ? 2 : 4) >= kStreamBytes;
+    if (j.bf16) many ? load_stream<uint16_t, kTwo>(j, stream, s) : load_stream<uint16_t, 1>(j, stream, s);
+    else many ? load_stream<float, kTwo>(j, stream, s) : load_stream<float, 1>(j, stream, s);
     return hipGetLastError();
 }
 
 hipError_t launch_act(const ActJob& j, hipStream_t s) { return launch_any(j, false, s); }
 hipError_t launch_act_bwd(const ActJob& j, hipStream_t s) { return launch_any(j, true, s); }
 
-int64_t ckpt8_units(int64_t rows, int64_t cols) { return units(rows, cols); }
+int64_t ckpt8_units(int64_t rows, int64_t cols) { return rows * blocks_of(cols) * (kCkpt8Block / 4); }
 
 }  // namespace ufp4

@@ -22,6 +22,7 @@ namespace {
 
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 
 #define INLINE __attribute__((always_inline))
 
@@ -692,6 +693,125 @@ using Tile256 = Tile<4, 2, 2, 4, Depth<PASS>::K, Depth<PASS>::kRing, 1>;  // 256
 template <int PASS>
 using Tile128 = Tile<2, 2, 2, 2, Depth<PASS>::K, Depth<PASS>::kRing, 2>;  // 128 x 128: 4 waves of 64 x 64, two workgroups per CU
 
+// ------------------------------------------------------------------------------------------------
+// Few rows (a decode step): bound by reading the weights of the groups that have any.
+// ------------------------------------------------------------------------------------------------
+
+// A workgroup takes 16 CT columns of one group's product and reads its rows of W once, from memory to the registers of
+// v_mfma_f32_16x16x32_bf16 (16 rows x 64 consecutive bytes a load); its waves split the reduction in chunks of 64 places and add their sums
+// in order. RT tiles of 16 rows at a time; of more rows W is read again, from the L2. Any size, stride and alignment.
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewChunk = 64;
+
+template <int OUT, int CT, int RT>
+__global__ __launch_bounds__(kFewThreads) void gemm_bf16_few_kernel(Bf16GemmJob j) {
+    constexpr int kTiles = CT * RT;
+    __shared__ float4 sums[kFewWaves][kTiles * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), quarter = lane >> 4, l16 = lane & 15;
+    const uint32_t chunks = (uint32_t)((j.N + 16 * CT - 1) / (16 * CT)), rank = blockIdx.x / chunks;
+    const int64_t col0 = (int64_t)(blockIdx.x % chunks) * (16 * CT);
+    // the group: the rank-th of those that have rows
+    int64_t start = 0, rows = 0;
+    int g = -1;
+    uint32_t before = 0;
+    for (int g0 = 0; g0 < j.G && g < 0; g0 += 64) {
+        const int e = g0 + lane;
+        const int64_t from = e < j.G ? clamped(j.offsets[e], j.tokens) : 0, m = e < j.G ? clamped(j.offsets[e + 1], j.tokens) - from : 0;
+        uint64_t some = __ballot(m > 0);
+        const uint32_t n = (uint32_t)__popcll(some);
+        if (before + n > rank) {
+            for (uint32_t skip = rank - before; skip > 0; --skip) some &= some - 1;
+            const int at = uniform(__builtin_ctzll(some));
+            g = g0 + at;
+            start = __builtin_amdgcn_readlane((int)from, at);
+            rows = __builtin_amdgcn_readlane((int)m, at);
+        }
+        before += n;
+    }
+    if (g < 0) return;
+    const uint16_t* w[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {  // columns past the last one are not stored
+        const int64_t n = col0 + t * 16 + l16;
+        w[t] = j.b + ((int64_t)g * j.N + (n < j.N ? n : j.N - 1)) * j.ldb;
+    }
+    for (int64_t r0 = 0; r0 < rows; r0 += 16 * RT) {
+        const uint16_t* x[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int64_t r = r0 + t * 16 + l16;
+            x[t] = j.a + (start + (r < rows ? r : rows - 1)) * j.lda;
+        }
+        v4f acc[CT][RT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc[c][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        constexpr int kSteps = kFewChunk / 32;
+        struct Chunk {
+            u32x4_any w[CT][kSteps], x[RT][kSteps];
+        };
+        auto load = [&](Chunk& c, int64_t k0) INLINE {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int64_t k = k0 + s * 32 + quarter * 8;
+#pragma unroll
+                for (int t = 0; t < CT; ++t) c.w[t][s] = Piece<uint16_t>::load(w[t] + k, j.red - k);
+#pragma unroll
+                for (int t = 0; t < RT; ++t) c.x[t][s] = Piece<uint16_t>::load(x[t] + k, j.red - k);
+            }
+        };
+        auto multiply = [&](const Chunk& c) INLINE {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int n = 0; n < CT; ++n)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, c.w[n][s]), __builtin_bit_cast(v8b, c.x[t][s]),
+                                                                            acc[n][t], 0, 0, 0);
+        };
+        constexpr int64_t kStep = kFewWaves * kFewChunk;
+        int64_t k = wave * kFewChunk;
+        Chunk c0, c1;
+        if (k < j.red) load(c0, k);
+        for (; k + kStep < j.red; k += 2 * kStep) {
+            load(c1, k + kStep);
+            multiply(c0);
+            if (k + 2 * kStep < j.red) load(c0, k + 2 * kStep);
+            multiply(c1);
+        }
+        if (k < j.red) multiply(c0);
+        // A lane has columns 4 quarter .. + 3 of row l16 of each tile.
+#pragma unroll
+        for (int n = 0; n < CT; ++n)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) sums[wave][(n * RT + t) * 64 + lane] = make_float4(acc[n][t][0], acc[n][t][1], acc[n][t][2], acc[n][t][3]);
+        __syncthreads();
+        for (int i = tid; i < kTiles * 64; i += kFewThreads) {
+            float4 v = sums[0][i];
+#pragma unroll
+            for (int o = 1; o < kFewWaves; ++o) {
+                const float4 u = sums[o][i];
+                v.x += u.x;
+                v.y += u.y;
+                v.z += u.z;
+                v.w += u.w;
+            }
+            const int64_t r = r0 + (i / 64 % RT) * 16 + (i & 15), c = col0 + (i / 64 / RT) * 16 + (i >> 4 & 3) * 4;
+            const float f[4] = {v.x, v.y, v.z, v.w};
+            if (r >= rows) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c + e >= j.N) continue;
+                const int64_t at = (start + r) * j.ldc + c + e;
+                if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[at] = f[e];
+                else static_cast<uint16_t*>(j.c)[at] = __builtin_bit_cast(uint16_t, (__bf16)f[e]);
+            }
+        }
+        __syncthreads();  // the sums are read before the next rows' are written
+    }
+}
+
 // Tile rows that a launch provides for; ragged rows: every group may end in a partial tile.
 int64_t tile_rows(const Bf16GemmJob& j, int bm) {
     return j.pass != kBf16BwdDw ? (j.tokens + bm - 1) / bm + j.G : (j.M + bm - 1) / bm;
@@ -740,6 +860,26 @@ hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
     return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false>(j, s);
 }
 
+// Which products the few-row kernel takes: up to 8 rows a group on average, or 64 in all. Past that its rows of W come through the L2 more than
+// once, and 128-row tiles read them less often. Measured, us, few-row kernel / 128 x 128 tiles:
+//     64 experts 2048 -> 1408, 6 a token: 42 rows 21.0 / 35.3, 96 45 / 47, 192 51 / 82, 384 83 / 99, 768 110 / 108, 1536 144 / 114;
+//     8 experts 512 -> 1312, 2 a token: 2 rows 5.5 / 8.3, 32 5.6 / 8.4, 64 7.1 / 8.4, 128 9.0 / 8.5;
+//     8 experts 5120 -> 4096: 2 rows 15.8 / 48.3, 32 62 / 75, 64 77 / 75, 128 110 / 80;
+//     one group 2048 -> 8192: 1 row 7.4 / 20.6, 32 10.9 / 22.0, 64 15.3 / 22.3, 128 27.8 / 23.1.
+bool few(const Bf16GemmJob& j) { return j.pass == kBf16FwdY && (j.tokens <= 64 || j.tokens <= 8 * (int64_t)j.G); }
+
+// 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8).
+constexpr int kFewCols = 2;
+template <int OUT>
+hipError_t launch_few(const Bf16GemmJob& j, hipStream_t s) {
+    const int64_t groups = j.tokens < j.G ? j.tokens : j.G;  // that can have rows
+    const unsigned n = (unsigned)((j.N + 16 * kFewCols - 1) / (16 * kFewCols) * groups);
+    if (j.tokens <= 16 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 1><<<n, kFewThreads, 0, s>>>(j);
+    else if (j.tokens <= 32 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 2><<<n, kFewThreads, 0, s>>>(j);
+    else gemm_bf16_few_kernel<OUT, kFewCols, 4><<<n, kFewThreads, 0, s>>>(j);
+    return hipGetLastError();
+}
+
 template <int OUT>
 hipError_t launch_any(const Bf16GemmJob& j, hipStream_t s) {
     const unsigned n = (unsigned)grid_tiles(j, kAnyTile, kAnyTile);
@@ -756,6 +896,7 @@ hipError_t launch_any(const Bf16GemmJob& j, hipStream_t s) {
 template <int OUT>
 hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
     if (grid_tiles(j, kAnyTile, kAnyTile) == 0) return hipSuccess;
+    if (few(j)) return launch_few<OUT>(j, s);
     if (!pieces(j)) return launch_any<OUT>(j, s);
     switch (j.pass) {
         case kBf16FwdY: return launch_pass<OUT, kBf16FwdY>(j, s);
@@ -767,11 +908,15 @@ hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
 }  // namespace
 
 int64_t bf16_gemm_workspace(const Bf16GemmJob& j) {
+    if (few(j)) return 0;
     const int tile = large(j) ? 256 : 128, resident = large(j) ? Tile256<kBf16FwdY>::kResident : Tile128<kBf16FwdY>::kResident;
     return grid_tiles(j, tile, tile) > resident ? kCounters * 4 : 0;
 }
 
-bool bf16_gemm_fits(const Bf16GemmJob& j) { return grid_tiles(j, kAnyTile, kAnyTile) < int64_t(1) << 24; }
+bool bf16_gemm_fits(const Bf16GemmJob& j) {
+    constexpr int64_t kMost = int64_t(1) << 23;  // a grid holds fewer than 2^32 threads
+    return grid_tiles(j, kAnyTile, kAnyTile) < kMost && (!few(j) || (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * j.G < kMost);
+}
 
 hipError_t launch_gemm_bf16(const Bf16GemmJob& j, hipStream_t s) {
     return j.out_dtype == kOutBF16 ? launch_out<kOutBF16>(j, s) : launch_out<kOutF32>(j, s);
