@@ -628,8 +628,10 @@ int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void *dy_dev, int64_t tokens, int6
  * that is more (magnitudes from 1.9375 2^127 on are kept as 1.875 2^127, the next level being no fp32 number); an infinity or NaN is kept as NaN and leaves its block's other values alone. Every kept value is a bf16 number.
  * A row of `cols` values has ceil(cols / 32) scales and 32 ceil(cols / 32) codes, those past `cols` 0.
  *
- * ufp4_ckpt8_ld -- the smallest leading dimensions (bytes) of codes and scales of a row in `parts` parts of `cols` values each, every
- *   part in blocks of its own (parts 1; 2 for the input of a gated activation).
+ * ufp4_ckpt8_ld -- leading dimensions (bytes) of codes and scales of a row in `parts` parts of `cols` values each, every part in blocks of
+ *   its own (parts 1; 2 for the input of a gated activation): the blocks, scales filled up to a multiple of 4. Other ones are taken as long
+ *   as the blocks fit. Where scales_dev and scale_ld are multiples of 4, scales are read 4 at a time: every row, the last one too, must
+ *   then be readable to such a multiple.
  * ufp4_ckpt8_save, ufp4_ckpt8_load -- a tensor [rows, cols] of type `dtype` to codes and scales, and back. Codes 16-byte aligned with
  *   code_ld % 16 == 0.
  */

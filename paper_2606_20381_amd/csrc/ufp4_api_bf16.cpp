@@ -135,7 +135,7 @@ int ufp4_ckpt8_ld(int64_t cols, int parts, int64_t* code_ld, int64_t* scale_ld) 
     if (cols < 0 || parts < 1 || parts > 2) return UFP4_ERR_INVALID_ARG;
     if (cols > kMostCols) return UFP4_ERR_UNSUPPORTED;
     if (code_ld) *code_ld = parts * blocks_of(cols) * kCkpt8Block;
-    if (scale_ld) *scale_ld = parts * blocks_of(cols);
+    if (scale_ld) *scale_ld = (parts * blocks_of(cols) + 3) / 4 * 4;
     return UFP4_OK;
 }
 

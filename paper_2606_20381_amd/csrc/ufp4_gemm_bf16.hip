@@ -349,14 +349,19 @@ __global__ void clear_counters_kernel(uint32_t* counters) { counters[threadIdx.x
 
 // The pipeline: a ring of stages in LDS, filled by direct-to-LDS loads; each wave keeps two sets of operands in registers: while the
 // matrix core works on one step of a stage, the next step's operands (past the barrier, the next stage's first) are read from LDS.
-template <int OUT, class C, int PASS, bool STREAM>
+// SAVED (bwd_dw): B is an 8-bit checkpoint. The ring holds its codes and scales; a stage of them becomes bf16, in one of two further slots,
+// one stage before it is multiplied, 16 codes of one scale a thread.
+template <int OUT, class C, int PASS, bool STREAM, bool SAVED>
 __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16GemmJob j) {
     using P = Pass<PASS>;
     constexpr int BM = C::BM, BN = C::BN, WTM = C::WTM, WTN = C::WTN, kRing = C::kRing;
     using SA = Stage<BM, C::K, P::kAcrossA>;
     using SB = Stage<BN, C::K, P::kAcrossB>;
-    constexpr uint32_t kSlot = SA::kSize + SB::kSize;
+    static_assert(!SAVED || (C::K == 32 && C::kLoadsB == 2 && kRing >= 3), "a wave's two loads are 1 KiB of codes and the scales");
+    constexpr uint32_t kCodes = C::K * BN, kScales = 256;  // bytes of a stage of a checkpoint
+    constexpr uint32_t kSlot = SA::kSize + (SAVED ? kCodes + kScales : SB::kSize);
     __shared__ __align__(16) uint8_t ring[kRing * kSlot];
+    __shared__ __align__(16) uint8_t unpacked[SAVED ? 2 * SB::kSize : 16];
     __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
     __shared__ uint32_t s_next;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -389,14 +394,15 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     // One output tile: its operands' places of stage 0, this lane's pieces of a stage, and where the results go. A reduction of no whole
     // stages begins inside stage 0: its first `gap` places are zeroed in LDS (memory is read from the first place on).
     struct Work {
-        const uint8_t *a, *b;
+        const uint8_t *a, *b, *s;  // s: a checkpoint's scales
         uint32_t va[C::kLoadsA], vb[C::kLoadsB];
         int nst, gap;
         int row0, rows, col0;
         int64_t c_base;
         bool idle;  // this wave's part is outside of the output: it loads with the others, and multiplies nothing
     };
-    const uint32_t stepA = P::kAcrossA ? (uint32_t)(C::K * 2 * j.lda) : C::K * 2, stepB = P::kAcrossB ? (uint32_t)(C::K * 2 * j.ldb) : C::K * 2;
+    const uint32_t stepA = P::kAcrossA ? (uint32_t)(C::K * 2 * j.lda) : C::K * 2, stepB = P::kAcrossB ? (uint32_t)(C::K * (SAVED ? 1 : 2) * j.ldb) : C::K * 2;
+    const uint32_t stepS = SAVED ? (uint32_t)(C::K * j.ldbs) : 0;
     // Lane's piece of load q (unit wave * loads + q of the stage: 64 pieces in the LDS's order), as an offset from the operand's first
     // row and place. Rows past the last one are replaced by it: they only feed outputs that are not stored. Places before `gap` (a
     // multiple of 8 along the reduction) are replaced by that one.
@@ -409,7 +415,20 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         return ((r < have ? r : (uint32_t)have - 1) * (uint32_t)ld + k) * 2;
     };
     auto offset_a = [&](const Work& w, int q, int gap) INLINE { return offset(SA{}, wave * C::kLoadsA + q, j.lda, w.rows, gap); };
-    auto offset_b = [&](const Work& w, int q, int gap) INLINE { return offset(SB{}, wave * C::kLoadsB + q, j.ldb, j.N - w.col0, gap); };
+    auto offset_b = [&](const Work& w, int q, int gap) INLINE {
+        if constexpr (!SAVED) {
+            return offset(SB{}, wave * C::kLoadsB + q, j.ldb, j.N - w.col0, gap);
+        } else {  // 16 codes, or 4 scales; past the last block's the last ones
+            constexpr uint32_t kEach = BN / 16, kWords = BN / 128;
+            const uint32_t blocks = (uint32_t)((j.N - w.col0 + kCkpt8Block - 1) / kCkpt8Block);
+            const uint32_t i = q == 0 ? (uint32_t)wave * 64 + lane : (uint32_t)lane % (C::K * kWords);
+            uint32_t k = i / (q == 0 ? kEach : kWords), at = i % (q == 0 ? kEach : kWords);
+            k = k < (uint32_t)gap ? (uint32_t)gap : k;
+            const uint32_t most = q == 0 ? blocks * 2 : (blocks + 3) / 4;
+            at = at < most ? at : most - 1;
+            return q == 0 ? k * (uint32_t)j.ldb + at * 16 : k * (uint32_t)j.ldbs + at * 4;
+        }
+    };
     auto locate = [&](uint32_t L, Work& w) INLINE {
         int tm, tn;
         int64_t k0 = 0, k1 = j.red, row0, rows;
@@ -437,7 +456,12 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         w.idle = wm * WTM * 32 >= rows || wn * WTN * 32 >= j.N - w.col0;
         const int64_t k = k0 - w.gap;
         w.a = reinterpret_cast<const uint8_t*>(j.a) + uniform64((P::kAcrossA ? k * j.lda + row0 : row0 * j.lda + k) * 2);
-        w.b = reinterpret_cast<const uint8_t*>(b) + uniform64((P::kAcrossB ? k * j.ldb + w.col0 : w.col0 * j.ldb + k) * 2);
+        if constexpr (SAVED) {
+            w.b = j.b8 + uniform64(k * j.ldb + w.col0);
+            w.s = j.bs + uniform64(k * j.ldbs + w.col0 / kCkpt8Block);
+        } else {
+            w.b = reinterpret_cast<const uint8_t*>(b) + uniform64((P::kAcrossB ? k * j.ldb + w.col0 : w.col0 * j.ldb + k) * 2);
+        }
 #pragma unroll
         for (int q = 0; q < C::kLoadsA; ++q) w.va[q] = offset_a(w, q, 0);
 #pragma unroll
@@ -451,6 +475,14 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         if constexpr (decltype(first)::value) v = is_a ? offset_a(w, u, w.gap) : offset_b(w, u, w.gap);
         else v = is_a ? w.va[u] : w.vb[u];
         // the address in scalar registers whatever the compiler took it for
+        if constexpr (SAVED) {
+            if (!is_a) {
+                const int64_t from = uniform64(u == 0 ? (int64_t)w.b + (int64_t)i * stepB : (int64_t)w.s + (int64_t)i * stepS);
+                if (u == 0) to_lds16(v, reinterpret_cast<const void*>(from), ring + slot + SA::kSize + wave * 1024);
+                else to_lds4(v, reinterpret_cast<const void*>(from), ring + slot + SA::kSize + kCodes);  // every wave the same
+                return;
+            }
+        }
         const int64_t base = uniform64(is_a ? (int64_t)w.a + (int64_t)i * stepA : (int64_t)w.b + (int64_t)i * stepB);
         to_lds16(v, reinterpret_cast<const void*>(base), ring + slot + (is_a ? 0 : SA::kSize) + (wave * (is_a ? C::kLoadsA : C::kLoadsB) + u) * 1024);
     };
@@ -463,11 +495,12 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
 #pragma unroll
             for (int q = 0; q < C::kWaveLoads; ++q) issue_one(w, q, i, i * kSlot, std::false_type{});
     };
-    // Zeros over the places before the gap's end, in what this wave has loaded of stage 0.
+    // Zeros over the places before the gap's end, in what this wave has loaded of stage 0. (A checkpoint's codes stay, those of a row of the
+    // group, no infinity among them: a NaN makes the whole column NaN with or without them, all else is multiplied by A's zeros.)
     auto close_gap = [&](const Work& w, uint32_t slot) INLINE {
         const u32x4_any zero = {0, 0, 0, 0};
 #pragma unroll
-        for (int q = 0; q < C::kWaveLoads; ++q) {
+        for (int q = 0; q < (SAVED ? C::kLoadsA : C::kWaveLoads); ++q) {
             const bool is_a = q < C::kLoadsA;
             const int unit = is_a ? wave * C::kLoadsA + q : wave * C::kLoadsB + q - C::kLoadsA;
             uint32_t r, k;
@@ -482,8 +515,28 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         v8b v[kOps];
     };
     const uint32_t arow = (uint32_t)wm * WTM * 32, bcol = (uint32_t)wn * WTN * 32;
-    auto read_one = [&](int t, uint32_t slot, int ks, Operands& f) INLINE {
-        f.v[t] = t < WTN ? SB::read(ring + slot + SA::kSize, bcol + t * 32, ks) : SA::read(ring + slot, arow + (t - WTN) * 32, ks);
+    uint32_t b_slot = 0;  // SAVED: where the present stage's B is in `unpacked`; the next one's is in the other
+    // Operand t of the present stage at `slot`, or (`ahead`) of the next one.
+    auto read_one = [&](int t, uint32_t slot, int ks, bool ahead, Operands& f) INLINE {
+        if (t >= WTN) f.v[t] = SA::read(ring + slot, arow + (t - WTN) * 32, ks);
+        else if constexpr (SAVED) f.v[t] = SB::read(unpacked + (ahead ? b_slot ^ SB::kSize : b_slot), bcol + t * 32, ks);
+        else f.v[t] = SB::read(ring + slot + SA::kSize, bcol + t * 32, ks);
+    };
+    // SAVED: this thread's 16 codes of the stage at `slot` to bf16, in `unpacked` at `to`; in two steps, reading and the rest.
+    u32x4_any codes;
+    uint32_t code_scale = 0;
+    auto unpack_read = [&](uint32_t slot) INLINE {
+        constexpr uint32_t kEach = BN / 16;
+        const uint8_t* const from = ring + slot + SA::kSize;
+        codes = *reinterpret_cast<const u32x4_any*>(from + tid * 16);
+        code_scale = from[kCodes + tid / kEach * (BN / 32) + tid % kEach / 2];
+    };
+    auto unpack_write = [&](uint32_t to) INLINE {
+        constexpr uint32_t kEach = BN / 16;
+        u32x4_any lo, hi;
+        ckpt8_to_bf16(codes, code_scale, lo, hi);
+        *reinterpret_cast<u32x4_any*>(unpacked + to + SB::across(tid / kEach, tid % kEach * 2)) = lo;
+        *reinterpret_cast<u32x4_any*>(unpacked + to + SB::across(tid / kEach, tid % kEach * 2 + 1)) = hi;
     };
     // B's rows are the instruction's rows, so that a lane gets runs of consecutive columns of one row of C.
     v16f acc[WTM][WTN];
@@ -529,7 +582,12 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
                 if (last ? kMore : !decltype(idle)::value) {
 #pragma unroll
                     for (int t = k * kOpsPer; t < (k + 1) * kOpsPer && t < kOps; ++t)
-                        read_one(t, last ? next : cur, last ? 0 : ks + 1, f[(ks + 1) & 1]);
+                        read_one(t, last ? next : cur, last ? 0 : ks + 1, last, f[(ks + 1) & 1]);
+                }
+                if constexpr (SAVED && kMore) {  // the stage after the next, over the present one's B, which has been read
+                    static_assert(!SAVED || kTiles >= 4, "");
+                    if (last && k == 0) unpack_read(next == (kRing - 1) * kSlot ? 0 : next + kSlot);
+                    if (last && k == kTiles - 2) unpack_write(b_slot);
                 }
                 if constexpr (kLoads) {
                     if (last)
@@ -571,10 +629,18 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     auto advance = [&] INLINE {
         cur = next;
         next = next == (kRing - 1) * kSlot ? 0 : next + kSlot;
+        if constexpr (SAVED) b_slot ^= SB::kSize;
     };
     auto begin = [&] INLINE {
+        if constexpr (SAVED) {  // the first two stages
+            unpack_read(cur);
+            unpack_write(b_slot);
+            unpack_read(next);
+            unpack_write(b_slot ^ SB::kSize);
+            __syncthreads();
+        }
 #pragma unroll
-        for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, f[0]);
+        for (int t = 0; t < kOps; ++t) read_one(t, cur, 0, false, f[0]);
     };
     using std::integral_constant;
     constexpr int L1 = C::kWaveLoads;
@@ -586,9 +652,10 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     // reads the first's operands. A tile's stores are then younger than those loads, and memory operations complete in order, so the next
     // tile's first waits count them in instead of waiting for them.
     constexpr int kLong = 2 * kRing;
+    constexpr int kAhead = SAVED ? 2 : 1;  // what a stage's barrier lets be read has landed up to this many stages on
+    constexpr integral_constant<int, (kRing - 1 - kAhead) * L1> kept{};
     if (w.nst >= kLong) {
-        constexpr integral_constant<int, (kRing - 2) * L1> kept{};
-        arrive(integral_constant<int, (kRing - 1) * L1>{}, yes, w, cur);
+        arrive(integral_constant<int, (kRing - kAhead) * L1>{}, yes, w, cur);
         begin();
         bool behind = false;  // kStores stores were issued after the loads
         while (true) {
@@ -600,8 +667,8 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
             auto run = [&](auto idle) INLINE {
                 int i = 0;
                 if (behind) {
-                    for (; i < kRing - 1; ++i) {
-                        stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1 + kStores>{}, w, i + kRing, yes, no, no);
+                    for (; i < kRing - kAhead; ++i) {
+                        stage(idle, cur, next, integral_constant<int, (kRing - 1 - kAhead) * L1 + kStores>{}, w, i + kRing, yes, no, no);
                         advance();
                     }
                 }
@@ -646,13 +713,13 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     while (true) {
         clear();
         if (w.nst > 0) {
-            cur = 0, next = kSlot;
+            cur = 0, next = kSlot, b_slot = 0;
             arrive(integral_constant<int, 0>{}, yes, w, cur);
             begin();
             auto body = [&](auto idle) INLINE {
                 int i = 0;
                 for (; i + kRing < w.nst; ++i) {
-                    stage(idle, cur, next, integral_constant<int, (kRing - 2) * L1>{}, w, i + kRing, yes, no, no);
+                    stage(idle, cur, next, kept, w, i + kRing, yes, no, no);
                     advance();
                 }
                 for (; i + 1 < w.nst; ++i) {  // the loads are on their way: wait for all of them
@@ -823,14 +890,15 @@ int64_t grid_tiles(const Bf16GemmJob& j, int bm, int bn) {
 // Whether every row is whole 16-byte pieces, and a tile's rows (or a stage's) lie within 32 bits.
 bool pieces(const Bf16GemmJob& j) {
     constexpr int64_t kMost = int64_t(1) << 22;
-    const int64_t wide_a = j.pass == kBf16BwdDw ? j.M : j.red, wide_b = j.pass == kBf16FwdY ? j.red : j.N;
-    return !j.b8 && wide_a % 8 == 0 && wide_b % 8 == 0 && j.lda % 8 == 0 && j.ldb % 8 == 0 && j.lda <= kMost && j.ldb <= kMost &&
+    const int64_t wide_a = j.pass == kBf16BwdDw ? j.M : j.red, wide_b = j.pass == kBf16FwdY ? j.red : j.b8 ? 0 : j.N;
+    if (j.b8 && (j.ldbs % 4 != 0 || j.ldbs > kMost || reinterpret_cast<uintptr_t>(j.bs) % 4 != 0)) return false;  // codes are whole pieces
+    return wide_a % 8 == 0 && wide_b % 8 == 0 && j.lda % 8 == 0 && j.ldb % 8 == 0 && j.lda <= kMost && j.ldb <= kMost &&
            reinterpret_cast<uintptr_t>(j.a) % 16 == 0 && reinterpret_cast<uintptr_t>(j.b) % 16 == 0;
 }
 
 constexpr int kCounters = 8 * kCounterStride;
 
-template <int OUT, class C, int PASS, bool STREAM>
+template <int OUT, class C, int PASS, bool STREAM, bool SAVED>
 hipError_t launch_tile(Bf16GemmJob j, hipStream_t s) {
     int64_t tiles = grid_tiles(j, C::BM, C::BN);
     if (tiles > C::kResident) {  // the workgroups that are resident take the tiles as they get done
@@ -839,7 +907,7 @@ hipError_t launch_tile(Bf16GemmJob j, hipStream_t s) {
     } else {
         j.counters = nullptr;
     }
-    gemm_bf16_kernel<OUT, C, PASS, STREAM><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
+    gemm_bf16_kernel<OUT, C, PASS, STREAM, SAVED><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
     return hipGetLastError();
 }
 
@@ -854,10 +922,10 @@ bool streams(const Bf16GemmJob& j) {
     return (dw ? j.M * j.G : j.tokens) * j.N * (j.out_dtype == kOutF32 ? 4 : 2) >= (dw ? int64_t(64) << 20 : kStreamBytes);
 }
 
-template <int OUT, int PASS>
+template <int OUT, int PASS, bool SAVED = false>
 hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
-    if (!large(j)) return launch_tile<OUT, Tile128<PASS>, PASS, false>(j, s);
-    return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false>(j, s);
+    if (!large(j)) return launch_tile<OUT, Tile128<PASS>, PASS, false, SAVED>(j, s);
+    return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true, SAVED>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false, SAVED>(j, s);
 }
 
 // Which products the few-row kernel takes: up to 8 rows a group on average, or 64 in all. Past that its rows of W come through the L2 more than
@@ -901,7 +969,7 @@ hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
     switch (j.pass) {
         case kBf16FwdY: return launch_pass<OUT, kBf16FwdY>(j, s);
         case kBf16BwdDx: return launch_pass<OUT, kBf16BwdDx>(j, s);
-        default: return launch_pass<OUT, kBf16BwdDw>(j, s);
+        default: return j.b8 ? launch_pass<OUT, kBf16BwdDw, true>(j, s) : launch_pass<OUT, kBf16BwdDw>(j, s);
     }
 }
 

@@ -743,6 +743,7 @@ bool bytes_of(PyObject* o, const char* what, int64_t cols, const at::Tensor*& t,
 bool kept_of(PyObject* codes, PyObject* scales, int64_t cols, int parts, Kept& k, const at::Tensor*& t) {
     int64_t cld, sld;
     if (!check(ufp4_ckpt8_ld(cols, parts, &cld, &sld), "ufp4_ckpt8_ld")) return false;
+    sld = cld / 32;  // the blocks; what fills a row up need not be there
     const at::Tensor* s;
     if (!bytes_of(codes, "codes", cld, t, k.code_ld) || !bytes_of(scales, "scales", sld, s, k.scale_ld)) return false;
     if (s->size(0) != t->size(0)) return refuse("scales", "of the rows of codes");
@@ -908,10 +909,10 @@ CALL(checkpoint8_load, 7)
     if (!product_out(a[5], *codes, shape, code, out)) return nullptr;
     if (!unlocked([&]() -> Done {
             product_new(*codes, shape, code, out);
-            int64_t cld = 0, sld = 0;
-            ufp4_ckpt8_ld(cols, 1, &cld, &sld);
+            int64_t cld = 0;
+            ufp4_ckpt8_ld(cols, 1, &cld, nullptr);
             for (int p = 0; p < parts; ++p) {
-                const int st = ufp4_ckpt8_load(code_of(out), k.codes + p * cld, k.code_ld, k.scales + p * sld, k.scale_ld, k.rows, cols,
+                const int st = ufp4_ckpt8_load(code_of(out), k.codes + p * cld, k.code_ld, k.scales + p * (cld / 32), k.scale_ld, k.rows, cols,
                                                static_cast<uint8_t*>(out.data_ptr()) + p * cols * out.element_size(), out.stride(0), stream);
                 if (st != UFP4_OK) return {st, "ufp4_ckpt8_load"};
             }

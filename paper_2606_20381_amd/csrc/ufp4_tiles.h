@@ -16,6 +16,12 @@ __device__ __forceinline__ void to_lds16(uint32_t voff, const void* sbase, const
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(m0) : "memory");
 }
 
+// The same with 4 bytes per lane, landing at lds_base + 4 i.
+__device__ __forceinline__ void to_lds4(uint32_t voff, const void* sbase, const void* lds_base) {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t) reinterpret_cast<uintptr_t>(lds_base));
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "s"(m0) : "memory");
+}
+
 // Waits until at most N vector-memory operations are outstanding and no LDS operation is (gfx9's s_waitcnt immediate).
 template <int N>
 __device__ __forceinline__ void wait_loads() {

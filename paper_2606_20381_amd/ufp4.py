@@ -829,7 +829,7 @@ def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, rows: torch.Tensor, off
 
 class Checkpoint8:
     """A tensor [rows, cols] kept in 8 bits (ufp4_ckpt8_save): E4M3 `codes`, uint8 [rows, whole blocks], and one power of two per 32
-    values of a row, uint8 `scales`. `parts` 2 (the input of a gated activation): the two halves of a row are kept each in blocks of
+    values of a row, uint8 `scales` [rows, blocks filled up to a multiple of 4]. `parts` 2 (the input of a gated activation): the two halves of a row are kept each in blocks of
     its own."""
 
     __slots__ = ("codes", "scales", "cols", "parts")

@@ -84,7 +84,8 @@ def test_product_from_a_checkpoint_refusals(lib):
 
 def test_checkpoint_sizes(lib):
     c, s = ctypes.c_int64(), ctypes.c_int64()
-    for cols, parts, code_ld, scale_ld in ((0, 1, 0, 0), (1, 1, 32, 1), (32, 1, 32, 1), (33, 1, 64, 2), (1411, 2, 2880, 90), (64, 2, 128, 4)):
+    for cols, parts, code_ld, scale_ld in ((0, 1, 0, 0), (1, 1, 32, 4), (32, 1, 32, 4), (33, 1, 64, 4), (129, 1, 160, 8), (1411, 2, 2880, 92),
+                                            (64, 2, 128, 4)):
         assert lib.ufp4_ckpt8_ld(cols, parts, R(c), R(s)) == OK and (c.value, s.value) == (code_ld, scale_ld)
     assert lib.ufp4_ckpt8_ld(8, 1, None, None) == OK
     assert lib.ufp4_ckpt8_ld(-1, 1, R(c), R(s)) == INVALID and lib.ufp4_ckpt8_ld(8, 0, R(c), R(s)) == INVALID

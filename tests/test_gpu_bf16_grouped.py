@@ -44,7 +44,7 @@ def _reference(what, x, dy, w, offsets, tokens, N, K):
     outs = []
     for f in (lambda t: t.double(), lambda t: t.double().abs()):
         spans = _spans(offsets, tokens)
-        if what == "dw":
+        if what in ("dw", "dw8"):
             r = torch.zeros(len(spans), N, K, dtype=torch.float64, device="cuda")
         else:
             r = torch.full((tokens, N if what == "fwd" else K), FILL, dtype=torch.float64, device="cuda")
@@ -53,7 +53,7 @@ def _reference(what, x, dy, w, offsets, tokens, N, K):
                 r[a:b] = f(x[a:b]) @ f(w[e * N : (e + 1) * N]).t()
             elif what == "dx" and b > a:
                 r[a:b] = f(dy[a:b]) @ f(w[e * N : (e + 1) * N])
-            elif what == "dw":
+            elif what in ("dw", "dw8"):
                 r[e] = f(dy[a:b]).t() @ f(x[a:b])
         outs.append(r)
     return outs
@@ -64,11 +64,13 @@ def _call(what, x, dy, w, offsets, out, dtype):
         return U.bf16_gemm_fwd_y_grouped(x, w, offsets, dtype, out=out)
     if what == "dx":
         return U.bf16_gemm_bwd_dx_grouped(dy, w, offsets, dtype, out=out)
+    if what == "dw8":  # whole numbers to 15 are kept as they are
+        return U.bf16_gemm_bwd_dw_grouped(dy, U.checkpoint8_save(x), offsets, dtype, out=out)
     return U.bf16_gemm_bwd_dw_grouped(dy, x, offsets, dtype, out=out)
 
 
 def _out(what, tokens, N, K, G, dtype, pad=0):
-    if what == "dw":
+    if what in ("dw", "dw8"):
         return torch.full((G, N, K + pad), FILL, dtype=dtype, device="cuda")[:, :, :K]
     cols = N if what == "fwd" else K
     return torch.full((tokens, cols + pad), FILL, dtype=dtype, device="cuda")[:, :cols]
@@ -81,7 +83,7 @@ COUNTS = [
 SIZES = [(1, 1), (8, 8), (7, 9), (64, 64), (129, 40), (40, 129), (256, 320), (257, 65), (520, 96), (96, 520), (131, 259)]
 
 
-@pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("what", ["fwd", "dx", "dw", "dw8"])
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("counts", COUNTS, ids=lambda c: f"{len(c)}x{max(c)}")
 def test_whole_numbers(what, dtype, counts):
@@ -118,7 +120,7 @@ def test_real_numbers(what, dtype, counts, N, K):
     assert got.dtype == dtype and bool(((got.double() - ref).abs() <= tol).all())
 
 
-@pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("what", ["fwd", "dx", "dw", "dw8"])
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("counts,N,K", [([4000, 10, 3500, 0, 900, 1], 2568, 2056), ([300] * 40, 1032, 776), ([1, 20000], 640, 1024),
                                         ([130] * 70 + [5000], 392, 1288), ([66, 65, 2, 700] * 25, 1160, 904)])
@@ -133,7 +135,7 @@ def test_more_tiles_than_workgroups(what, dtype, counts, N, K):
         assert torch.equal(_call(what, x, dy, w, offsets, _out(what, tokens, N, K, G, dtype), dtype), ref.to(dtype))
 
 
-@pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("what", ["fwd", "dx", "dw", "dw8"])
 @pytest.mark.parametrize("N,K", [(264, 72), (33, 35)])
 def test_offsets_that_lie(what, N, K):
     """Offsets past the rows, below zero or falling: cut to the rows; a group that ends before it starts has none."""
@@ -145,7 +147,7 @@ def test_offsets_that_lie(what, N, K):
         ref, _ = _reference(what, x, dy, w, offsets, tokens, N, K)
         got = _call(what, x, dy, w, offsets, _out(what, tokens, N, K, 4, F32), F32)
         if off[3] == 100:  # the last two groups claim the rows 100 .. 149 of the second again: any of them may have written those
-            if what != "dw":
+            if what in ("fwd", "dx"):
                 got[100:150] = ref[100:150]
         assert torch.equal(got.double(), ref), off
 
@@ -183,7 +185,7 @@ def test_nothing_to_do(what):
         assert tuple(got.shape) == (4, 8) and not got.any()
 
 
-@pytest.mark.parametrize("what", ["fwd", "dx", "dw"])
+@pytest.mark.parametrize("what", ["fwd", "dx", "dw", "dw8"])
 def test_rows_past_32_bits(what):
     """Tensors of more than 2^32 bytes: the last group's rows lie behind them."""
     g = _gen(5)
@@ -197,7 +199,7 @@ def test_rows_past_32_bits(what):
     offsets = torch.tensor([tokens - 300, tokens - 129, tokens], device="cuda")
     got = _call(what, x, dy, w, offsets, None, F32)
     ref, _ = _reference(what, x[-300:], dy[-300:], w, offsets - (tokens - 300), 300, N, K)
-    assert torch.equal(got.double() if what == "dw" else got[-300:].double(), ref)
+    assert torch.equal(got.double() if what in ("dw", "dw8") else got[-300:].double(), ref)
 
 
 @pytest.mark.parametrize("K", [40, 512, 1411])
@@ -217,11 +219,11 @@ def test_weight_gradient_from_a_checkpoint(K, counts):
         assert bool(((got.double() - ref).abs() <= tol).all())
     # a checkpoint inside a wider one: rows further apart, columns from a block on
     if K > 64:
-        part = U.Checkpoint8(kept.codes[:, 32:], kept.scales[:, 1:], K - 32)
-        if kept.codes.stride(0) % 16 == 0:
+        for c in (32, 128):  # scales that lie anywhere, and in words of four
+            part = U.Checkpoint8(kept.codes[:, c:], kept.scales[:, c // 32 : -(-K // 32)], K - c)
             got = U.bf16_gemm_bwd_dw_grouped(dy, part, offsets)
             tol = max(counts) * 2.0**-23 * size + 2.0**-24 * ref.abs()
-            assert bool(((got.double() - ref[:, :, 32:]).abs() <= tol[:, :, 32:]).all())
+            assert bool(((got.double() - ref[:, :, c:]).abs() <= tol[:, :, c:]).all())
 
 
 def test_streams_and_graph():

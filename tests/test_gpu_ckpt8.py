@@ -63,7 +63,7 @@ def _values(rows, cols, dtype, seed, hard=True):
 def test_save_and_load(rows, cols, dtype):
     x = _values(rows, cols, dtype, rows + cols)
     c = U.checkpoint8_save(x)
-    assert c.shape == (rows, cols) and c.codes.shape == (rows, -(-cols // 32) * 32) and c.scales.shape == (rows, -(-cols // 32))
+    assert c.shape == (rows, cols) and c.codes.shape == (rows, -(-cols // 32) * 32) and c.scales.shape == (rows, -(-cols // 128) * 4)
     ref = _kept(x)
     for out in (F32, BF):
         got = U.checkpoint8_load(c, out)
