@@ -258,3 +258,15 @@ def test_streams_and_graph():
         torch.cuda.synchronize()
         for p, c, e in zip(("fwd", "dx", "dw", "dw"), captured, eager):
             assert torch.equal(c, e) and torch.equal(c.double(), _reference(p, x, dy, w, offsets, tokens, N, K)[0])
+
+
+@pytest.mark.parametrize("counts,N,K", [([37, 0, 300, 5], 136, 72), ([9, 8], 33, 515), ([600, 500], 384, 1032)])
+def test_adjoint(counts, N, K):
+    """<dy, x w^T> = <dx, x> = <dw, w>, in whole numbers exactly."""
+    g = _gen(7)
+    tokens, G = sum(counts), len(counts)
+    offsets, _ = U.group_offsets(counts)
+    x, dy, w = _whole(g, tokens, K), _whole(g, tokens, N), _whole(g, G * N, K)
+    y, dx, dw = (_call(p, x, dy, w, offsets, None, F32).double() for p in ("fwd", "dx", "dw"))
+    a = (dy.double() * y).sum()
+    assert a == (dx * x.double()).sum() and a == (dw.view(G * N, K) * w.double()).sum()
