@@ -78,6 +78,7 @@ int ufp4_bf16_gemm_grouped_workspace(int pass, int64_t tokens, int64_t N, int64_
     j.tokens = tokens;
     j.M = pass == UFP4_PASS_BWD_DW ? N : 0;
     j.N = pass == UFP4_PASS_FWD_Y ? N : K;
+    j.red = pass == UFP4_PASS_FWD_Y ? K : pass == UFP4_PASS_BWD_DX ? N : 0;
     j.G = G;
     if (!bf16_gemm_fits(j)) return UFP4_ERR_UNSUPPORTED;
     *bytes = (size_t)bf16_gemm_workspace(j);

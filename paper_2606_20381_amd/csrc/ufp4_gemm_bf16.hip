@@ -14,6 +14,8 @@
 #include "ufp4_rows.h"
 #include "ufp4_tiles.h"
 
+#include <math.h>
+
 #include <type_traits>
 
 namespace ufp4 {
@@ -137,7 +139,7 @@ struct Pass {
 constexpr int kAnyTile = 128, kAnyThreads = 256, kAnyK = 32;
 
 template <int OUT, int PASS, bool SAVED>
-__global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJob j) {
+__global__ __launch_bounds__(kAnyThreads, 3) void gemm_bf16_any_kernel(Bf16GemmJob j) {
     using P = Pass<PASS>;
     constexpr int BM = kAnyTile, BN = kAnyTile;
     using SA = Stage<BM, kAnyK, P::kAcrossA>;
@@ -145,8 +147,8 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     constexpr uint32_t kSlot = SA::kSize + SB::kSize;
     __shared__ __align__(16) uint8_t ring[2 * kSlot];
     __shared__ typename std::conditional<P::kRagged, GroupRows<BM>, int>::type groups;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int wm = wave >> 1, wn = wave & 1, h = lane >> 5, l32 = lane & 31;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
 
     // This workgroup's tile: rows of A and B from row0 / col0, reduction [k0, k1).
     const uint32_t gx = (uint32_t)((j.N + BN - 1) / BN);
@@ -157,8 +159,9 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     if constexpr (P::kRagged) {
         if (tid < 64) groups.build(j);
         __syncthreads();
-        const uint32_t gy = (uint32_t)uniform(groups.tile[j.G]);
-        if (blockIdx.x >= (uint64_t)gx * gy) return;
+        const uint32_t bound = (uint32_t)((j.tokens + BM - 1) / BM + j.G), have = (uint32_t)uniform(groups.tile[j.G]);
+        const uint32_t gy = have < bound ? have : bound;
+        if (blockIdx.x >= gx * gy) return;
         tile_at(blockIdx.x, gy, gx, tm, tn);
         const int g = groups.of(j.G, tm), lt = tm - uniform(groups.tile[g]);
         row0 = (int64_t)uniform(groups.start[g]) + (int64_t)lt * BM;
@@ -175,24 +178,64 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
     }
     const int64_t col0 = (int64_t)tn * BN, cols = j.N - col0;
 
-    // Piece q of this thread: 16 bytes of operand A (B) of the stage from place k on; zero outside.
+    // Pieces q of this thread: 16 bytes of operand A (B) of a stage, where they come from at the reduction's first place, and the place in
+    // the stage. Rows past the last one are zeros (across the reduction) or the first one again: they only feed outputs that are not
+    // stored. A piece that the row's end cuts is loaded from before its place, so that it ends with the row, and moved down on its way to
+    // the LDS: loading it value by value would wait for memory in every stage.
     constexpr int kEach = SA::kSize / 16 / kAnyThreads;
     static_assert(SA::kSize == SB::kSize, "");
-    auto fetch = [&](const uint16_t* p, int64_t ld, bool across, int64_t first, int64_t have, int64_t k, int q) INLINE {
-        const int i = q * kAnyThreads + tid;
-        u32x4_any zero = {0, 0, 0, 0};
-        if (across) {  // place k + i / (rows / 8), rows 8 (i % (rows / 8)) ..
-            const int64_t kk = k + i / (BM / 8), r = (i % (BM / 8)) * 8;
-            return kk < k1 && r < have ? Piece<uint16_t>::load(p + kk * ld + first + r, have - r) : zero;
+    struct Source {
+        const uint16_t* p;
+        int place, have;  // `have` of its 8 rows, across the reduction
+    };
+    const bool narrow_a = (P::kAcrossA ? j.M : j.red) < 8, narrow_b = (P::kAcrossB ? j.N : j.red) < 8;  // no 8 values before a row's end
+    auto source = [&](auto stage, const uint16_t* base, int64_t ld, int64_t first, int64_t rows_have, bool narrow, int q) INLINE {
+        using S = decltype(stage);
+        uint32_t r, k;
+        S::piece((uint32_t)(q * kAnyThreads + tid), r, k);
+        Source s;
+        s.place = (int)k;
+        if constexpr (S::kAcross) {
+            const int64_t left = rows_have - r;
+            s.have = left < 0 ? 0 : left < 8 ? (int)left : 8;
+            s.p = base + (k0 + k) * ld + first + r - (narrow || s.have == 0 ? 0 : 8 - s.have);
+        } else {
+            s.have = 8;
+            s.p = base + (first + (r < rows_have ? r : 0)) * ld + k0 + k;
         }
-        const int64_t r = i / 4, kk = k + (i % 4) * 8;
-        return r < have && kk < k1 ? Piece<uint16_t>::load(p + (first + r) * ld + kk, k1 - kk) : zero;
+        return s;
     };
-    auto place = [&](bool across, int q) INLINE {
-        const uint32_t i = q * kAnyThreads + tid;
-        return across ? SA::across(i / (BM / 8), i % (BM / 8)) : SA::along(i / 4, i % 4);
+    // Values of the piece that exist at place k of the reduction, where whether a whole stage is left is the same for all.
+    auto existing = [&](auto stage, const Source& s, int64_t k) INLINE {
+        if (k + kAnyK <= k1) return s.have;
+        const int64_t left = k1 - k - s.place;
+        if (decltype(stage)::kAcross) return left > 0 ? s.have : 0;
+        return left < 0 ? 0 : left < 8 ? (int)left : 8;
     };
-    // A checkpoint's 16 codes: place k + i / 8, columns 16 (i % 8) ..
+    auto fetch = [&](auto stage, const Source& s, int64_t ld, int64_t k, bool narrow) INLINE {
+        using S = decltype(stage);
+        const uint16_t* const p = s.p + (S::kAcross ? (k - k0) * ld : k - k0);
+        const int n = existing(stage, s, k);
+        u32x4_any v = {0, 0, 0, 0};
+        if (narrow) v = Piece<uint16_t>::load(p, n);
+        else if (n > 0) v = *reinterpret_cast<const u32x4_any*>(S::kAcross ? p : p - (8 - n));
+        return v;
+    };
+    auto place_at = [&](auto stage, const Source& s, int64_t k, bool narrow, const u32x4_any& v, uint8_t* to) INLINE {
+        const int n = existing(stage, s, k);
+        u32x4_any x = v;
+        if (n < 8 && !narrow) {  // down by 8 - n values; n 0: zeros already
+            const int by = 8 - n;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = by & 1 ? __builtin_amdgcn_alignbit(w < 3 ? v[w + 1] : 0, v[w], 16) : v[w];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = by & 2 ? (w < 3 ? x[w + 1] : 0) : x[w];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = by & 4 ? (w < 2 ? x[w + 2] : 0) : x[w];
+        }
+        *reinterpret_cast<u32x4_any*>(to) = x;
+    };
+    // A checkpoint's 16 codes: place k + tid / 8, columns 16 (tid % 8) ..
     auto fetch_saved = [&](int64_t k, u32x4_any& codes, uint32_t& scale) INLINE {
         const int64_t kk = k + tid / 8, c = (tid % 8) * 16;
         codes = u32x4_any{0, 0, 0, 0};
@@ -211,36 +254,51 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
 
-    u32x4_any ra[kEach], rb[kEach];
-    uint32_t scale = 127;
-    auto load = [&](int64_t k) INLINE {
+    Source from_a[kEach], from_b[kEach];
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) ra[q] = fetch(a, j.lda, P::kAcrossA, row0, rows, k, q);
+    for (int q = 0; q < kEach; ++q) {
+        from_a[q] = source(SA{}, a, j.lda, row0, rows, narrow_a, q);
+        if constexpr (!SAVED) from_b[q] = source(SB{}, b, j.ldb, col0, cols, narrow_b, q);
+    }
+    // Two stages are on their way in registers (three or four cost the second workgroup of a CU: 8192 x 4099 x 4099 forward 497 us, 505, 581).
+    struct Pieces {
+        u32x4_any a[kEach], b[kEach];
+        uint32_t scale;
+    };
+    Pieces held[2];
+    auto load = [&](Pieces& h, int64_t k) INLINE {
+        if (k >= k1) return;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) h.a[q] = fetch(SA{}, from_a[q], j.lda, k, narrow_a);
         if constexpr (SAVED) {
-            fetch_saved(k, rb[0], scale);
+            fetch_saved(k, h.b[0], h.scale);
         } else {
 #pragma unroll
-            for (int q = 0; q < kEach; ++q) rb[q] = fetch(b, j.ldb, P::kAcrossB, col0, cols, k, q);
+            for (int q = 0; q < kEach; ++q) h.b[q] = fetch(SB{}, from_b[q], j.ldb, k, narrow_b);
         }
     };
-    if (k0 < k1) load(k0);
-    uint32_t slot = 0;
-    for (int64_t k = k0; k < k1; k += kAnyK) {
+    auto write = [&](const Pieces& h, int64_t k, uint32_t slot) INLINE {
         uint8_t* const sa = ring + slot;
         uint8_t* const sb = sa + SA::kSize;
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) *reinterpret_cast<u32x4_any*>(sa + place(P::kAcrossA, q)) = ra[q];
+        for (int q = 0; q < kEach; ++q) place_at(SA{}, from_a[q], k, narrow_a, h.a[q], sa + (q * kAnyThreads + tid) * 16);
         if constexpr (SAVED) {
             u32x4_any lo, hi;
-            ckpt8_to_bf16(rb[0], scale, lo, hi);
+            ckpt8_to_bf16(h.b[0], h.scale, lo, hi);
             *reinterpret_cast<u32x4_any*>(sb + SB::across(tid / 8, (tid % 8) * 2)) = lo;
             *reinterpret_cast<u32x4_any*>(sb + SB::across(tid / 8, (tid % 8) * 2 + 1)) = hi;
         } else {
 #pragma unroll
-            for (int q = 0; q < kEach; ++q) *reinterpret_cast<u32x4_any*>(sb + place(P::kAcrossB, q)) = rb[q];
+            for (int q = 0; q < kEach; ++q) place_at(SB{}, from_b[q], k, narrow_b, h.b[q], sb + (q * kAnyThreads + tid) * 16);
         }
+    };
+    uint32_t slot = 0;
+    auto stage = [&](Pieces& h, int64_t k) INLINE {
+        write(h, k, slot);
         __syncthreads();  // two slots: the next stage is written to the other one, which everyone has read
-        if (k + kAnyK < k1) load(k + kAnyK);
+        load(h, k + 2 * kAnyK);
+        const uint8_t* const sa = ring + slot;
+        const uint8_t* const sb = sa + SA::kSize;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             v8b fa[2], fb[2];
@@ -255,24 +313,14 @@ __global__ __launch_bounds__(kAnyThreads, 2) void gemm_bf16_any_kernel(Bf16GemmJ
                 for (int y = 0; y < 2; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[y], fa[x], acc[x][y], 0, 0, 0);
         }
         slot ^= kSlot;
+    };
+    load(held[0], k0);
+    load(held[1], k0 + kAnyK);
+    for (int64_t k = k0; k < k1; k += 2 * kAnyK) {
+        stage(held[0], k);
+        if (k + kAnyK < k1) stage(held[1], k + kAnyK);
     }
-
-    // B's rows are the instruction's rows: a lane holds columns 8 q + 4 h .. + 3 of row l32 of each tile.
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int64_t r = wm * 64 + x * 32 + l32;
-        if (r >= rows) continue;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int64_t c = wn * 64 + y * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
-                if (c >= cols) continue;
-                const int64_t at = c_base + (row0 + r) * j.ldc + col0 + c;
-                if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[at] = acc[x][y][i];
-                else static_cast<uint16_t*>(j.c)[at] = __builtin_bit_cast(uint16_t, (__bf16)acc[x][y][i]);
-            }
-    }
+    store_tile<OUT, 2, 2, false, false>(acc, j.c, c_base, (int)row0, (int)col0, j.ldc, rows < BM ? (int)rows : BM, j.N, wm, wn);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -911,9 +959,36 @@ hipError_t launch_tile(Bf16GemmJob j, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The larger tile moves half the bytes per product, and wins where its tiles fill the chip: 98304 x 1408 x 2048 of 64 experts,
-// us, 256 / 128: forward 611 / 810, input's gradient 564 / 820, weights' gradient 695 / 761.
-bool large(const Bf16GemmJob& j) { return grid_tiles(j, 256, 256) >= 256; }
+// Which tile takes a product of whole pieces: the one with the smaller estimated time, in us, from the tiles that a CU gets (t, ragged rows
+// with half a tile lost per group) and the reduction (of a weights' gradient the average group's; the longest is taken as three times that,
+// and no tile of it ends sooner than alone on a CU). Measured on gfx950, 256 / 128, us:
+//     one group, forward: 2048^3 43 / 25, 4096 x 4096 x 1024 36 / 39, 4096 x 2048 x 8192 143 / 123, 2048 x 8192 x 2048 60 / 68;
+//     8 experts, 8192 rows, 2048 -> 1408: forward 50 / 57, gradients 71 / 64, 87 / 69; 4096 rows, 2048 -> 4096: 94 / 83, 80 / 105, 107 / 116;
+//     16 experts, 16384 rows, 1312 -> 512: 37 / 45, 36 / 36, 89 / 62; 64 experts, 24576 rows, 2048 -> 1408: 181 / 202, 175 / 241, 262 / 313,
+//     6144 rows: 106 / 89, 108 / 102, 156 / 178.
+double estimate(const Bf16GemmJob& j, bool big) {
+    const double tile = big ? 256.0 : 128.0, cols = ceil((double)j.N / tile);
+    const bool dw = j.pass == kBf16BwdDw;
+    const double rows = dw ? ceil((double)j.M / tile) * j.G : (double)j.tokens / tile + (j.tokens < j.G ? j.tokens : j.G) * 0.5;
+    const double red = dw ? (double)j.tokens / j.G : (double)j.red, t = ceil(rows) * cols / 256.0;
+    const double longest = dw && j.G > 1 ? (3.0 * red < j.tokens ? 3.0 * red : j.tokens) : red;
+    double us, alone;
+    if (big) {  // per 64 of the reduction: a full round of tiles 1.65, a partial one less
+        const double part = t - floor(t);
+        us = 9.0 + red / 64.0 * (floor(t) * 1.65 + (part > 0.0 ? 1.05 + 0.6 * part : 0.0));
+        alone = 9.0 + longest / 64.0 * 1.1;
+    } else {  // per 32: two tiles a CU 0.5 (many: 0.64), one 0.31
+        const double part = t - 2.0 * floor(t / 2.0);
+        us = 6.0 + red / 32.0 * (floor(t / 2.0) * (t <= 4.0 ? 0.5 : 0.64) + (part > 1.0 ? 0.45 : part > 0.0 ? 0.31 : 0.0));
+        alone = 6.0 + longest / 32.0 * 0.31;
+    }
+    return us > alone ? us : alone;
+}
+bool large(const Bf16GemmJob& j) {
+    // many tiles of a weights' gradient are bound by their stores, which the larger ones make nontemporally
+    if (j.pass == kBf16BwdDw && grid_tiles(j, 256, 256) >= 1024) return true;
+    return estimate(j, true) < estimate(j, false);
+}
 
 // Outputs that no cache holds are stored nontemporally; weights' gradients, which are read when a step's have all been computed, from
 // 64 MiB on.
