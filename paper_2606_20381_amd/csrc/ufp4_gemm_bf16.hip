@@ -1080,3 +1080,15 @@ hipError_t launch_gemm_bf16(const Bf16GemmJob& j, hipStream_t s) {
 }
 
 }  // namespace ufp4
+
+extern "C" int ufp4_plan_gemm_bf16(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int whole_pieces) {
+    using namespace ufp4;
+    Bf16GemmJob j{};
+    j.pass = pass;
+    j.tokens = tokens;
+    j.M = pass == kBf16BwdDw ? N : 0;
+    j.N = pass == kBf16FwdY ? N : K;
+    j.red = pass == kBf16FwdY ? K : pass == kBf16BwdDx ? N : 0;
+    j.G = G;
+    return few(j) ? 0 : !whole_pieces ? 1 : large(j) ? 3 : 2;
+}

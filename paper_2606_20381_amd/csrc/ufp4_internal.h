@@ -380,6 +380,8 @@ int ufp4_plan_gemm(int mode, int format, int64_t M, int64_t N, int64_t red, int3
 int ufp4_plan_gemm_mx(int mode, int64_t M, int64_t N, int64_t red, int32_t G, int64_t a_rows, int64_t* threads_x);
 // The microscaled 4-bit GEMM's rule: 0 the 256 x 256 tile, 1 128 x 128, 2 64 x 64, 3 64 x 64 in four teams.
 int ufp4_plan_gemm_mxfp4(int mode, int64_t M, int64_t N, int64_t red, int32_t G, int64_t a_rows);
+// The grouped bf16 products' rule: 0 the few-row kernel, 1 the one of any alignment, 2 tiles of 128 x 128, 3 of 256 x 256.
+int ufp4_plan_gemm_bf16(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int whole_pieces);
 // Threads in x of the (largest) launch of the transposed quantizer's tile kernel for an RHT block of 32, 64 or 128.
 int64_t ufp4_plan_cols_wide(int rht_block, int64_t cols);
 // Workgroups of a grouped quantizer over `tiles` tiles (mx: power-of-two scales), and the most tiles one of them takes.

@@ -164,3 +164,34 @@ def test_binding_refuses_other_arguments(lib, monkeypatch):
     for call in (lambda: U.checkpoint8_save(3), lambda: U.activation_bwd(3, x), lambda: U.bf16_gemm_fwd_y_grouped(None, x, x)):
         with pytest.raises((TypeError, AttributeError)):
             call()
+
+
+# (pass, rows, N, K, groups, us of the kernels 0 few rows, 2 tiles of 128, 3 tiles of 256 on an MI355X; None: not measured)
+FWD, DX, DW = range(3)
+MEASURED = [
+    (FWD, 42, 1408, 2048, 64, (21.0, 35.3, None)), (FWD, 384, 1408, 2048, 64, (82.5, 99.0, None)), (FWD, 1536, 1408, 2048, 64, (143.6, 113.9, None)),
+    (FWD, 2, 1312, 512, 8, (5.5, 8.3, None)), (FWD, 512, 1312, 512, 8, (17.6, 8.7, None)), (FWD, 2, 4096, 5120, 8, (15.8, 48.3, None)),
+    (FWD, 256, 4096, 5120, 8, (148.4, 81.2, None)), (FWD, 1, 8192, 2048, 1, (7.6, 20.6, None)), (FWD, 64, 8192, 2048, 1, (15.3, 22.3, None)),
+    (FWD, 256, 8192, 2048, 1, (52.5, 23.4, None)),
+    (FWD, 2048, 2048, 2048, 1, (None, 24.7, 42.8)), (FWD, 4096, 4096, 1024, 1, (None, 39.1, 36.3)), (DX, 4096, 4096, 1024, 1, (None, 37.2, 76.1)),
+    (DW, 4096, 4096, 1024, 1, (None, 39.2, 80.1)), (DX, 4096, 2048, 8192, 1, (None, 149.8, 116.1)), (DW, 4096, 2048, 8192, 1, (None, 130.3, 116.3)),
+    (FWD, 2048, 8192, 2048, 1, (None, 68.2, 60.3)), (DX, 2048, 8192, 2048, 1, (None, 70.2, 141.2)), (DX, 4096, 4096, 2048, 8, (None, 104.8, 80.2)),
+    (DW, 16384, 512, 1312, 16, (None, 62.0, 89.3)), (FWD, 24576, 1408, 2048, 64, (None, 201.7, 180.9)), (DX, 24576, 1408, 2048, 64, (None, 240.7, 174.6)),
+    (DW, 24576, 1408, 2048, 64, (None, 313.0, 261.7)), (DW, 6144, 1408, 2048, 64, (None, 178.4, 156.3)), (FWD, 6144, 1408, 2048, 64, (None, 88.8, 106.2)),
+    (FWD, 98304, 1408, 2048, 64, (None, 810.2, 556.0)), (DX, 98304, 1408, 2048, 64, (None, 819.7, 557.0)), (DW, 98304, 1408, 2048, 64, (None, 761.5, 623.0)),
+]
+
+
+@pytest.mark.parametrize("p,rows,N,K,G,us", MEASURED)
+def test_rule_takes_a_fast_kernel(lib, p, rows, N, K, G, us):
+    """The kernel that the rule picks is within 25% of the best measured one."""
+    pick = lib.ufp4_plan_gemm_bf16(p, ctypes.c_int64(rows), ctypes.c_int64(N), ctypes.c_int64(K), G, 1)
+    took = {0: us[0], 2: us[1], 3: us[2]}[pick]
+    assert took is not None and took <= 1.25 * min(v for v in us if v is not None)
+
+
+def test_rule_on_other_alignment_and_passes(lib):
+    plan = lambda p, rows, N, K, G, whole: lib.ufp4_plan_gemm_bf16(p, *(ctypes.c_int64(v) for v in (rows, N, K)), G, whole)  # noqa: E731
+    assert plan(FWD, 98304, 1408, 2048, 64, 0) == 1 and plan(FWD, 64, 1408, 2048, 1, 0) == 0  # the few-row kernel takes any alignment
+    assert plan(DX, 1, 1408, 2048, 1, 1) == 2 and plan(DW, 1, 1408, 2048, 1, 1) == 2
+    assert plan(FWD, 0, 0, 0, 1, 1) == 0 and plan(DW, 0, 0, 0, 1, 1) in (2, 3)
