@@ -13,8 +13,8 @@
 // registers (any alignment), and one for the few rows of a decode step.
 //
 // Bound, where the tiles fill the chip, by the matrix cores' power: the instruction alone, on registers, reaches 1.54-1.75 PFLOP/s on random
-// numbers (2.3 on zeros: power takes the clock to 1.5-1.7 GHz). 8192^3 takes 0.80-0.84 ms in every pass = 1.31-1.37 (matrix cores busy 79-82%
-// of the time at 1.57 GHz; 0.79 with every load from the same L2-resident place, 0.69 without the loads). 98304 x 1408 x 2048 of 64 experts with
+// numbers (2.3 on zeros: power takes the clock to 1.5-1.7 GHz). 8192^3 takes 0.79-0.86 ms in every pass = 1.28-1.39 (matrix cores busy 78-81%
+// of the CUs' busy cycles, at 1.6-1.75 GHz; 0.79 with every load from the same L2-resident place, 0.69 without the loads). 98304 x 1408 x 2048 of 64 experts with
 // a power law's loads: forward and input's gradient 0.55-0.57 ms = 1.0 PFLOP/s of the products asked for (busy 64%: tiles that end outside
 // of a group or of the 1408 columns, W new in every tile row, workgroups that end 12% apart), weights' gradient 0.62-0.64 ms, its
 // 738 MB of results alone 0.15.
