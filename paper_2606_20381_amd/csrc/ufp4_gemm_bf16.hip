@@ -580,7 +580,9 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
         else if constexpr (SAVED) f.v[t] = SB::read(unpacked + (ahead ? b_slot ^ SB::kSize : b_slot), bcol + t * 32, ks);
         else f.v[t] = SB::read(ring + slot + SA::kSize, bcol + t * 32, ks);
     };
-    // SAVED: this thread's 16 codes of the stage at `slot` to bf16, in `unpacked` at `to`; in two steps, reading and the rest.
+    // SAVED: this thread's 16 codes of the stage at `slot` to bf16, in `unpacked` at `to`; in two steps, reading and the rest. The two
+    // writes have bank conflicts (5% of the CUs' cycles); halves swapped by bit 2 of the thread have none, but the selects cost more
+    // (x saved and 64 experts' 98304 x 1408 x 2048: 828-835 us instead of 812-815).
     u32x4_any codes;
     uint32_t code_scale = 0;
     auto unpack_read = [&](uint32_t slot) INLINE {
