@@ -1083,14 +1083,28 @@ hipError_t launch_gemm_bf16(const Bf16GemmJob& j, hipStream_t s) {
 
 }  // namespace ufp4
 
-extern "C" int ufp4_plan_gemm_bf16(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int whole_pieces) {
-    using namespace ufp4;
-    Bf16GemmJob j{};
+namespace {
+
+ufp4::Bf16GemmJob planned(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G) {
+    ufp4::Bf16GemmJob j{};
     j.pass = pass;
     j.tokens = tokens;
-    j.M = pass == kBf16BwdDw ? N : 0;
-    j.N = pass == kBf16FwdY ? N : K;
-    j.red = pass == kBf16FwdY ? K : pass == kBf16BwdDx ? N : 0;
+    j.M = pass == ufp4::kBf16BwdDw ? N : 0;
+    j.N = pass == ufp4::kBf16FwdY ? N : K;
+    j.red = pass == ufp4::kBf16FwdY ? K : pass == ufp4::kBf16BwdDx ? N : 0;
     j.G = G;
-    return few(j) ? 0 : !whole_pieces ? 1 : large(j) ? 3 : 2;
+    return j;
+}
+
+}  // namespace
+
+extern "C" int ufp4_plan_gemm_bf16(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int whole_pieces) {
+    const ufp4::Bf16GemmJob j = planned(pass, tokens, N, K, G);
+    return ufp4::few(j) ? 0 : !whole_pieces ? 1 : ufp4::large(j) ? 3 : 2;
+}
+
+extern "C" int ufp4_plan_gemm_bf16_streams(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int out_dtype) {
+    ufp4::Bf16GemmJob j = planned(pass, tokens, N, K, G);
+    j.out_dtype = out_dtype;
+    return !ufp4::few(j) && ufp4::large(j) && ufp4::streams(j);
 }

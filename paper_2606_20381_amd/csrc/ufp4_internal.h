@@ -382,6 +382,8 @@ int ufp4_plan_gemm_mx(int mode, int64_t M, int64_t N, int64_t red, int32_t G, in
 int ufp4_plan_gemm_mxfp4(int mode, int64_t M, int64_t N, int64_t red, int32_t G, int64_t a_rows);
 // The grouped bf16 products' rule: 0 the few-row kernel, 1 the one of any alignment, 2 tiles of 128 x 128, 3 of 256 x 256.
 int ufp4_plan_gemm_bf16(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int whole_pieces);
+// Whether that kernel stores nontemporally (rows of whole pieces, an output of type out_dtype).
+int ufp4_plan_gemm_bf16_streams(int pass, int64_t tokens, int64_t N, int64_t K, int32_t G, int out_dtype);
 // Threads in x of the (largest) launch of the transposed quantizer's tile kernel for an RHT block of 32, 64 or 128.
 int64_t ufp4_plan_cols_wide(int rht_block, int64_t cols);
 // Workgroups of a grouped quantizer over `tiles` tiles (mx: power-of-two scales), and the most tiles one of them takes.
