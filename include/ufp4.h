@@ -593,9 +593,9 @@ int ufp4_moe_combine_bwd(int dtype, const void *dout_dev, int64_t tokens, int64_
  *   ufp4_bf16_gemm_bwd_dw_grouped_ckpt8: the same with X an 8-bit checkpoint (ufp4_ckpt8_save), read as it is
  *
  * Group g has the rows offsets[g] .. offsets[g + 1] - 1 of the `tokens` rows of x, dy, y and dx (offsets int64 [num_groups + 1] on the
- * device, rising, as ufp4_moe_sort writes them; each is cut to 0 .. tokens, and a group whose end is not past its start has no rows; which
- * result a row gets that falling offsets give to several groups is not defined). w is [num_groups * N, K], dw [num_groups, N, K] with rows
- * ldc apart and groups N rows apart. Rows of y and dx outside the groups are left as they were; dw of a group without rows is zero.
+ * device, rising, as ufp4_moe_sort writes them; each is cut to 0 .. tokens, and a group whose end is not past its start has no rows; where
+ * they fall, y and dx are as if none were below those before it, and dw_g is the sum over group g's own rows). w is [num_groups * N, K],
+ * dw [num_groups, N, K] with rows ldc apart and groups N rows apart. Rows of y and dx outside the groups are left as they were; dw of a group without rows is zero.
  * Any sizes, leading dimensions (elements, at least the row's) and alignment of a whole element; rows of 16-byte pieces (sizes and
  * leading dimensions multiples of 8, bases 16-byte aligned) are faster. fp32 sums, in an order that follows the sizes and offsets, not
  * the values nor the run; out_dtype UFP4_OUT_F32 or UFP4_OUT_BF16 (one rounding). num_groups 1 .. 1024, tokens below 2^31, N and K up to

@@ -94,8 +94,26 @@ struct Stage {
 
 __device__ __forceinline__ int64_t clamped(int64_t v, int64_t most) { return v < 0 ? 0 : v < most ? v : most; }
 
-// Ragged rows: each group's first token (clamped to the tensor) and first tile row, in LDS, built by the first wave, 64 groups
-// at a time. Offsets that do not rise can claim more tiles than the grid has; what they claim past it is not computed.
+// The rows of group g0 + lane, [from, from + m), of ragged rows: its offsets cut to the tensor and, where they fall, to no less than those
+// before them (`before`: the largest start of the groups before g0, 0 at first), so that no row has two groups, and groups with rows, or
+// their tiles, are never more than a grid for rising offsets holds.
+__device__ __forceinline__ void group_rows(const Bf16GemmJob& j, int g0, int& before, int& from, int& m) {
+    const int lane = threadIdx.x & 63, g = g0 + lane;
+    from = g < j.G ? (int)clamped(j.offsets[g], j.tokens) : 0;
+    const int to = g < j.G ? (int)clamped(j.offsets[g + 1], j.tokens) : 0;
+    if (__ballot(g < j.G && (to < from || from < before))) {
+        from = from > before ? from : before;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(from, d, 64);
+            if (lane >= d) from = v > from ? v : from;
+        }
+    }
+    m = to > from ? to - from : 0;
+    before = __builtin_amdgcn_readlane(from, 63);  // of 64 groups; after fewer nothing follows
+}
+
+// Ragged rows: each group's first token and first tile row, in LDS, built by the first wave, 64 groups at a time.
 template <int BM>
 struct GroupRows {
     static constexpr int kN = kBf16Groups + 1;
@@ -103,12 +121,11 @@ struct GroupRows {
 
     __device__ __forceinline__ void build(const Bf16GemmJob& j) {
         const int G = j.G, lane = threadIdx.x & 63;
-        int64_t tiles = 0;
-        auto cut = [](int64_t v) { return v > INT32_MAX ? INT32_MAX : (int)v; };
+        int tiles = 0, before = 0;
         for (int g0 = 0; g0 < G; g0 += 64) {
             const int g = g0 + lane;
-            const int64_t from = g < G ? clamped(j.offsets[g], j.tokens) : 0, to = g < G ? clamped(j.offsets[g + 1], j.tokens) : 0;
-            const int m = to > from ? (int)(to - from) : 0;
+            int from, m;
+            group_rows(j, g0, before, from, m);
             const int cnt = (int)(((int64_t)m + BM - 1) / BM);
             int inc = cnt;
 #pragma unroll
@@ -117,13 +134,13 @@ struct GroupRows {
                 if (lane >= d) inc += v;
             }
             if (g < G) {
-                start[g] = (int)from;
+                start[g] = from;
                 rows[g] = m;
-                tile[g] = cut(tiles + (inc - cnt));
+                tile[g] = tiles + (inc - cnt);
             }
             tiles += __shfl(inc, 63, 64);
         }
-        if (lane == 0) tile[G] = cut(tiles);
+        if (lane == 0) tile[G] = tiles;
     }
     // The group that holds tile row t: the last one whose first tile row is at most t (empty groups share their successor's).
     __device__ __forceinline__ int of(int G, int t) const {
@@ -169,8 +186,7 @@ __global__ __launch_bounds__(kAnyThreads, 3) void gemm_bf16_any_kernel(Bf16GemmJ
     if constexpr (P::kRagged) {
         if (tid < 64) groups.build(j);
         __syncthreads();
-        const uint32_t bound = (uint32_t)((j.tokens + BM - 1) / BM + j.G), have = (uint32_t)uniform(groups.tile[j.G]);
-        const uint32_t gy = have < bound ? have : bound;
+        const uint32_t gy = (uint32_t)uniform(groups.tile[j.G]);
         if (blockIdx.x >= gx * gy) return;
         tile_at(blockIdx.x, gy, gx, tm, tn);
         const int g = groups.of(j.G, tm), lt = tm - uniform(groups.tile[g]);
@@ -439,8 +455,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerEU) void gemm_bf16_kernel(Bf16G
     if constexpr (P::kRagged) {
         if (tid < 64) groups.build(j);
         __syncthreads();
-        const uint32_t bound = (uint32_t)((j.tokens + BM - 1) / BM + j.G), have = (uint32_t)uniform(groups.tile[j.G]);
-        gy = have < bound ? have : bound;
+        gy = (uint32_t)uniform(groups.tile[j.G]);
         total = gx * gy;
     } else {
         gy = (uint32_t)((j.M + BM - 1) / BM);
@@ -839,19 +854,19 @@ __global__ __launch_bounds__(kFewThreads) void gemm_bf16_few_kernel(Bf16GemmJob 
     const int64_t col0 = (int64_t)(blockIdx.x % chunks) * (16 * CT);
     // the group: the rank-th of those that have rows
     int64_t start = 0, rows = 0;
-    int g = -1;
+    int g = -1, claimed = 0;
     uint32_t before = 0;
     for (int g0 = 0; g0 < j.G && g < 0; g0 += 64) {
-        const int e = g0 + lane;
-        const int64_t from = e < j.G ? clamped(j.offsets[e], j.tokens) : 0, m = e < j.G ? clamped(j.offsets[e + 1], j.tokens) - from : 0;
+        int from, m;
+        group_rows(j, g0, claimed, from, m);
         uint64_t some = __ballot(m > 0);
         const uint32_t n = (uint32_t)__popcll(some);
         if (before + n > rank) {
             for (uint32_t skip = rank - before; skip > 0; --skip) some &= some - 1;
             const int at = uniform(__builtin_ctzll(some));
             g = g0 + at;
-            start = __builtin_amdgcn_readlane((int)from, at);
-            rows = __builtin_amdgcn_readlane((int)m, at);
+            start = __builtin_amdgcn_readlane(from, at);
+            rows = __builtin_amdgcn_readlane(m, at);
         }
         before += n;
     }
