@@ -955,6 +955,8 @@ __global__ __launch_bounds__(kFewThreads) void gemm_bf16_few_kernel(Bf16GemmJob 
     }
 }
 
+constexpr int64_t kMostGroups = int64_t(1) << 23;  // workgroups: a grid holds fewer than 2^32 threads
+
 // Tile rows that a launch provides for; ragged rows: every group may end in a partial tile.
 int64_t tile_rows(const Bf16GemmJob& j, int bm) {
     return j.pass != kBf16BwdDw ? (j.tokens + bm - 1) / bm + j.G : (j.M + bm - 1) / bm;
@@ -1034,20 +1036,25 @@ hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
     return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true, SAVED>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false, SAVED>(j, s);
 }
 
+// 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8).
+constexpr int kFewCols = 2;
+// Its workgroups: those of the columns for each group that can have rows. Where they would be too many, the tiles take the product.
+int64_t few_grid(const Bf16GemmJob& j) { return (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * (j.tokens < j.G ? j.tokens : j.G); }
+
 // Which products the few-row kernel takes: up to 8 rows a group on average, or 64 in all. Past that its rows of W come through the L2 more than
 // once, and 128-row tiles read them less often. Measured, us, few-row kernel / 128 x 128 tiles:
 //     64 experts 2048 -> 1408, 6 a token: 42 rows 21.0 / 35.3, 96 45 / 47, 192 51 / 82, 384 83 / 99, 768 110 / 108, 1536 144 / 114;
 //     8 experts 512 -> 1312, 2 a token: 2 rows 5.5 / 8.3, 32 5.6 / 8.4, 64 7.1 / 8.4, 128 9.0 / 8.5;
 //     8 experts 5120 -> 4096: 2 rows 15.8 / 48.3, 32 62 / 75, 64 77 / 75, 128 110 / 80;
 //     one group 2048 -> 8192: 1 row 7.4 / 20.6, 32 10.9 / 22.0, 64 15.3 / 22.3, 128 27.8 / 23.1.
-bool few(const Bf16GemmJob& j) { return j.pass == kBf16FwdY && (j.tokens <= 64 || j.tokens <= 8 * (int64_t)j.G); }
+bool few(const Bf16GemmJob& j) {
+    return j.pass == kBf16FwdY && (j.tokens <= 64 || j.tokens <= 8 * (int64_t)j.G) && few_grid(j) < kMostGroups;
+}
 
-// 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8).
-constexpr int kFewCols = 2;
 template <int OUT>
 hipError_t launch_few(const Bf16GemmJob& j, hipStream_t s) {
     const int64_t groups = j.tokens < j.G ? j.tokens : j.G;  // that can have rows
-    const unsigned n = (unsigned)((j.N + 16 * kFewCols - 1) / (16 * kFewCols) * groups);
+    const unsigned n = (unsigned)few_grid(j);
     if (j.tokens <= 16 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 1><<<n, kFewThreads, 0, s>>>(j);
     else if (j.tokens <= 32 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 2><<<n, kFewThreads, 0, s>>>(j);
     else gemm_bf16_few_kernel<OUT, kFewCols, 4><<<n, kFewThreads, 0, s>>>(j);
@@ -1087,10 +1094,7 @@ int64_t bf16_gemm_workspace(const Bf16GemmJob& j) {
     return counted(j, grid_tiles(j, tile, tile), resident) ? kCounters * 4 : 0;
 }
 
-bool bf16_gemm_fits(const Bf16GemmJob& j) {
-    constexpr int64_t kMost = int64_t(1) << 23;  // a grid holds fewer than 2^32 threads
-    return grid_tiles(j, kAnyTile, kAnyTile) < kMost && (!few(j) || (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * j.G < kMost);
-}
+bool bf16_gemm_fits(const Bf16GemmJob& j) { return grid_tiles(j, kAnyTile, kAnyTile) < kMostGroups; }
 
 hipError_t launch_gemm_bf16(const Bf16GemmJob& j, hipStream_t s) {
     return j.out_dtype == kOutBF16 ? launch_out<kOutBF16>(j, s) : launch_out<kOutF32>(j, s);
