@@ -840,9 +840,9 @@ using Tile128 = Tile<2, 2, 2, 2, Depth<PASS>::K, Depth<PASS>::kRing, 2>;  // 128
 // Few rows (a decode step): bound by reading the weights of the groups that have any.
 // ------------------------------------------------------------------------------------------------
 
-// A workgroup takes 16 CT columns of one group's product and reads its rows of W once, from memory to the registers of
-// v_mfma_f32_16x16x32_bf16 (16 rows x 64 consecutive bytes a load); its waves split the reduction in chunks of 64 places and add their sums
-// in order. RT tiles of 16 rows at a time; of more rows W is read again, from the L2. Any size, stride and alignment.
+// A workgroup takes 16 CT columns of 16 RT rows of one group's product and reads its rows of W once, from memory (where other rows of the group
+// came first, the L2) to the registers of v_mfma_f32_16x16x32_bf16 (16 rows x 64 consecutive bytes a load); its waves split the reduction in
+// chunks of 64 places and add their sums in order. Any size, stride and alignment.
 constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kFewChunk = 64;
 
 template <int OUT, int CT, int RT>
@@ -852,23 +852,43 @@ __global__ __launch_bounds__(kFewThreads) void gemm_bf16_few_kernel(Bf16GemmJob 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), quarter = lane >> 4, l16 = lane & 15;
     const uint32_t chunks = (uint32_t)((j.N + 16 * CT - 1) / (16 * CT)), rank = blockIdx.x / chunks;
     const int64_t col0 = (int64_t)(blockIdx.x % chunks) * (16 * CT);
-    // the group: the rank-th of those that have rows
-    int64_t start = 0, rows = 0;
+    // the group, and its rows from r0 on: the rank-th block of rows, counted over the groups
+    constexpr int kRows = 16 * RT;
+    int64_t start = 0, rows = 0, r0 = 0;
     int g = -1, claimed = 0;
     uint32_t before = 0;
     for (int g0 = 0; g0 < j.G && g < 0; g0 += 64) {
         int from, m;
         group_rows(j, g0, claimed, from, m);
-        uint64_t some = __ballot(m > 0);
-        const uint32_t n = (uint32_t)__popcll(some);
-        if (before + n > rank) {
-            for (uint32_t skip = rank - before; skip > 0; --skip) some &= some - 1;
-            const int at = uniform(__builtin_ctzll(some));
-            g = g0 + at;
-            start = __builtin_amdgcn_readlane(from, at);
-            rows = __builtin_amdgcn_readlane(m, at);
+        const uint64_t some = __ballot(m > 0);
+        if (!__ballot(m > kRows)) {  // a block each
+            const uint32_t n = (uint32_t)__popcll(some);
+            if (before + n > rank) {
+                uint64_t left = some;
+                for (uint32_t skip = rank - before; skip > 0; --skip) left &= left - 1;
+                g = uniform(__builtin_ctzll(left));
+            }
+            before += n;
+        } else {
+            const uint32_t n = (uint32_t)(((int64_t)m + kRows - 1) / kRows);
+            uint32_t upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t v = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += v;
+            }
+            const uint64_t past = __ballot(before + upto > rank);
+            if (past) {
+                g = uniform(__builtin_ctzll(past));
+                r0 = (int64_t)(rank - before - (uint32_t)__builtin_amdgcn_readlane((int)(upto - n), g)) * kRows;
+            }
+            before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-        before += n;
+        if (g >= 0) {
+            start = __builtin_amdgcn_readlane(from, g);
+            rows = __builtin_amdgcn_readlane(m, g);
+            g += g0;
+        }
     }
     if (g < 0) return;
     const uint16_t* w[CT];
@@ -877,81 +897,78 @@ __global__ __launch_bounds__(kFewThreads) void gemm_bf16_few_kernel(Bf16GemmJob 
         const int64_t n = col0 + t * 16 + l16;
         w[t] = j.b + ((int64_t)g * j.N + (n < j.N ? n : j.N - 1)) * j.ldb;
     }
-    for (int64_t r0 = 0; r0 < rows; r0 += 16 * RT) {
-        const uint16_t* x[RT];
+    const uint16_t* x[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int64_t r = r0 + t * 16 + l16;
-            x[t] = j.a + (start + (r < rows ? r : rows - 1)) * j.lda;
+    for (int t = 0; t < RT; ++t) {
+        const int64_t r = r0 + t * 16 + l16;
+        x[t] = j.a + (start + (r < rows ? r : rows - 1)) * j.lda;
+    }
+    v4f acc[CT][RT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[c][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kSteps = kFewChunk / 32;
+    struct Chunk {
+        u32x4_any w[CT][kSteps], x[RT][kSteps];
+    };
+    auto load = [&](Chunk& c, int64_t k0) INLINE {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int64_t k = k0 + s * 32 + quarter * 8;
+#pragma unroll
+            for (int t = 0; t < CT; ++t) c.w[t][s] = Piece<uint16_t>::load(w[t] + k, j.red - k);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) c.x[t][s] = Piece<uint16_t>::load(x[t] + k, j.red - k);
         }
-        v4f acc[CT][RT];
+    };
+    auto multiply = [&](const Chunk& c) INLINE {
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[c][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        constexpr int kSteps = kFewChunk / 32;
-        struct Chunk {
-            u32x4_any w[CT][kSteps], x[RT][kSteps];
-        };
-        auto load = [&](Chunk& c, int64_t k0) INLINE {
+            for (int n = 0; n < CT; ++n)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int64_t k = k0 + s * 32 + quarter * 8;
+                for (int t = 0; t < RT; ++t)
+                    acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, c.w[n][s]), __builtin_bit_cast(v8b, c.x[t][s]),
+                                                                        acc[n][t], 0, 0, 0);
+    };
+    constexpr int64_t kStep = kFewWaves * kFewChunk;
+    int64_t k = wave * kFewChunk;
+    Chunk c0, c1;
+    if (k < j.red) load(c0, k);
+    for (; k + kStep < j.red; k += 2 * kStep) {
+        load(c1, k + kStep);
+        multiply(c0);
+        if (k + 2 * kStep < j.red) load(c0, k + 2 * kStep);
+        multiply(c1);
+    }
+    if (k < j.red) multiply(c0);
+    // A lane has columns 4 quarter .. + 3 of row l16 of each tile.
 #pragma unroll
-                for (int t = 0; t < CT; ++t) c.w[t][s] = Piece<uint16_t>::load(w[t] + k, j.red - k);
+    for (int n = 0; n < CT; ++n)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) c.x[t][s] = Piece<uint16_t>::load(x[t] + k, j.red - k);
-            }
-        };
-        auto multiply = [&](const Chunk& c) INLINE {
+        for (int t = 0; t < RT; ++t) sums[wave][(n * RT + t) * 64 + lane] = make_float4(acc[n][t][0], acc[n][t][1], acc[n][t][2], acc[n][t][3]);
+    __syncthreads();
+    for (int i = tid; i < kTiles * 64; i += kFewThreads) {
+        float4 v = sums[0][i];
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-                for (int n = 0; n < CT; ++n)
-#pragma unroll
-                    for (int t = 0; t < RT; ++t)
-                        acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, c.w[n][s]), __builtin_bit_cast(v8b, c.x[t][s]),
-                                                                            acc[n][t], 0, 0, 0);
-        };
-        constexpr int64_t kStep = kFewWaves * kFewChunk;
-        int64_t k = wave * kFewChunk;
-        Chunk c0, c1;
-        if (k < j.red) load(c0, k);
-        for (; k + kStep < j.red; k += 2 * kStep) {
-            load(c1, k + kStep);
-            multiply(c0);
-            if (k + 2 * kStep < j.red) load(c0, k + 2 * kStep);
-            multiply(c1);
+        for (int o = 1; o < kFewWaves; ++o) {
+            const float4 u = sums[o][i];
+            v.x += u.x;
+            v.y += u.y;
+            v.z += u.z;
+            v.w += u.w;
         }
-        if (k < j.red) multiply(c0);
-        // A lane has columns 4 quarter .. + 3 of row l16 of each tile.
+        const int64_t r = r0 + (i / 64 % RT) * 16 + (i & 15), c = col0 + (i / 64 / RT) * 16 + (i >> 4 & 3) * 4;
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        if (r >= rows) continue;
 #pragma unroll
-        for (int n = 0; n < CT; ++n)
-#pragma unroll
-            for (int t = 0; t < RT; ++t) sums[wave][(n * RT + t) * 64 + lane] = make_float4(acc[n][t][0], acc[n][t][1], acc[n][t][2], acc[n][t][3]);
-        __syncthreads();
-        for (int i = tid; i < kTiles * 64; i += kFewThreads) {
-            float4 v = sums[0][i];
-#pragma unroll
-            for (int o = 1; o < kFewWaves; ++o) {
-                const float4 u = sums[o][i];
-                v.x += u.x;
-                v.y += u.y;
-                v.z += u.z;
-                v.w += u.w;
-            }
-            const int64_t r = r0 + (i / 64 % RT) * 16 + (i & 15), c = col0 + (i / 64 / RT) * 16 + (i >> 4 & 3) * 4;
-            const float f[4] = {v.x, v.y, v.z, v.w};
-            if (r >= rows) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (c + e >= j.N) continue;
-                const int64_t at = (start + r) * j.ldc + c + e;
-                if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[at] = f[e];
-                else static_cast<uint16_t*>(j.c)[at] = __builtin_bit_cast(uint16_t, (__bf16)f[e]);
-            }
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= j.N) continue;
+            const int64_t at = (start + r) * j.ldc + c + e;
+            if constexpr (OUT == kOutF32) static_cast<float*>(j.c)[at] = f[e];
+            else static_cast<uint16_t*>(j.c)[at] = __builtin_bit_cast(uint16_t, (__bf16)f[e]);
         }
-        __syncthreads();  // the sums are read before the next rows' are written
     }
 }
 
@@ -1038,26 +1055,40 @@ hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
 
 // 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8).
 constexpr int kFewCols = 2;
-// Its workgroups: those of the columns for each group that can have rows. Where they would be too many, the tiles take the product.
-int64_t few_grid(const Bf16GemmJob& j) { return (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * (j.tokens < j.G ? j.tokens : j.G); }
+// Rows of a workgroup, by the average of the groups that can have any.
+int few_tiles(const Bf16GemmJob& j) {
+    const int64_t groups = j.tokens < j.G ? j.tokens : j.G;
+    return j.tokens <= 16 * groups ? 1 : j.tokens <= 32 * groups ? 2 : 4;
+}
+// Its workgroups: those of the columns for each block of rows, of which every group may leave one partial.
+int64_t few_grid(const Bf16GemmJob& j) {
+    const int64_t groups = j.tokens < j.G ? j.tokens : j.G;
+    return (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * (groups + (j.tokens - groups) / (16 * few_tiles(j)));
+}
 
-// Which products the few-row kernel takes: up to 8 rows a group on average, or 64 in all. Past that its rows of W come through the L2 more than
-// once, and 128-row tiles read them less often. Measured, us, few-row kernel / 128 x 128 tiles:
-//     64 experts 2048 -> 1408, 6 a token: 42 rows 21.0 / 35.3, 96 45 / 47, 192 51 / 82, 384 83 / 99, 768 110 / 108, 1536 144 / 114;
-//     8 experts 512 -> 1312, 2 a token: 2 rows 5.5 / 8.3, 32 5.6 / 8.4, 64 7.1 / 8.4, 128 9.0 / 8.5;
-//     8 experts 5120 -> 4096: 2 rows 15.8 / 48.3, 32 62 / 75, 64 77 / 75, 128 110 / 80;
-//     one group 2048 -> 8192: 1 row 7.4 / 20.6, 32 10.9 / 22.0, 64 15.3 / 22.3, 128 27.8 / 23.1.
+// Which products the few-row kernel takes: 64 rows in all, or of up to 64 groups 8 rows a group on average; and where its grid fits. Past that its
+// rows of W come through the L2 more than once, and 128-row tiles read them less often; and the offsets of more groups are not one load.
+// The loads are known on the GPU only. Measured, us, few-row kernel / 128 x 128 tiles, for a power law's loads, even ones and all rows in one
+// group (a single pair: a power law's):
+//     64 experts 2048 -> 1408: 42 rows 28 / 26, 48 / 38, 9 / 18; 192 53 / 68, 82 / 85, 20 / 18; 384 71 / 75, 84 / 85, 31 / 18;
+//         510 82 / 82, 85 / 85, 37 / 19 (a workgroup that takes all blocks of a group in turn: 104, 86, 188); 768 110 / 87;
+//     8 experts 512 -> 1312: 2 rows 5.6 / 8.7, 64 5.8 / 8.8 in every case, 128 9.0 / 8.5;
+//     8 experts 5120 -> 4096: 2 rows 16 / 49, 32 63 / 76, 71 / 80, 18 / 48, 64 83 / 82, 77 / 82, 31 / 48, 128 110 / 80;
+//     one group 2048 -> 8192: 1 row 7.7 / 21.5, 32 11 / 22, 64 15.9 / 22.9, 128 27.8 / 23.1;
+//     128 experts 2048 -> 1408: 64 rows 37 / 33, 80 / 97, 14 / 18; 256 94 / 95, 150 / 146, 32 / 19; 512 122 / 109, 155 / 147, 48 / 19;
+//     256 experts 1024 -> 512: 256 rows 34 / 22, 58 / 46, 22 / 14; 1024 experts 512 -> 512: 512 rows 123 / 39, 93 / 63, 109 / 20.
 bool few(const Bf16GemmJob& j) {
-    return j.pass == kBf16FwdY && (j.tokens <= 64 || j.tokens <= 8 * (int64_t)j.G) && few_grid(j) < kMostGroups;
+    return j.pass == kBf16FwdY && (j.tokens <= 64 || (j.G <= 64 && j.tokens <= 8 * (int64_t)j.G)) && few_grid(j) < kMostGroups;
 }
 
 template <int OUT>
 hipError_t launch_few(const Bf16GemmJob& j, hipStream_t s) {
-    const int64_t groups = j.tokens < j.G ? j.tokens : j.G;  // that can have rows
     const unsigned n = (unsigned)few_grid(j);
-    if (j.tokens <= 16 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 1><<<n, kFewThreads, 0, s>>>(j);
-    else if (j.tokens <= 32 * groups) gemm_bf16_few_kernel<OUT, kFewCols, 2><<<n, kFewThreads, 0, s>>>(j);
-    else gemm_bf16_few_kernel<OUT, kFewCols, 4><<<n, kFewThreads, 0, s>>>(j);
+    switch (few_tiles(j)) {
+        case 1: gemm_bf16_few_kernel<OUT, kFewCols, 1><<<n, kFewThreads, 0, s>>>(j); break;
+        case 2: gemm_bf16_few_kernel<OUT, kFewCols, 2><<<n, kFewThreads, 0, s>>>(j); break;
+        default: gemm_bf16_few_kernel<OUT, kFewCols, 4><<<n, kFewThreads, 0, s>>>(j);
+    }
     return hipGetLastError();
 }
 
