@@ -1035,8 +1035,12 @@ double estimate(const Bf16GemmJob& j, bool big) {
     return us > alone ? us : alone;
 }
 bool large(const Bf16GemmJob& j) {
-    // many tiles of a weights' gradient are bound by their stores, which the larger ones make nontemporally
-    if (j.pass == kBf16BwdDw && grid_tiles(j, 256, 256) >= 1024) return true;
+    // Many tiles of a weights' gradient are bound by their stores, which the larger ones make nontemporally, unless those cover much more than the
+    // smaller ones (up to 3/2: 1024 of them are then 64 MiB of fp32 results at least). Measured, us, 256 / 128, results in fp32:
+    //     1024 groups 64 x 64, 32 rows each 194 / 95, 128 rows 219 / 106; 64 groups 64 x 4096, 256 rows 60 / 45; 1024 groups 128 x 256, 64 rows
+    //     205 / 204; 136 x 264 414 / 577.
+    const int64_t most = grid_tiles(j, 256, 256);
+    if (j.pass == kBf16BwdDw && most >= 1024 && 8 * most <= 3 * grid_tiles(j, 128, 128)) return true;
     return estimate(j, true) < estimate(j, false);
 }
 

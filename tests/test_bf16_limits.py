@@ -1,4 +1,5 @@
-"""Sizes at the documented limits of the grouped bf16 products: what the header allows is taken. On the host, and one of them on the GPU."""
+"""Sizes at the documented limits of the grouped bf16 products: what the header allows is taken. On the host, and one of them on the GPU. And narrow
+weights of many groups: the kernel that fits them."""
 
 import ctypes
 import os
@@ -30,6 +31,20 @@ def test_few_rows_of_wide_weights(tokens, N, G):
     """Fewer than 2^23 tiles of 128 x 128: taken, with however few rows."""
     assert (_workspace(0, tokens, N, 8, G) == OK) == (_tiles(tokens, N, G) < 1 << 23)
     assert _workspace(0, tokens, 1 << 30, 8, 1024) == UNSUPPORTED
+
+
+# (rows of a group, N, K, groups, us of tiles of 128 x 128 and of 256 x 256 on an MI355X)
+NARROW = [(32, 64, 64, 1024, 95, 194), (128, 64, 64, 1024, 106, 219), (256, 64, 4096, 64, 45, 60), (64, 128, 256, 1024, 204, 205)]
+
+
+@pytest.mark.parametrize("rows,N,K,G,small,large", NARROW)
+def test_many_narrow_weight_gradients(rows, N, K, G, small, large):
+    """As for fewer groups, the tile that covers less outside of the results."""
+    assert small < large
+    for groups in (G, G - 1):
+        assert U.lib().ufp4_plan_gemm_bf16(2, *(ctypes.c_int64(v) for v in (rows * groups, N, K)), groups, 1) == 2
+    for wide in ((98304, 1408, 2048, 64), (32768, 1416, 2056, 64), (65536, 136, 264, 1024)):  # tiles that hardly cover more
+        assert U.lib().ufp4_plan_gemm_bf16(2, *(ctypes.c_int64(v) for v in wide[:3]), wide[3], 1) == 3
 
 
 @pytest.mark.gpu
