@@ -53,7 +53,10 @@ struct Stage {
         static_assert(K == 32 || K == 64, "");
         return K == 32 ? ((r >> 1 ^ r >> 3) & 1) | (r >> 1 & 2) : (r ^ (r >> 3 & 3)) & 7;
     }
-    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) { return ROWS < 128 ? k & 2 : (k << 1 & 6) | (k >> 1 & 1); }
+    static __device__ __forceinline__ uint32_t turn_k(uint32_t k) {
+        static_assert(ROWS >= 128, "eight segments at least");
+        return (k << 1 & 6) | (k >> 1 & 1);
+    }
 
     // Byte address of the piece of row r with places 8 p .. of the reduction.
     static __device__ __forceinline__ uint32_t along(uint32_t r, uint32_t p) { return r * (K * 2) + (p ^ turn_row(r)) * 16; }
