@@ -625,7 +625,8 @@ int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void *dy_dev, int64_t tokens, int6
  * Activations kept in 8 bits between the forward and the backward pass. Per 32 values of a row one scale 2^e, stored as the byte
  * e + 127: e is the smallest integer >= -124 with |x| <= 448 2^e for every finite x of the block; and per value the E4M3 number (OCP, one
  * byte, no infinity) nearest to x 2^-e, ties to the even code. A value is off by at most 2^-4 of itself or half of 2^(e - 9), where
- * that is more (magnitudes from 1.9375 2^127 on are kept as 1.875 2^127, the next level being no fp32 number); an infinity or NaN is kept as NaN and leaves its block's other values alone. Every kept value is a bf16 number.
+ * that is more (magnitudes from 1.9375 2^127 on are kept as 1.875 2^127, the next level being no fp32 number); an infinity or NaN is kept as
+ * NaN and leaves its block's other values alone. Every kept value is a bf16 number.
  * A row of `cols` values has ceil(cols / 32) scales and 32 ceil(cols / 32) codes, those past `cols` 0.
  *
  * ufp4_ckpt8_ld -- leading dimensions (bytes) of codes and scales of a row in `parts` parts of `cols` values each, every part in blocks of
@@ -633,7 +634,7 @@ int ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(const void *dy_dev, int64_t tokens, int6
  *   as the blocks fit. Where scales_dev and scale_ld are multiples of 4, scales are read 4 at a time: every row, the last one too, must
  *   then be readable to such a multiple.
  * ufp4_ckpt8_save, ufp4_ckpt8_load -- a tensor [rows, cols] of type `dtype` to codes and scales, and back. Codes 16-byte aligned with
- *   code_ld % 16 == 0.
+ *   code_ld % 16 == 0. Up to 2^30 columns, 2^36 rows and 2^34 - 2^10 values, rows counted in whole blocks (else UFP4_ERR_UNSUPPORTED).
  */
 int ufp4_ckpt8_ld(int64_t cols, int parts, int64_t *code_ld, int64_t *scale_ld);
 int ufp4_ckpt8_save(int dtype, const void *x_dev, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes_dev, int64_t code_ld,
@@ -648,7 +649,7 @@ int ufp4_ckpt8_load(int dtype, const uint8_t *codes_dev, int64_t code_ld, const 
  *                   du = (da v silu'(g), da silu(g))
  * ufp4_activation -- a, and with codes_dev u's checkpoint from the same read (parts 1 or, of the gated one, 2).
  * ufp4_activation_bwd -- du from da and u, or (u_dev NULL) u's checkpoint; with a_dev also a of that u, which the weights' gradient of
- *   the next product needs. Outputs must not overlap inputs.
+ *   the next product needs. Sizes of a as those of a checkpoint. Outputs must not overlap inputs.
  */
 typedef enum { UFP4_ACT_RELU2 = 0, UFP4_ACT_SWIGLU = 1 } ufp4_act_t;
 int ufp4_activation(int kind, int dtype, const void *u_dev, int64_t rows, int64_t cols, int64_t ldu, void *a_dev, int64_t lda,

@@ -41,10 +41,10 @@ int check_codes(const uint8_t* codes, int64_t code_ld, const uint8_t* scales, in
     return code_ld % 16 == 0 && aligned(codes, 16) ? UFP4_OK : UFP4_ERR_ALIGN;
 }
 
-// A grid holds fewer than 2^32 threads.
+// A grid holds fewer than 2^32 threads, whole workgroups of 256 of them.
 int check_size(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 0) return UFP4_ERR_INVALID_ARG;
-    if (cols > kMostCols || rows > int64_t(1) << 36 || ckpt8_units(rows, cols) >= int64_t(1) << 32) return UFP4_ERR_UNSUPPORTED;
+    if (cols > kMostCols || rows > int64_t(1) << 36 || ckpt8_units(rows, cols) > (int64_t(1) << 32) - 256) return UFP4_ERR_UNSUPPORTED;
     return UFP4_OK;
 }
 

@@ -47,6 +47,13 @@ def test_many_narrow_weight_gradients(rows, N, K, G, small, large):
         assert U.lib().ufp4_plan_gemm_bf16(2, *(ctypes.c_int64(v) for v in wide[:3]), wide[3], 1) == 3
 
 
+def test_activation_of_as_many_threads_as_a_grid_holds():
+    """A lane takes 4 fp32 values of a block of 32: workgroups of 256 lanes that would make 2^32 of them are refused before the launch."""
+    rows, cols, p = (1 << 29) - 1, 32, 1 << 20
+    assert U.lib().ufp4_activation(0, U.OUT_F32, p, rows, cols, cols, p, cols, None, 0, None, 0, None) == UNSUPPORTED
+    assert U.lib().ufp4_activation_bwd(0, U.OUT_F32, p, rows, cols, cols, p, cols, None, 0, None, 0, p, cols, None, 0, None) == UNSUPPORTED
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("tokens,N,K,G", [(2, 1 << 28, 1, 1), (3, (1 << 27) + 40, 8, 3)])
 def test_few_rows_of_wide_weights_run(tokens, N, K, G):
