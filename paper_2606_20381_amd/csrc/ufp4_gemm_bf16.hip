@@ -102,9 +102,11 @@ __device__ __forceinline__ int64_t clamped(int64_t v, int64_t most) { return v <
 // their tiles, are never more than a grid for rising offsets holds.
 __device__ __forceinline__ void group_rows(const Bf16GemmJob& j, int g0, int& before, int& from, int& m) {
     const int lane = threadIdx.x & 63, g = g0 + lane;
-    from = g < j.G ? (int)clamped(j.offsets[g], j.tokens) : 0;
-    const int to = g < j.G ? (int)clamped(j.offsets[g + 1], j.tokens) : 0;
-    if (__ballot(g < j.G && (to < from || from < before))) {
+    const int64_t* const at = j.offsets + (g < j.G ? g : j.G - 1);  // both loads at once, without a branch
+    from = (int)clamped(at[0], j.tokens);
+    int to = (int)clamped(at[1], j.tokens);
+    to = g < j.G ? to : from;
+    if (__ballot(to < from || from < before)) {
         from = from > before ? from : before;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
