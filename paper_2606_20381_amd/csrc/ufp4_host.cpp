@@ -444,10 +444,16 @@ bool product_out(PyObject* o, const at::Tensor& like, const Shape& s, int code, 
                          (long long)cols);
         return false;
     }
-    if (groups > 1 && t->stride(0) != rows * t->stride(1)) return refuse("out", "of groups that lie their rows apart");
+    if (groups > 1 && rows > 1 && t->stride(0) != rows * t->stride(1)) return refuse("out", "of groups that lie their rows apart");
     if (code_of(*t) < 0) return refuse("out", "float32 or bfloat16");
     out = *t;
     return true;
+}
+
+// Leading dimension of an output. A dimension of one place may have any stride; of lone rows of groups the groups' distance is theirs.
+int64_t product_ld(const at::Tensor& out) {
+    if (out.size(-2) > 1) return out.stride(-2);
+    return out.dim() == 3 && out.size(0) > 1 ? out.stride(0) : out.size(-1);
 }
 
 void product_new(const at::Tensor& like, const Shape& s, int code, at::Tensor& out) {
@@ -561,7 +567,7 @@ CALL(mxfp4_dequantize, 4)
     }
     if (!unlocked([&]() -> Done {
             if (!out.defined()) out = at::empty({d->rows, d->red}, codes->options().dtype(at::kBFloat16));
-            return {ufp4_mxfp4_dequantize(d, out.data_ptr(), out.stride(0), stream), "ufp4_mxfp4_dequantize"};
+            return {ufp4_mxfp4_dequantize(d, out.data_ptr(), product_ld(out), stream), "ufp4_mxfp4_dequantize"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -582,7 +588,7 @@ PyObject* product(const char* name, PyObject* const* a, Py_ssize_t n_args) {
     if (!product_out(a[4], *codes, shape, code, out)) return nullptr;
     if (!unlocked([&]() -> Done {
             product_new(*codes, shape, code, out);
-            return {GEMM(x, w, out.data_ptr(), out.stride(0), code_of(out), stream), name};
+            return {GEMM(x, w, out.data_ptr(), product_ld(out), code_of(out), stream), name};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -615,7 +621,7 @@ PyObject* product_rows(const char* name, PyObject* const* a, Py_ssize_t n_args) 
     if (!product_out(a[6], *codes, shape, code, out)) return nullptr;
     if (!unlocked([&]() -> Done {
             product_new(*codes, shape, code, out);
-            return {GEMM(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, rows, out.data_ptr(), out.stride(0), code_of(out), stream), name};
+            return {GEMM(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, rows, out.data_ptr(), product_ld(out), code_of(out), stream), name};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -644,7 +650,7 @@ CALL(mxfp4_gemm_bwd_dw_grouped, 7)
     if (!product_out(a[5], *codes, shape, code, out)) return nullptr;
     if (!unlocked([&]() -> Done {
             product_new(*codes, shape, code, out);
-            return {ufp4_mxfp4_gemm_bwd_dw_grouped(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, out.data_ptr(), out.stride(1),
+            return {ufp4_mxfp4_gemm_bwd_dw_grouped(x, w, static_cast<int64_t*>(offsets), (int32_t)groups, out.data_ptr(), product_ld(out),
                                                    code_of(out), stream), "ufp4_mxfp4_gemm_bwd_dw_grouped"};
         }))
         return nullptr;
@@ -673,7 +679,7 @@ CALL(mxfp4_linear, 6)
     if (!unlocked([&]() -> Done {
             product_new(*x, shape, code, out);
             if (tokens <= most && w->rht_block == 0)
-                return {ufp4_mxfp4_linear(x->data_ptr(), tokens, x->stride(0), w, out.data_ptr(), out.stride(0), code_of(out), stream),
+                return {ufp4_mxfp4_linear(x->data_ptr(), tokens, x->stride(0), w, out.data_ptr(), product_ld(out), code_of(out), stream),
                         "ufp4_mxfp4_linear"};
             ufp4_qtensor d;  // x as W was rotated
             at::Tensor codes, scales;
@@ -682,7 +688,7 @@ CALL(mxfp4_linear, 6)
             done = {ufp4_mxfp4_quantize(x->data_ptr(), tokens, red, x->stride(0), 0, w->rht_block != 0, w->rht_block ? w->sign_words[0] : 0,
                                         UFP4_ROUND_RTNE, 0, 0, &d, stream), "ufp4_mxfp4_quantize"};
             if (done.status != UFP4_OK) return done;
-            return {ufp4_mxfp4_gemm_fwd_y(&d, w, out.data_ptr(), out.stride(0), code_of(out), stream), "ufp4_mxfp4_gemm_fwd_y"};
+            return {ufp4_mxfp4_gemm_fwd_y(&d, w, out.data_ptr(), product_ld(out), code_of(out), stream), "ufp4_mxfp4_gemm_fwd_y"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -811,9 +817,9 @@ PyObject* bf16_rows_product(PyObject* const* a, Py_ssize_t n_args) {
             if (done.status != UFP4_OK) return done;
             if (BACK)
                 return {ufp4_bf16_gemm_bwd_dx_grouped(x.data(), x.rows, n, x.ld, w.data(), w.cols, w.ld, static_cast<int64_t*>(offsets), g,
-                                                      out.data_ptr(), out.stride(0), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dx_grouped"};
+                                                      out.data_ptr(), product_ld(out), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dx_grouped"};
             return {ufp4_bf16_gemm_fwd_y_grouped(x.data(), x.rows, x.cols, x.ld, w.data(), n, w.ld, static_cast<int64_t*>(offsets), g,
-                                                 out.data_ptr(), out.stride(0), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_fwd_y_grouped"};
+                                                 out.data_ptr(), product_ld(out), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_fwd_y_grouped"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -859,10 +865,10 @@ CALL(bf16_gemm_bwd_dw_grouped, 9)
             if (done.status != UFP4_OK) return done;
             if (saved)
                 return {ufp4_bf16_gemm_bwd_dw_grouped_ckpt8(dy.data(), dy.rows, dy.cols, dy.ld, k.codes, k.code_ld, k.scales, k.scale_ld, cols,
-                                                            off, g, out.data_ptr(), out.stride(1), code_of(out), scratch, bytes, stream),
+                                                            off, g, out.data_ptr(), product_ld(out), code_of(out), scratch, bytes, stream),
                         "ufp4_bf16_gemm_bwd_dw_grouped_ckpt8"};
             return {ufp4_bf16_gemm_bwd_dw_grouped(dy.data(), dy.rows, dy.cols, dy.ld, x.data(), cols, x.ld, off, g, out.data_ptr(),
-                                                  out.stride(1), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dw_grouped"};
+                                                  product_ld(out), code_of(out), scratch, bytes, stream), "ufp4_bf16_gemm_bwd_dw_grouped"};
         }))
         return nullptr;
     return THPVariable_Wrap(out);
@@ -913,7 +919,7 @@ CALL(checkpoint8_load, 7)
             ufp4_ckpt8_ld(cols, 1, &cld, nullptr);
             for (int p = 0; p < parts; ++p) {
                 const int st = ufp4_ckpt8_load(code_of(out), k.codes + p * cld, k.code_ld, k.scales + p * (cld / 32), k.scale_ld, k.rows, cols,
-                                               static_cast<uint8_t*>(out.data_ptr()) + p * cols * out.element_size(), out.stride(0), stream);
+                                               static_cast<uint8_t*>(out.data_ptr()) + p * cols * out.element_size(), product_ld(out), stream);
                 if (st != UFP4_OK) return {st, "ufp4_ckpt8_load"};
             }
             return {UFP4_OK, nullptr};
