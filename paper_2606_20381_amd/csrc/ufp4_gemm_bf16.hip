@@ -13,11 +13,11 @@
 // registers (any alignment), and one for the few rows of a decode step.
 //
 // Bound, where the tiles fill the chip, by the matrix cores' power: the instruction alone, on registers, reaches 1.54-1.75 PFLOP/s on random
-// numbers (2.3 on zeros: power takes the clock to 1.5-1.7 GHz). 8192^3 takes 0.79-0.86 ms in every pass = 1.28-1.39 (matrix cores busy 78-81%
-// of the CUs' busy cycles, at 1.6-1.75 GHz; 0.79 with every load from the same L2-resident place, 0.69 without the loads). 98304 x 1408 x 2048 of 64 experts with
-// a power law's loads: forward and input's gradient 0.55-0.57 ms = 1.0 PFLOP/s of the products asked for (busy 64%: tiles that end outside
-// of a group or of the 1408 columns, W new in every tile row, workgroups that end 12% apart), weights' gradient 0.62-0.64 ms, its
-// 738 MB of results alone 0.15.
+// numbers (2.3 on zeros: power takes the clock to 1.5-1.7 GHz). 8192^3 takes 0.79-0.87 ms in every pass = 1.26-1.39 (matrix cores busy 78-81%
+// of the CUs' busy cycles, at 1.6-1.75 GHz; 0.79 with every load from the same L2-resident place, 0.69 without the loads). 98304 x 1408 x 2048
+// of 64 experts with a power law's loads: forward and input's gradient 0.55-0.58 ms = 1.0 PFLOP/s of the products asked for (busy 64%: tiles
+// that end outside of a group or of the 1408 columns, W new in every tile row, workgroups that end 12% apart), weights' gradient 0.61-0.65 ms,
+// its 738 MB of results alone 0.15.
 
 #include "ufp4_internal.h"
 #include "ufp4_ckpt8.h"
@@ -1062,7 +1062,7 @@ hipError_t launch_pass(const Bf16GemmJob& j, hipStream_t s) {
     return streams(j) ? launch_tile<OUT, Tile256<PASS>, PASS, true, SAVED>(j, s) : launch_tile<OUT, Tile256<PASS>, PASS, false, SAVED>(j, s);
 }
 
-// 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8).
+// 32 columns a workgroup (16: 42 rows of 64 experts 21.9 us, 64: 23.5; 5120 -> 4096 2 rows 15.8, 23.8; W in the memory-side cache).
 constexpr int kFewCols = 2;
 // Rows of a workgroup, by the average of the groups that can have any.
 int few_tiles(const Bf16GemmJob& j) {
@@ -1075,19 +1075,18 @@ int64_t few_grid(const Bf16GemmJob& j) {
     return (j.N + 16 * kFewCols - 1) / (16 * kFewCols) * (groups + (j.tokens - groups) / (16 * few_tiles(j)));
 }
 
-// Which products the few-row kernel takes: 64 rows in all, or of up to 64 groups 8 rows a group on average; and where its grid fits. Past that its
-// rows of W come through the L2 more than once, and 128-row tiles read them less often; and the offsets of more groups are not one load.
-// The loads are known on the GPU only. Measured, us, few-row kernel / 128 x 128 tiles, for a power law's loads, even ones and all rows in one
-// group (a single pair: a power law's):
-//     64 experts 2048 -> 1408: 42 rows 28 / 26, 48 / 38, 9 / 18; 192 53 / 68, 82 / 85, 20 / 18; 384 71 / 75, 84 / 85, 31 / 18;
-//         510 82 / 82, 85 / 85, 37 / 19 (a workgroup that takes all blocks of a group in turn: 104, 86, 188); 768 110 / 87;
-//     8 experts 512 -> 1312: 2 rows 5.6 / 8.7, 64 5.8 / 8.8 in every case, 128 9.0 / 8.5;
-//     8 experts 5120 -> 4096: 2 rows 16 / 49, 32 63 / 76, 71 / 80, 18 / 48, 64 83 / 82, 77 / 82, 31 / 48, 128 110 / 80;
-//     one group 2048 -> 8192: 1 row 7.7 / 21.5, 32 11 / 22, 64 15.9 / 22.9, 128 27.8 / 23.1;
-//     128 experts 2048 -> 1408: 64 rows 37 / 33, 80 / 97, 14 / 18; 256 94 / 95, 150 / 146, 32 / 19; 512 122 / 109, 155 / 147, 48 / 19;
-//     256 experts 1024 -> 512: 256 rows 34 / 22, 58 / 46, 22 / 14; 1024 experts 512 -> 512: 512 rows 123 / 39, 93 / 63, 109 / 20.
+// Which products the few-row kernel takes: of 64 rows in all, or of up to 128 groups up to 8 rows a group on average and 512 in all; and where its
+// grid fits. Past that its rows of W come through the L2 more than once, 128-row tiles read them less often, and finding a workgroup's group
+// takes one load after the other. Measured, us, few-row kernel / 128 x 128 tiles, a power law's loads, weights that no cache holds:
+//     64 experts 2048 -> 1408: 6 rows 12 / 23, 42 33 / 40, 96 44 / 49, 192 60 / 83, 384 76 / 89, 504 83 / 90;
+//     8 experts 5120 -> 4096: 2 rows 20 / 72, 42 76 / 82, 64 86 / 82; 512 -> 1312: 2 rows 5.8 / 9.4, 64 7.7 / 12.0;
+//     one group 2048 -> 8192: 1 row 11 / 32, 64 19 / 32;
+//     128 experts 2048 -> 1408: 96 rows 51 / 53, 192 77 / 88, 512 118 / 131, 1024 158 / 150; 512 -> 512: 192 14.3 / 13.7, 512 20 / 16;
+//     256 experts 1024 -> 512: 96 rows 15 / 20, 192 27 / 24, 512 47 / 43; 1024 experts 512 -> 512: 96 rows 21 / 22, 512 103 / 39;
+// and all rows in one group, which the caches then hold (loads are known on the GPU only):
+//     64 experts 2048 -> 1408: 42 rows 9 / 18, 192 20 / 18, 510 37 / 19 (a workgroup that takes all blocks of its group in turn: 188).
 bool few(const Bf16GemmJob& j) {
-    return j.pass == kBf16FwdY && (j.tokens <= 64 || (j.G <= 64 && j.tokens <= 8 * (int64_t)j.G)) && few_grid(j) < kMostGroups;
+    return j.pass == kBf16FwdY && (j.tokens <= 64 || (j.G <= 128 && j.tokens <= 8 * (j.G < 64 ? j.G : 64))) && few_grid(j) < kMostGroups;
 }
 
 template <int OUT>
