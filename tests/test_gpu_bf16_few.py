@@ -48,7 +48,7 @@ def _spread(tokens, G, how):
 
 
 @pytest.mark.parametrize("how", ["first", "last", "two", "one each, then the rest", "blocks"])
-@pytest.mark.parametrize("tokens,G", [(1, 1), (33, 1), (64, 1), (64, 2), (62, 3), (64, 5), (40, 130), (62, 201), (130, 17), (510, 64)])
+@pytest.mark.parametrize("tokens,G", [(1, 1), (33, 1), (64, 1), (64, 2), (62, 3), (64, 5), (40, 130), (62, 201), (130, 17), (510, 64), (500, 128), (300, 101)])
 @pytest.mark.parametrize("dtype", [F32, BF])
 def test_uneven_loads(tokens, G, how, dtype):
     g = torch.Generator(device="cuda").manual_seed(tokens + G)

@@ -45,7 +45,7 @@ def _lists(tokens, groups, seed):
 
 
 # kernel of the forward pass and of the input's gradient as ufp4_plan_gemm_bf16 names them; odd widths: the one of any alignment
-CASES = [(2, 5, 40, 72, 0, 2), (40, 70, 264, 136, 0, 2), (60, 130, 33, 35, 0, 1), (300, 40, 72, 40, 0, 2), (1000, 130, 33, 35, 1, 1), (1200, 20, 264, 136, 2, 2), (1200, 90, 131, 67, 1, 1),
+CASES = [(2, 5, 40, 72, 0, 2), (40, 70, 264, 136, 0, 2), (60, 130, 33, 35, 0, 1), (300, 40, 72, 40, 0, 2), (400, 100, 72, 40, 0, 2), (1000, 130, 33, 35, 1, 1), (1200, 20, 264, 136, 2, 2), (1200, 90, 131, 67, 1, 1),
          (8192, 8, 1408, 2048, 2, 3), (4096, 8, 4096, 2048, 3, 3)]
 
 
